@@ -18,7 +18,7 @@
  *    pos[r] = seg_delta[i] + (r - seg_off[i]).  Row t sees key k iff pos[k] <= pos[t].
  *  - `stream` is a cudaStream_t (0 = default stream).  Calls enqueue work and return; the
  *    only blocking calls are rk_create / rk_request_create / rk_poll_status / *_destroy and
- *    rk_layer_host.
+ *    rk_layer_host.  The decode calls can be captured into a CUDA graph.
  *  - The library allocates device memory only inside rk_create and rk_request_create (small
  *    tables) and frees it in the matching destroy.  kv, weights and z_off are never written.
  *  - No kernel traps: a device-side wait that expires records RK_ERR_TIMEOUT in a status
@@ -111,8 +111,9 @@ rk_status rk_create_ex(const rk_profile* profile, uint32_t flags, rk_ctx** out);
 rk_status rk_destroy(rk_ctx* ctx);
 /* Message of the last failing call on this context (valid until the next call). */
 const char* rk_last_error(const rk_ctx* ctx);
-/* Synchronises `stream`, returns the device status word (RK_OK, RK_ERR_TIMEOUT, or RK_ERR_ROWS from the
- * bounds-checked build) and clears it. */
+/* Synchronises `stream`, returns the device status word and clears it: RK_OK, RK_ERR_TIMEOUT, RK_ERR_ROWS (a bad
+ * entry in the tables of a decode call, or a report of the bounds-checked build), RK_ERR_WORKSPACE or RK_ERR_LAYOUT
+ * (a decode plan that is too small, or made for another call).  The first report wins. */
 rk_status rk_poll_status(rk_ctx* ctx, void* stream);
 /* Per-wait time limit of device-side waits, in milliseconds (default 2000). */
 rk_status rk_set_wait_limit_ms(rk_ctx* ctx, int32_t ms);
@@ -341,6 +342,111 @@ typedef struct rk_layer_io {
  * returns.  Every request must belong to `ctx`; the sets must be large enough for every layer. */
 rk_status rk_layer_stack_host(rk_ctx* ctx, int32_t n_layers, const rk_layer_io* layers, const rk_layer_buffers* dev0,
                               const rk_layer_buffers* dev1, void* stream);
+
+/* ---- Decode: generating tokens after the online step ------------------------------------------------------
+ *
+ * The latent rows live in a paged cache that holds the latent in 4 bits.  A SEGMENT is a document, or the suffix
+ * that a request has generated so far; its row j is stored at canonical position j (like every document here),
+ * so a document's pages serve every request that reuses it, at whatever offset it appears there.
+ *
+ * A page holds 64 rows of one segment in RK_CACHE4_PAGE_BYTES = 26 units of 16 bytes per row, unit-major: byte
+ * u * 1024 + row * 16 + i is byte i of unit u of the row.
+ *   units 0-15   latent dims 32 u .. 32 u + 31 as 4-bit codes n + 8: dim 32 u + 8 w + 2 i + e is the four bits at
+ *                16 e + 4 i of the unit's w-th 32-bit word
+ *   units 16-17  scale bytes: group g (dims 16 g .. 16 g + 15) is byte 4 (g >> 3) + (g & 3) of unit 16 + ((g >> 2) & 1);
+ *                byte b is the scale 2^((b >> 3) - 20) * (1 + (b & 7) / 8), and 255 is NaN
+ *   units 18-25  the 64 rope dims (bf16), turned by R(j)
+ * The stored latent value is n * scale, which is a bf16 number exactly.
+ *
+ * The segment and page tables are device arrays: a captured graph can be replayed after their contents changed.  They
+ * are bounds-checked on the device; a bad entry is skipped and rk_poll_status() returns RK_ERR_ROWS.  The
+ * context's device must be the current one (RK_ERR_CUDA otherwise), and these calls need a context without
+ * RK_VALUE_PHASE (RK_ERR_UNSUPPORTED otherwise). */
+#define RK_CACHE4_PAGE_ROWS 64
+#define RK_CACHE4_PAGE_BYTES 26624
+
+typedef struct rk_cache4_table {
+  int32_t n_segs;
+  int64_t n_listed;          /* entries of page_ids */
+  const int32_t* seg_len;    /* device [n_segs]: rows of each segment */
+  const int32_t* page_off;   /* device [n_segs + 1]: its pages are page_ids[page_off[s]] .. page_ids[page_off[s+1] - 1] */
+  const int32_t* page_ids;   /* device [n_listed]: row j of the segment is row j % 64 of its page j / 64 */
+} rk_cache4_table;
+
+/* Appends rows to segments.  Rows new_off[s] .. new_off[s+1] - 1 of the inputs become the LAST rows of segment s, whose
+ * seg_len already counts them; rows from new_off[n_segs] on are padding and are not read into the cache.
+ *   c       device bf16: latent of row i at c + i * c_stride (512 values; stride in elements, a multiple of 8)
+ *   k_rope  device bf16: key rope part of row i BEFORE rotation at k_rope + i * r_stride (64 values; likewise)
+ *   new_off device int32 [n_segs + 1], ascending from 0
+ * Every 16 latent dims share the scale nearest to max|c| / 7 among the scales above (ties to the even byte), at least
+ * 2^-20 and at most 3584; the codes are c / scale rounded half to even and limited to -7..7.  A group that holds an
+ * infinity or a NaN is stored as NaN.  k_rope is turned by R(row index in its segment) in fp32 and rounded to bf16.
+ * Only the units of the appended rows are written.  Pages that the call writes must each belong to one segment of
+ * the table: a page listed for two growing segments holds a mixture afterwards.  Calls on different streams must
+ * not write the same rows. */
+rk_status rk_cache4_append(rk_ctx* ctx, void* pages, int64_t n_pages, const rk_cache4_table* table, const void* c,
+                           int64_t c_stride, const void* k_rope, int64_t r_stride, const int32_t* new_off, int64_t n_new,
+                           void* stream);
+
+/* Reads rows back as the packed bf16 stream [c | k_rope] that rk_mla_online_attn takes: rows row_off[s] ..
+ * row_off[s+1] - 1 of kv are the LAST row_off[s+1] - row_off[s] rows of segment s (the whole segment where that is
+ * its length).
+ *   kv  device bf16 [n_rows][576]; rows from row_off[n_segs] on, and rows of bad table entries, are left as they were */
+rk_status rk_cache4_read(rk_ctx* ctx, const void* pages, int64_t n_pages, const rk_cache4_table* table,
+                         const int32_t* row_off, int64_t n_rows, void* kv, void* stream);
+
+/* Shape of a decode step: n_seqs requests with q_len query tokens each, which see n_items segments together, in at
+ * most max_tiles key tiles (a tile is up to 128 consecutive rows of one segment; the sum over the items of
+ * ceil(rows / 128)).  Limits: n_seqs * q_len * n_heads < 2^31 - 256, q_len <= 64, max_tiles <= 2^20. */
+typedef struct rk_decode_shape {
+  int32_t n_seqs, q_len, n_items, max_tiles;
+} rk_decode_shape;
+
+/* The work list of a decode step, for all layers whose caches share the tables: made once per step, on the device.
+ *   seq_off    device int32 [n_seqs + 1]: request b sees items seq_off[b] .. seq_off[b+1] - 1
+ *   item_seg   device int32 [n_items]: the segment; one segment may be an item of several requests
+ *   item_delta device int32 [n_items]: the request position of its row 0, >= 0
+ *   q_pos      device int32 [n_seqs][q_len]: request positions of the query tokens
+ *   plan       device, rk_decode_plan_bytes() bytes, 256-byte aligned
+ * Row j of an item sits at position item_delta + j; query token t sees it iff item_delta + j <= q_pos[t] (so a
+ * padding request is one without items, or with negative positions).  A bad item is left out (RK_ERR_ROWS); more key tiles than
+ * max_tiles make an empty plan (RK_ERR_WORKSPACE). Both are reported by rk_poll_status(). */
+rk_status rk_decode_plan_bytes(const rk_ctx* ctx, const rk_decode_shape* shape, size_t* out);
+rk_status rk_decode_plan(rk_ctx* ctx, const rk_decode_shape* shape, const rk_cache4_table* table, int64_t n_pages,
+                         const int32_t* seq_off, const int32_t* item_seg, const int32_t* item_delta, const int32_t* q_pos,
+                         void* plan, size_t plan_bytes, void* stream);
+
+/* Absorbed-MLA attention of the query tokens over the cache (all heads):
+ *   q    device bf16 [n_seqs][q_len][n_heads][576], at the request positions; relocated by R(-item_delta) per item
+ *   O    device bf16 [n_seqs][q_len][n_heads][512];  lse  device fp32 [n_seqs][q_len][n_heads] (natural log)
+ * A row that sees no key gets O = 0, lse = -inf.  `plan` must come from rk_decode_plan with this shape, head count and
+ * n_pages (else RK_ERR_LAYOUT from rk_poll_status, O and lse left as they were) and the pages it names must still hold the rows; the plan
+ * and the pages are only read, so concurrent calls may share them.  The workspace may not be shared by calls that overlap. A row of
+ * the cache that holds a NaN makes every query row of the sequences that see it NaN, also the query tokens before it.
+ * The result does not depend on timing: partial results are joined in a fixed order. */
+rk_status rk_cache4_attn_workspace_bytes(const rk_ctx* ctx, const rk_decode_shape* shape, size_t* out);
+rk_status rk_cache4_attn(rk_ctx* ctx, const rk_decode_shape* shape, const void* plan, size_t plan_bytes, const void* pages,
+                         int64_t n_pages, const void* q, void* O, float* lse, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
+/* 4-bit weight matrices for products with a few token rows (the decode-time W_uv, W_a, W_b).  A row's weights share
+ * a bf16 scale per `group` columns: scale = bf16(max|w| / 7), codes w / scale rounded half to even and limited to
+ * -7..7; a group with a non-finite weight has the scale NaN.  codes and scales are laid out for the kernel.
+ * group is 32, 64 or 128; n_out a multiple of 16; k a multiple of 64 and of group. */
+typedef struct rk_w4 {
+  int32_t n_mat, n_out, k, group;
+  void* codes;    /* device, n_mat * n_out * k / 2 bytes, 16-byte aligned */
+  void* scales;   /* device, n_mat * n_out * (k / group) * 2 bytes, 16-byte aligned */
+} rk_w4;
+
+/* Lays out weights: w device bf16 [n_mat][n_out][k] -> w4->codes, w4->scales. */
+rk_status rk_quant4(rk_ctx* ctx, const void* w, const rk_w4* w4, void* stream);
+
+/* y[t][m] = W[m] x[t][m] for n_tok token rows; sums in fp32.
+ *   x  device bf16: token t at x + t * x_stride, [n_mat][k] (stride in elements, a multiple of 8, >= n_mat * k)
+ *   y  device bf16 (out_dtype 0) or fp32 (out_dtype 1): token t at y + t * y_stride, [n_mat][n_out] (>= n_mat * n_out) */
+rk_status rk_matvec4(rk_ctx* ctx, const rk_w4* w4, const void* x, int64_t x_stride, int64_t n_tok, void* y,
+                     int64_t y_stride, int32_t out_dtype, void* stream);
 
 #ifdef __cplusplus
 }

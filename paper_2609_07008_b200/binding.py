@@ -53,12 +53,31 @@ class rk_layer_io(C.Structure):
                                           "y_host")]
 
 
+class rk_cache4_table(C.Structure):
+    _fields_ = [("n_segs", C.c_int32), ("n_listed", C.c_int64), ("seg_len", C.c_void_p), ("page_off", C.c_void_p),
+                ("page_ids", C.c_void_p)]
+
+
+class rk_decode_shape(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("q_len", C.c_int32), ("n_items", C.c_int32), ("max_tiles", C.c_int32)]
+
+
+class rk_w4(C.Structure):
+    _fields_ = [("n_mat", C.c_int32), ("n_out", C.c_int32), ("k", C.c_int32), ("group", C.c_int32),
+                ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+CACHE4_PAGE_ROWS = 64
+CACHE4_PAGE_BYTES = 26624
+
 EXPORTS = ["rk_version", "rk_status_string", "rk_create", "rk_destroy", "rk_last_error", "rk_poll_status",
            "rk_create_ex", "rk_segmented_merge_phase", "rk_check_selftest", "rk_set_wait_limit_ms", "rk_test_starve_loads", "rk_request_create", "rk_request_destroy", "rk_check_request",
            "rk_request_get_info", "rk_workspace_bytes", "rk_relocate_q", "rk_mla_online_attn",
            "rk_segmented_merge", "rk_group_sliced_proj", "rk_group_sliced_proj_static", "rk_combine_offline",
            "rk_layer_host", "rk_layer_stack_host", "rk_mla_off_workspace_bytes", "rk_mla_off_build",
-           "rk_protected_rows_workspace_bytes", "rk_protected_rows", "rk_moe_fanout"]
+           "rk_protected_rows_workspace_bytes", "rk_protected_rows", "rk_moe_fanout",
+           "rk_cache4_append", "rk_cache4_read", "rk_decode_plan_bytes", "rk_decode_plan",
+           "rk_cache4_attn_workspace_bytes", "rk_cache4_attn", "rk_quant4", "rk_matvec4"]
 
 
 def _load() -> C.CDLL:
@@ -102,6 +121,15 @@ def _load() -> C.CDLL:
     lib.rk_protected_rows.argtypes = [vp, C.POINTER(rk_layout), C.POINTER(rk_policy), vp, i64, vp, vp, vp, vp,
                                       C.c_size_t, vp]
     lib.rk_moe_fanout.argtypes = [vp, vp, i64, C.c_float, i32, vp, vp, vp]
+    ptab, pshape, pw4 = C.POINTER(rk_cache4_table), C.POINTER(rk_decode_shape), C.POINTER(rk_w4)
+    lib.rk_cache4_append.argtypes = [vp, vp, i64, ptab, vp, i64, vp, i64, vp, i64, vp]
+    lib.rk_cache4_read.argtypes = [vp, vp, i64, ptab, vp, i64, vp, vp]
+    lib.rk_decode_plan_bytes.argtypes = [vp, pshape, C.POINTER(C.c_size_t)]
+    lib.rk_decode_plan.argtypes = [vp, pshape, ptab, i64, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.rk_cache4_attn_workspace_bytes.argtypes = [vp, pshape, C.POINTER(C.c_size_t)]
+    lib.rk_cache4_attn.argtypes = [vp, pshape, vp, C.c_size_t, vp, i64, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.rk_quant4.argtypes = [vp, vp, pw4, vp]
+    lib.rk_matvec4.argtypes = [vp, pw4, vp, i64, i64, vp, i64, i32, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int:  # default restype: rk_status
@@ -133,6 +161,50 @@ def _empty(shape, dtype, device):
 
 def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
+
+
+def _need(t: torch.Tensor, name: str, dtype, shape=None, contiguous=True) -> torch.Tensor:
+    """Type, shape, layout and device of one argument of a decode call (the C ABI sees pointers only)."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and (t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape))):
+        raise ValueError(f"{name} must have the shape {tuple('*' if w is None else w for w in shape)}, not {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device, not on {t.device}")
+    return t
+
+
+class CacheTable:
+    """Segments of a 4-bit paged cache and their pages: device int32 seg_len [S], page_off [S + 1], page_ids [n].
+    The tensors are used as they are at the time of each call; their contents may change between calls."""
+
+    def __init__(self, seg_len: torch.Tensor, page_off: torch.Tensor, page_ids: torch.Tensor):
+        self.seg_len = _need(seg_len, "seg_len", torch.int32, (None,))
+        self.page_off = _need(page_off, "page_off", torch.int32, (seg_len.numel() + 1,))
+        self.page_ids = _need(page_ids, "page_ids", torch.int32, (None,))
+        self.n_segs = seg_len.numel()
+
+    def struct(self) -> rk_cache4_table:
+        return rk_cache4_table(self.n_segs, self.page_ids.numel(), _ptr(self.seg_len), _ptr(self.page_off), _ptr(self.page_ids))
+
+
+class DecodePlan:
+    """Work list of one decode step (rk_decode_plan): shape, pool size and the device buffer."""
+
+    def __init__(self, shape: rk_decode_shape, n_pages: int, buf: torch.Tensor):
+        self.shape, self.n_pages, self.buf = shape, n_pages, buf
+
+
+class W4:
+    """4-bit weight matrices laid out by rk_quant4."""
+
+    def __init__(self, n_mat: int, n_out: int, k: int, group: int, codes: torch.Tensor, scales: torch.Tensor):
+        self.n_mat, self.n_out, self.k, self.group, self.codes, self.scales = n_mat, n_out, k, group, codes, scales
+
+    def struct(self) -> rk_w4:
+        return rk_w4(self.n_mat, self.n_out, self.k, self.group, _ptr(self.codes), _ptr(self.scales))
 
 
 def make_layout_struct(seg_off, seg_delta, seg_has_artifact):
@@ -339,6 +411,112 @@ class Context:
                                         _ptr(W_uv), _ptr(W_a), _ptr(z_off_rows), _ptr(workspace), workspace.numel(),
                                         _stream()))
         return z_off_rows
+
+    # -- decode -------------------------------------------------------------------------------
+    def rk_cache4_append(self, pages: torch.Tensor, table: CacheTable, c: torch.Tensor, k_rope: torch.Tensor,
+                         new_off: torch.Tensor):
+        """Rows new_off[s] .. new_off[s+1] of c [n, 512] and k_rope [n, 64] (before rotation) become the last rows of
+        segment s; table.seg_len already counts them.  pages: uint8 [n_pages, 26624].  Rows may be strided."""
+        n = c.shape[0]
+        _need(pages, "pages", torch.uint8, (None, CACHE4_PAGE_BYTES))
+        _need(c, "c", torch.bfloat16, (None, 512), contiguous=False)
+        _need(k_rope, "k_rope", torch.bfloat16, (n, 64), contiguous=False)
+        _need(new_off, "new_off", torch.int32, (table.n_segs + 1,))
+        if n > 0 and (c.stride(1) != 1 or k_rope.stride(1) != 1):
+            raise ValueError("the values of a row of c and k_rope must be contiguous")
+        tab = table.struct()
+        # a single row's stride is arbitrary and never used
+        self.check(lib.rk_cache4_append(self.handle, _ptr(pages), pages.shape[0], C.byref(tab), c.data_ptr(),
+                                        c.stride(0) if n > 1 else 512, k_rope.data_ptr(), k_rope.stride(0) if n > 1 else 64,
+                                        _ptr(new_off), n, _stream()))
+
+    def rk_cache4_read(self, pages: torch.Tensor, table: CacheTable, row_off: torch.Tensor, n_rows: int, kv=None) -> torch.Tensor:
+        """The last row_off[s+1] - row_off[s] rows of every segment s as packed bf16 rows kv [n_rows, 576]; rows from
+        row_off[n_segs] on are left as they were."""
+        _need(pages, "pages", torch.uint8, (None, CACHE4_PAGE_BYTES))
+        _need(row_off, "row_off", torch.int32, (table.n_segs + 1,))
+        if kv is None:
+            kv = _empty((n_rows, 576), dtype=torch.bfloat16, device=pages.device)
+        _need(kv, "kv", torch.bfloat16, (n_rows, 576))
+        tab = table.struct()
+        self.check(lib.rk_cache4_read(self.handle, _ptr(pages), pages.shape[0], C.byref(tab), _ptr(row_off), n_rows, _ptr(kv),
+                                      _stream()))
+        return kv
+
+    def rk_decode_plan(self, table: CacheTable, n_pages: int, seq_off: torch.Tensor, item_seg: torch.Tensor,
+                       item_delta: torch.Tensor, q_pos: torch.Tensor, *, max_tiles: int, plan: Optional[DecodePlan] = None) -> DecodePlan:
+        """Work list of a decode step: request b sees the segments item_seg[seq_off[b]:seq_off[b+1]] at the request offsets
+        item_delta; q_pos [n_seqs, q_len] are its query tokens' positions.  max_tiles bounds the sum over the items of
+        ceil(rows / 128).  With plan= its buffer is filled anew (a captured graph keeps using it)."""
+        _need(q_pos, "q_pos", torch.int32, (None, None))
+        _need(seq_off, "seq_off", torch.int32, (q_pos.shape[0] + 1,))
+        _need(item_seg, "item_seg", torch.int32, (None,))
+        _need(item_delta, "item_delta", torch.int32, (item_seg.numel(),))
+        shape = rk_decode_shape(q_pos.shape[0], q_pos.shape[1], item_seg.numel(), int(max_tiles))
+        need = C.c_size_t(0)
+        self.check(lib.rk_decode_plan_bytes(self.handle, C.byref(shape), C.byref(need)))
+        if plan is None:
+            plan = DecodePlan(shape, int(n_pages), _empty(need.value, dtype=torch.uint8, device=q_pos.device))
+        else:
+            plan.shape, plan.n_pages = shape, int(n_pages)
+            _need(plan.buf, "plan.buf", torch.uint8, (None,))
+        tab = table.struct()
+        self.check(lib.rk_decode_plan(self.handle, C.byref(shape), C.byref(tab), int(n_pages), _ptr(seq_off), _ptr(item_seg),
+                                      _ptr(item_delta), _ptr(q_pos), _ptr(plan.buf), plan.buf.numel(), _stream()))
+        return plan
+
+    def rk_cache4_attn(self, pages: torch.Tensor, plan: DecodePlan, q: torch.Tensor, O=None, lse=None, workspace=None):
+        """q [n_seqs, q_len, n_heads, 576] -> (O [n_seqs, q_len, n_heads, 512] bf16, lse fp32)."""
+        sh = plan.shape
+        rows = (sh.n_seqs, sh.q_len, self.n_heads)
+        _need(pages, "pages", torch.uint8, (None, CACHE4_PAGE_BYTES))
+        _need(q, "q", torch.bfloat16, rows + (576,))
+        if O is None:
+            O = _empty(rows + (512,), dtype=torch.bfloat16, device=q.device)
+        if lse is None:
+            lse = _empty(rows, dtype=torch.float32, device=q.device)
+        _need(O, "O", torch.bfloat16, rows + (512,))
+        _need(lse, "lse", torch.float32, rows)
+        if workspace is None:
+            need = C.c_size_t(0)
+            self.check(lib.rk_cache4_attn_workspace_bytes(self.handle, C.byref(sh), C.byref(need)))
+            workspace = _empty(need.value, dtype=torch.uint8, device=q.device)
+        _need(workspace, "workspace", torch.uint8, (None,))
+        self.check(lib.rk_cache4_attn(self.handle, C.byref(sh), _ptr(plan.buf), plan.buf.numel(), _ptr(pages), pages.shape[0],
+                                      _ptr(q), _ptr(O), _ptr(lse), _ptr(workspace), workspace.numel(), _stream()))
+        return O, lse
+
+    def rk_quant4(self, w: torch.Tensor, group: int, w4: Optional[W4] = None) -> W4:
+        """Lays out w [n_mat, n_out, k] bf16 as 4-bit codes with one bf16 scale per `group` columns of a row."""
+        _need(w, "w", torch.bfloat16, (None, None, None))
+        n_mat, n_out, k = w.shape
+        if w4 is None:
+            n = w.numel()
+            w4 = W4(n_mat, n_out, k, int(group), _empty(max(n // 2, 16), dtype=torch.uint8, device=w.device),
+                    _empty(max(n // max(int(group), 1), 8), dtype=torch.bfloat16, device=w.device))
+        elif (w4.n_mat, w4.n_out, w4.k, w4.group) != (n_mat, n_out, k, int(group)):
+            raise ValueError("w4 has another shape")
+        st = w4.struct()
+        self.check(lib.rk_quant4(self.handle, _ptr(w), C.byref(st), _stream()))
+        return w4
+
+    def rk_matvec4(self, w4: W4, x: torch.Tensor, y: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
+        """x [n_tok, n_mat, k] bf16 (tokens may be strided) -> y [n_tok, n_mat, n_out], bf16 or float32."""
+        n = x.shape[0]
+        _need(x, "x", torch.bfloat16, (None, w4.n_mat, w4.k), contiguous=False)
+        _need(w4.codes, "w4.codes", torch.uint8)
+        _need(w4.scales, "w4.scales", torch.bfloat16)
+        if y is None:
+            y = _empty((n, w4.n_mat, w4.n_out), dtype=out_dtype, device=x.device)
+        _need(y, "y", y.dtype, (n, w4.n_mat, w4.n_out), contiguous=False)
+        for t, name in ((x, "x"), (y, "y")):
+            if n > 0 and not t[0].is_contiguous():
+                raise ValueError(f"the values of a token of {name} must be contiguous")
+        dt = {torch.bfloat16: 0, torch.float32: 1}[y.dtype]
+        st = w4.struct()
+        self.check(lib.rk_matvec4(self.handle, C.byref(st), x.data_ptr(), x.stride(0) if n > 1 else w4.n_mat * w4.k, n, y.data_ptr(),
+                                  y.stride(0) if n > 1 else w4.n_mat * w4.n_out, dt, _stream()))
+        return y
 
     def alloc_layer_buffers(self, req, device) -> dict:
         G, L, T, A = self.n_groups, self.n_local, req.T, req.A

@@ -1,0 +1,371 @@
+// The 4-bit paged latent cache of the decode step: appending new rows (key rotation and quantisation on the
+// way), reading rows back as the packed bf16 stream of the online step, and the plan that the single-token
+// attention over the cache (rk_decode.cu) walks.
+//
+// A cached row is 416 bytes instead of 1152: 512 latent dims as 4-bit codes n in -7..7 (stored as n + 8) with one
+// 8-bit scale per 16 dims, and the 64 rope dims in bf16 (the rotated key is what positions hang on).  A scale has
+// four significant bits, a code three, so every value n * s has seven and IS a bf16 number: the attention's tensor
+// cores take it without a further rounding.  Pages hold 64 rows, unit-major: 26 units of 16 bytes, each a
+// contiguous 1 KB block of 64 rows, so that a warp whose lanes are rows reads 512 contiguous bytes per load.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include "rk_internal.h"
+
+namespace rk {
+namespace {
+
+constexpr int kRowsPerBlock = 32;                 // rows staged per block: 8 warps x 4 rows
+constexpr int kUnitStride = kRowsPerBlock * 16 + 16;  // padded: the lanes of a warp write 16 different units
+
+// Largest s in [0, n) with off[s] <= i, found by all lanes of a warp together, 32 probes per round: two dependent
+// loads for up to 1024 segments where a binary search takes ten.
+__device__ __forceinline__ int warp_find_segment(const int32_t* __restrict__ off, int n, int i) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, len = n;  // the answer is in [lo, lo + len)
+  while (len > 1) {
+    const int step = (len + 31) >> 5;
+    const int at = lo + lane * step;
+    const bool le = at < lo + len && __ldg(off + at) <= i;
+    const unsigned b = __ballot_sync(0xffffffffu, le);
+    const int k = b == 0u ? 0 : 31 - __clz((int)b);
+    const int end = lo + len;
+    lo += k * step;
+    len = min(step, end - lo);
+  }
+  return lo;
+}
+
+// Page-relative byte address of row i of a ragged batch (the last off[s+1] - off[s] rows of every segment s), or -1.
+// Rows beyond off[n_segs] are no rows of the batch and are skipped silently; whatever the tables say is bounds
+// checked, a bad entry is reported and its row skipped.
+__device__ __forceinline__ int64_t row_address(const Cache4Table& t, const int32_t* __restrict__ off, int64_t i, int64_t n_pages,
+                                               DeviceStatus* st, int* index_in_segment) {
+  *index_in_segment = 0;
+  if (t.n_segs == 0 || i >= __ldg(off + t.n_segs)) return -1;
+  const int s = warp_find_segment(off, t.n_segs, (int)i);
+  const int o0 = __ldg(off + s), o1 = __ldg(off + s + 1), len = __ldg(t.seg_len + s);
+  const int p0 = __ldg(t.page_off + s), p1 = __ldg(t.page_off + s + 1);
+  const long long j = (long long)len - ((long long)o1 - o0) + (i - o0);
+  const long long pi = (long long)p0 + (j >> 6);
+  if (i < o0 || j < 0 || j >= len || p0 < 0 || pi >= p1 || pi >= t.n_listed) {
+    if ((threadIdx.x & 31) == 0) report_status(st, 4 /*RK_ERR_ROWS*/, RK_CHK_CACHE_ROW, (int)i);
+    return -1;
+  }
+  const int page = __ldg(t.page_ids + pi);
+  if (page < 0 || page >= n_pages) {
+    if ((threadIdx.x & 31) == 0) report_status(st, 4 /*RK_ERR_ROWS*/, RK_CHK_CACHE_PAGE, page);
+    return -1;
+  }
+  *index_in_segment = (int)j;
+  return (int64_t)page * kCache4PageBytes + (j & 63) * 16;
+}
+
+// 32 rows per block.  Lane g of a warp owns scale group g of a row (16 dims, 32 contiguous bytes), so the group's
+// maximum never leaves the lane.  The finished units are staged in shared memory and leave with the row index
+// running fastest: consecutive rows of a page are consecutive 16-byte pieces.
+// Rounding: x * (1 / s) may sit a hair beside a tie; no quotient of an 8-bit and a 4-bit significand lies closer
+// than 2^-9 to a half-integer without being one, so snapping it to multiples of 2^-11 (adding and subtracting
+// 6144) restores exact ties, and the result is round-half-even of the true quotient.
+// Bound by HBM (1152 bytes in, 416 out per row).  Measured: see the table of the decode operators.
+__global__ void __launch_bounds__(256) cache4_append_kernel(uint8_t* __restrict__ pages, int64_t n_pages, Cache4Table tab,
+                                                            const __nv_bfloat16* __restrict__ c, int64_t c_stride,
+                                                            const __nv_bfloat16* __restrict__ kr, int64_t r_stride,
+                                                            const int32_t* __restrict__ new_off, int64_t n_new,
+                                                            RopeTurns rope, DeviceStatus* status) {
+  __shared__ __align__(16) uint8_t stage[kCache4Units * kUnitStride];
+  __shared__ int64_t addr[kRowsPerBlock];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row0 = (int64_t)blockIdx.x * kRowsPerBlock + warp * 4;
+  // all loads of the warp's four rows first; the segment search runs under them
+  uint4 x[4][2];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    x[r][0] = x[r][1] = make_uint4(0, 0, 0, 0);
+    if (row0 + r < n_new) {
+      const uint4* src = reinterpret_cast<const uint4*>(c + (row0 + r) * c_stride + lane * 16);
+      x[r][0] = __ldcs(src);
+      x[r][1] = __ldcs(src + 1);
+    }
+  }
+  const int rr = lane >> 3, rc = lane & 7;  // rope: lane covers 8 dims of one of the four rows
+  uint4 xr = make_uint4(0, 0, 0, 0);
+  if (row0 + rr < n_new) xr = __ldcs(reinterpret_cast<const uint4*>(kr + (row0 + rr) * r_stride + rc * 8));
+  int my_j = 0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    int j = 0;
+    int64_t a = -1;
+    if (row0 + r < n_new) a = row_address(tab, new_off, row0 + r, n_pages, status, &j);
+    if (lane == 0) addr[warp * 4 + r] = a;
+    if (rr == r) my_j = j;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const uint32_t w[8] = {x[r][0].x, x[r][0].y, x[r][0].z, x[r][0].w, x[r][1].x, x[r][1].y, x[r][1].z, x[r][1].w};
+    uint32_t mx = 0u;  // two 15-bit magnitudes at a time: bf16 orders like its bits
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mx = __vmaxu2(mx, w[e] & 0x7fff7fffu);
+    const uint32_t top = max(mx & 0xffffu, mx >> 16);
+    const bool finite = top < 0x7f80u;
+    const float t = __fdiv_rn(__uint_as_float(top << 16), 7.0f);
+    uint32_t u = __float_as_uint(t);
+    u += 0x7ffffu + ((u >> 20) & 1u);  // round to four significant bits, ties to even
+    int code = (int)(u >> 20) - (107 << 3);
+    code = finite ? min(max(code, 0), 254) : 255;
+    const float inv = __fdiv_rn(1.0f, __uint_as_float((uint32_t)(code + (107 << 3)) << 20));
+    uint32_t q[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const uint32_t word = w[e >> 1];
+      const float v = __uint_as_float((e & 1) ? (word & 0xffff0000u) : (word << 16));
+      float y = fminf(fmaxf(v * inv, -7.0f), 7.0f);
+      y = __fadd_rn(__fadd_rn(y, 6144.0f), -6144.0f);
+      q[e] = __float_as_uint(__fadd_rn(y, 12582920.0f)) & 15u;  // 1.5 * 2^23 + 8: the low bits are n + 8
+    }
+    uint2 out;
+    out.x = q[0] | q[2] << 4 | q[4] << 8 | q[6] << 12 | q[1] << 16 | q[3] << 20 | q[5] << 24 | q[7] << 28;
+    out.y = q[8] | q[10] << 4 | q[12] << 8 | q[14] << 12 | q[9] << 16 | q[11] << 20 | q[13] << 24 | q[15] << 28;
+    const int row = warp * 4 + r;
+    *reinterpret_cast<uint2*>(stage + (lane >> 1) * kUnitStride + row * 16 + (lane & 1) * 8) = out;
+    stage[(16 + ((lane >> 2) & 1)) * kUnitStride + row * 16 + 4 * (lane >> 3) + (lane & 3)] = (uint8_t)code;
+  }
+  {  // R(j): the stored key is in the position-zero frame of its segment
+    const uint32_t in[4] = {xr.x, xr.y, xr.z, xr.w};
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float cs, sn;
+      rope_cos_sin(rope, my_j, 4 * rc + e, cs, sn);
+      const float x0 = __uint_as_float(in[e] << 16), x1 = __uint_as_float(in[e] & 0xffff0000u);
+      o[e] = pack_bf16(x0 * cs - x1 * sn, x0 * sn + x1 * cs);
+    }
+    *reinterpret_cast<uint4*>(stage + (18 + rc) * kUnitStride + (warp * 4 + rr) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
+  __syncthreads();
+  for (int idx = threadIdx.x; idx < kCache4Units * kRowsPerBlock; idx += 256) {
+    const int unit = idx >> 5, row = idx & 31;
+    const int64_t a = addr[row];
+    if (a >= 0) *reinterpret_cast<uint4*>(pages + a + unit * 1024) = *reinterpret_cast<const uint4*>(stage + unit * kUnitStride + row * 16);
+  }
+}
+
+// The way back: 32 rows per block, units in with the row index running fastest, 16-byte pieces of bf16 rows out with
+// the column running fastest.  A 32-bit word holds the codes of one 16-byte output piece.
+__global__ void __launch_bounds__(256) cache4_read_kernel(const uint8_t* __restrict__ pages, int64_t n_pages, Cache4Table tab,
+                                                          const int32_t* __restrict__ row_off, int64_t n_rows,
+                                                          __nv_bfloat16* __restrict__ kv, DeviceStatus* status) {
+  __shared__ __align__(16) uint8_t stage[kCache4Units * kUnitStride];
+  __shared__ int64_t addr[kRowsPerBlock];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row0 = (int64_t)blockIdx.x * kRowsPerBlock;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    int j;
+    int64_t a = -1;
+    if (row0 + warp * 4 + r < n_rows) a = row_address(tab, row_off, row0 + warp * 4 + r, n_pages, status, &j);
+    if (lane == 0) addr[warp * 4 + r] = a;
+  }
+  __syncthreads();
+  for (int idx = threadIdx.x; idx < kCache4Units * kRowsPerBlock; idx += 256) {
+    const int unit = idx >> 5, row = idx & 31;
+    const int64_t a = addr[row];
+    if (a >= 0) *reinterpret_cast<uint4*>(stage + unit * kUnitStride + row * 16) = __ldcs(reinterpret_cast<const uint4*>(pages + a + unit * 1024));
+  }
+  __syncthreads();
+  for (int idx = threadIdx.x; idx < 72 * kRowsPerBlock; idx += 256) {
+    const int row = idx / 72, piece = idx - row * 72;
+    if (addr[row] < 0) continue;
+    uint4 o;
+    if (piece < 64) {  // latent dims 8 piece .. 8 piece + 7: word piece & 3 of unit piece >> 2, scale group piece >> 1
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(stage + (piece >> 2) * kUnitStride + row * 16 + (piece & 3) * 4);
+      const int g = piece >> 1;
+      const uint32_t s = cache4_scale(stage[(16 + ((g >> 2) & 1)) * kUnitStride + row * 16 + 4 * (g >> 3) + (g & 3)]);
+      o = cache4_dequant(v, s);
+    } else {
+      o = *reinterpret_cast<const uint4*>(stage + (18 + piece - 64) * kUnitStride + row * 16);
+    }
+    __stcs(reinterpret_cast<uint4*>(kv + (row0 + row) * kDQK + piece * 8), o);
+  }
+}
+
+// ---- plan -------------------------------------------------------------------------------------------------
+// Pass 1 (one block): key tiles of every item (a segment in a sequence) and their running sum.
+constexpr int kPlanThreads = 1024;
+
+__global__ void __launch_bounds__(kPlanThreads) decode_plan_scan_kernel(DecodePlanArgs a) {
+  __shared__ int warp_sums[32];
+  __shared__ long long carry;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) carry = 0;
+  for (int i = tid; i < a.n_seqs * a.q_len; i += kPlanThreads) a.pos_out[i] = a.q_pos[i];
+  __syncthreads();
+  for (int base = 0; base < a.n_items; base += kPlanThreads) {
+    const int i = base + tid;
+    int n = 0;
+    if (i < a.n_items) {
+      int lo = 0, hi = a.n_seqs - 1;  // largest b with seq_off[b] <= i
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__ldg(a.seq_off + mid) <= i) lo = mid; else hi = mid - 1;
+      }
+      const bool listed = __ldg(a.seq_off + lo) <= i && i < __ldg(a.seq_off + lo + 1);
+      const int seg = a.item_seg[i];
+      if (seg < 0 || seg >= a.tab.n_segs) {
+        if (listed) report_status(a.status, 4, RK_CHK_PLAN_ITEM, i);
+      } else if (listed) {
+        int pmax = -1;
+        for (int t = 0; t < a.q_len; ++t) pmax = max(pmax, a.q_pos[lo * a.q_len + t]);
+        const int delta = a.item_delta[i], len = a.tab.seg_len[seg];
+        const int p0 = a.tab.page_off[seg], p1 = a.tab.page_off[seg + 1];
+        long long seen = (long long)pmax - delta + 1;
+        seen = seen < 0 ? 0 : (seen < len ? seen : len);
+        const long long np = (seen + 63) >> 6;
+        if (delta < 0 || len < 0 || p0 < 0 || (seen > 0 && (p0 + np > p1 || p0 + np > a.tab.n_listed)) ||
+            (long long)delta + len > (1ll << 30)) {
+          report_status(a.status, 4, RK_CHK_PLAN_ITEM, i);
+        } else {
+          // one tile more than fits is as good as any larger number, and keeps the block's sum inside 32 bits
+          n = (int)min((seen + 127) >> 7, (long long)a.max_tiles + 1);
+        }
+      }
+    }
+    int v = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += y;
+    }
+    if (lane == 31) warp_sums[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+      int s = warp_sums[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += y;
+      }
+      warp_sums[lane] = s;
+    }
+    __syncthreads();
+    const long long before = carry + (warp ? warp_sums[warp - 1] : 0) + v - n;
+    if (i < a.n_items) a.item_tile[i] = (int)(before < 0x7fffffff ? before : 0x7fffffff);
+    __syncthreads();
+    if (tid == kPlanThreads - 1) carry = before + n;
+    __syncthreads();
+  }
+  const long long total = carry;
+  const bool fits = total <= a.max_tiles;
+  if (tid == 0) {
+    if (!fits) report_status(a.status, 6 /*RK_ERR_WORKSPACE*/, RK_CHK_PLAN_ITEM, (int)total);
+    a.item_tile[a.n_items] = fits ? (int)total : 0;
+    DecodePlanHeader h = {};
+    h.magic = kDecodePlanMagic;
+    h.n_seqs = a.n_seqs;
+    h.q_len = a.q_len;
+    h.n_items = a.n_items;
+    h.max_tiles = a.max_tiles;
+    h.n_heads = a.n_heads;
+    h.n_pages = a.n_pages;
+    h.n_tiles = fits ? (int)total : 0;
+    const long long work = (long long)h.n_tiles * a.n_row_tiles;
+    h.chunk = (int)((work + a.n_ctas - 1) / a.n_ctas);
+    if (h.chunk < 1) h.chunk = 1;
+    *a.header = h;
+  }
+  __syncthreads();
+  for (int b = tid; b <= a.n_seqs; b += kPlanThreads) {
+    const int at = a.seq_off[b];
+    const bool ok = at >= 0 && at <= a.n_items && (b == 0 || at >= a.seq_off[b - 1]);
+    if (!ok) report_status(a.status, 4, RK_CHK_PLAN_ITEM, b);
+    // a malformed list makes an empty plan: the running sum below must never decrease
+    if (!ok) a.header->n_tiles = 0;
+  }
+  __syncthreads();
+  __threadfence_block();
+  const bool empty = *(volatile int*)&a.header->n_tiles == 0;
+  for (int b = tid; b <= a.n_seqs; b += kPlanThreads) a.seq_tile[b] = empty ? 0 : a.item_tile[a.seq_off[b]];
+}
+
+// Pass 2: one thread per key tile; the first threads also find where every CTA of the attention starts.
+__global__ void __launch_bounds__(256) decode_plan_fill_kernel(DecodePlanArgs a) {
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  const int n_tiles = a.header->n_tiles;
+  if (t < a.n_ctas) {
+    const long long w = (long long)t * a.header->chunk;
+    int4 start = make_int4(0, 0, 0, 0);
+    if (w < (long long)n_tiles * a.n_row_tiles) {
+      int lo = 0, hi = a.n_seqs - 1;  // largest b with n_row_tiles * seq_tile[b] <= w
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((long long)a.seq_tile[mid] * a.n_row_tiles <= w) lo = mid; else hi = mid - 1;
+      }
+      const int n_b = a.seq_tile[lo + 1] - a.seq_tile[lo];
+      const long long rest = w - (long long)a.seq_tile[lo] * a.n_row_tiles;
+      start = make_int4(lo, (int)(rest / n_b), (int)(rest % n_b), 1);
+    }
+    a.cta_start[t] = start;
+  }
+  if (t >= n_tiles) return;
+  int lo = 0, hi = a.n_items - 1;  // largest i with item_tile[i] <= t: the last of equal entries owns the tile
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.item_tile[mid] <= t) lo = mid; else hi = mid - 1;
+  }
+  int b = 0, bh = a.n_seqs - 1;
+  while (b < bh) {
+    const int mid = (b + bh + 1) >> 1;
+    if (a.seq_off[mid] <= lo) b = mid; else bh = mid - 1;
+  }
+  int pmax = -1;
+  for (int k = 0; k < a.q_len; ++k) pmax = max(pmax, a.pos_out[b * a.q_len + k]);
+  const int seg = a.item_seg[lo], delta = a.item_delta[lo];
+  const int j0 = (t - a.item_tile[lo]) * kDecodeKeys;
+  const int seen = min(a.tab.seg_len[seg], pmax - delta + 1);
+  const int n = min(seen - j0, kDecodeKeys);
+  const int p0 = a.tab.page_off[seg] + (j0 >> 6);
+  DecodeTile rec;
+  rec.page0 = a.tab.page_ids[p0];
+  rec.page1 = n > 64 ? a.tab.page_ids[p0 + 1] : rec.page0;
+  rec.base = delta + j0;
+  rec.n = n;
+  if (rec.page0 < 0 || rec.page0 >= a.n_pages || rec.page1 < 0 || rec.page1 >= a.n_pages) {
+    report_status(a.status, 4, RK_CHK_CACHE_PAGE, (rec.page0 < 0 || rec.page0 >= a.n_pages) ? rec.page0 : rec.page1);
+    rec.page0 = rec.page1 = rec.n = 0;  // no row of the tile is read; its keys count as unseen
+  }
+  rec.delta = delta;
+  rec.pad[0] = rec.pad[1] = rec.pad[2] = 0;
+  a.tiles[t] = rec;
+}
+
+}  // namespace
+
+cudaError_t launch_cache4_append(void* pages, int64_t n_pages, const Cache4Table& tab, const void* c, int64_t c_stride,
+                                 const void* k_rope, int64_t r_stride, const int32_t* new_off, int64_t n_new,
+                                 const RopeTurns& rope, DeviceStatus* status, cudaStream_t stream) {
+  const int64_t blocks = (n_new + kRowsPerBlock - 1) / kRowsPerBlock;
+  cache4_append_kernel<<<(unsigned)blocks, 256, 0, stream>>>(static_cast<uint8_t*>(pages), n_pages, tab,
+                                                             static_cast<const __nv_bfloat16*>(c), c_stride,
+                                                             static_cast<const __nv_bfloat16*>(k_rope), r_stride, new_off, n_new,
+                                                             rope, status);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_cache4_read(const void* pages, int64_t n_pages, const Cache4Table& tab, const int32_t* row_off, int64_t n_rows,
+                               void* kv, DeviceStatus* status, cudaStream_t stream) {
+  const int64_t blocks = (n_rows + kRowsPerBlock - 1) / kRowsPerBlock;
+  cache4_read_kernel<<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const uint8_t*>(pages), n_pages, tab, row_off, n_rows,
+                                                           static_cast<__nv_bfloat16*>(kv), status);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_decode_plan(const DecodePlanArgs& a, cudaStream_t stream) {
+  decode_plan_scan_kernel<<<1, kPlanThreads, 0, stream>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  const int n = a.max_tiles > a.n_ctas ? a.max_tiles : a.n_ctas;
+  decode_plan_fill_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace rk

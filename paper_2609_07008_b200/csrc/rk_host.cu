@@ -271,6 +271,7 @@ rk_status rk_create_ex(const rk_profile* prof, uint32_t flags, rk_ctx** out) {
   if (e == cudaSuccess) e = gemm_setup();
   if (e == cudaSuccess) e = stream_setup();
   if (e == cudaSuccess) e = proj_fused_setup();
+  if (e == cudaSuccess) e = decode_attn_setup();
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&ctx->d_status), sizeof(DeviceStatus));
   if (e == cudaSuccess) e = cudaMemset(ctx->d_status, 0, sizeof(DeviceStatus));
   if (e != cudaSuccess) {
@@ -377,8 +378,18 @@ rk_status rk_poll_status(rk_ctx* ctx, void* stream) {
   if (e != cudaSuccess) return cuda_fail(ctx, e, "status readback");
   if (h.code != 0) {
     cudaMemset(ctx->d_status, 0, sizeof(DeviceStatus));
-    if (h.code == RK_ERR_ROWS)  // only the bounds-checked build reports this
+    if (h.code == RK_ERR_ROWS && h.where < RK_CHK_CACHE_ROW)  // only the bounds-checked build reports this
       return fail(ctx, RK_ERR_ROWS, "device index check failed: table %d, block %d, value %d", h.where, h.block, h.aux);
+    switch (h.where) {  // the decode calls check their device tables in every build
+      case RK_CHK_CACHE_ROW:
+        return fail(ctx, RK_ERR_ROWS, "cache row %d: its segment's length, row range and page list do not fit together", h.aux);
+      case RK_CHK_CACHE_PAGE: return fail(ctx, RK_ERR_ROWS, "page id %d is outside the pool", h.aux);
+      case RK_CHK_PLAN_ITEM:
+        if (h.code == RK_ERR_WORKSPACE) return fail(ctx, RK_ERR_WORKSPACE, "the decode step has %d key tiles, more than max_tiles", h.aux);
+        return fail(ctx, RK_ERR_ROWS, "decode plan: entry %d is invalid", h.aux);
+      case RK_CHK_PLAN_MATCH:
+        return fail(ctx, RK_ERR_LAYOUT, "the plan was not made by rk_decode_plan for this shape, head count and number of pages");
+    }
     return fail(ctx, RK_ERR_TIMEOUT, "device wait expired: tag %d, block %d, aux %d", h.where, h.block, h.aux);
   }
   return RK_OK;
@@ -1133,6 +1144,285 @@ rk_status rk_moe_fanout(rk_ctx* ctx, const float* p, int64_t n, float tau, int32
   cudaError_t e = launch_moe_fanout(p, n, tau, fence != 0, k_out, keep_out, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(ctx, e, "fan-out kernel");
   return RK_OK;
+}
+
+// ------------------------------------------------------------------------------------------
+// Decode: 4-bit paged latent cache, attention over it, 4-bit matrix-vector products
+
+// what every decode call needs: the context's device is current, values are the 512-wide latent
+static rk_status decode_check(rk_ctx* ctx) {
+  int device = -1;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "cudaGetDevice");
+  if (device != ctx->device) return fail(ctx, RK_ERR_CUDA, "the context's device is not current");
+  if (ctx->value_phase) return fail(ctx, RK_ERR_UNSUPPORTED, "the decode calls need a context without RK_VALUE_PHASE");
+  return RK_OK;
+}
+
+static rk_status cache_check(rk_ctx* ctx, const void* pages, int64_t n_pages, const rk_cache4_table* tab, Cache4Table* out) {
+  if (!tab) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (n_pages < 0 || n_pages > 0x7fffffff || tab->n_segs < 0 || tab->n_listed < 0)
+    return fail(ctx, RK_ERR_LAYOUT, "negative or too large page, segment or list count");
+  if ((n_pages > 0 && !pages) || (tab->n_segs > 0 && (!tab->seg_len || !tab->page_off)) || (tab->n_listed > 0 && !tab->page_ids))
+    return fail(ctx, RK_ERR_NULL, "null argument");
+  if (!aligned16(pages)) return fail(ctx, RK_ERR_ALIGN, "pages must be 16-byte aligned");
+  out->seg_len = tab->seg_len;
+  out->page_off = tab->page_off;
+  out->page_ids = tab->page_ids;
+  out->n_listed = tab->n_listed;
+  out->n_segs = tab->n_segs;
+  return RK_OK;
+}
+
+static RopeTurns rope_turns_of(const rk_ctx* ctx) {
+  RopeTurns r;
+  memcpy(r.t, ctx->rope_turns, sizeof(r.t));
+  return r;
+}
+
+rk_status rk_cache4_append(rk_ctx* ctx, void* pages, int64_t n_pages, const rk_cache4_table* table, const void* c,
+                           int64_t c_stride, const void* k_rope, int64_t r_stride, const int32_t* new_off, int64_t n_new,
+                           void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  Cache4Table tab;
+  rk_status s = cache_check(ctx, pages, n_pages, table, &tab);
+  if (s != RK_OK) return s;
+  if (n_new < 0 || n_new >= ((int64_t)1 << 30)) return fail(ctx, RK_ERR_ROWS, "n_new out of range");
+  if (n_new > 0 && (!c || !k_rope || !new_off)) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (n_new > 0 && (c_stride < kDLatent || r_stride < kDRope)) return fail(ctx, RK_ERR_LAYOUT, "row strides smaller than a row");
+  if (!aligned16(c) || !aligned16(k_rope) || c_stride % 8 != 0 || r_stride % 8 != 0)
+    return fail(ctx, RK_ERR_ALIGN, "c and k_rope must be 16-byte aligned and their strides multiples of 8 elements");
+  s = decode_check(ctx);
+  if (s != RK_OK || n_new == 0) return s;
+  cudaError_t e = launch_cache4_append(pages, n_pages, tab, c, c_stride, k_rope, r_stride, new_off, n_new, rope_turns_of(ctx),
+                                       ctx->d_status, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "cache append launch");
+}
+
+rk_status rk_cache4_read(rk_ctx* ctx, const void* pages, int64_t n_pages, const rk_cache4_table* table,
+                         const int32_t* row_off, int64_t n_rows, void* kv, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  Cache4Table tab;
+  rk_status s = cache_check(ctx, pages, n_pages, table, &tab);
+  if (s != RK_OK) return s;
+  if (n_rows < 0 || n_rows >= ((int64_t)1 << 30)) return fail(ctx, RK_ERR_ROWS, "n_rows out of range");
+  if (n_rows > 0 && (!kv || !row_off)) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (!aligned16(kv)) return fail(ctx, RK_ERR_ALIGN, "kv must be 16-byte aligned");
+  s = decode_check(ctx);
+  if (s != RK_OK || n_rows == 0) return s;
+  cudaError_t e = launch_cache4_read(pages, n_pages, tab, row_off, n_rows, kv, ctx->d_status, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "cache read launch");
+}
+
+static rk_status shape_check(const rk_ctx* ctx, const rk_decode_shape* sh) {
+  if (!sh) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (sh->n_seqs < 0 || sh->q_len <= 0 || sh->q_len > 64 || sh->n_items < 0 || sh->n_items > (1 << 28) || sh->max_tiles < 0 ||
+      sh->max_tiles > (1 << 20))
+    return fail(ctx, RK_ERR_LAYOUT, "decode shape out of range: %d sequences, %d query tokens, %d items, %d tiles", sh->n_seqs,
+                sh->q_len, sh->n_items, sh->max_tiles);
+  if ((int64_t)sh->n_seqs * sh->q_len * ctx->prof.n_heads >= ((int64_t)1 << 31) - 256)
+    return fail(ctx, RK_ERR_LAYOUT, "query rows x heads of one call must stay below 2^31 - 256");
+  return RK_OK;
+}
+
+// The parts of a plan buffer, each 256-byte aligned; null base: only the size is of interest.
+struct PlanView {
+  DecodePlanHeader* header;
+  int4* cta_start;
+  int32_t *pos, *seq_tile, *item_tile;
+  DecodeTile* tiles;
+  size_t bytes;
+};
+static PlanView plan_view(const rk_ctx* ctx, const rk_decode_shape* sh, const void* base) {
+  PlanView v;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return reinterpret_cast<uintptr_t>(base) + here;
+  };
+  v.header = reinterpret_cast<DecodePlanHeader*>(take(sizeof(DecodePlanHeader)));
+  v.cta_start = reinterpret_cast<int4*>(take((size_t)ctx->sm_count * sizeof(int4)));
+  v.pos = reinterpret_cast<int32_t*>(take((size_t)sh->n_seqs * sh->q_len * 4));
+  v.seq_tile = reinterpret_cast<int32_t*>(take((size_t)(sh->n_seqs + 1) * 4));
+  v.item_tile = reinterpret_cast<int32_t*>(take((size_t)(sh->n_items + 1) * 4));
+  v.tiles = reinterpret_cast<DecodeTile*>(take((size_t)sh->max_tiles * sizeof(DecodeTile)));
+  v.bytes = at;
+  return v;
+}
+static int decode_row_tiles(const rk_ctx* ctx, const rk_decode_shape* sh) {
+  const int rows = sh->q_len * ctx->prof.n_heads, tile = decode_row_tile(rows);
+  return (rows + tile - 1) / tile;
+}
+
+rk_status rk_decode_plan_bytes(const rk_ctx* ctx, const rk_decode_shape* shape, size_t* out) {
+  if (!ctx || !out) return RK_ERR_NULL;
+  rk_status s = shape_check(ctx, shape);
+  if (s != RK_OK) return s;
+  *out = plan_view(ctx, shape, nullptr).bytes;
+  return RK_OK;
+}
+
+rk_status rk_decode_plan(rk_ctx* ctx, const rk_decode_shape* shape, const rk_cache4_table* table, int64_t n_pages,
+                         const int32_t* seq_off, const int32_t* item_seg, const int32_t* item_delta, const int32_t* q_pos,
+                         void* plan, size_t plan_bytes, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  rk_status s = shape_check(ctx, shape);
+  if (s != RK_OK) return s;
+  Cache4Table tab;
+  s = cache_check(ctx, nullptr, 0, table, &tab);
+  if (s != RK_OK) return s;
+  if (n_pages < 0 || n_pages > 0x7fffffff) return fail(ctx, RK_ERR_LAYOUT, "n_pages out of range");
+  if (!plan || (shape->n_seqs > 0 && (!seq_off || !q_pos)) || (shape->n_items > 0 && (!item_seg || !item_delta)))
+    return fail(ctx, RK_ERR_NULL, "null argument");
+  if ((reinterpret_cast<uintptr_t>(plan) & 255u) != 0) return fail(ctx, RK_ERR_ALIGN, "the plan must be 256-byte aligned");
+  const PlanView v = plan_view(ctx, shape, plan);
+  if (plan_bytes < v.bytes) return fail(ctx, RK_ERR_WORKSPACE, "plan buffer too small: need %zu bytes", v.bytes);
+  s = decode_check(ctx);
+  if (s != RK_OK || shape->n_seqs == 0) return s;
+  DecodePlanArgs a;
+  memset(&a, 0, sizeof(a));
+  a.tab = tab;
+  a.seq_off = seq_off;
+  a.item_seg = item_seg;
+  a.item_delta = item_delta;
+  a.q_pos = q_pos;
+  a.header = v.header;
+  a.pos_out = v.pos;
+  a.item_tile = v.item_tile;
+  a.seq_tile = v.seq_tile;
+  a.cta_start = v.cta_start;
+  a.tiles = v.tiles;
+  a.status = ctx->d_status;
+  a.n_pages = n_pages;
+  a.n_seqs = shape->n_seqs;
+  a.q_len = shape->q_len;
+  a.n_items = shape->n_items;
+  a.max_tiles = shape->max_tiles;
+  a.n_heads = ctx->prof.n_heads;
+  a.n_row_tiles = decode_row_tiles(ctx, shape);
+  a.n_ctas = ctx->sm_count;
+  cudaError_t e = launch_decode_plan(a, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "decode plan launch");
+}
+
+static size_t decode_lse_offset(const rk_ctx* ctx) {
+  return (size_t)ctx->sm_count * 2 * kDecodeMaxRows * kDLatent * sizeof(float);
+}
+
+rk_status rk_cache4_attn_workspace_bytes(const rk_ctx* ctx, const rk_decode_shape* shape, size_t* out) {
+  if (!ctx || !out) return RK_ERR_NULL;
+  rk_status s = shape_check(ctx, shape);
+  if (s != RK_OK) return s;
+  *out = decode_lse_offset(ctx) + (size_t)ctx->sm_count * 2 * kDecodeMaxRows * sizeof(float);
+  return RK_OK;
+}
+
+rk_status rk_cache4_attn(rk_ctx* ctx, const rk_decode_shape* shape, const void* plan, size_t plan_bytes, const void* pages,
+                         int64_t n_pages, const void* q, void* O, float* lse, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  rk_status s = shape_check(ctx, shape);
+  if (s != RK_OK) return s;
+  if (n_pages < 0 || n_pages > 0x7fffffff) return fail(ctx, RK_ERR_LAYOUT, "n_pages out of range");
+  if (!plan || !workspace || (n_pages > 0 && !pages) || (shape->n_seqs > 0 && (!q || !O || !lse)))
+    return fail(ctx, RK_ERR_NULL, "null argument");
+  if (!aligned16(pages) || !aligned16(q) || !aligned16(O) || (reinterpret_cast<uintptr_t>(lse) & 3u) ||
+      (reinterpret_cast<uintptr_t>(plan) & 255u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return fail(ctx, RK_ERR_ALIGN, "pages, q and O must be 16-byte aligned, plan and workspace 256-byte aligned");
+  const PlanView v = plan_view(ctx, shape, plan);
+  if (plan_bytes < v.bytes) return fail(ctx, RK_ERR_WORKSPACE, "plan buffer too small: need %zu bytes", v.bytes);
+  size_t need = 0;
+  rk_cache4_attn_workspace_bytes(ctx, shape, &need);
+  if (workspace_bytes < need) return fail(ctx, RK_ERR_WORKSPACE, "workspace too small: need %zu bytes", need);
+  s = decode_check(ctx);
+  if (s != RK_OK || shape->n_seqs == 0) return s;
+  DecodeAttnParams p;
+  memset(&p, 0, sizeof(p));
+  const int rows_per_seq = shape->q_len * ctx->prof.n_heads, tile = decode_row_tile(rows_per_seq);
+  s = make_tmap(ctx, &p.tm_q, q, (uint64_t)shape->n_seqs * rows_per_seq, kDQK, kDQK, 64, (uint32_t)tile);
+  if (s != RK_OK) return s;
+  p.header = v.header;
+  p.pos = v.pos;
+  p.seq_tile = v.seq_tile;
+  p.cta_start = v.cta_start;
+  p.tiles = v.tiles;
+  p.pages = static_cast<const uint8_t*>(pages);
+  p.q = q;
+  p.O = O;
+  p.lse = lse;
+  p.part_o = static_cast<float*>(workspace);
+  p.part_lse = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + decode_lse_offset(ctx));
+  p.status = ctx->d_status;
+  p.wait_ns = ctx->wait_ns;
+  p.rope = rope_turns_of(ctx);
+  p.n_pages = n_pages;
+  p.scale_log2 = ctx->prof.sm_scale * 1.44269504088896340736f;
+  p.n_seqs = shape->n_seqs;
+  p.q_len = shape->q_len;
+  p.n_items = shape->n_items;
+  p.max_tiles = shape->max_tiles;
+  p.n_heads = ctx->prof.n_heads;
+  p.n_row_tiles = decode_row_tiles(ctx, shape);
+  p.n_ctas = ctx->sm_count;
+  cudaError_t e = launch_decode_attn(p, tile, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "decode attention launch");
+}
+
+static rk_status w4_check(rk_ctx* ctx, const rk_w4* w4) {
+  if (!w4) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (w4->group != 32 && w4->group != 64 && w4->group != 128) return fail(ctx, RK_ERR_UNSUPPORTED, "group must be 32, 64 or 128");
+  if (w4->n_mat <= 0 || w4->n_out <= 0 || w4->k <= 0 || w4->n_out % 16 != 0 || w4->k % 64 != 0 || w4->k % w4->group != 0)
+    return fail(ctx, RK_ERR_UNSUPPORTED, "n_out must be a multiple of 16, k of 64 and of the group, all positive");
+  // block counts and the matrices' rows stay inside 32 bits
+  if ((int64_t)w4->n_mat * w4->n_out >= ((int64_t)1 << 30) || (int64_t)w4->n_mat * w4->n_out * (w4->k / 32) >= ((int64_t)1 << 38))
+    return fail(ctx, RK_ERR_LAYOUT, "too many weight rows");
+  if (!w4->codes || !w4->scales) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (!aligned16(w4->codes) || !aligned16(w4->scales)) return fail(ctx, RK_ERR_ALIGN, "codes and scales must be 16-byte aligned");
+  return RK_OK;
+}
+
+rk_status rk_quant4(rk_ctx* ctx, const void* w, const rk_w4* w4, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  rk_status s = w4_check(ctx, w4);
+  if (s != RK_OK) return s;
+  if (!w) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (!aligned16(w)) return fail(ctx, RK_ERR_ALIGN, "w must be 16-byte aligned");
+  s = decode_check(ctx);
+  if (s != RK_OK) return s;
+  cudaError_t e = launch_quant4(w, w4->n_mat, w4->n_out, w4->k, w4->group, w4->codes, w4->scales, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "weight layout launch");
+}
+
+rk_status rk_matvec4(rk_ctx* ctx, const rk_w4* w4, const void* x, int64_t x_stride, int64_t n_tok, void* y,
+                     int64_t y_stride, int32_t out_dtype, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  rk_status s = w4_check(ctx, w4);
+  if (s != RK_OK) return s;
+  if (n_tok < 0 || n_tok > 65535 * 16) return fail(ctx, RK_ERR_ROWS, "n_tok out of range");
+  if (n_tok > 0 && (!x || !y)) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (out_dtype != 0 && out_dtype != 1) return fail(ctx, RK_ERR_UNSUPPORTED, "out_dtype must be 0 (bf16) or 1 (fp32)");
+  if (n_tok > 0 && (x_stride < (int64_t)w4->n_mat * w4->k || y_stride < (int64_t)w4->n_mat * w4->n_out))
+    return fail(ctx, RK_ERR_LAYOUT, "token strides smaller than a token's values");
+  if (!aligned16(x) || x_stride % 8 != 0 || (reinterpret_cast<uintptr_t>(y) & (out_dtype ? 3u : 1u)))
+    return fail(ctx, RK_ERR_ALIGN, "x must be 16-byte aligned, its stride a multiple of 8 elements, and y aligned to its type");
+  s = decode_check(ctx);
+  if (s != RK_OK || n_tok == 0) return s;
+  Matvec4Params p;
+  p.codes = static_cast<const uint4*>(w4->codes);
+  p.scales = static_cast<const uint32_t*>(w4->scales);
+  p.x = x;
+  p.y = y;
+  p.x_stride = x_stride;
+  p.y_stride = y_stride;
+  p.n_tok = n_tok;
+  p.n_mat = w4->n_mat;
+  p.n_out = w4->n_out;
+  p.k = w4->k;
+  p.group = w4->group;
+  p.out_f32 = out_dtype;
+  cudaError_t e = launch_matvec4(p, ctx->sm_count, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "matrix-vector launch");
 }
 
 }  // extern "C"

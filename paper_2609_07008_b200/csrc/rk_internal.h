@@ -155,4 +155,128 @@ cudaError_t launch_protected_rows(const PolicyHost& h, cudaStream_t stream);
 cudaError_t launch_moe_fanout(const float* p, int64_t n, float tau, int fence, uint8_t* k_out, uint8_t* keep_out,
                               cudaStream_t stream);
 
+// ---- 4-bit paged latent cache, single-token attention over it ------------------------------------
+constexpr int kCache4PageRows = 64;
+constexpr int kCache4Units = 26;  // 16-byte units of a row: 16 of codes, 2 of scales, 8 of rope dims
+constexpr int64_t kCache4PageBytes = kCache4Units * kCache4PageRows * 16;
+constexpr int kDecodeKeys = 128;   // keys per tile of the decode attention (two pages)
+constexpr int kDecodeMaxRows = 64; // query rows (token x head) per row tile
+
+struct Cache4Table {  // device arrays
+  const int32_t* seg_len;
+  const int32_t* page_off;
+  const int32_t* page_ids;
+  int64_t n_listed;
+  int32_t n_segs;
+};
+
+struct RopeTurns {
+  double t[32];  // theta_j / (2 pi)
+};
+
+constexpr int32_t kDecodePlanMagic = 0x524b4450;
+struct DecodePlanHeader {
+  int64_t n_pages;
+  int32_t magic, n_seqs, q_len, n_items, max_tiles, n_heads;
+  int32_t n_tiles;  // key tiles over all sequences
+  int32_t chunk;    // tiles per CTA of the attention: CTA i takes [i * chunk, (i + 1) * chunk) of (sequence, row tile, key tile)
+};
+struct __align__(32) DecodeTile {  // at most 128 keys of one segment, as one sequence sees it
+  int32_t page0, page1;  // pages of keys 0-63 and 64-127
+  int32_t base;          // request position of key 0
+  int32_t n;             // keys some query token of the sequence may see
+  int32_t delta;         // request offset of the segment: the queries' rope part is turned by R(-delta)
+  int32_t pad[3];
+};
+
+struct DecodePlanArgs {
+  Cache4Table tab;
+  const int32_t* seq_off;     // [n_seqs + 1] into the items
+  const int32_t* item_seg;    // [n_items]
+  const int32_t* item_delta;  // [n_items]
+  const int32_t* q_pos;       // [n_seqs][q_len]
+  DecodePlanHeader* header;
+  int32_t* pos_out;    // copy of q_pos
+  int32_t* item_tile;  // [n_items + 1]
+  int32_t* seq_tile;   // [n_seqs + 1]
+  int4* cta_start;     // [n_ctas] (sequence, row tile, key tile, used)
+  DecodeTile* tiles;   // [max_tiles]
+  DeviceStatus* status;
+  int64_t n_pages;
+  int32_t n_seqs, q_len, n_items, max_tiles, n_heads, n_row_tiles, n_ctas;
+};
+
+struct DecodeAttnParams {
+  CUtensorMap tm_q;  // [n_seqs * q_len * n_heads][576] bf16, box 64 columns x row-tile rows
+  const DecodePlanHeader* header;
+  const int32_t* pos;
+  const int32_t* seq_tile;
+  const int4* cta_start;
+  const DecodeTile* tiles;
+  const uint8_t* pages;
+  const void* q;
+  void* O;       // bf16 [rows][512]
+  float* lse;    // [rows]
+  float* part_o;    // [n_ctas][2][64][512] normalised partial results of rows whose keys several CTAs share
+  float* part_lse;  // [n_ctas][2][64] base-2
+  DeviceStatus* status;
+  unsigned long long wait_ns;
+  RopeTurns rope;
+  int64_t n_pages;
+  float scale_log2;
+  int32_t n_seqs, q_len, n_items, max_tiles, n_heads, n_row_tiles, n_ctas;
+};
+
+int decode_row_tile(int rows_per_seq);  // 16, 32 or 64 query rows per CTA
+cudaError_t decode_attn_setup();
+cudaError_t launch_decode_attn(const DecodeAttnParams& p, int row_tile, cudaStream_t stream);
+cudaError_t launch_decode_plan(const DecodePlanArgs& a, cudaStream_t stream);
+cudaError_t launch_cache4_append(void* pages, int64_t n_pages, const Cache4Table& tab, const void* c, int64_t c_stride,
+                                 const void* k_rope, int64_t r_stride, const int32_t* new_off, int64_t n_new,
+                                 const RopeTurns& rope, DeviceStatus* status, cudaStream_t stream);
+cudaError_t launch_cache4_read(const void* pages, int64_t n_pages, const Cache4Table& tab, const int32_t* row_off, int64_t n_rows,
+                               void* kv, DeviceStatus* status, cudaStream_t stream);
+
+// ---- 4-bit matrix-vector products ----------------------------------------------------------------
+struct Matvec4Params {
+  const uint4* codes;      // [n_mat][n_out / 16][k / 64][32 lanes]
+  const uint32_t* scales;  // [n_mat][n_out / 16][k / group][8] pairs (row g, row g + 8) of bf16
+  const void* x;           // bf16, token t at x + t * x_stride: [n_mat][k]
+  void* y;                 // token t at y + t * y_stride: [n_mat][n_out]
+  int64_t x_stride, y_stride, n_tok;
+  int32_t n_mat, n_out, k, group, out_f32;
+};
+cudaError_t launch_quant4(const void* w, int32_t n_mat, int32_t n_out, int32_t k, int32_t group, void* codes, void* scales,
+                          cudaStream_t stream);
+cudaError_t launch_matvec4(const Matvec4Params& p, int sm_count, cudaStream_t stream);
+
+#ifdef __CUDACC__
+// scale byte -> the bf16 value in both halves: 2^((b >> 3) - 20) (1 + (b & 7) / 8); 255 is NaN
+__device__ __forceinline__ uint32_t cache4_scale(uint32_t b) {
+  const uint32_t v = b == 255u ? 0x7fc0u : (b << 4) + (107u << 7);
+  return v * 0x10001u;
+}
+// Eight 4-bit codes times a scale -> eight bf16 values, exactly: 0x4300 | code is the bf16 number 128 + code,
+// minus 136 is n, and n * scale has at most seven significant bits.
+__device__ __forceinline__ uint4 cache4_dequant(uint32_t v, uint32_t scale2) {
+  const uint32_t k136 = 0x43084308u;
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t t = ((v >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+    const __nv_bfloat162 n = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&t), *reinterpret_cast<const __nv_bfloat162*>(&k136));
+    const __nv_bfloat162 r = __hmul2(n, *reinterpret_cast<const __nv_bfloat162*>(&scale2));
+    o[i] = *reinterpret_cast<const uint32_t*>(&r);
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+// (cos, sin) of d * theta_j: the angle is reduced in double in units of turns, so that positions of any size are exact
+// to float rounding
+__device__ __forceinline__ void rope_cos_sin(const RopeTurns& r, int d, int j, float& c, float& s) {
+  const double t = (double)d * r.t[j];
+  const float f = (float)(t - rint(t));
+  sincospif(2.f * f, &s, &c);
+}
+#endif
+
 }  // namespace rk

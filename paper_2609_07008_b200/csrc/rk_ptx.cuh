@@ -29,12 +29,24 @@ __device__ __forceinline__ void report_timeout(DeviceStatus* st, int where, int 
   }
 }
 
+// Records a status from a device-side check that is always on (the decode operators read their segment and page
+// tables on the device): `code` is the rk_status, `where` names the check, `aux` holds the offending value.
+__device__ __forceinline__ void report_status(DeviceStatus* st, int code, int where, int aux) {
+  if (st != nullptr && atomicCAS(&st->code, 0, code) == 0) {
+    st->where = where;
+    st->block = (int)blockIdx.x;
+    st->aux = aux;
+    __threadfence();
+  }
+}
+
 // Bounds-checked build (-DRK_CHECK, a debugging aid: run the small cases on it): every index that device
 // code derives from a request table (protected-row list, inverse row map, work list, compaction offsets) is
 // tested before it is used; a bad one is recorded in the status word (code RK_ERR_ROWS, `where` names the
 // table, `aux` holds the value) and the access is skipped.  Nothing traps.  In the ordinary build the
 // function is the constant true and the test disappears.
-enum { RK_CHK_PROT_ROW = 101, RK_CHK_WORK_TILE = 102, RK_CHK_INV_MAP = 103, RK_CHK_COMPACT = 104, RK_CHK_SELFTEST = 199 };
+enum { RK_CHK_PROT_ROW = 101, RK_CHK_WORK_TILE = 102, RK_CHK_INV_MAP = 103, RK_CHK_COMPACT = 104, RK_CHK_SELFTEST = 199,
+       RK_CHK_CACHE_ROW = 201, RK_CHK_CACHE_PAGE = 202, RK_CHK_PLAN_ITEM = 203, RK_CHK_PLAN_MATCH = 204 };
 #ifdef RK_CHECK
 __device__ __forceinline__ bool rk_index_ok(bool ok, DeviceStatus* st, int where, long long value) {
   if (!ok && st != nullptr && atomicCAS(&st->code, 0, 4 /*RK_ERR_ROWS*/) == 0) {
@@ -227,6 +239,16 @@ __device__ __forceinline__ bool named_barrier_and(int id, int n_threads, bool pr
       : "memory");
   return r != 0;
 }
+// ... that ORs a predicate over its participants
+__device__ __forceinline__ bool named_barrier_or(int id, int n_threads, bool pred) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.or.pred p, %2, %3, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)pred), "r"(id), "r"(n_threads)
+      : "memory");
+  return r != 0;
+}
 // 2D tile load into this CTA's shared memory of a CTA pair; completion bytes are counted on
 // `cluster_bar`, a shared::cluster address that may be the peer (leader) CTA's barrier.
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* m, uint32_t cluster_bar, int c0,
@@ -391,6 +413,21 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t* r) {
       "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
       ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_x8(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
