@@ -163,15 +163,29 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
-def _need(t: torch.Tensor, name: str, dtype, shape=None, contiguous=True) -> torch.Tensor:
-    """Type, shape, layout and device of one argument of a decode call (the C ABI sees pointers only)."""
-    if t.dtype != dtype:
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _quick_stream() -> int:
+    """The same stream without building torch's Stream object (for calls that take a few microseconds)."""
+    return _raw_stream(_current_device())
+
+
+def _need(t: torch.Tensor, name: str, dtype, shape, contiguous=True) -> torch.Tensor:
+    """Type, shape, layout and device of one argument of a decode call (the C ABI sees pointers only).  shape: None for
+    any, else a tuple with -1 for any extent.  Written for speed: a decode step makes a handful of these calls per layer."""
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if shape is not None and (t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape))):
-        raise ValueError(f"{name} must have the shape {tuple('*' if w is None else w for w in shape)}, not {tuple(t.shape)}")
+    if shape is not None and t.shape != shape:
+        got = t.shape
+        if len(got) != len(shape):
+            raise ValueError(f"{name} must have {len(shape)} dimensions, not {len(got)}")
+        for want, have in zip(shape, got):
+            if want != -1 and want != have:
+                raise ValueError(f"{name} must have the shape {shape} (-1: any), not {tuple(got)}")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.get_device() != _current_device():
         raise ValueError(f"{name} must be on the current CUDA device, not on {t.device}")
     return t
 
@@ -181,13 +195,12 @@ class CacheTable:
     The tensors are used as they are at the time of each call; their contents may change between calls."""
 
     def __init__(self, seg_len: torch.Tensor, page_off: torch.Tensor, page_ids: torch.Tensor):
-        self.seg_len = _need(seg_len, "seg_len", torch.int32, (None,))
+        self.seg_len = _need(seg_len, "seg_len", torch.int32, (-1,))
         self.page_off = _need(page_off, "page_off", torch.int32, (seg_len.numel() + 1,))
-        self.page_ids = _need(page_ids, "page_ids", torch.int32, (None,))
+        self.page_ids = _need(page_ids, "page_ids", torch.int32, (-1,))
         self.n_segs = seg_len.numel()
-
-    def struct(self) -> rk_cache4_table:
-        return rk_cache4_table(self.n_segs, self.page_ids.numel(), _ptr(self.seg_len), _ptr(self.page_off), _ptr(self.page_ids))
+        self.struct = rk_cache4_table(self.n_segs, page_ids.numel(), _ptr(seg_len), _ptr(page_off), _ptr(page_ids))
+        self.ref = C.byref(self.struct)
 
 
 class DecodePlan:
@@ -195,16 +208,20 @@ class DecodePlan:
 
     def __init__(self, shape: rk_decode_shape, n_pages: int, buf: torch.Tensor):
         self.shape, self.n_pages, self.buf = shape, n_pages, buf
+        self.rows = (shape.n_seqs, shape.q_len)
+        self.ref = C.byref(shape)
 
 
 class W4:
     """4-bit weight matrices laid out by rk_quant4."""
 
     def __init__(self, n_mat: int, n_out: int, k: int, group: int, codes: torch.Tensor, scales: torch.Tensor):
-        self.n_mat, self.n_out, self.k, self.group, self.codes, self.scales = n_mat, n_out, k, group, codes, scales
-
-    def struct(self) -> rk_w4:
-        return rk_w4(self.n_mat, self.n_out, self.k, self.group, _ptr(self.codes), _ptr(self.scales))
+        self.n_mat, self.n_out, self.k, self.group = n_mat, n_out, k, group
+        self.codes, self.scales = _need(codes, "codes", torch.uint8, None), _need(scales, "scales", torch.bfloat16, None)
+        if codes.numel() < n_mat * n_out * k // 2 or scales.numel() < n_mat * n_out * (k // max(group, 1)):
+            raise ValueError("codes or scales are too small for the shape")
+        self.struct = rk_w4(n_mat, n_out, k, group, _ptr(codes), _ptr(scales))
+        self.ref = C.byref(self.struct)
 
 
 def make_layout_struct(seg_off, seg_delta, seg_has_artifact):
@@ -418,29 +435,27 @@ class Context:
         """Rows new_off[s] .. new_off[s+1] of c [n, 512] and k_rope [n, 64] (before rotation) become the last rows of
         segment s; table.seg_len already counts them.  pages: uint8 [n_pages, 26624].  Rows may be strided."""
         n = c.shape[0]
-        _need(pages, "pages", torch.uint8, (None, CACHE4_PAGE_BYTES))
-        _need(c, "c", torch.bfloat16, (None, 512), contiguous=False)
+        _need(pages, "pages", torch.uint8, (-1, CACHE4_PAGE_BYTES))
+        _need(c, "c", torch.bfloat16, (-1, 512), contiguous=False)
         _need(k_rope, "k_rope", torch.bfloat16, (n, 64), contiguous=False)
         _need(new_off, "new_off", torch.int32, (table.n_segs + 1,))
         if n > 0 and (c.stride(1) != 1 or k_rope.stride(1) != 1):
             raise ValueError("the values of a row of c and k_rope must be contiguous")
-        tab = table.struct()
         # a single row's stride is arbitrary and never used
-        self.check(lib.rk_cache4_append(self.handle, _ptr(pages), pages.shape[0], C.byref(tab), c.data_ptr(),
+        self.check(lib.rk_cache4_append(self.handle, _ptr(pages), pages.shape[0], table.ref, c.data_ptr(),
                                         c.stride(0) if n > 1 else 512, k_rope.data_ptr(), k_rope.stride(0) if n > 1 else 64,
-                                        _ptr(new_off), n, _stream()))
+                                        _ptr(new_off), n, _quick_stream()))
 
     def rk_cache4_read(self, pages: torch.Tensor, table: CacheTable, row_off: torch.Tensor, n_rows: int, kv=None) -> torch.Tensor:
         """The last row_off[s+1] - row_off[s] rows of every segment s as packed bf16 rows kv [n_rows, 576]; rows from
         row_off[n_segs] on are left as they were."""
-        _need(pages, "pages", torch.uint8, (None, CACHE4_PAGE_BYTES))
+        _need(pages, "pages", torch.uint8, (-1, CACHE4_PAGE_BYTES))
         _need(row_off, "row_off", torch.int32, (table.n_segs + 1,))
         if kv is None:
             kv = _empty((n_rows, 576), dtype=torch.bfloat16, device=pages.device)
         _need(kv, "kv", torch.bfloat16, (n_rows, 576))
-        tab = table.struct()
-        self.check(lib.rk_cache4_read(self.handle, _ptr(pages), pages.shape[0], C.byref(tab), _ptr(row_off), n_rows, _ptr(kv),
-                                      _stream()))
+        self.check(lib.rk_cache4_read(self.handle, _ptr(pages), pages.shape[0], table.ref, _ptr(row_off), n_rows, _ptr(kv),
+                                      _quick_stream()))
         return kv
 
     def rk_decode_plan(self, table: CacheTable, n_pages: int, seq_off: torch.Tensor, item_seg: torch.Tensor,
@@ -448,9 +463,9 @@ class Context:
         """Work list of a decode step: request b sees the segments item_seg[seq_off[b]:seq_off[b+1]] at the request offsets
         item_delta; q_pos [n_seqs, q_len] are its query tokens' positions.  max_tiles bounds the sum over the items of
         ceil(rows / 128).  With plan= its buffer is filled anew (a captured graph keeps using it)."""
-        _need(q_pos, "q_pos", torch.int32, (None, None))
+        _need(q_pos, "q_pos", torch.int32, (-1, -1))
         _need(seq_off, "seq_off", torch.int32, (q_pos.shape[0] + 1,))
-        _need(item_seg, "item_seg", torch.int32, (None,))
+        _need(item_seg, "item_seg", torch.int32, (-1,))
         _need(item_delta, "item_delta", torch.int32, (item_seg.numel(),))
         shape = rk_decode_shape(q_pos.shape[0], q_pos.shape[1], item_seg.numel(), int(max_tiles))
         need = C.c_size_t(0)
@@ -458,18 +473,15 @@ class Context:
         if plan is None:
             plan = DecodePlan(shape, int(n_pages), _empty(need.value, dtype=torch.uint8, device=q_pos.device))
         else:
-            plan.shape, plan.n_pages = shape, int(n_pages)
-            _need(plan.buf, "plan.buf", torch.uint8, (None,))
-        tab = table.struct()
-        self.check(lib.rk_decode_plan(self.handle, C.byref(shape), C.byref(tab), int(n_pages), _ptr(seq_off), _ptr(item_seg),
-                                      _ptr(item_delta), _ptr(q_pos), _ptr(plan.buf), plan.buf.numel(), _stream()))
+            plan.__init__(shape, int(n_pages), _need(plan.buf, "plan.buf", torch.uint8, (-1,)))
+        self.check(lib.rk_decode_plan(self.handle, C.byref(shape), table.ref, int(n_pages), _ptr(seq_off), _ptr(item_seg),
+                                      _ptr(item_delta), _ptr(q_pos), _ptr(plan.buf), plan.buf.numel(), _quick_stream()))
         return plan
 
     def rk_cache4_attn(self, pages: torch.Tensor, plan: DecodePlan, q: torch.Tensor, O=None, lse=None, workspace=None):
         """q [n_seqs, q_len, n_heads, 576] -> (O [n_seqs, q_len, n_heads, 512] bf16, lse fp32)."""
-        sh = plan.shape
-        rows = (sh.n_seqs, sh.q_len, self.n_heads)
-        _need(pages, "pages", torch.uint8, (None, CACHE4_PAGE_BYTES))
+        rows = plan.rows + (self.n_heads,)
+        _need(pages, "pages", torch.uint8, (-1, CACHE4_PAGE_BYTES))
         _need(q, "q", torch.bfloat16, rows + (576,))
         if O is None:
             O = _empty(rows + (512,), dtype=torch.bfloat16, device=q.device)
@@ -479,16 +491,16 @@ class Context:
         _need(lse, "lse", torch.float32, rows)
         if workspace is None:
             need = C.c_size_t(0)
-            self.check(lib.rk_cache4_attn_workspace_bytes(self.handle, C.byref(sh), C.byref(need)))
+            self.check(lib.rk_cache4_attn_workspace_bytes(self.handle, plan.ref, C.byref(need)))
             workspace = _empty(need.value, dtype=torch.uint8, device=q.device)
-        _need(workspace, "workspace", torch.uint8, (None,))
-        self.check(lib.rk_cache4_attn(self.handle, C.byref(sh), _ptr(plan.buf), plan.buf.numel(), _ptr(pages), pages.shape[0],
-                                      _ptr(q), _ptr(O), _ptr(lse), _ptr(workspace), workspace.numel(), _stream()))
+        _need(workspace, "workspace", torch.uint8, (-1,))
+        self.check(lib.rk_cache4_attn(self.handle, plan.ref, _ptr(plan.buf), plan.buf.numel(), _ptr(pages), pages.shape[0],
+                                      _ptr(q), _ptr(O), _ptr(lse), _ptr(workspace), workspace.numel(), _quick_stream()))
         return O, lse
 
     def rk_quant4(self, w: torch.Tensor, group: int, w4: Optional[W4] = None) -> W4:
         """Lays out w [n_mat, n_out, k] bf16 as 4-bit codes with one bf16 scale per `group` columns of a row."""
-        _need(w, "w", torch.bfloat16, (None, None, None))
+        _need(w, "w", torch.bfloat16, (-1, -1, -1))
         n_mat, n_out, k = w.shape
         if w4 is None:
             n = w.numel()
@@ -496,26 +508,23 @@ class Context:
                     _empty(max(n // max(int(group), 1), 8), dtype=torch.bfloat16, device=w.device))
         elif (w4.n_mat, w4.n_out, w4.k, w4.group) != (n_mat, n_out, k, int(group)):
             raise ValueError("w4 has another shape")
-        st = w4.struct()
-        self.check(lib.rk_quant4(self.handle, _ptr(w), C.byref(st), _stream()))
+        self.check(lib.rk_quant4(self.handle, _ptr(w), w4.ref, _quick_stream()))
         return w4
 
     def rk_matvec4(self, w4: W4, x: torch.Tensor, y: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
         """x [n_tok, n_mat, k] bf16 (tokens may be strided) -> y [n_tok, n_mat, n_out], bf16 or float32."""
         n = x.shape[0]
-        _need(x, "x", torch.bfloat16, (None, w4.n_mat, w4.k), contiguous=False)
-        _need(w4.codes, "w4.codes", torch.uint8)
-        _need(w4.scales, "w4.scales", torch.bfloat16)
+        _need(x, "x", torch.bfloat16, (n, w4.n_mat, w4.k), contiguous=False)
         if y is None:
             y = _empty((n, w4.n_mat, w4.n_out), dtype=out_dtype, device=x.device)
-        _need(y, "y", y.dtype, (n, w4.n_mat, w4.n_out), contiguous=False)
+        else:
+            _need(y, "y", y.dtype, (n, w4.n_mat, w4.n_out), contiguous=False)
         for t, name in ((x, "x"), (y, "y")):
-            if n > 0 and not t[0].is_contiguous():
+            if n > 0 and not t.is_contiguous() and not t[0].is_contiguous():
                 raise ValueError(f"the values of a token of {name} must be contiguous")
         dt = {torch.bfloat16: 0, torch.float32: 1}[y.dtype]
-        st = w4.struct()
-        self.check(lib.rk_matvec4(self.handle, C.byref(st), x.data_ptr(), x.stride(0) if n > 1 else w4.n_mat * w4.k, n, y.data_ptr(),
-                                  y.stride(0) if n > 1 else w4.n_mat * w4.n_out, dt, _stream()))
+        self.check(lib.rk_matvec4(self.handle, w4.ref, x.data_ptr(), x.stride(0) if n > 1 else w4.n_mat * w4.k, n, y.data_ptr(),
+                                  y.stride(0) if n > 1 else w4.n_mat * w4.n_out, dt, _quick_stream()))
         return y
 
     def alloc_layer_buffers(self, req, device) -> dict:

@@ -114,18 +114,30 @@ __global__ void __launch_bounds__(256) cache4_append_kernel(uint8_t* __restrict_
     int code = (int)(u >> 20) - (107 << 3);
     code = finite ? min(max(code, 0), 254) : 255;
     const float inv = __fdiv_rn(1.0f, __uint_as_float((uint32_t)(code + (107 << 3)) << 20));
-    uint32_t q[16];
+    float y[16];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[2 * e] = __uint_as_float(w[e] << 16) * inv;
+      y[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u) * inv;
+    }
+    // max|c| / scale is at most 7 * 17 / 16 and rounds to 7, unless the scale was limited or the group is NaN
+    if (__any_sync(0xffffffffu, code >= 254)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] = fminf(fmaxf(y[e], -7.0f), 7.0f);
+    }
+    // The float bits of 1.5 * 2^23 + 8 + n are 0x4b400008 + n: eight of them, shifted and summed modulo 2^32, are the
+    // packed codes plus a constant.  That keeps the packing on the multiply-add pipe.
+    uint2 out = make_uint2(0u, 0u);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const uint32_t word = w[e >> 1];
-      const float v = __uint_as_float((e & 1) ? (word & 0xffff0000u) : (word << 16));
-      float y = fminf(fmaxf(v * inv, -7.0f), 7.0f);
-      y = __fadd_rn(__fadd_rn(y, 6144.0f), -6144.0f);
-      q[e] = __float_as_uint(__fadd_rn(y, 12582920.0f)) & 15u;  // 1.5 * 2^23 + 8: the low bits are n + 8
+      const float q = __fadd_rn(__fadd_rn(__fadd_rn(y[e], 6144.0f), -6144.0f), 12582920.0f);
+      const uint32_t at = 1u << (4 * ((e & 7) >> 1) + 16 * (e & 1));
+      (e < 8 ? out.x : out.y) += (__float_as_uint(q)) * at;
     }
-    uint2 out;
-    out.x = q[0] | q[2] << 4 | q[4] << 8 | q[6] << 12 | q[1] << 16 | q[3] << 20 | q[5] << 24 | q[7] << 28;
-    out.y = q[8] | q[10] << 4 | q[12] << 8 | q[14] << 12 | q[9] << 16 | q[11] << 20 | q[13] << 24 | q[15] << 28;
+    // 0x4b400000 times the sum of the eight place values
+    const uint32_t bias = (uint32_t)(0x4b400000ull * 0x11111111ull);
+    out.x -= bias;
+    out.y -= bias;
     const int row = warp * 4 + r;
     *reinterpret_cast<uint2*>(stage + (lane >> 1) * kUnitStride + row * 16 + (lane & 1) * 8) = out;
     stage[(16 + ((lane >> 2) & 1)) * kUnitStride + row * 16 + 4 * (lane >> 3) + (lane & 3)] = (uint8_t)code;
@@ -150,8 +162,9 @@ __global__ void __launch_bounds__(256) cache4_append_kernel(uint8_t* __restrict_
   }
 }
 
-// The way back: 32 rows per block, units in with the row index running fastest, 16-byte pieces of bf16 rows out with
-// the column running fastest.  A 32-bit word holds the codes of one 16-byte output piece.
+// The way back: 32 rows per block.  Units come in with the row index running fastest; then a warp writes a row at a time,
+// 16-byte pieces of eight values with the column running fastest (a 32-bit word holds the codes of one piece), so that
+// every lane's places in a row are fixed.
 __global__ void __launch_bounds__(256) cache4_read_kernel(const uint8_t* __restrict__ pages, int64_t n_pages, Cache4Table tab,
                                                           const int32_t* __restrict__ row_off, int64_t n_rows,
                                                           __nv_bfloat16* __restrict__ kv, DeviceStatus* status) {
@@ -167,26 +180,36 @@ __global__ void __launch_bounds__(256) cache4_read_kernel(const uint8_t* __restr
     if (lane == 0) addr[warp * 4 + r] = a;
   }
   __syncthreads();
-  for (int idx = threadIdx.x; idx < kCache4Units * kRowsPerBlock; idx += 256) {
-    const int unit = idx >> 5, row = idx & 31;
-    const int64_t a = addr[row];
-    if (a >= 0) *reinterpret_cast<uint4*>(stage + unit * kUnitStride + row * 16) = __ldcs(reinterpret_cast<const uint4*>(pages + a + unit * 1024));
+  {
+    const int64_t a = addr[lane];  // unit = warp + 8 i, row = lane
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int unit = warp + 8 * i;
+      if (unit < kCache4Units && a >= 0)
+        *reinterpret_cast<uint4*>(stage + unit * kUnitStride + lane * 16) = __ldcs(reinterpret_cast<const uint4*>(pages + a + unit * 1024));
+    }
   }
   __syncthreads();
-  for (int idx = threadIdx.x; idx < 72 * kRowsPerBlock; idx += 256) {
-    const int row = idx / 72, piece = idx - row * 72;
+  // latent piece q of a row: word q & 3 of unit q >> 2, scale group q >> 1; this lane has pieces lane and lane + 32
+  const uint8_t* code_at = stage + (lane >> 2) * kUnitStride + (lane & 3) * 4;
+  const int g = lane >> 1;
+  const uint8_t* scale_at = stage + (16 + ((g >> 2) & 1)) * kUnitStride + 4 * (g >> 3) + (g & 3);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = warp * 4 + r;
     if (addr[row] < 0) continue;
-    uint4 o;
-    if (piece < 64) {  // latent dims 8 piece .. 8 piece + 7: word piece & 3 of unit piece >> 2, scale group piece >> 1
-      const uint32_t v = *reinterpret_cast<const uint32_t*>(stage + (piece >> 2) * kUnitStride + row * 16 + (piece & 3) * 4);
-      const int g = piece >> 1;
-      const uint32_t s = cache4_scale(stage[(16 + ((g >> 2) & 1)) * kUnitStride + row * 16 + 4 * (g >> 3) + (g & 3)]);
-      o = cache4_dequant(v, s);
-    } else {
-      o = *reinterpret_cast<const uint4*>(stage + (18 + piece - 64) * kUnitStride + row * 16);
+    uint4* dst = reinterpret_cast<uint4*>(kv + (row0 + row) * kDQK) + lane;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(code_at + row * 16 + half * 8 * kUnitStride);
+      const uint32_t s = cache4_scale(scale_at[row * 16 + half * 8]);
+      __stcs(dst + 32 * half, cache4_dequant(v, s, cache4_offset(s)));
     }
-    __stcs(reinterpret_cast<uint4*>(kv + (row0 + row) * kDQK + piece * 8), o);
   }
+  const int row = warp * 4 + (lane >> 3);  // rope: eight pieces of each of the four rows
+  if (addr[row] >= 0)
+    __stcs(reinterpret_cast<uint4*>(kv + (row0 + row) * kDQK) + 64 + (lane & 7),
+           *reinterpret_cast<const uint4*>(stage + (18 + (lane & 7)) * kUnitStride + row * 16));
 }
 
 // ---- plan -------------------------------------------------------------------------------------------------
@@ -285,27 +308,71 @@ __global__ void __launch_bounds__(kPlanThreads) decode_plan_scan_kernel(DecodePl
   __threadfence_block();
   const bool empty = *(volatile int*)&a.header->n_tiles == 0;
   for (int b = tid; b <= a.n_seqs; b += kPlanThreads) a.seq_tile[b] = empty ? 0 : a.item_tile[a.seq_off[b]];
+  __syncthreads();
+  // where every CTA of the attention starts, and which row tiles start in a CTA and go on in the next
+  const int chunk = a.header->chunk;
+  const long long work = empty ? 0 : (long long)total * a.n_row_tiles;
+  auto locate = [&](long long w, int* first) -> int4 {  // (sequence, row tile, key tile) of work item w
+    int lo = 0, hi = a.n_seqs - 1;  // largest b with n_row_tiles * seq_tile[b] <= w
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((long long)a.seq_tile[mid] * a.n_row_tiles <= w) lo = mid; else hi = mid - 1;
+    }
+    const int n_b = a.seq_tile[lo + 1] - a.seq_tile[lo];
+    const long long rest = w - (long long)a.seq_tile[lo] * a.n_row_tiles;
+    *first = n_b;
+    return make_int4(lo, (int)(rest / n_b), (int)(rest % n_b), 1);
+  };
+  int4 join = make_int4(0, 0, 0, 0);
+  bool is_join = false;
+  if (tid < a.n_ctas) {
+    const long long w = (long long)tid * chunk, last = min(w + chunk, work) - 1;
+    int n_b;
+    a.cta_start[tid] = w < work ? locate(w, &n_b) : make_int4(0, 0, 0, 0);
+    if (w < work) {
+      const int4 e = locate(last, &n_b);
+      const long long begin = last - e.z, end = begin + n_b;  // the row tile that holds this CTA's last key tile
+      is_join = begin >= w && end > last + 1;
+      if (is_join) {
+        const int parts = (int)((end - 1) / chunk) - tid + 1;
+        join = make_int4(e.x * a.n_row_tiles + e.y, tid, parts, parts <= kJoinFewParts ? (a.row_tile + 15) / 16 : 2 * a.row_tile);
+      }
+    }
+  }
+  // compacted in CTA order, the work units summed up on the way
+  const unsigned ballot = __ballot_sync(0xffffffffu, is_join);
+  int units = is_join ? join.w : 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, units, o);
+    if (lane >= o) units += y;
+  }
+  __shared__ int warp_units[32];
+  __syncthreads();
+  if (lane == 31) {
+    warp_sums[warp] = __popc(ballot);
+    warp_units[warp] = units;
+  }
+  __syncthreads();
+  int at = __popc(ballot & ((1u << lane) - 1u)), n_joins = 0;
+  for (int i = 0; i < 32; ++i) {
+    if (i < warp) {
+      at += warp_sums[i];
+      units += warp_units[i];
+    }
+    n_joins += warp_sums[i];
+  }
+  if (is_join) {
+    join.w = units;
+    a.joins[at] = join;
+  }
+  if (tid == 0) a.header->n_joins = n_joins;
 }
 
-// Pass 2: one thread per key tile; the first threads also find where every CTA of the attention starts.
+// Pass 2: one thread per key tile.
 __global__ void __launch_bounds__(256) decode_plan_fill_kernel(DecodePlanArgs a) {
   const int t = blockIdx.x * 256 + threadIdx.x;
   const int n_tiles = a.header->n_tiles;
-  if (t < a.n_ctas) {
-    const long long w = (long long)t * a.header->chunk;
-    int4 start = make_int4(0, 0, 0, 0);
-    if (w < (long long)n_tiles * a.n_row_tiles) {
-      int lo = 0, hi = a.n_seqs - 1;  // largest b with n_row_tiles * seq_tile[b] <= w
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if ((long long)a.seq_tile[mid] * a.n_row_tiles <= w) lo = mid; else hi = mid - 1;
-      }
-      const int n_b = a.seq_tile[lo + 1] - a.seq_tile[lo];
-      const long long rest = w - (long long)a.seq_tile[lo] * a.n_row_tiles;
-      start = make_int4(lo, (int)(rest / n_b), (int)(rest % n_b), 1);
-    }
-    a.cta_start[t] = start;
-  }
   if (t >= n_tiles) return;
   int lo = 0, hi = a.n_items - 1;  // largest i with item_tile[i] <= t: the last of equal entries owns the tile
   while (lo < hi) {
@@ -363,8 +430,8 @@ cudaError_t launch_decode_plan(const DecodePlanArgs& a, cudaStream_t stream) {
   decode_plan_scan_kernel<<<1, kPlanThreads, 0, stream>>>(a);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int n = a.max_tiles > a.n_ctas ? a.max_tiles : a.n_ctas;
-  decode_plan_fill_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(a);
+  if (a.max_tiles == 0) return cudaSuccess;
+  decode_plan_fill_kernel<<<(unsigned)((a.max_tiles + 255) / 256), 256, 0, stream>>>(a);
   return cudaGetLastError();
 }
 

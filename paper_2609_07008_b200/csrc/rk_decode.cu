@@ -5,56 +5,74 @@
 // the KEYS in the M = 128 dimension of the tensor cores and the query rows in N = 16, 32 or 64:
 //   S^T[128 keys x N]   = K[128 x 576] Q^T          9 chunks of 64 dims, A K-major, B K-major
 //   O^T[512 dims x N]  += C^T[512 x 128] P^T        4 tiles of 128 dims, A MN-major, B MN-major
-// With the rows in M a 64-row tile would run the tensor cores at half rate (M = 64) and 16 rows at an eighth.  The
-// same shared-memory tile (128 keys x 64 dims per 16 KB chunk, 128-byte swizzle) is the K-major A operand of the
-// scores and the MN-major A operand of the values.
+// With the rows in M a 64-row tile would run the tensor cores at half rate (M = 64) and 16 rows at an eighth.
 //
-// Dequantisation happens between the HBM load and the shared-memory store: 256 threads, two per key, hold the next
-// tile's 13 16-byte units each in registers while this tile computes (53 KB in flight per SM) and write the bf16
-// values n * s, which are exact.  One tile (144 KB) and the queries (72 KB) fill the shared memory, so the tile is
-// refilled chunk pair by chunk pair as the value products release it; the scores' products of the next tile follow
-// behind.  P^T (16 KB) shares the space of the rope chunk, which only the scores read.
+// Dequantisation happens between the HBM load and the operands: 256 threads, two per key, hold a tile's 13 16-byte
+// units each in registers (53 KB in flight per SM) and turn them into the bf16 values n * s, which are exact.  They go
+// into tensor memory as the A operand of the scores (a lane is a key; 128 dims per slot, two slots); the softmax warps
+// copy them from there into shared memory as the A operand of the values (128 keys x 64 dims per 16 KB chunk, 128-byte
+// swizzle).  An M = 128, N = 64 product takes 33 clk with the keys in tensor memory and 49 with both operands in shared
+// memory (6 KB at 128 B/clk): 2900 clk of products per tile.
+// One tile's values (128 KB), the queries (80 KB) and P^T (16 KB) fill the shared memory, so the value chunks are
+// refilled pair by pair as the products release them.  The scores do not wait for that: the keys of the next pair
+// are already in tensor memory, and the products of the next tile's first pieces run under this tile's softmax.
 //
 // Statistics: running maximum per query row in shared memory, raised only when a tile exceeds it by more than 2^8
 // (then O^T is rescaled in tensor memory, columns = rows of the query); sums per (key lane, row) in registers in
 // fp32, added up over the lanes once per row tile.  P is rounded to bf16 for the tensor cores (relative 2^-9 per
-// key, averaged by the sum); the rotated query rope is rounded to bf16 like in the online step.
+// key, averaged by the sum); the turned query rope goes in as two bf16 parts, high and low (relative 2^-17 together):
+// the log-sum-exp is an fp32 output, and one part alone moves a logit by 1e-3.
 //
 // Work: the plan lists every (sequence, row tile, key tile) in order and gives each CTA an equal run of them.  A
 // row tile whose keys several CTAs share leaves normalised fp32 partial results and their log-sum-exp, which a
 // second kernel joins in CTA order (no atomics: results do not depend on timing).
 //
-// Warps (576 threads): 0 issues the MMAs, 1 loads the queries (TMA) and turns their rope part, 2-9 load and
-// dequantise keys, 10-17 softmax, correction and epilogue.
+// Warps (640 threads): 0 issues the MMAs, 1 loads the queries (TMA) and turns their rope part, 2 and 3 idle, 4-11 load
+// and dequantise keys, 12-19 softmax, correction and epilogue.
 #include <cuda_bf16.h>
+
+#include <type_traits>
 
 #include "rk_internal.h"
 
 namespace rk {
 namespace {
 
-constexpr int kThreads = 576;
+constexpr int kThreads = 640;      // x 96 registers
+constexpr int kKeyWarps = 8, kKeyWarp0 = 4, kSoftWarp0 = kKeyWarp0 + kKeyWarps;
+constexpr int kSoftWarps = 8, kSoftmax = 32 * kSoftWarps;
 constexpr uint32_t kKChunk = 16384;  // 128 keys x 64 dims bf16
 constexpr uint32_t kQChunk = 8192;   // up to 64 rows x 64 dims bf16
 
-constexpr uint32_t kOffQ = 0;                        // 8 latent chunks, then the turned rope chunk
-constexpr uint32_t kOffK = 9 * kQChunk;              // 8 latent chunks, then the rope chunk / P^T
-constexpr uint32_t kOffP = kOffK + 8 * kKChunk;
-constexpr uint32_t kOffBars = kOffK + 9 * kKChunk;
-enum { B_QFULL = 0, B_QROPE = 1, B_KFULL = 2 /*5*/, B_SFULL = 7, B_PREADY = 8, B_PVDONE = 9 /*4*/, B_COUNT = 13 };
+constexpr uint32_t kOffQ = 0;                        // 8 latent chunks, then the turned rope chunk: high and low parts
+constexpr uint32_t kOffV = 10 * kQChunk;             // 8 latent chunks of the keys
+constexpr uint32_t kOffP = kOffV + 8 * kKChunk;      // P^T
+constexpr uint32_t kOffBars = kOffP + kKChunk;
+enum { B_QFULL = 0, B_QROPE = 1, B_KFULL = 2 /*2*/, B_KFREE = 4 /*2*/, B_VFULL = 6 /*4*/, B_SFULL = 10, B_PREADY = 11,
+       B_PVDONE = 12 /*4*/, B_COUNT = 16 };
 constexpr uint32_t kOffTmem = kOffBars + B_COUNT * 8;
 constexpr uint32_t kOffAbort = kOffTmem + 4;
-constexpr uint32_t kOffMax = kOffBars + 128;         // float [64]: running maximum of each row, base-2 units
+constexpr uint32_t kOffFlag = kOffTmem + 8;          // int: 1 + the last tile some row's maximum has to be raised for
+constexpr uint32_t kOffMax = kOffBars + 144;         // float [64]: running maximum of each row, base-2 units
 constexpr uint32_t kOffPos = kOffMax + 256;          // int [64]: request position of each row (-1: no row)
 constexpr uint32_t kOffRed = kOffPos + 256;          // float [4][64]: per lane quarter
 constexpr uint32_t kOffAlpha = kOffRed + 1024;       // float [64]: factor of the last raise of a row's maximum
 constexpr uint32_t kSmemUsed = kOffAlpha + 256;
-constexpr uint32_t kSmemBytes = kSmemUsed + 1024;    // alignment slack
+constexpr uint32_t kSmemBytes = kSmemUsed;
 
-constexpr uint32_t kColS = 256;      // O^T takes 4 x N columns from 0
+// tensor memory columns: O^T takes 4 x N from 0; two score buffers; two slots of 128 dims of the keys (bf16 pairs)
+constexpr uint32_t kColS = 256, kColK = 384;
 constexpr float kNoMax = -1e30f;     // "no key seen yet": finite, so that differences stay defined
 
-enum { W_QFULL = 41, W_QROPE, W_KFULL, W_SFULL, W_PREADY, W_PVDONE };
+// Registers per thread out of the launch's 640 x 96, by warpgroup: (1 x 56 + 2 x 112 + 2 x 96) x 128 = 60416 of 61440.  Nothing in
+// the loops may spill: shared memory takes nearly all of L1, so a spilled register comes back from L2.
+constexpr int kRegsIssue = 56, kRegsKeys = 112, kRegsSoftmax = 96;
+template <int N>
+__device__ __forceinline__ void reg_raise() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void reg_lower() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+enum { W_QFULL = 41, W_QROPE, W_KFULL, W_KFREE, W_VFULL, W_SFULL, W_PREADY, W_PVDONE };
 
 // Walks one CTA's run of key tiles.  A "group" is the part of one (sequence, row tile) that this CTA owns.
 struct Cursor {
@@ -100,38 +118,90 @@ struct Cursor {
   __device__ bool whole() const { return cnt == n_b; }
 };
 
-template <int N>
-__device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t* r) {
-  if constexpr (N == 8) tmem_ld_x8(a, r);
-  else if constexpr (N == 16) tmem_ld_x16(a, r);
-  else tmem_ld_x32(a, r);
-}
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
-// One key's share of a tile in one of its two threads: chunks h, h + 2, h + 4, h + 6 of the latent (two units each),
-// the scale unit h and rope units 4 h .. 4 h + 3.
-struct KeyRegs {
-  uint4 code[8];
-  uint4 scale;
-  uint4 rope[4];
-};
+__device__ __forceinline__ void prefetch_page(const uint8_t* page) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(page), "r"((uint32_t)kCache4PageBytes) : "memory");
+}
+
+// Shared-memory operand descriptors as their low words (start address and leading byte offset); the high word, stride
+// 1024 bytes, version 1 and 128-byte swizzle, is the same for every operand here.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return ((addr & 0x3FFFFu) >> 4) | ((lbo >> 4) << 16); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+      ::"r"(d), "r"(a_tmem), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      : "memory");
+}
+
+__device__ __forceinline__ uint32_t globaltimer_lo() {
+  uint32_t t;
+  asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
+  return t;
+}
+__device__ __forceinline__ uint32_t load_shared(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void load_shared4(float* r, uint32_t at) {
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void store_shared(uint32_t at, uint32_t v) {
+  asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
+__device__ __forceinline__ void put(uint32_t* r, const uint4& v) {
+  r[0] = v.x;
+  r[1] = v.y;
+  r[2] = v.z;
+  r[3] = v.w;
+}
 
 }  // namespace
 
 template <int kRows>
 __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __grid_constant__ DecodeAttnParams p) {
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t smem_base = smem_u32(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) -> uint32_t { return smem_base + kOffBars + 8u * i; };
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
   volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(smem + kOffTmem);
-  const uint64_t limit = p.wait_ns;
+  // Bounded wait on one of the barriers, kept short: it is inlined two dozen times, and the kernel's loops have to stay in
+  // the instruction cache.  The word at kOffAbort is the tag of the first wait that ran out (reported once, at the end),
+  // after which everyone gives up.
+  auto wait = [&](int b, uint32_t parity, int where) -> bool {
+    const uint32_t at = smem_base + kOffBars + 8u * (uint32_t)b;
+    uint32_t t0 = 0u;
+#pragma unroll 1
+    for (uint32_t n = 1; !mbar_try_wait(at, parity); ++n) {
+      if ((n & 63u) != 0u) continue;
+      if (load_shared(smem_base + kOffAbort) != 0u) return false;
+      const uint32_t now = globaltimer_lo();
+      if (n == 64u) t0 = now;
+      if (now - t0 > p.wait_ns) {
+        store_shared(smem_base + kOffAbort, (uint32_t)where);
+        return false;
+      }
+    }
+    return true;
+  };
 
   {  // the plan has to be the one of this call's shape, heads and pool
     const DecodePlanHeader* h = p.header;
@@ -143,13 +213,20 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     if (p.cta_start[blockIdx.x].w == 0) return;  // no work for this CTA
   }
   if (threadIdx.x == 0) {
-    *abort_flag = 0;
+    store_shared(smem_base + kOffAbort, 0u);
     mbar_init(bar(B_QFULL), 1);
     mbar_init(bar(B_QROPE), 1);
-    for (int i = 0; i < 5; ++i) mbar_init(bar(B_KFULL + i), 8);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(B_KFULL + i), kKeyWarps);
+      mbar_init(bar(B_KFREE + i), 1 + kSoftWarps);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(bar(B_VFULL + i), kSoftWarps);
+      mbar_init(bar(B_PVDONE + i), 1);
+    }
     mbar_init(bar(B_SFULL), 1);
-    mbar_init(bar(B_PREADY), 8);
-    for (int i = 0; i < 4; ++i) mbar_init(bar(B_PVDONE + i), 1);
+    mbar_init(bar(B_PREADY), 1);
+    *reinterpret_cast<volatile int*>(smem + kOffFlag) = 0;
     fence_mbar_init_cluster();
   }
   if (warp == 0) {
@@ -160,58 +237,82 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t tmem = *tmem_ptr;
+  // All 512 columns are this block's, so they start at 0; a constant keeps the MMA operands out of vector registers.
+  constexpr uint32_t tmem = 0u;
+  if (*tmem_ptr != tmem || (smem_base & 1023u) != 0u) {  // cannot happen; nothing has been started yet
+    if (threadIdx.x == 0) report_status(p.status, 8 /*RK_ERR_CUDA*/, RK_CHK_PLAN_MATCH, (int)*tmem_ptr);
+    __syncthreads();
+    if (warp == 0) tmem_dealloc<1>(*tmem_ptr, 512);
+    return;
+  }
+  if (warp < kKeyWarp0) reg_lower<kRegsIssue>();
   const int rows_per_seq = p.q_len * p.n_heads;
 
   if (warp == 0) {
     // ------------------------------ MMA issue (whole warp loops, one elected lane issues) ----------------------
+    // Scores of a tile come in five pieces as the keys reach tensor memory: rope, then four times 128 dims.  The first two
+    // pieces of a tile run under the softmax of the one before, the rest behind its value products.  The order is fixed
+    // and the products come in long batches: the tensor core's queue holds only a few products, so whatever this warp
+    // does between two batches beyond some 150 clocks leaves it idle (polling several barriers and taking the pieces in
+    // the order they arrived cost 500 clocks a batch).
     constexpr uint32_t id_qk = umma_idesc_bf16(128, kRows, 0, 0);
     constexpr uint32_t id_pv = umma_idesc_bf16(128, kRows, 1, 1);
-    uint32_t t = 0, groups = 0;  // tiles and groups done so far: their parities are the barriers' phases
+    uint32_t t = 0, groups = 0;  // tiles and groups so far: their parities are the barriers' phases
     bool ok = true;
+    // piece i of tile tq: the 5 tq + i-th piece of all, in slot (tq + i) & 1 as 5 is odd
+    auto piece = [&](auto index, uint32_t tq) {
+      constexpr int i = decltype(index)::value;
+      const uint32_t u = 5u * tq + i, slot = u & 1u;
+      ok = ok && wait(B_KFULL + slot, (u >> 1) & 1u, W_KFULL);
+      if (i == 0) ok = ok && wait(B_QROPE, tq & 1u, W_QROPE);
+      if (!ok) return;
+      tc_fence_after_sync();
+      const uint32_t ts = tmem + kColS + (tq & 1u) * 64u, tk = tmem + kColK + slot * 64u;
+      if (elect_one()) {
+        const uint32_t db = desc_lo(smem_base + kOffQ + (i == 0 ? 8 : 2 * (i - 1)) * kQChunk, 16);
+#pragma unroll
+        for (int s = 0; s < 8; ++s)  // rope: the same 64 dims of the keys against the high and the low part of the turned queries
+          mma_ts(ts, tk + 8u * (i == 0 ? (s & 3) : s), db + (uint32_t)(((s >> 2) * kQChunk + (s & 3) * 32) >> 4), id_qk,
+                 (i > 0 || s > 0) ? 1u : 0u);
+        umma_commit_1(bar(B_KFREE + slot));
+        if (i == 4) umma_commit_1(bar(B_SFULL));
+      }
+      __syncwarp();
+    };
+    using std::integral_constant;
     for (Cursor c(p); ok && c.next(); ++groups) {
-      ok = mbar_wait_bounded<false>(bar(B_QFULL), groups & 1u, limit, abort_flag, p.status, W_QFULL, (int)groups);
-      for (int k = 0; ok && k < c.cnt; ++k, ++t) {
-        for (int m = 0; ok && m < 4; ++m) {  // scores: chunk pairs in the order they are filled
-          ok = mbar_wait_bounded<false>(bar(B_KFULL + m), t & 1u, limit, abort_flag, p.status, W_KFULL, m);
-          if (!ok) break;
-          if (elect_one()) {
-            const uint64_t da = umma_desc_sw128(smem_base + kOffK + 2 * m * kKChunk, 16, 1024);
-            const uint64_t db = umma_desc_sw128(smem_base + kOffQ + 2 * m * kQChunk, 16, 1024);
-#pragma unroll
-            for (int s = 0; s < 8; ++s)
-              umma_f16<1>(tmem + kColS, da + (uint64_t)(((s >> 2) * kKChunk + (s & 3) * 32) >> 4),
-                          db + (uint64_t)(((s >> 2) * kQChunk + (s & 3) * 32) >> 4), id_qk, (m > 0 || s > 0) ? 1u : 0u);
-          }
-          __syncwarp();
+      ok = wait(B_QFULL, groups & 1u, W_QFULL);
+      piece(integral_constant<int, 0>(), t);
+      piece(integral_constant<int, 1>(), t);
+#pragma unroll 1
+      for (int k = 0;; ++k) {
+        piece(integral_constant<int, 2>(), t);
+        piece(integral_constant<int, 3>(), t);
+        piece(integral_constant<int, 4>(), t);
+        const bool last = k + 1 == c.cnt;  // the next group has other queries
+        if (!last) {
+          piece(integral_constant<int, 0>(), t + 1);
+          piece(integral_constant<int, 1>(), t + 1);
         }
-        ok = ok && mbar_wait_bounded<false>(bar(B_KFULL + 4), t & 1u, limit, abort_flag, p.status, W_KFULL, 4) &&
-             mbar_wait_bounded<false>(bar(B_QROPE), t & 1u, limit, abort_flag, p.status, W_QROPE, k);
-        if (!ok) break;
-        if (elect_one()) {
-          const uint64_t da = umma_desc_sw128(smem_base + kOffK + 8 * kKChunk, 16, 1024);
-          const uint64_t db = umma_desc_sw128(smem_base + kOffQ + 8 * kQChunk, 16, 1024);
-#pragma unroll
-          for (int s = 0; s < 4; ++s) umma_f16<1>(tmem + kColS, da + (uint64_t)(2 * s), db + (uint64_t)(2 * s), id_qk, 1u);
-          umma_commit_1(bar(B_SFULL));
-        }
-        __syncwarp();
-        ok = mbar_wait_bounded<false>(bar(B_PREADY), t & 1u, limit, abort_flag, p.status, W_PREADY, k);
+        ok = ok && wait(B_PREADY, t & 1u, W_PREADY);
+        for (int m = 0; m < 4; ++m) ok = ok && wait(B_VFULL + m, t & 1u, W_VFULL);
         if (!ok) break;
         tc_fence_after_sync();
         if (elect_one()) {
-          const uint64_t db = umma_desc_sw128(smem_base + kOffP, 16, 1024);
-#pragma unroll 1
+          const uint32_t db = desc_lo(smem_base + kOffP, 16);
+#pragma unroll
           for (int m = 0; m < 4; ++m) {  // 128 dims each: two 64-dim chunks, 16 KB apart
-            const uint64_t da = umma_desc_sw128(smem_base + kOffK + 2 * m * kKChunk, kKChunk, 1024);
+            const uint32_t da = desc_lo(smem_base + kOffV + 2 * m * kKChunk, kKChunk);
 #pragma unroll
             for (int s = 0; s < 8; ++s)
-              umma_f16<1>(tmem + (uint32_t)(m * kRows), da + (uint64_t)((s * 2048) >> 4), db + (uint64_t)((s * 2048) >> 4), id_pv,
-                          (k > 0 || s > 0) ? 1u : 0u);
+              mma_ss(tmem + (uint32_t)(m * kRows), da + (uint32_t)((s * 2048) >> 4), db + (uint32_t)((s * 2048) >> 4), id_pv,
+                     (k > 0 || s > 0) ? 1u : 0u);
             umma_commit_1(bar(B_PVDONE + m));
           }
         }
         __syncwarp();
+        ++t;
+        if (last) break;
       }
     }
   } else if (warp == 1) {
@@ -221,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     const int rc = lane & 7;
     for (Cursor c(p); ok && c.next(); ++groups) {
       // the previous group's scores are done with the query chunks (its last tile's S is complete)
-      if (t > 0) ok = mbar_wait_bounded<false>(bar(B_SFULL), (t - 1) & 1u, limit, abort_flag, p.status, W_SFULL, (int)t);
+      if (t > 0) ok = wait(B_SFULL, (t - 1) & 1u, W_SFULL);
       if (!ok) break;
       const int row0 = c.b * rows_per_seq + c.rt * kRows;
       if (elect_one()) {
@@ -234,7 +335,11 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
       int delta = -1;
       for (int k = 0; ok && k < c.cnt; ++k, ++t) {
         const int d = p.tiles[c.record(k)].delta;
-        if (k > 0) ok = mbar_wait_bounded<false>(bar(B_SFULL), (t - 1) & 1u, limit, abort_flag, p.status, W_SFULL, (int)t);
+        if (k + 2 < c.cnt && lane < 2) {  // pages of the tile after next into L2, where its loads will find them
+          const int4 v = *reinterpret_cast<const int4*>(&p.tiles[c.record(k + 2)]);
+          if (v.w > 64 * lane + 32) prefetch_page(p.pages + (int64_t)(lane == 0 ? v.x : v.y) * kCache4PageBytes);
+        }
+        if (k > 0) ok = wait(B_SFULL, (t - 1) & 1u, W_SFULL);
         if (!ok) break;
         if (d != delta) {
           delta = d;
@@ -242,19 +347,22 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
 #pragma unroll
           for (int e = 0; e < 4; ++e) rope_cos_sin(p.rope, d, 4 * rc + e, cs[e], sn[e]);
           const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + (int64_t)row0 * kDQK + kDLatent + rc * 8;
-#pragma unroll 4
+#pragma unroll 1
           for (int r = lane >> 3; r < kRows; r += 4) {
             uint4 v = make_uint4(0, 0, 0, 0);
             if (r < valid) v = *reinterpret_cast<const uint4*>(src + (int64_t)r * kDQK);
             const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-            uint32_t o[4];
+            uint32_t o[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float x0 = __uint_as_float(in[e] << 16), x1 = __uint_as_float(in[e] & 0xffff0000u);
-              o[e] = pack_bf16(x0 * cs[e] + x1 * sn[e], x1 * cs[e] - x0 * sn[e]);
+              const float y0 = x0 * cs[e] + x1 * sn[e], y1 = x1 * cs[e] - x0 * sn[e];
+              o[e] = pack_bf16(y0, y1);
+              lo[e] = pack_bf16(y0 - __uint_as_float(o[e] << 16), y1 - __uint_as_float(o[e] & 0xffff0000u));
             }
-            *reinterpret_cast<uint4*>(smem + kOffQ + 8 * kQChunk + sw128_offset((uint32_t)r, (uint32_t)rc)) =
-                make_uint4(o[0], o[1], o[2], o[3]);
+            uint8_t* dst = smem + kOffQ + 8 * kQChunk + sw128_offset((uint32_t)r, (uint32_t)rc);
+            *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(dst + kQChunk) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           }
           fence_proxy_async_smem();
         }
@@ -262,107 +370,163 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         if (lane == 0) mbar_arrive(bar(B_QROPE));
       }
     }
-  } else if (warp < 10) {
+  } else if (warp < 4) {
+    // a warp reaches the tensor memory lanes of its number modulo four: the next role starts at warp 4
+  } else if (warp < kSoftWarp0) {
     // ------------------------------ keys: HBM -> registers (4-bit) -> shared memory (bf16) --------------------
-    const int kw = warp - 2;
-    const int row = 32 * (kw & 3) + lane, h = kw >> 2;
-    const uint32_t xr = (uint32_t)(row & 7);
-    KeyRegs kr;
+    reg_raise<kRegsKeys>();
+    // Two threads per key: thread h has chunk 2 m + h (64 dims, two units) of every 128 dims m, the scale unit h (one word
+    // per chunk) and rope units 4 h .. 4 h + 3.
+    const int h = (warp - kKeyWarp0) >> 2;
+    const int row = 32 * (warp & 3) + lane;  // a warp reaches the tensor memory lanes of its quarter
+    const uint32_t t_k = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColK;
+    uint32_t code[32], scl[4], rope[16];
     const uint8_t* src = nullptr;  // this key's first unit in the tile being loaded, null for a row that is not there
-    auto open = [&](int rec) {
-      const int4 v = *reinterpret_cast<const int4*>(&p.tiles[rec]);
-      const int page = row < 64 ? v.x : v.y;
-      src = row < v.w ? p.pages + (int64_t)page * kCache4PageBytes + (row & 63) * 16 : nullptr;
-    };
     // rows that are not there become zeros (code 8): their scores are masked, and 0 * 0 adds nothing to O
     auto load_pair = [&](int m) {
-      const uint32_t z = 0x88888888u;
-      kr.code[2 * m] = kr.code[2 * m + 1] = make_uint4(z, z, z, z);
-      if (src != nullptr) {
-        kr.code[2 * m] = __ldg(reinterpret_cast<const uint4*>(src + (4 * m + 2 * h) * 1024));
-        kr.code[2 * m + 1] = __ldg(reinterpret_cast<const uint4*>(src + (4 * m + 2 * h + 1) * 1024));
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (src != nullptr) put(code + 8 * m + 4 * e, __ldg(reinterpret_cast<const uint4*>(src + h * 2048 + (4 * m + e) * 1024)));
+        else put(code + 8 * m + 4 * e, make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u));
       }
     };
-    auto load_scale = [&]() -> uint4 {
-      return src != nullptr ? __ldg(reinterpret_cast<const uint4*>(src + (16 + h) * 1024)) : make_uint4(0, 0, 0, 0);
+    auto load_scale = [&]() {
+      put(scl, src != nullptr ? __ldg(reinterpret_cast<const uint4*>(src + h * 1024 + 16 * 1024)) : make_uint4(0, 0, 0, 0));
     };
     auto load_rope = [&]() {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        kr.rope[e] = src != nullptr ? __ldg(reinterpret_cast<const uint4*>(src + (18 + 4 * h + e) * 1024)) : make_uint4(0, 0, 0, 0);
+        put(rope + 4 * e, src != nullptr ? __ldg(reinterpret_cast<const uint4*>(src + h * 4096 + (18 + e) * 1024)) : make_uint4(0, 0, 0, 0));
     };
-    uint32_t t = 0;
+    uint32_t u = 0;
     bool ok = true;
+    // a slot of keys in tensor memory may be overwritten once its last content has been multiplied and copied
+    auto slot_free = [&]() -> bool { return u < 2 || wait(B_KFREE + (u & 1u), ((u >> 1) - 1u) & 1u, W_KFREE); };
+    auto slot_filled = [&]() {
+      tmem_wait_st();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(B_KFULL + (u & 1u)));
+      ++u;
+    };
     Cursor c(p);
     bool more = c.next();
     int k = 0;
-    if (more) {
-      open(c.record(0));
-#pragma unroll
-      for (int m = 0; m < 4; ++m) load_pair(m);
-      kr.scale = load_scale();
-      load_rope();
-    }
-    while (ok && more) {
-      // the record after this one: its loads go out piece by piece as this tile's registers become free
-      if (++k == c.cnt) {
+    int page = 0, n = 0;  // record of the tile after the one in registers, fetched a tile ahead
+    auto fetch = [&]() {  // moves the cursor on and fetches that record
+      if (++k >= c.cnt) {
         more = c.next();
         k = 0;
       }
-      if (more) open(c.record(k));
-      else src = nullptr;
-      const uint4 next_scale = load_scale();
-      const uint32_t sw[4] = {kr.scale.x, kr.scale.y, kr.scale.z, kr.scale.w};
+      if (more) {
+        const int4 v = __ldg(reinterpret_cast<const int4*>(&p.tiles[c.record(k)]));
+        page = row < 64 ? v.x : v.y;
+        n = v.w;
+      }
+    };
+    auto open = [&]() { src = row < n ? p.pages + (int64_t)page * kCache4PageBytes + (row & 63) * 16 : nullptr; };
+    bool here = more;  // there is a tile in registers
+    if (more) {
+      k = -1;
+      fetch();
+      open();
+#pragma unroll
+      for (int m = 0; m < 4; ++m) load_pair(m);
+      load_scale();
+      load_rope();
+      fetch();
+    }
+    while (here) {
+      ok = slot_free();
+      if (!ok) break;
+      tc_fence_after_sync();
+      // a group whose scale is NaN (byte 255) makes the whole key NaN: its score then is, and with it every output
+      if ((cache4_nan_bytes(scl[0]) | cache4_nan_bytes(scl[1]) | cache4_nan_bytes(scl[2]) | cache4_nan_bytes(scl[3])) != 0u)
+        rope[0] = 0x7fc07fc0u;
+      tmem_st_x16(t_k + (u & 1u) * 64u + 16u * h, rope);
+      slot_filled();
+      const bool next = more;
+      if (next) {
+        open();
+        load_rope();
+      }
+      if (next) fetch();
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        if (t > 0) ok = mbar_wait_bounded<false>(bar(B_PVDONE + m), (t - 1) & 1u, limit, abort_flag, p.status, W_PVDONE, m);
-        if (!ok) break;
-        uint8_t* dst = smem + kOffK + (2 * m + h) * kKChunk + row * 128;
+        uint32_t v[32];  // 64 dims of this key
+        {
+          uint32_t s2[4];
+          cache4_scale_quad(scl[m], s2);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint4 v = kr.code[2 * m + u];
-          const uint32_t s0 = cache4_scale((sw[m] >> (16 * u)) & 255u), s1 = cache4_scale((sw[m] >> (16 * u + 8)) & 255u);
-          *reinterpret_cast<uint4*>(dst + (((4u * u + 0u) ^ xr) << 4)) = cache4_dequant(v.x, s0);
-          *reinterpret_cast<uint4*>(dst + (((4u * u + 1u) ^ xr) << 4)) = cache4_dequant(v.y, s0);
-          *reinterpret_cast<uint4*>(dst + (((4u * u + 2u) ^ xr) << 4)) = cache4_dequant(v.z, s1);
-          *reinterpret_cast<uint4*>(dst + (((4u * u + 3u) ^ xr) << 4)) = cache4_dequant(v.w, s1);
+          for (int g = 0; g < 4; ++g) {
+            const uint32_t o2 = cache4_offset(s2[g]);
+            put(v + 8 * g, cache4_dequant(code[8 * m + 2 * g], s2[g], o2));
+            put(v + 8 * g + 4, cache4_dequant(code[8 * m + 2 * g + 1], s2[g], o2));
+          }
         }
-        if (more) load_pair(m);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_KFULL + m));
+        // the next tile's loads go out as the registers become free: they have a whole tile's time to arrive
+        if (next) {
+          load_pair(m);
+          if (m == 3) load_scale();
+        }
+        ok = slot_free();
+        if (!ok) break;
+        tc_fence_after_sync();
+        tmem_st_x32(t_k + (u & 1u) * 64u + 32u * h, v);
+        slot_filled();
       }
       if (!ok) break;
-      // the rope chunk's space held P^T of the previous tile: every value product has completed (waited for above)
-      uint8_t* dst = smem + kOffK + 8 * kKChunk + row * 128;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(dst + (((4u * h + e) ^ xr) << 4)) = kr.rope[e];
-      if (more) load_rope();
-      kr.scale = next_scale;
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_KFULL + 4));
-      ++t;
+      here = next;
     }
   } else {
     // ------------------------------ softmax, correction, epilogue ---------------------------------------------
+    reg_raise<kRegsSoftmax>();
     // Thread = one key of the tile (TMEM lane) and half of the query rows (columns).
     constexpr int NC = kRows / 2;
     const int q = warp & 3;            // TMEM lane quarter
-    const int ch = (warp - 10) >> 2;   // column half
+    const int c0 = ((warp - kSoftWarp0) >> 2) * NC;
     const int key = 32 * q + lane;
-    const int c0 = ch * NC;
     const uint32_t lane_base = (uint32_t)(32 * q) << 16;
-    const uint32_t t_s = tmem + lane_base + kColS + (uint32_t)c0;
+    const uint32_t t_s0 = tmem + lane_base + kColS + (uint32_t)c0;
     const uint32_t t_o = tmem + lane_base + (uint32_t)c0;
     float* s_max = reinterpret_cast<float*>(smem + kOffMax);
     int* s_pos = reinterpret_cast<int*>(smem + kOffPos);
     float* s_red = reinterpret_cast<float*>(smem + kOffRed);
     float* s_alpha = reinterpret_cast<float*>(smem + kOffAlpha);
-    const int tid = threadIdx.x - 320;
+    volatile int* s_flag = reinterpret_cast<volatile int*>(smem + kOffFlag);
+    const int tid = threadIdx.x - 32 * kSoftWarp0;
+    const uint32_t max_at = smem_base + kOffMax + 4u * c0;
     const float scale = p.scale_log2;
-    uint32_t t = 0;
+    uint32_t t = 0, u = 0;
     bool ok = true;
+    // The values of tile tv: copied from tensor memory, where the key warps put them for the scores, into shared memory,
+    // chunk pair by chunk pair as the previous tile's products release the space.  Here and not in the key warps, which
+    // thereby never wait for the value products; the softmax warps have nothing else to do while those run.
+    auto copy_values = [&](uint32_t tv) -> bool {
+      if (lane == 0) mbar_arrive(bar(B_KFREE + (u & 1u)));  // the rope piece is not a value
+      ++u;
+      uint8_t* const v_row = smem + kOffV + (c0 ? 1 : 0) * kKChunk + key * 128;
+#pragma unroll 1
+      for (int m = 0; m < 4; ++m, ++u) {
+        if (!wait(B_KFULL + (u & 1u), (u >> 1) & 1u, W_KFULL)) return false;
+        tc_fence_after_sync();
+        uint32_t v[32];
+        __syncwarp();
+        tmem_ld_x32(tmem + lane_base + kColK + (u & 1u) * 64u + (c0 ? 32u : 0u), v);
+        tmem_wait_ld();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_KFREE + (u & 1u)));
+        if (tv > 0 && !wait(B_PVDONE + m, (tv - 1) & 1u, W_PVDONE)) return false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          *reinterpret_cast<uint4*>(v_row + 2 * m * kKChunk + ((e ^ (key & 7)) << 4)) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_VFULL + m));
+      }
+      return true;
+    };
     for (Cursor c(p); ok && c.next();) {
       // s_max, s_pos: every warp is done with the previous group (the barrier in its epilogue)
       int pmin = 0x7fffffff;
@@ -372,158 +536,170 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         s_max[tid] = kNoMax;
         s_pos[tid] = r < rows_per_seq ? p.pos[c.b * p.q_len + r / p.n_heads] : -1;
       }
-      named_barrier_sync(1, 256);
+      named_barrier_sync(1, kSoftmax);
       float l[NC];
 #pragma unroll
       for (int i = 0; i < NC; ++i) l[i] = 0.f;
       for (int k = 0; ok && k < c.cnt; ++k, ++t) {
         const int4 rec = *reinterpret_cast<const int4*>(&p.tiles[c.record(k)]);
         const bool full = rec.w == kDecodeKeys && pmin - rec.z + 1 >= kDecodeKeys;  // no key of the tile is masked
-        ok = mbar_wait_bounded<false>(bar(B_SFULL), t & 1u, limit, abort_flag, p.status, W_SFULL, k);
-        // a warp that gave up must not leave the others in a named barrier: the vote below ends them together
-        if (ok) tc_fence_after_sync();
-        uint32_t s[NC];
-        float top = -INFINITY;
-        if (ok) {
-          tmem_ld<NC>(t_s, s);
-          tmem_wait_ld();
-          if (!full) {
+        const bool fast = k > 0 && full;
+        const uint32_t t_s = t_s0 + (t & 1u) * 64u;
+        // p = 2^(score - max), eight rows at a time: added to the sums and written as P^T, one 128-byte row per key,
+        // query rows contiguous.  `raised`: with masks, the maxima being final (see below).  Returns the largest exponent.
+        auto write_p = [&](auto raised) -> float {
+          float top = -INFINITY;
+          uint8_t* dst = smem + kOffP + key * 128;
 #pragma unroll
-            for (int i = 0; i < NC; ++i)
-              if (key >= rec.w || rec.z + key > s_pos[c0 + i]) s[i] = 0xff800000u;
+          for (int i = 0; i < NC; i += 8) {
+            uint32_t s[8], pk[4];
+            tmem_ld_x8(t_s + (uint32_t)i, s);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+              float mx[4], al[4], pv[4];
+              load_shared4(mx, max_at + 4u * (i + j));
+              if constexpr (decltype(raised)::value) load_shared4(al, max_at + (kOffAlpha - kOffMax) + 4u * (i + j));
+#pragma unroll
+              for (int n = 0; n < 4; ++n) {
+                float e = fmaf(__uint_as_float(s[j + n]), scale, -mx[n]);
+                if (decltype(raised)::value && (key >= rec.w || rec.z + key > s_pos[c0 + i + j + n])) e = -INFINITY;
+                top = fmaxf(top, e);
+                pv[n] = fast_exp2(e);
+                if constexpr (!decltype(raised)::value) l[i + j + n] += pv[n];
+                else l[i + j + n] = al[n] < 1e-27f ? pv[n] : fmaf(l[i + j + n], al[n], fast ? 0.f : pv[n]);
+              }
+              pk[j / 2] = pack_bf16(pv[0], pv[1]);
+              pk[j / 2 + 1] = pack_bf16(pv[2], pv[3]);
+            }
+            *reinterpret_cast<uint4*>(dst + ((((uint32_t)((c0 + i) / 8)) ^ (uint32_t)(key & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
           }
+          fence_proxy_async_smem();
+          return top;
+        };
+        ok = copy_values(t) && wait(B_SFULL, t & 1u, W_SFULL);
+        tc_fence_after_sync();
+        // First try with the maxima as they are (S of this tile is complete, so P^T of the previous one has been read).
+        // A warp that finds an exponent above 8, or that gave up waiting, raises the flag; everyone sees it behind
+        // the barrier.  Not tried for the first tile of a group, which has no maxima yet, and for the rare tiles with
+        // masked keys, which the longer way below handles.
+        const bool all_ok = __all_sync(0xffffffffu, ok);
+        float top = INFINITY;
+        if (fast && all_ok) top = write_p(std::false_type());
+        if (top > 8.f) *s_flag = (int)t + 1;
+        tc_fence_before_sync();
+        named_barrier_sync(1, kSoftmax);
+        if (*s_flag == (int)t + 1) {
+          ok = named_barrier_and(2, kSoftmax, ok);  // a warp that gave up must not leave the others in a barrier
+          if (!ok) break;
+          // exact maxima of the tile; a row's maximum is raised where the tile exceeds it by more than 2^8
+#pragma unroll 1
+          for (int i = 0; i < NC; i += 8) {
+            uint32_t s[8];
+            tmem_ld_x8(t_s + (uint32_t)i, s);
+            tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < NC; i += 4) {
-            const float4 mx = *reinterpret_cast<const float4*>(s_max + c0 + i);
-            top = fmaxf(fmaxf(top, fmaf(__uint_as_float(s[i]), scale, -mx.x)), fmaf(__uint_as_float(s[i + 1]), scale, -mx.y));
-            top = fmaxf(fmaxf(top, fmaf(__uint_as_float(s[i + 2]), scale, -mx.z)), fmaf(__uint_as_float(s[i + 3]), scale, -mx.w));
+            for (int j = 0; j < 8; ++j) {
+              const bool masked = !full && (key >= rec.w || rec.z + key > s_pos[c0 + i + j]);
+              float v = masked ? -INFINITY : __uint_as_float(s[j]) * scale;
+#pragma unroll
+              for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+              if (lane == 0) s_red[q * 64 + c0 + i + j] = v;
+            }
           }
-        }
-        ok = named_barrier_and(2, 256, ok);
-        if (!ok) break;
-        if (named_barrier_or(1, 256, top > 8.f)) {
-          // some row's maximum grows by more than 2^8 (always so for the first visible keys): exact maxima of the tile
-#pragma unroll
-          for (int i = 0; i < NC; ++i) {
-            float v = __uint_as_float(s[i]) * scale;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-            if (lane == 0) s_red[q * 64 + c0 + i] = v;
-          }
-          named_barrier_sync(1, 256);
+          named_barrier_sync(1, kSoftmax);
+          bool raise = false;
           if (tid < kRows) {
             const float v = fmaxf(fmaxf(s_red[tid], s_red[64 + tid]), fmaxf(s_red[128 + tid], s_red[192 + tid]));
             const float old = s_max[tid];
-            const bool raise = v > old + 8.f;
+            raise = v > old + 8.f;
             s_alpha[tid] = raise ? fast_exp2(old - v) : 1.f;
             if (raise) s_max[tid] = v;
           }
-          named_barrier_sync(1, 256);
-#pragma unroll
-          for (int i = 0; i < NC; ++i) l[i] *= s_alpha[c0 + i];
-          if (k > 0) {  // S of this tile is complete, so every value product before it is too
+          if (named_barrier_or(1, kSoftmax, raise) && k > 0) {  // S of this tile is complete, so every value product before it is too
 #pragma unroll 1
-            for (int m = 0; m < 4; ++m) {
-#pragma unroll 1
-              for (int i0 = 0; i0 < NC; i0 += 8) {
-                uint32_t o[8];
-                tmem_ld_x8(t_o + (uint32_t)(m * kRows + i0), o);
-                tmem_wait_ld();
+            for (int i0 = 0; i0 < 4 * NC; i0 += 8) {
+              const uint32_t col = (uint32_t)(i0 / NC * kRows + i0 % NC);
+              uint32_t o[8];
+              tmem_ld_x8(t_o + col, o);
+              tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * s_alpha[c0 + i0 + i]);
-                tmem_st_x8(t_o + (uint32_t)(m * kRows + i0), o);
-              }
+              for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * s_alpha[c0 + i0 % NC + i]);
+              tmem_st_x8(t_o + col, o);
             }
             tmem_wait_st();
           }
+          // Where the first try was made, the sums already hold this tile's p against the old maximum, and the factor makes
+          // them right for the new one; otherwise this tile's p are added here.
+          // Where the maximum rose by more than 2^90 (or there was none) they may have overflowed: there, what was
+          // summed up before is below 2^-60 of the new sum and is dropped.
+          write_p(std::true_type());
+          tc_fence_before_sync();
+          named_barrier_sync(1, kSoftmax);
         }
-        uint32_t pk[NC / 2];
-#pragma unroll
-        for (int i = 0; i < NC; i += 4) {
-          const float4 mx = *reinterpret_cast<const float4*>(s_max + c0 + i);
-          const float p0 = fast_exp2(fmaf(__uint_as_float(s[i]), scale, -mx.x));
-          const float p1 = fast_exp2(fmaf(__uint_as_float(s[i + 1]), scale, -mx.y));
-          const float p2 = fast_exp2(fmaf(__uint_as_float(s[i + 2]), scale, -mx.z));
-          const float p3 = fast_exp2(fmaf(__uint_as_float(s[i + 3]), scale, -mx.w));
-          l[i] += p0;
-          l[i + 1] += p1;
-          l[i + 2] += p2;
-          l[i + 3] += p3;
-          pk[i / 2] = pack_bf16(p0, p1);
-          pk[i / 2 + 1] = pack_bf16(p2, p3);
-        }
-        // P^T, one 128-byte row per key, query rows contiguous; the rope chunk it replaces has been read (S is complete)
-        uint8_t* dst = smem + kOffP + key * 128;
-#pragma unroll
-        for (int i = 0; i < NC / 8; ++i)
-          *reinterpret_cast<uint4*>(dst + ((((uint32_t)(c0 / 8 + i)) ^ (uint32_t)(key & 7)) << 4)) =
-              make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
-        fence_proxy_async_smem();
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_PREADY));
+        if (tid == 0) mbar_arrive(bar(B_PREADY));
       }
       if (!ok) break;
       // ---- epilogue of the group: sums over the key lanes, then O^T / l ----
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        float v = l[i];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0) s_red[q * 64 + c0 + i] = v;
-      }
-      ok = mbar_wait_bounded<false>(bar(B_PVDONE + 3), (t - 1) & 1u, limit, abort_flag, p.status, W_PVDONE, 4);
-      ok = named_barrier_and(2, 256, ok);
+      // (through the value chunks' space, free once the last value product is done: 128 keys x 64 rows in fp32)
+      ok = wait(B_PVDONE + 3, (t - 1) & 1u, W_PVDONE);
+      ok = named_barrier_and(2, kSoftmax, ok);
       if (!ok) break;
       tc_fence_after_sync();
+      float* const s_sum = reinterpret_cast<float*>(smem + kOffV);
+#pragma unroll
+      for (int i = 0; i < NC; i += 4)
+        *reinterpret_cast<float4*>(s_sum + key * 64 + (((c0 + i) ^ (4 * (key & 7))) & 63)) = make_float4(l[i], l[i + 1], l[i + 2], l[i + 3]);
+      named_barrier_sync(1, kSoftmax);
+      if (tid < 4 * kRows) {  // four threads per row, 32 keys each
+        const int r = tid & (kRows - 1), part = tid / kRows;
+        float v = 0.f;
+#pragma unroll 8
+        for (int j = 0; j < 32; ++j) v += s_sum[(32 * part + j) * 64 + (r ^ (4 * (j & 7)))];
+        s_red[part * 64 + r] = v;
+      }
+      named_barrier_sync(1, kSoftmax);
       const bool whole = c.whole();
       const int slot = 2 * blockIdx.x + (c.tile > 0 ? 0 : 1);
       const int valid = min(rows_per_seq - c.rt * kRows, kRows);
       const int64_t row0 = (int64_t)c.b * rows_per_seq + c.rt * kRows;
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        const int col = c0 + i;
-        const float tot = (s_red[col] + s_red[64 + col]) + (s_red[128 + col] + s_red[192 + col]);
-        l[i] = tot;
+      if (tid < kRows) {
+        // a NaN score makes its row NaN; a row without visible keys has the sum 0
+        const float tot = (s_red[tid] + s_red[64 + tid]) + (s_red[128 + tid] + s_red[192 + tid]);
+        const float lse2 = tot == 0.f ? -INFINITY : s_max[tid] + log2f(tot);
+        s_alpha[tid] = tot == 0.f ? 0.f : 1.f / tot;
+        if (!whole) p.part_lse[(int64_t)slot * 64 + tid] = lse2;
+        else if (tid < valid) p.lse[row0 + tid] = lse2 * 0.69314718055994530942f;
       }
-      if (lane == 0 && q == 0) {
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-          const int col = c0 + i;
-          // tot > 0 or NaN: a NaN score makes its row NaN, a row without visible keys has the sum 0
-          const float lse2 = l[i] == 0.f ? -INFINITY : s_max[col] + log2f(l[i]);
-          if (!whole) p.part_lse[(int64_t)slot * 64 + col] = lse2;
-          else if (col < valid) p.lse[row0 + col] = lse2 * 0.69314718055994530942f;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < NC; ++i) l[i] = l[i] == 0.f ? 0.f : 1.f / l[i];
+      named_barrier_sync(1, kSoftmax);
 #pragma unroll 1
-      for (int m = 0; m < 4; ++m) {
-        uint32_t o[NC];
-        tmem_ld<NC>(t_o + (uint32_t)(m * kRows), o);
+      for (int i0 = 0; i0 < 4 * NC; i0 += 8) {  // 128 dims, then eight rows
+        const int m = i0 / NC, r = c0 + i0 % NC;
+        uint32_t o[8];
+        tmem_ld_x8(t_o + (uint32_t)(m * kRows + i0 % NC), o);
         tmem_wait_ld();
         const int dim = 128 * m + key;
         if (whole) {
-          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.O) + row0 * kDLatent + dim;
+          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.O) + (row0 + r) * kDLatent + dim;
 #pragma unroll
-          for (int i = 0; i < NC; ++i)
-            if (c0 + i < valid) out[(int64_t)(c0 + i) * kDLatent] = __float2bfloat16_rn(__uint_as_float(o[i]) * l[i]);
+          for (int i = 0; i < 8; ++i)
+            if (r + i < valid) out[i * kDLatent] = __float2bfloat16_rn(__uint_as_float(o[i]) * s_alpha[r + i]);
         } else {
-          float* out = p.part_o + ((int64_t)slot * 64) * kDLatent + dim;
+          float* out = p.part_o + ((int64_t)slot * 64 + r) * kDLatent + dim;
 #pragma unroll
-          for (int i = 0; i < NC; ++i)
-            if (c0 + i < valid) out[(int64_t)(c0 + i) * kDLatent] = __uint_as_float(o[i]) * l[i];
+          for (int i = 0; i < 8; ++i)
+            if (r + i < valid) out[i * kDLatent] = __uint_as_float(o[i]) * s_alpha[r + i];
         }
       }
       tc_fence_before_sync();
-      named_barrier_sync(1, 256);  // s_red, s_max and s_pos may be overwritten from here on
+      named_barrier_sync(1, kSoftmax);  // s_red, s_max and s_pos may be overwritten from here on
     }
   }
 
   // ------------------------------ teardown -------------------------------------------------------------------
   // after a wait has expired: copies and products in flight get a bounded time to finish
-  if (*abort_flag != 0) {
+  if (load_shared(smem_base + kOffAbort) != 0u) {
+    if (threadIdx.x == 0) report_timeout(p.status, (int)load_shared(smem_base + kOffAbort), 0);
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
   }
   __syncwarp();
@@ -536,71 +712,123 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
 }
 
 // Joins the partial results of row tiles whose keys several CTAs share, in CTA order: lse = log2 sum 2^lse_j,
-// O = sum 2^(lse_j - lse) O_j.  One block per query row; four groups of 128 threads take every fourth part, 16 bytes
-// of the row each, so that a row shared by all CTAs has four times eight loads in flight.  Rows of sequences that see
-// nothing get O = 0, lse = -inf; rows that one CTA finished alone are already written.
-__global__ void __launch_bounds__(512) rk_decode_join_kernel(const __grid_constant__ DecodeAttnParams p, int row_tile) {
+// O = sum 2^(lse_j - lse) O_j.  The plan lists those row tiles (at most one per CTA) with a running count of work units,
+// which the blocks take in turn.  Few parts (a batch: two or three): a unit is 16 rows, one per warp.  Many parts (one
+// long request: up to one per CTA): a unit is half a row; eight groups of 64 threads take every eighth part, 16 bytes
+// each, so that the 2 KB rows of many parts are in flight at once.  Rows of sequences that see nothing get O = 0,
+// lse = -inf; rows that one CTA finished alone are already written.
+constexpr int kJoinThreads = 512;
+__global__ void __launch_bounds__(kJoinThreads) rk_decode_join_kernel(const __grid_constant__ DecodeAttnParams p, int row_tile) {
   const DecodePlanHeader* h = p.header;
   if (h->magic != kDecodePlanMagic || h->n_seqs != p.n_seqs || h->q_len != p.q_len || h->n_items != p.n_items ||
       h->max_tiles != p.max_tiles || h->n_heads != p.n_heads || h->n_pages != p.n_pages)
     return;  // reported by the attention kernel
+  __shared__ float s_w[kDecodeMaxCtas];
+  __shared__ float4 s_acc[7][64];
+  __shared__ float s_red[32];
   const int rows_per_seq = p.q_len * p.n_heads;
-  const int64_t row = blockIdx.x;
-  const int b = (int)(row / rows_per_seq), r = (int)(row - (int64_t)b * rows_per_seq);
-  const int rt = r / row_tile, col = r - rt * row_tile;
-  const int tile0 = p.seq_tile[b], n_b = p.seq_tile[b + 1] - tile0;
-  const int part = threadIdx.x >> 7, d4 = threadIdx.x & 127;
-  __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.O) + row * kDLatent + d4 * 4;
-  if (n_b == 0) {
-    if (part == 0) *reinterpret_cast<uint2*>(out) = make_uint2(0u, 0u);
-    if (threadIdx.x == 0) p.lse[row] = -INFINITY;
-    return;
+  const int tid = threadIdx.x, lane = tid & 31;
+  for (int b = blockIdx.x; b < p.n_seqs; b += gridDim.x) {
+    if (p.seq_tile[b + 1] != p.seq_tile[b]) continue;
+    uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O) + (int64_t)b * rows_per_seq * kDLatent);
+    for (int i = tid; i < rows_per_seq * (kDLatent / 8); i += kJoinThreads) out[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < rows_per_seq; i += kJoinThreads) p.lse[(int64_t)b * rows_per_seq + i] = -INFINITY;
   }
-  const long long x = (long long)tile0 * p.n_row_tiles + (long long)rt * n_b, y = x + n_b;
-  const int ca = (int)(x / h->chunk), cb = (int)((y - 1) / h->chunk);
-  if (ca == cb) return;
-  // a part is in slot 1 of the CTA that starts the row tile, in slot 0 of the ones that go on with it
-  auto slot = [&](int cta) -> int64_t { return (int64_t)2 * cta + (cta == ca ? 1 : 0); };
-  float mx = -INFINITY;
-  bool nan = false;
-  for (int i = ca; i <= cb; ++i) {
-    const float v = __ldg(p.part_lse + slot(i) * 64 + col);
-    mx = fmaxf(mx, v);
-    nan |= v != v;
-  }
-  const float base = mx == -INFINITY ? 0.f : mx;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float tot = 0.f;
-#pragma unroll 8
-  for (int i = ca + part; i <= cb; i += 4) {
-    const float w = exp2f(__ldg(p.part_lse + slot(i) * 64 + col) - base);
-    const float4 v = __ldg(reinterpret_cast<const float4*>(p.part_o + (slot(i) * 64 + col) * kDLatent) + d4);
-    tot += w;
-    if (w != 0.f) {
-      acc.x = fmaf(w, v.x, acc.x);
-      acc.y = fmaf(w, v.y, acc.y);
-      acc.z = fmaf(w, v.z, acc.z);
-      acc.w = fmaf(w, v.w, acc.w);
+  const int n_joins = h->n_joins;
+  const int n_units = n_joins > 0 ? p.joins[n_joins - 1].w : 0;
+  for (int unit = blockIdx.x; unit < n_units; unit += gridDim.x) {
+    int lo = 0, hi = n_joins - 1;  // first join whose running count exceeds the unit
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (p.joins[mid].w > unit) hi = mid; else lo = mid + 1;
     }
-  }
-  __shared__ float4 s_acc[3][128];
-  __shared__ float s_tot[4];
-  if (part > 0) s_acc[part - 1][d4] = acc;
-  if (d4 == 0) s_tot[part] = tot;
-  __syncthreads();
-  if (part > 0) return;
-  const float all = (s_tot[0] + s_tot[1]) + (s_tot[2] + s_tot[3]);
-  const float inv = all == 0.f ? 0.f : 1.f / all;
+    const int4 j = p.joins[lo];  // (sequence, row tile), first CTA, parts, units so far
+    const int n = j.z, at = unit - (lo > 0 ? p.joins[lo - 1].w : 0), b = j.x / p.n_row_tiles, rt = j.x - b * p.n_row_tiles;
+    // a part is in slot 1 of the CTA that starts the row tile, in slot 0 of the ones that go on with it
+    auto slot = [&](int i) -> int64_t { return (int64_t)2 * (j.y + i) + (i == 0 ? 1 : 0); };
+    if (n <= kJoinFewParts) {
+      const int col = 16 * at + (tid >> 5), r = rt * row_tile + col;
+      if (r < rows_per_seq) {
+        const int64_t row = (int64_t)b * rows_per_seq + r;
+        const float mine = lane < n ? __ldg(p.part_lse + slot(lane) * 64 + col) : -INFINITY;
+        float mx = mine;
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float base = mx == -INFINITY ? 0.f : mx;
+        const float w = lane < n ? exp2f(mine - base) : 0.f;  // a NaN stays one; an empty part has the weight 0
+        float sum = w;
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        float4 acc[4];
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const float4 v = s_acc[i][d4];
-    acc.x += v.x;
-    acc.y += v.y;
-    acc.z += v.z;
-    acc.w += v.w;
+        for (int e = 0; e < 4; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int i = 0; i < n; ++i) {
+          const float wi = __shfl_sync(0xffffffffu, w, i);
+          const float4* src = reinterpret_cast<const float4*>(p.part_o + (slot(i) * 64 + col) * kDLatent) + lane;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float4 v = __ldg(src + 32 * e);
+            acc[e].x = fmaf(wi, v.x, acc[e].x);
+            acc[e].y = fmaf(wi, v.y, acc[e].y);
+            acc[e].z = fmaf(wi, v.z, acc[e].z);
+            acc[e].w = fmaf(wi, v.w, acc[e].w);
+          }
+        }
+        uint2* out = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.O) + row * kDLatent) + lane;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[32 * e] = make_uint2(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv));
+        if (lane == 0) p.lse[row] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994530942f;
+      }
+      continue;
+    }
+    const int col = at >> 1, half = at & 1, r = rt * row_tile + col;
+    if (r >= rows_per_seq) continue;
+    const int part = tid >> 6, d4 = tid & 63;
+    const int64_t row = (int64_t)b * rows_per_seq + r;
+    const float mine = tid < n ? __ldg(p.part_lse + slot(tid) * 64 + col) : -INFINITY;
+    float mx = mine, sum = 0.f;
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    if (lane == 0) s_red[tid >> 5] = mx;
+    __syncthreads();
+    mx = s_red[0];
+    for (int i = 1; i < kJoinThreads / 32; ++i) mx = fmaxf(mx, s_red[i]);
+    const float base = mx == -INFINITY ? 0.f : mx;
+    const float w = tid < n ? exp2f(mine - base) : 0.f;
+    if (tid < n) s_w[tid] = w;
+    sum = w;
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_red[16 + (tid >> 5)] = sum;
+    __syncthreads();
+    sum = s_red[16];
+    for (int i = 1; i < kJoinThreads / 32; ++i) sum += s_red[16 + i];
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int i = part; i < n; i += 8) {
+      const float wi = s_w[i];
+      const float4 v = __ldg(reinterpret_cast<const float4*>(p.part_o + (slot(i) * 64 + col) * kDLatent + half * 256) + d4);
+      acc.x = fmaf(wi, v.x, acc.x);
+      acc.y = fmaf(wi, v.y, acc.y);
+      acc.z = fmaf(wi, v.z, acc.z);
+      acc.w = fmaf(wi, v.w, acc.w);
+    }
+    if (part > 0) s_acc[part - 1][d4] = acc;
+    __syncthreads();
+    if (part == 0) {
+#pragma unroll
+      for (int i = 0; i < 7; ++i) {
+        const float4 v = s_acc[i][d4];
+        acc.x += v.x;
+        acc.y += v.y;
+        acc.z += v.z;
+        acc.w += v.w;
+      }
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.O) + row * kDLatent + half * 256 + d4 * 4;
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+      if (tid == 0 && half == 0) p.lse[row] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994530942f;
+    }
+    __syncthreads();
   }
-  *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-  if (threadIdx.x == 0) p.lse[row] = nan ? NAN : (all == 0.f ? -INFINITY : (base + log2f(all)) * 0.69314718055994530942f);
 }
 
 int decode_row_tile(int rows_per_seq) { return rows_per_seq <= 16 ? 16 : (rows_per_seq <= 32 ? 32 : 64); }
@@ -619,8 +847,7 @@ cudaError_t launch_decode_attn(const DecodeAttnParams& p, int row_tile, cudaStre
   else rk_decode_attn_kernel<64><<<grid, kThreads, kSmemBytes, stream>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int64_t rows = (int64_t)p.n_seqs * p.q_len * p.n_heads;
-  rk_decode_join_kernel<<<(unsigned)rows, 512, 0, stream>>>(p, row_tile);
+  rk_decode_join_kernel<<<(unsigned)(2 * p.n_ctas), kJoinThreads, 0, stream>>>(p, row_tile);
   return cudaGetLastError();
 }
 

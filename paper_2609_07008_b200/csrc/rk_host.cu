@@ -258,6 +258,7 @@ rk_status rk_create_ex(const rk_profile* prof, uint32_t flags, rk_ctx** out) {
     return RK_ERR_UNSUPPORTED;
   }
   ctx->sm_count = dp.multiProcessorCount;
+  if (ctx->sm_count > kDecodeMaxCtas) ctx->sm_count = kDecodeMaxCtas;  // grid sizes only
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult qres;
   e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
@@ -272,6 +273,7 @@ rk_status rk_create_ex(const rk_profile* prof, uint32_t flags, rk_ctx** out) {
   if (e == cudaSuccess) e = stream_setup();
   if (e == cudaSuccess) e = proj_fused_setup();
   if (e == cudaSuccess) e = decode_attn_setup();
+  if (e == cudaSuccess) e = matvec4_setup();
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&ctx->d_status), sizeof(DeviceStatus));
   if (e == cudaSuccess) e = cudaMemset(ctx->d_status, 0, sizeof(DeviceStatus));
   if (e != cudaSuccess) {
@@ -1228,7 +1230,7 @@ static rk_status shape_check(const rk_ctx* ctx, const rk_decode_shape* sh) {
 // The parts of a plan buffer, each 256-byte aligned; null base: only the size is of interest.
 struct PlanView {
   DecodePlanHeader* header;
-  int4* cta_start;
+  int4 *cta_start, *joins;
   int32_t *pos, *seq_tile, *item_tile;
   DecodeTile* tiles;
   size_t bytes;
@@ -1243,6 +1245,7 @@ static PlanView plan_view(const rk_ctx* ctx, const rk_decode_shape* sh, const vo
   };
   v.header = reinterpret_cast<DecodePlanHeader*>(take(sizeof(DecodePlanHeader)));
   v.cta_start = reinterpret_cast<int4*>(take((size_t)ctx->sm_count * sizeof(int4)));
+  v.joins = reinterpret_cast<int4*>(take((size_t)ctx->sm_count * sizeof(int4)));
   v.pos = reinterpret_cast<int32_t*>(take((size_t)sh->n_seqs * sh->q_len * 4));
   v.seq_tile = reinterpret_cast<int32_t*>(take((size_t)(sh->n_seqs + 1) * 4));
   v.item_tile = reinterpret_cast<int32_t*>(take((size_t)(sh->n_items + 1) * 4));
@@ -1292,6 +1295,7 @@ rk_status rk_decode_plan(rk_ctx* ctx, const rk_decode_shape* shape, const rk_cac
   a.item_tile = v.item_tile;
   a.seq_tile = v.seq_tile;
   a.cta_start = v.cta_start;
+  a.joins = v.joins;
   a.tiles = v.tiles;
   a.status = ctx->d_status;
   a.n_pages = n_pages;
@@ -1301,6 +1305,7 @@ rk_status rk_decode_plan(rk_ctx* ctx, const rk_decode_shape* shape, const rk_cac
   a.max_tiles = shape->max_tiles;
   a.n_heads = ctx->prof.n_heads;
   a.n_row_tiles = decode_row_tiles(ctx, shape);
+  a.row_tile = decode_row_tile(shape->q_len * ctx->prof.n_heads);
   a.n_ctas = ctx->sm_count;
   cudaError_t e = launch_decode_plan(a, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "decode plan launch");
@@ -1346,6 +1351,7 @@ rk_status rk_cache4_attn(rk_ctx* ctx, const rk_decode_shape* shape, const void* 
   p.pos = v.pos;
   p.seq_tile = v.seq_tile;
   p.cta_start = v.cta_start;
+  p.joins = v.joins;
   p.tiles = v.tiles;
   p.pages = static_cast<const uint8_t*>(pages);
   p.q = q;
@@ -1354,7 +1360,7 @@ rk_status rk_cache4_attn(rk_ctx* ctx, const rk_decode_shape* shape, const void* 
   p.part_o = static_cast<float*>(workspace);
   p.part_lse = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + decode_lse_offset(ctx));
   p.status = ctx->d_status;
-  p.wait_ns = ctx->wait_ns;
+  p.wait_ns = (uint32_t)std::min<unsigned long long>(ctx->wait_ns, 4000000000ull);
   p.rope = rope_turns_of(ctx);
   p.n_pages = n_pages;
   p.scale_log2 = ctx->prof.sm_scale * 1.44269504088896340736f;
@@ -1408,7 +1414,7 @@ rk_status rk_matvec4(rk_ctx* ctx, const rk_w4* w4, const void* x, int64_t x_stri
     return fail(ctx, RK_ERR_ALIGN, "x must be 16-byte aligned, its stride a multiple of 8 elements, and y aligned to its type");
   s = decode_check(ctx);
   if (s != RK_OK || n_tok == 0) return s;
-  Matvec4Params p;
+  Matvec4Params p = {};
   p.codes = static_cast<const uint4*>(w4->codes);
   p.scales = static_cast<const uint32_t*>(w4->scales);
   p.x = x;
@@ -1421,7 +1427,9 @@ rk_status rk_matvec4(rk_ctx* ctx, const rk_w4* w4, const void* x, int64_t x_stri
   p.k = w4->k;
   p.group = w4->group;
   p.out_f32 = out_dtype;
-  cudaError_t e = launch_matvec4(p, ctx->sm_count, static_cast<cudaStream_t>(stream));
+  p.status = ctx->d_status;
+  p.wait_ns = ctx->wait_ns;
+  cudaError_t e = launch_matvec4(p, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "matrix-vector launch");
 }
 

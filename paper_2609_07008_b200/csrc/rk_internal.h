@@ -161,6 +161,8 @@ constexpr int kCache4Units = 26;  // 16-byte units of a row: 16 of codes, 2 of s
 constexpr int64_t kCache4PageBytes = kCache4Units * kCache4PageRows * 16;
 constexpr int kDecodeKeys = 128;   // keys per tile of the decode attention (two pages)
 constexpr int kDecodeMaxRows = 64; // query rows (token x head) per row tile
+constexpr int kDecodeMaxCtas = 512; // bound of n_ctas (one per SM)
+constexpr int kJoinFewParts = 16;   // up to here a row's partial results are joined by one warp
 
 struct Cache4Table {  // device arrays
   const int32_t* seg_len;
@@ -179,6 +181,7 @@ struct DecodePlanHeader {
   int64_t n_pages;
   int32_t magic, n_seqs, q_len, n_items, max_tiles, n_heads;
   int32_t n_tiles;  // key tiles over all sequences
+  int32_t n_joins;  // row tiles whose keys several CTAs share
   int32_t chunk;    // tiles per CTA of the attention: CTA i takes [i * chunk, (i + 1) * chunk) of (sequence, row tile, key tile)
 };
 struct __align__(32) DecodeTile {  // at most 128 keys of one segment, as one sequence sees it
@@ -200,10 +203,11 @@ struct DecodePlanArgs {
   int32_t* item_tile;  // [n_items + 1]
   int32_t* seq_tile;   // [n_seqs + 1]
   int4* cta_start;     // [n_ctas] (sequence, row tile, key tile, used)
+  int4* joins;         // [n_ctas] (sequence * n_row_tiles + row tile, first CTA, parts, work units up to here)
   DecodeTile* tiles;   // [max_tiles]
   DeviceStatus* status;
   int64_t n_pages;
-  int32_t n_seqs, q_len, n_items, max_tiles, n_heads, n_row_tiles, n_ctas;
+  int32_t n_seqs, q_len, n_items, max_tiles, n_heads, n_row_tiles, n_ctas, row_tile;
 };
 
 struct DecodeAttnParams {
@@ -212,6 +216,7 @@ struct DecodeAttnParams {
   const int32_t* pos;
   const int32_t* seq_tile;
   const int4* cta_start;
+  const int4* joins;
   const DecodeTile* tiles;
   const uint8_t* pages;
   const void* q;
@@ -220,7 +225,7 @@ struct DecodeAttnParams {
   float* part_o;    // [n_ctas][2][64][512] normalised partial results of rows whose keys several CTAs share
   float* part_lse;  // [n_ctas][2][64] base-2
   DeviceStatus* status;
-  unsigned long long wait_ns;
+  uint32_t wait_ns;  // limit of one device-side wait (the low word of the timer: at most 4 s)
   RopeTurns rope;
   int64_t n_pages;
   float scale_log2;
@@ -245,10 +250,14 @@ struct Matvec4Params {
   void* y;                 // token t at y + t * y_stride: [n_mat][n_out]
   int64_t x_stride, y_stride, n_tok;
   int32_t n_mat, n_out, k, group, out_f32;
+  int32_t stages, stage_toks;  // pipeline depth and tokens per stage (set by the launcher)
+  DeviceStatus* status;
+  unsigned long long wait_ns;
 };
 cudaError_t launch_quant4(const void* w, int32_t n_mat, int32_t n_out, int32_t k, int32_t group, void* codes, void* scales,
                           cudaStream_t stream);
-cudaError_t launch_matvec4(const Matvec4Params& p, int sm_count, cudaStream_t stream);
+cudaError_t matvec4_setup();
+cudaError_t launch_matvec4(Matvec4Params p, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // scale byte -> the bf16 value in both halves: 2^((b >> 3) - 20) (1 + (b & 7) / 8); 255 is NaN
@@ -256,16 +265,32 @@ __device__ __forceinline__ uint32_t cache4_scale(uint32_t b) {
   const uint32_t v = b == 255u ? 0x7fc0u : (b << 4) + (107u << 7);
   return v * 0x10001u;
 }
-// Eight 4-bit codes times a scale -> eight bf16 values, exactly: 0x4300 | code is the bf16 number 128 + code,
-// minus 136 is n, and n * scale has at most seven significant bits.
-__device__ __forceinline__ uint4 cache4_dequant(uint32_t v, uint32_t scale2) {
-  const uint32_t k136 = 0x43084308u;
+// four scale bytes -> the bf16 values, each in both halves; 255 comes out as a number here, see cache4_nan_bytes
+__device__ __forceinline__ void cache4_scale_quad(uint32_t b, uint32_t* s2) {
+  const uint32_t even = (b & 0x00ff00ffu) * 16u + 0x35803580u, odd = ((b >> 8) & 0x00ff00ffu) * 16u + 0x35803580u;
+  s2[0] = __byte_perm(even, 0u, 0x1010);
+  s2[1] = __byte_perm(odd, 0u, 0x1010);
+  s2[2] = __byte_perm(even, 0u, 0x3232);
+  s2[3] = __byte_perm(odd, 0u, 0x3232);
+}
+// the top bit of every byte that is 255
+__device__ __forceinline__ uint32_t cache4_nan_bytes(uint32_t b) { return ((b & 0x7f7f7f7fu) + 0x01010101u) & b & 0x80808080u; }
+// -24 times a scale, in both halves (exact: 24 has two significant bits)
+__device__ __forceinline__ uint32_t cache4_offset(uint32_t scale2) {
+  const uint32_t k = 0xc1c0c1c0u;
+  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&k), *reinterpret_cast<const __nv_bfloat162*>(&scale2));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Eight 4-bit codes n + 8 times a scale -> eight bf16 values n * scale, exactly: a code in mantissa bits 3-6 of 0x4180
+// is the bf16 number 16 + code = 24 + n; one fused product and sum with -24 * scale leaves n * scale, which has at
+// most seven significant bits.
+__device__ __forceinline__ uint4 cache4_dequant(uint32_t v, uint32_t scale2, uint32_t offset2) {
   uint32_t o[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t t = ((v >> (4 * i)) & 0x000f000fu) | 0x43004300u;
-    const __nv_bfloat162 n = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&t), *reinterpret_cast<const __nv_bfloat162*>(&k136));
-    const __nv_bfloat162 r = __hmul2(n, *reinterpret_cast<const __nv_bfloat162*>(&scale2));
+    const uint32_t t = ((i == 0 ? v << 3 : v >> (4 * i - 3)) & 0x00780078u) | 0x41804180u;
+    const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&t), *reinterpret_cast<const __nv_bfloat162*>(&scale2),
+                                     *reinterpret_cast<const __nv_bfloat162*>(&offset2));
     o[i] = *reinterpret_cast<const uint32_t*>(&r);
   }
   return make_uint4(o[0], o[1], o[2], o[3]);
