@@ -29,6 +29,7 @@ struct rk_ctx {
   int device = 0;
   int sm_count = 0;
   int n_pairs = 0;
+  int32_t matvec_slots[4] = {};
   DeviceStatus* d_status = nullptr;
   GemmBatch* d_batches = nullptr;  // [uv_g: G][uv_l: L][wa_g: G][wa_l: G][wb: 1]
   int off_uv_g = 0, off_uv_l = 0, off_wa_g = 0, off_wa_l = 0, off_wb = 0;
@@ -273,7 +274,7 @@ rk_status rk_create_ex(const rk_profile* prof, uint32_t flags, rk_ctx** out) {
   if (e == cudaSuccess) e = stream_setup();
   if (e == cudaSuccess) e = proj_fused_setup();
   if (e == cudaSuccess) e = decode_attn_setup();
-  if (e == cudaSuccess) e = matvec4_setup();
+  if (e == cudaSuccess) e = matvec4_setup(ctx->matvec_slots, ctx->sm_count);
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&ctx->d_status), sizeof(DeviceStatus));
   if (e == cudaSuccess) e = cudaMemset(ctx->d_status, 0, sizeof(DeviceStatus));
   if (e != cudaSuccess) {
@@ -1429,7 +1430,7 @@ rk_status rk_matvec4(rk_ctx* ctx, const rk_w4* w4, const void* x, int64_t x_stri
   p.out_f32 = out_dtype;
   p.status = ctx->d_status;
   p.wait_ns = ctx->wait_ns;
-  cudaError_t e = launch_matvec4(p, static_cast<cudaStream_t>(stream));
+  cudaError_t e = launch_matvec4(p, ctx->matvec_slots, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "matrix-vector launch");
 }
 

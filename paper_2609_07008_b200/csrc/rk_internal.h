@@ -250,14 +250,18 @@ struct Matvec4Params {
   void* y;                 // token t at y + t * y_stride: [n_mat][n_out]
   int64_t x_stride, y_stride, n_tok;
   int32_t n_mat, n_out, k, group, out_f32;
-  int32_t stages, stage_toks;  // pipeline depth and tokens per stage (set by the launcher)
+  // set by the launcher: thread blocks along k, rounds of them, 64-wide blocks of k per thread block; tiles per run, runs per
+  // matrix; pipeline depth and shared memory
+  int32_t split, passes, slice, run, runs, stages;
+  uint32_t stage_bytes, red_bytes;
   DeviceStatus* status;
   unsigned long long wait_ns;
 };
 cudaError_t launch_quant4(const void* w, int32_t n_mat, int32_t n_out, int32_t k, int32_t group, void* codes, void* scales,
                           cudaStream_t stream);
-cudaError_t matvec4_setup();
-cudaError_t launch_matvec4(Matvec4Params p, cudaStream_t stream);
+// slots[i]: clusters of 1 << i thread blocks that run at the same time on the current device
+cudaError_t matvec4_setup(int32_t* slots, int sm_count);
+cudaError_t launch_matvec4(Matvec4Params p, const int32_t* slots, cudaStream_t stream);
 
 #ifdef __CUDACC__
 // scale byte -> the bf16 value in both halves: 2^((b >> 3) - 20) (1 + (b & 7) / 8); 255 is NaN

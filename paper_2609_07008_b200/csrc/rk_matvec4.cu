@@ -18,24 +18,38 @@
 namespace rk {
 namespace {
 
-constexpr int kWarps = 8;            // consumers; one more warp issues the copies
-constexpr int kChunkBlocks = 16;     // 64-wide blocks of k per pipeline stage
-constexpr uint32_t kTileBytes = kChunkBlocks * 512;        // codes of 16 output rows
-constexpr uint32_t kTokBytes = kChunkBlocks * 128 + 64;    // x of one token; padded so that two rows fill the 32 banks
-constexpr int kMaxStages = 4;
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kMaxBlocks = 4;                           // 64-wide blocks of k whose x a warp keeps in registers
+constexpr int kSliceBlocks = kWarps * kMaxBlocks;       // blocks of k of one thread block at a time: 2048 k
+constexpr int kMaxSplit = 8;                            // thread blocks that share k (a portable cluster)
+constexpr int kStages = 2;
+constexpr int kBatch = 2;                               // tiles per stage
+constexpr int kUnit = 512;                              // fp32 sums of one 16 x 8 product, in fragment order
+constexpr int kMaxRun = 32;                             // products of one thread block in all
+constexpr int kSmemBytes = 108 * 1024;                  // two thread blocks share an SM
 
+// d = a b + (first ? 0 : d)
+template <bool kFirst>
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  if constexpr (kFirst) {
+    asm(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+  } else {
+    asm(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
 }
 
 __device__ __forceinline__ void unpack_codes(uint32_t v, uint32_t (&a)[4]) {
   const uint32_t k136 = 0x43084308u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t t = ((v >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+    uint32_t t;  // (v >> 4 i) & 0x000f000f | 0x43004300
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(t) : "r"(v >> (4 * i)), "r"(0x000f000fu), "r"(0x43004300u));
     const __nv_bfloat162 n = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&t), *reinterpret_cast<const __nv_bfloat162*>(&k136));
     a[i] = *reinterpret_cast<const uint32_t*>(&n);
   }
@@ -47,176 +61,196 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 
-// One block: RT tiles of 16 output rows, up to 8 * NT tokens.  Codes and x of 1024 k at a time come in by bulk copies, up
-// to four stages ahead, which keeps tens of KB in flight per SM without holding them in registers (with plain loads in the
-// consuming warps the copies of a warp were serialised by its products: 14.8 us instead of 5 for 17 MB).  The warps
-// take the 64-wide blocks of a stage in turn and add their sums up in shared memory in warp order.
-template <int RT, int NT>
-__global__ void __launch_bounds__(kWarps * 32 + 32) rk_matvec4_kernel(const __grid_constant__ Matvec4Params p) {
+__device__ __forceinline__ float load_peer(uint32_t at) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// A thread block owns a slice of k and a run of 16-row tiles; x of its slice stays in its warps' registers (as B
+// fragments, kBlocks blocks of 64 per warp) while the weights of tile after tile pass by, two tiles' slices of codes and
+// scales per pipeline stage.  So x is read once per cluster and not once per tile: for 16 tokens x weighs twice a tile's
+// codes.  The thread blocks of a cluster hold the slices of the same run; sums go lanes -> warps (in warp order, through
+// shared memory) -> slices (in rank order, out of the peers' shared memory), so that results do not depend on timing.
+template <int NT, int kGroup, int kBlocks>
+__global__ void __launch_bounds__(kThreads, 2) rk_matvec4_kernel(const __grid_constant__ Matvec4Params p) {
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float red[kWarps][RT * NT][128];
-  __shared__ __align__(8) uint64_t bars[2 * kMaxStages];
+  __shared__ __align__(8) uint64_t bars[kStages];
   __shared__ int abort_word;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int g = lane >> 2, t = lane & 3;
+  constexpr int kUnits = kBatch * NT;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int tiles = p.n_out >> 4, kb = p.k >> 6;
-  const int per_mat = (tiles + RT - 1) / RT;
-  const int mat = (int)(blockIdx.x / per_mat), tile0 = (int)(blockIdx.x % per_mat) * RT;
+  const int rank = (int)(blockIdx.x % p.split), unit = (int)(blockIdx.x / p.split);
+  const int mat = unit / p.runs, tile0 = (unit - mat * p.runs) * p.run;
+  const int n_tiles = min(p.run, tiles - tile0), n_batches = (n_tiles + kBatch - 1) / kBatch;
   const int64_t tok0 = (int64_t)blockIdx.y * 8 * NT;
   const int n_tok = (int)min((int64_t)8 * NT, p.n_tok - tok0);
-  const int chunks = (kb + kChunkBlocks - 1) / kChunkBlocks;
-  const uint32_t stage_bytes = RT * kTileBytes + (uint32_t)p.stage_toks * kTokBytes;
   const uint32_t smem_base = smem_u32(smem), bar0 = smem_u32(bars);
-  auto full = [&](int s) -> uint32_t { return bar0 + 8u * s; };
-  auto empty = [&](int s) -> uint32_t { return bar0 + 8u * (kMaxStages + s); };
+  const uint32_t tile_bytes = p.stage_bytes / kBatch, off_red = p.stages * p.stage_bytes, off_out = off_red + p.red_bytes;
   volatile int* abort_flag = &abort_word;
+  // 64-wide blocks of k in this thread block's slice of a pass; none behind the end
+  auto blocks = [&](int pass) -> int { return max(0, min(p.slice, kb - (pass * p.split + rank) * p.slice)); };
+  auto load = [&](int pass, int batch, int s) {  // one thread
+    const int b0 = (pass * p.split + rank) * p.slice, nb = blocks(pass);
+    if (nb == 0) return;
+    const int g0 = b0 * 64 / kGroup, ng = nb * 64 / kGroup, groups = p.k / kGroup;
+    const int n = min(kBatch, n_tiles - batch * kBatch);
+    const int64_t tile = (int64_t)mat * tiles + tile0 + batch * kBatch;
+    mbar_arrive_expect_tx(bar0 + 8u * s, (uint32_t)(n * (nb * 512 + ng * 32)));
+    for (int i = 0; i < n; ++i) {
+      const uint32_t dst = smem_base + (uint32_t)s * p.stage_bytes + (uint32_t)i * tile_bytes;
+      bulk_load(dst, p.codes + ((tile + i) * kb + b0) * 32, (uint32_t)nb * 512u, bar0 + 8u * s);
+      bulk_load(dst + (uint32_t)p.slice * 512u, p.scales + ((tile + i) * groups + g0) * 8, (uint32_t)ng * 32u, bar0 + 8u * s);
+    }
+  };
+  int next_pass = 0, next_batch = 0;  // of the next load
+  auto load_next = [&](int s) {
+    if (next_pass == p.passes) return;
+    if (threadIdx.x == 0) load(next_pass, next_batch, s);
+    if (++next_batch == n_batches) {
+      next_batch = 0;
+      ++next_pass;
+    }
+  };
   if (threadIdx.x == 0) {
     abort_word = 0;
-    for (int s = 0; s < p.stages; ++s) {
-      mbar_init(full(s), 1);
-      mbar_init(empty(s), kWarps);
-    }
+    for (int s = 0; s < kStages; ++s) mbar_init(bar0 + 8u * s, 1);
     fence_mbar_init_cluster();
   }
+  for (int s = 0; s < p.stages; ++s) load_next(s);
   __syncthreads();
-  const int groups = p.k / p.group;
-  float acc[RT][NT][4];
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[r][n][e] = 0.f;
 
-  if (warp == kWarps) {
-    // ------------------------------ copies ------------------------------
-    if (lane == 0) {
-      const int n_t = min(RT, tiles - tile0);
-      const uint4* w = p.codes + ((int64_t)mat * tiles + tile0) * kb * 32;
-      const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(p.x) + tok0 * p.x_stride + (int64_t)mat * p.k;
-      for (int c = 0, s = 0, phase = 0; c < chunks; ++c) {
-        if (c >= p.stages &&
-            !mbar_wait_bounded<false>(empty(s), (uint32_t)(phase ^ 1), p.wait_ns, abort_flag, p.status, 61, c))
-          break;
-        const int nb = min(kChunkBlocks, kb - c * kChunkBlocks);
-        const uint32_t dst = smem_base + (uint32_t)s * stage_bytes;
-        mbar_arrive_expect_tx(full(s), (uint32_t)(n_t * nb * 512 + n_tok * nb * 128));
-        for (int r = 0; r < n_t; ++r)
-          bulk_load(dst + r * kTileBytes, w + ((int64_t)r * kb + c * kChunkBlocks) * 32, (uint32_t)nb * 512u, full(s));
-        for (int n = 0; n < n_tok; ++n)
-          bulk_load(dst + RT * kTileBytes + n * kTokBytes, x + n * p.x_stride + c * kChunkBlocks * 64, (uint32_t)nb * 128u, full(s));
-        if (++s == p.stages) {
-          s = 0;
-          phase ^= 1;
+  float* const out = reinterpret_cast<float*>(smem + off_out);
+  int s = 0;
+  uint32_t phases = 0u;  // bit s: the parity of stage s
+  bool ok = true;
+  for (int pass = 0; ok && pass < p.passes; ++pass) {
+    const int b0 = (pass * p.split + rank) * p.slice, nb = blocks(pass);
+    // This warp's blocks are warp * kBlocks + i.  One beyond the slice has x = 0 and the weights of the slice's last block, so it adds
+    // zeros (or the NaN that block gives anyway).
+    uint4 xv[kBlocks][NT][2];
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) {
+      const int at = warp * kBlocks + i;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        // a token beyond the last repeats it: its column of the product is not stored, and columns do not mix
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.x) + (tok0 + min(8 * n + g, n_tok - 1)) * p.x_stride +
+                                   (int64_t)mat * p.k + (int64_t)(b0 + at) * 64 + t * 8;
+        xv[i][n][0] = xv[i][n][1] = make_uint4(0u, 0u, 0u, 0u);
+        if (at < nb) {
+          xv[i][n][0] = __ldg(reinterpret_cast<const uint4*>(src));
+          xv[i][n][1] = __ldg(reinterpret_cast<const uint4*>(src + 32));
         }
       }
     }
-  } else {
-    // ------------------------------ products ------------------------------
-    const bool g32 = p.group == 32;
-    const int gshift = p.group == 128 ? 1 : 0;
-    const uint32_t* sc[RT];
+#pragma unroll 1
+    for (int batch = 0; batch < n_batches; ++batch) {
+      uint8_t* const red = smem + off_red;
+      if (nb > 0) ok = mbar_wait_bounded<false>(bar0 + 8u * s, (phases >> s) & 1u, p.wait_ns, abort_flag, p.status, 62, batch);
+      ok = __all_sync(0xffffffffu, ok);
+      const uint8_t* tile = smem + (uint32_t)s * p.stage_bytes;
+      const int n = min(kBatch, n_tiles - batch * kBatch);
+#pragma unroll 1
+      for (int j = 0; j < n; ++j, tile += tile_bytes) {
+        float acc[NT][4];
 #pragma unroll
-    for (int r = 0; r < RT; ++r)  // a tile beyond the last (odd counts) repeats the last one's scales; it is not stored
-      sc[r] = p.scales + ((int64_t)mat * tiles + min(tile0 + r, tiles - 1)) * groups * 8 + g;
-    bool ok = true;
-    for (int c = 0, s = 0, phase = 0; c < chunks && ok; ++c) {
-      // this warp's blocks of the stage: warp, warp + 8; their scales come straight from memory, ahead of the wait
-      uint32_t s0[2][RT], s1[2][RT];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int b = c * kChunkBlocks + warp + 8 * i;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          s0[i][r] = s1[i][r] = 0u;
-          if (b < kb) {
-            s0[i][r] = __ldg(sc[r] + (g32 ? 2 * b : b >> gshift) * 8);
-            if (g32) s1[i][r] = __ldg(sc[r] + (2 * b + 1) * 8);
-          }
-        }
-      }
-      ok = mbar_wait_bounded<false>(full(s), (uint32_t)phase, p.wait_ns, abort_flag, p.status, 62, c);
-      if (!ok) break;
-      const uint8_t* stage = smem + (uint32_t)s * stage_bytes;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int at = warp + 8 * i;
-        if (c * kChunkBlocks + at >= kb) break;
-        uint4 xv[NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          // a token beyond n_tok has whatever is there: its column of the product is not stored, and columns do not mix
-          const int tok = min(8 * n + g, n_tok - 1);
-          const uint8_t* xs = stage + RT * kTileBytes + tok * kTokBytes + at * 128 + t * 16;
-          xv[n][0] = *reinterpret_cast<const uint4*>(xs);
-          xv[n][1] = *reinterpret_cast<const uint4*>(xs + 64);
-        }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const uint4 wv = *reinterpret_cast<const uint4*>(stage + r * kTileBytes + at * 512 + lane * 16);
+        for (int u = 0; u < NT; ++u) acc[u][0] = acc[u][1] = acc[u][2] = acc[u][3] = 0.f;
+        if (ok && nb > 0) {
+          const uint32_t* sc = reinterpret_cast<const uint32_t*>(tile + (uint32_t)p.slice * 512u) + g;
           float d[NT][4];
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[n][e] = 0.f;
-          const uint32_t words[4] = {wv.x, wv.y, wv.z, wv.w};
           auto add = [&](uint32_t sv) {
             const float lo = __uint_as_float(sv << 16), hi = __uint_as_float(sv & 0xffff0000u);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              acc[r][n][0] = fmaf(d[n][0], lo, acc[r][n][0]);
-              acc[r][n][1] = fmaf(d[n][1], lo, acc[r][n][1]);
-              acc[r][n][2] = fmaf(d[n][2], hi, acc[r][n][2]);
-              acc[r][n][3] = fmaf(d[n][3], hi, acc[r][n][3]);
-              d[n][0] = d[n][1] = d[n][2] = d[n][3] = 0.f;
+            for (int u = 0; u < NT; ++u) {
+              acc[u][0] = fmaf(d[u][0], lo, acc[u][0]);
+              acc[u][1] = fmaf(d[u][1], lo, acc[u][1]);
+              acc[u][2] = fmaf(d[u][2], hi, acc[u][2]);
+              acc[u][3] = fmaf(d[u][3], hi, acc[u][3]);
             }
           };
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t a[4];
-            unpack_codes(words[q], a);
+          for (int i = 0; i < kBlocks; ++i) {
+            const int at = min(warp * kBlocks + i, nb - 1);
+            const uint4 wv = *reinterpret_cast<const uint4*>(tile + at * 512 + lane * 16);
+            const uint32_t words[4] = {wv.x, wv.y, wv.z, wv.w};
+            // two blocks make a group of 128 where a warp has both; slices are even, so they are its blocks 0, 1 and 2, 3
+            constexpr bool kPairs = kGroup == 128 && kBlocks > 1;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const uint4 v = xv[n][q >> 1];
-              mma_16816(d[n], a, (q & 1) ? v.z : v.x, (q & 1) ? v.w : v.y);
+            for (int q = 0; q < 4; ++q) {
+              uint32_t a[4];
+              unpack_codes(words[q], a);
+#pragma unroll
+              for (int u = 0; u < NT; ++u) {
+                const uint4 v = xv[i][u][q >> 1];
+                const uint32_t x0 = (q & 1) ? v.z : v.x, x1 = (q & 1) ? v.w : v.y;
+                if ((q == 0 && !(kPairs && (i & 1))) || (q == 2 && kGroup == 32)) mma_16816<true>(d[u], a, x0, x1);
+                else mma_16816<false>(d[u], a, x0, x1);
+              }
+              if (q == 1 && kGroup == 32) add(sc[16 * at]);  // the first 32 of the block are a group of their own
             }
-            if (q == 1 && g32) add(s0[i][r]);  // the first 32 of the block are a group of their own
+            if (!kPairs || (i & 1)) add(sc[8 * (kGroup == 32 ? 2 * at + 1 : kGroup == 64 ? at : at >> 1)]);
           }
-          add(g32 ? s1[i][r] : s0[i][r]);
         }
+        if (j == 0 && batch + pass > 0) named_barrier_sync(2, kThreads);  // the last batch's sums have been read
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+          *reinterpret_cast<float4*>(red + (warp * kUnits + j * NT + u) * kUnit + lane * 16) = make_float4(acc[u][0], acc[u][1], acc[u][2], acc[u][3]);
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(empty(s));
-      if (++s == p.stages) {
-        s = 0;
-        phase ^= 1;
+      ok = named_barrier_and(1, kThreads, ok);  // a warp that gave up must not leave the others in a barrier
+      if (!ok) break;
+      load_next(s);  // everyone is done with this stage
+      if (nb > 0) phases ^= 1u << s;
+      if (++s == p.stages) s = 0;
+      // sums over the warps, kUnits * 128 of them
+      constexpr int kEach = kUnits * 128 / kThreads;
+      const int u = (int)threadIdx.x * kEach / 128;
+      if (u < n * NT) {
+        float v[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) v[e] = 0.f;
+        const float* src = reinterpret_cast<const float*>(red) + threadIdx.x * kEach;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k)
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) v[e] += src[k * kUnits * (kUnit / 4) + e];
+        float* dst = out + batch * kUnits * (kUnit / 4) + threadIdx.x * kEach;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) dst[e] = pass > 0 ? dst[e] + v[e] : v[e];
       }
     }
-    // accumulator e of lane (g, t): row g + 8 (e >> 1), token 2 t + (e & 1); stored as [token][row] of 8 x 16
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) red[warp][r * NT + n][(2 * t + (e & 1)) * 16 + g + 8 * (e >> 1)] = acc[r][n][e];
   }
   if (*abort_flag != 0) {  // a wait has run out: copies in flight get a bounded time to land before the block goes away
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
   }
-  __syncthreads();
-  if (*abort_flag != 0) return;
-  for (int i = threadIdx.x; i < RT * NT * 128; i += kWarps * 32 + 32) {
-    const int rn = i >> 7, at = i & 127, r = rn / NT, n = rn - r * NT;
+  auto join = [&]() {
+    if (p.split > 1) {
+      __syncwarp();
+      cluster_arrive();
+      cluster_wait();
+    } else {
+      __syncthreads();
+    }
+  };
+  join();
+  // A peer that gave up has reported it; its sums are garbage then, like every result of a call that failed.
+  const int n_sums = n_tiles * NT * 128;
+  for (int i = rank * kThreads + threadIdx.x; i < n_sums; i += p.split * kThreads) {
+    // element e of lane (g, t) in a product: row g + 8 (e >> 1), token 2 t + (e & 1)
+    const int row = i & 15, col = (i >> 4) & 7, at = i >> 7, n = at % NT;
+    const uint32_t src = off_out + (uint32_t)(at * kUnit + ((row & 7) * 4 + (col >> 1)) * 16 + ((row >> 3) * 2 + (col & 1)) * 4);
+    if (8 * n + col >= n_tok) continue;
     float v = 0.f;
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) v += red[k][rn][at];
-    const int64_t tok = tok0 + 8 * n + (at >> 4);
-    const int tile = tile0 + r;
-    if (tok >= p.n_tok || tile >= tiles) continue;
-    const int64_t o = tok * p.y_stride + (int64_t)mat * p.n_out + tile * 16 + (at & 15);
+    if (p.split > 1) {
+      for (int r = 0; r < p.split; ++r) v += load_peer(mapa_shared(smem_base + src, (uint32_t)r));
+    } else {
+      v = *reinterpret_cast<const float*>(smem + src);
+    }
+    const int64_t o = (tok0 + 8 * n + col) * p.y_stride + (int64_t)mat * p.n_out + (tile0 + at / NT) * 16 + row;
     if (p.out_f32) static_cast<float*>(p.y)[o] = v;
     else static_cast<__nv_bfloat16*>(p.y)[o] = __float2bfloat16_rn(v);
   }
+  if (p.split > 1) join();  // shared memory has to outlive the peers' reads
 }
 
 // ---- laying the weights out (once) ------------------------------------------------------------------------
@@ -298,26 +332,77 @@ cudaError_t launch_quant4(const void* w, int32_t n_mat, int32_t n_out, int32_t k
   return cudaGetLastError();
 }
 
-cudaError_t matvec4_setup() {
-  cudaError_t e = cudaFuncSetAttribute(rk_matvec4_kernel<1, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxStages * (int)(kTileBytes + 8 * kTokBytes));
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(rk_matvec4_kernel<2, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxStages * (int)(2 * kTileBytes + 16 * kTokBytes));
-  return e;
+namespace {
+using Matvec4Kernel = void (*)(const Matvec4Params);
+template <int NT, int kGroup>
+Matvec4Kernel matvec4_pick(int blocks) {
+  return blocks == 1 ? rk_matvec4_kernel<NT, kGroup, 1> : blocks == 2 ? rk_matvec4_kernel<NT, kGroup, 2> : rk_matvec4_kernel<NT, kGroup, 4>;
+}
+Matvec4Kernel matvec4_kernel(int nt, int group, int blocks) {
+  if (nt == 1) return group == 32 ? matvec4_pick<1, 32>(blocks) : group == 64 ? matvec4_pick<1, 64>(blocks) : matvec4_pick<1, 128>(blocks);
+  return group == 32 ? matvec4_pick<2, 32>(blocks) : group == 64 ? matvec4_pick<2, 64>(blocks) : matvec4_pick<2, 128>(blocks);
+}
+void matvec4_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute& attr, int split) {
+  cfg.blockDim = dim3(kThreads);
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)split;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = split > 1 ? 1 : 0;
+}
+}  // namespace
+
+cudaError_t matvec4_setup(int32_t* slots, int sm_count) {
+  for (int nt = 1; nt <= 2; ++nt)
+    for (int group = 32; group <= 128; group *= 2)
+      for (int blocks = 1; blocks <= 4; blocks *= 2) {
+        cudaError_t e = cudaFuncSetAttribute(matvec4_kernel(nt, group, blocks), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+        if (e != cudaSuccess) return e;
+      }
+  slots[0] = 2 * sm_count;
+  for (int i = 1; i < 4; ++i) {  // clusters of 1 << i thread blocks that run at the same time
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr = {};
+    matvec4_config(cfg, attr, 1 << i);
+    cfg.gridDim = dim3(1u << i);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    int n = 0;
+    cudaError_t e = cudaOccupancyMaxActiveClusters(&n, matvec4_kernel(2, 128, kMaxBlocks), &cfg);
+    if (e != cudaSuccess) return e;
+    slots[i] = n > 0 ? n : 1;
+  }
+  return cudaSuccess;
 }
 
-cudaError_t launch_matvec4(Matvec4Params p, cudaStream_t stream) {
-  const int tiles = p.n_out / 16, chunks = (p.k / 64 + kChunkBlocks - 1) / kChunkBlocks;
-  p.stages = chunks < kMaxStages ? chunks : kMaxStages;
-  // up to eight tokens one tile per block; above that x weighs as much as the codes, and two tiles share it
-  if (p.n_tok <= 8) {
-    p.stage_toks = (int32_t)p.n_tok;
-    rk_matvec4_kernel<1, 1><<<dim3((unsigned)(p.n_mat * tiles), 1), kWarps * 32 + 32, p.stages * (kTileBytes + p.stage_toks * kTokBytes), stream>>>(p);
-  } else {
-    p.stage_toks = (int32_t)(p.n_tok < 16 ? p.n_tok : 16);
-    rk_matvec4_kernel<2, 2><<<dim3((unsigned)(p.n_mat * ((tiles + 1) / 2)), (unsigned)((p.n_tok + 15) / 16)), kWarps * 32 + 32,
-                              p.stages * (2 * kTileBytes + p.stage_toks * kTokBytes), stream>>>(p);
-  }
-  return cudaGetLastError();
+cudaError_t launch_matvec4(Matvec4Params p, const int32_t* slots, cudaStream_t stream) {
+  const int tiles = p.n_out / 16, kb = p.k / 64, nt = p.n_tok <= 8 ? 1 : 2;
+  const int64_t tok_blocks = (p.n_tok + 8 * nt - 1) / (8 * nt);
+  // k goes over as many thread blocks as its slices of up to 2048 need, beyond eight in several passes
+  int log_split = 0;
+  while ((1 << log_split) < kMaxSplit && (kSliceBlocks << log_split) < kb) ++log_split;
+  p.split = 1 << log_split;
+  p.passes = (kb + kSliceBlocks * p.split - 1) / (kSliceBlocks * p.split);
+  const int parts = p.split * p.passes;
+  p.slice = ((kb + parts - 1) / parts + 1) & ~1;  // even: a group of 128 is two blocks
+  const int blocks = p.slice <= kWarps ? 1 : p.slice <= 2 * kWarps ? 2 : kMaxBlocks;
+  // tiles per thread block: one round of what fits the device, within the sums' space
+  const int64_t all = (int64_t)p.n_mat * tiles * tok_blocks;
+  int64_t run = (all + slots[log_split] - 1) / slots[log_split];
+  if (run > kMaxRun / nt) run = kMaxRun / nt;
+  if (run > tiles) run = tiles;
+  p.runs = (tiles + (int)run - 1) / (int)run;
+  p.run = (tiles + p.runs - 1) / p.runs;
+  p.stage_bytes = (uint32_t)(kBatch * (p.slice * 512 + p.slice * 64 / p.group * 32));
+  const int per_pass = (p.run + kBatch - 1) / kBatch, batches = p.passes * per_pass;
+  p.red_bytes = (uint32_t)(kWarps * kBatch * nt * kUnit);
+  p.stages = batches < kStages ? batches : kStages;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr = {};
+  matvec4_config(cfg, attr, p.split);
+  cfg.gridDim = dim3((unsigned)((int64_t)p.n_mat * p.runs * p.split), (unsigned)tok_blocks);
+  cfg.dynamicSmemBytes = p.stages * p.stage_bytes + p.red_bytes + (uint32_t)(per_pass * kBatch * nt * kUnit);
+  cfg.stream = stream;
+  return cudaLaunchKernelEx(&cfg, matvec4_kernel(nt, p.group, blocks), p);
 }
 
 }  // namespace rk
