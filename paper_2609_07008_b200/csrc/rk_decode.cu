@@ -46,33 +46,35 @@ constexpr uint32_t kQChunk = 8192;   // up to 64 rows x 64 dims bf16
 
 constexpr uint32_t kOffQ = 0;                        // 8 latent chunks, then the turned rope chunk: high and low parts
 constexpr uint32_t kOffV = 10 * kQChunk;             // 8 latent chunks of the keys
-constexpr uint32_t kOffP = kOffV + 8 * kKChunk;      // P^T
+constexpr uint32_t kOffP = kOffV + 8 * kKChunk;      // rope chunk of the keys until the scores are done, then P^T
 constexpr uint32_t kOffBars = kOffP + kKChunk;
-enum { B_QFULL = 0, B_QROPE = 1, B_KFULL = 2 /*2*/, B_KFREE = 4 /*2*/, B_VFULL = 6 /*4*/, B_SFULL = 10, B_PREADY = 11,
-       B_PVDONE = 12 /*4*/, B_COUNT = 16 };
+// every one of them has one phase per tile (B_QFULL: per group)
+enum { B_QFULL = 0, B_QROPE = 1, B_KROPE = 2, B_KFULL = 3 /*4*/, B_KFREE = 7 /*4*/, B_SFULL = 11, B_PREADY = 12, B_PVDONE = 13 /*4*/,
+       B_COUNT = 17 };
 constexpr uint32_t kOffTmem = kOffBars + B_COUNT * 8;
 constexpr uint32_t kOffAbort = kOffTmem + 4;
 constexpr uint32_t kOffFlag = kOffTmem + 8;          // int: 1 + the last tile some row's maximum has to be raised for
-constexpr uint32_t kOffMax = kOffBars + 144;         // float [64]: running maximum of each row, base-2 units
+constexpr uint32_t kOffMax = kOffBars + 160;         // float [64]: running maximum of each row, base-2 units
 constexpr uint32_t kOffPos = kOffMax + 256;          // int [64]: request position of each row (-1: no row)
 constexpr uint32_t kOffRed = kOffPos + 256;          // float [4][64]: per lane quarter
 constexpr uint32_t kOffAlpha = kOffRed + 1024;       // float [64]: factor of the last raise of a row's maximum
-constexpr uint32_t kSmemUsed = kOffAlpha + 256;
+constexpr uint32_t kOffNan = kOffAlpha + 256;         // uint8 [2][2][128]: tile parity, half of the key's groups, key: a scale is NaN
+constexpr uint32_t kSmemUsed = kOffNan + 512;
 constexpr uint32_t kSmemBytes = kSmemUsed;
 
 // tensor memory columns: O^T takes 4 x N from 0; two score buffers; two slots of 128 dims of the keys (bf16 pairs)
 constexpr uint32_t kColS = 256, kColK = 384;
 constexpr float kNoMax = -1e30f;     // "no key seen yet": finite, so that differences stay defined
 
-// Registers per thread out of the launch's 640 x 96, by warpgroup: (1 x 56 + 2 x 112 + 2 x 96) x 128 = 60416 of 61440.  Nothing in
+// Registers per thread out of the launch's 640 x 96, by warpgroup: (1 x 56 + 2 x 96 + 2 x 112) x 128 = 60416 of 61440.  Nothing in
 // the loops may spill: shared memory takes nearly all of L1, so a spilled register comes back from L2.
-constexpr int kRegsIssue = 56, kRegsKeys = 112, kRegsSoftmax = 96;
+constexpr int kRegsIssue = 56, kRegsKeys = 96, kRegsSoftmax = 112;
 template <int N>
 __device__ __forceinline__ void reg_raise() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void reg_lower() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-enum { W_QFULL = 41, W_QROPE, W_KFULL, W_KFREE, W_VFULL, W_SFULL, W_PREADY, W_PVDONE };
+enum { W_QFULL = 41, W_QROPE, W_KROPE, W_KFULL, W_KFREE, W_SFULL, W_PREADY, W_PVDONE };
 
 // Walks one CTA's run of key tiles.  A "group" is the part of one (sequence, row tile) that this CTA owns.
 struct Cursor {
@@ -132,13 +134,15 @@ __device__ __forceinline__ void prefetch_page(const uint8_t* page) {
 // 1024 bytes, version 1 and 128-byte swizzle, is the same for every operand here.
 constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
 __device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return ((addr & 0x3FFFFu) >> 4) | ((lbo >> 4) << 16); }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+// the keys' rope chunk as it is in the pages: 8 rows x 16 bytes contiguous, the next 8 rows 128 bytes on, no swizzle
+constexpr uint32_t kDescHiPlain = (128u >> 4) | (1u << 14);
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t a_hi, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
-      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "mov.b64 da, {%1, %6};\n\tmov.b64 db, {%2, %5};\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
-      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kDescHi), "r"(a_hi)
       : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, uint32_t accumulate) {
@@ -151,6 +155,11 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b, 
       : "memory");
 }
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
 __device__ __forceinline__ uint32_t globaltimer_lo() {
   uint32_t t;
   asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
@@ -216,12 +225,10 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     store_shared(smem_base + kOffAbort, 0u);
     mbar_init(bar(B_QFULL), 1);
     mbar_init(bar(B_QROPE), 1);
-    for (int i = 0; i < 2; ++i) {
+    mbar_init(bar(B_KROPE), 1);
+    for (int i = 0; i < 4; ++i) {
       mbar_init(bar(B_KFULL + i), kKeyWarps);
       mbar_init(bar(B_KFREE + i), 1 + kSoftWarps);
-    }
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(bar(B_VFULL + i), kSoftWarps);
       mbar_init(bar(B_PVDONE + i), 1);
     }
     mbar_init(bar(B_SFULL), 1);
@@ -250,69 +257,74 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
 
   if (warp == 0) {
     // ------------------------------ MMA issue (whole warp loops, one elected lane issues) ----------------------
-    // Scores of a tile come in five pieces as the keys reach tensor memory: rope, then four times 128 dims.  The first two
-    // pieces of a tile run under the softmax of the one before, the rest behind its value products.  The order is fixed
-    // and the products come in long batches: the tensor core's queue holds only a few products, so whatever this warp
-    // does between two batches beyond some 150 clocks leaves it idle (polling several barriers and taking the pieces in
-    // the order they arrived cost 500 clocks a batch).
+    // Scores of a tile come in five pieces: four times 128 dims as the keys reach tensor memory, then rope.  The first two
+    // run under the softmax of the tile before, the rest behind its value products.  The order is fixed and the products come in
+    // long batches: the tensor core's queue holds only a few products, so whatever this warp does between two batches beyond some
+    // 150 clocks leaves it idle.  And everything is kept small: with the pieces and their descriptors unrolled the role spilled, and
+    // every reload cost the tensor core an L2 latency.
     constexpr uint32_t id_qk = umma_idesc_bf16(128, kRows, 0, 0);
     constexpr uint32_t id_pv = umma_idesc_bf16(128, kRows, 1, 1);
     uint32_t t = 0, groups = 0;  // tiles and groups so far: their parities are the barriers' phases
     bool ok = true;
-    // piece i of tile tq: the 5 tq + i-th piece of all, in slot (tq + i) & 1 as 5 is odd
-    auto piece = [&](auto index, uint32_t tq) {
-      constexpr int i = decltype(index)::value;
-      const uint32_t u = 5u * tq + i, slot = u & 1u;
-      ok = ok && wait(B_KFULL + slot, (u >> 1) & 1u, W_KFULL);
-      if (i == 0) ok = ok && wait(B_QROPE, tq & 1u, W_QROPE);
+    // 128 dims of tile tq, slot i & 1.  The reduction turns the loop's counters into uniform values for the compiler, as the
+    // products' operands have to be.
+    auto piece = [&](int i, uint32_t tq) {
+      ok = ok && wait(B_KFULL + i, tq & 1u, W_KFULL);
       if (!ok) return;
       tc_fence_after_sync();
-      const uint32_t ts = tmem + kColS + (tq & 1u) * 64u, tk = tmem + kColK + slot * 64u;
+      const uint32_t w = __reduce_max_sync(0xffffffffu, (uint32_t)i | ((tq & 1u) << 3)), iu = w & 3u;
+      const uint32_t ts = tmem + kColS + (w >> 3) * 64u, tk = tmem + kColK + (iu & 1u) * 64u;
+      const uint32_t db = desc_lo(smem_base + kOffQ, 16) + 2u * iu * (kQChunk >> 4);
       if (elect_one()) {
-        const uint32_t db = desc_lo(smem_base + kOffQ + (i == 0 ? 8 : 2 * (i - 1)) * kQChunk, 16);
 #pragma unroll
-        for (int s = 0; s < 8; ++s)  // rope: the same 64 dims of the keys against the high and the low part of the turned queries
-          mma_ts(ts, tk + 8u * (i == 0 ? (s & 3) : s), db + (uint32_t)(((s >> 2) * kQChunk + (s & 3) * 32) >> 4), id_qk,
-                 (i > 0 || s > 0) ? 1u : 0u);
-        umma_commit_1(bar(B_KFREE + slot));
-        if (i == 4) umma_commit_1(bar(B_SFULL));
+        for (int s = 0; s < 8; ++s)
+          mma_ts(ts, tk + 8u * s, db + (uint32_t)(((s >> 2) * kQChunk + (s & 3) * 32) >> 4), id_qk, s > 0 ? 1u : iu);
+        umma_commit_1(bar(B_KFREE) + 8u * iu);
       }
       __syncwarp();
     };
-    using std::integral_constant;
     for (Cursor c(p); ok && c.next(); ++groups) {
       ok = wait(B_QFULL, groups & 1u, W_QFULL);
-      piece(integral_constant<int, 0>(), t);
-      piece(integral_constant<int, 1>(), t);
 #pragma unroll 1
-      for (int k = 0;; ++k) {
-        piece(integral_constant<int, 2>(), t);
-        piece(integral_constant<int, 3>(), t);
-        piece(integral_constant<int, 4>(), t);
-        const bool last = k + 1 == c.cnt;  // the next group has other queries
-        if (!last) {
-          piece(integral_constant<int, 0>(), t + 1);
-          piece(integral_constant<int, 1>(), t + 1);
+      for (int k = -1; ok && k < c.cnt; ++k) {
+        if (k >= 0) {  // what is left of this tile's scores
+          piece(2, t);
+          piece(3, t);
+          ok = ok && wait(B_QROPE, t & 1u, W_QROPE) && wait(B_KROPE, t & 1u, W_KROPE);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint32_t ts = tmem + kColS + __reduce_max_sync(0xffffffffu, t & 1u) * 64u;
+          if (elect_one()) {
+            const uint32_t da = desc_lo(smem_base + kOffP, 2048), db = desc_lo(smem_base + kOffQ + 8 * kQChunk, 16);
+#pragma unroll
+            for (int s = 0; s < 8; ++s)  // the same 64 dims of the keys against the high and the low part of the turned queries
+              mma_ss(ts, da + (uint32_t)(((s & 3) * 4096) >> 4), kDescHiPlain, db + (uint32_t)(((s >> 2) * kQChunk + (s & 3) * 32) >> 4), id_qk, 1u);
+            umma_commit_1(bar(B_SFULL));
+          }
+          __syncwarp();
         }
+        if (k + 1 < c.cnt) {  // the first half of the next tile's (the next group has other queries)
+          piece(0, k < 0 ? t : t + 1u);
+          piece(1, k < 0 ? t : t + 1u);
+        }
+        if (k < 0) continue;
         ok = ok && wait(B_PREADY, t & 1u, W_PREADY);
-        for (int m = 0; m < 4; ++m) ok = ok && wait(B_VFULL + m, t & 1u, W_VFULL);
         if (!ok) break;
         tc_fence_after_sync();
         if (elect_one()) {
           const uint32_t db = desc_lo(smem_base + kOffP, 16);
-#pragma unroll
-          for (int m = 0; m < 4; ++m) {  // 128 dims each: two 64-dim chunks, 16 KB apart
-            const uint32_t da = desc_lo(smem_base + kOffV + 2 * m * kKChunk, kKChunk);
+          uint32_t da = desc_lo(smem_base + kOffV, kKChunk);
+#pragma unroll 1
+          for (int m = 0; m < 4; ++m, da += (2 * kKChunk) >> 4) {  // 128 dims each: two 64-dim chunks, 16 KB apart
 #pragma unroll
             for (int s = 0; s < 8; ++s)
-              mma_ss(tmem + (uint32_t)(m * kRows), da + (uint32_t)((s * 2048) >> 4), db + (uint32_t)((s * 2048) >> 4), id_pv,
-                     (k > 0 || s > 0) ? 1u : 0u);
-            umma_commit_1(bar(B_PVDONE + m));
+              mma_ss(tmem + (uint32_t)(m * kRows), da + (uint32_t)((s * 2048) >> 4), kDescHi, db + (uint32_t)((s * 2048) >> 4), id_pv,
+                     s > 0 ? 1u : (uint32_t)k);
+            umma_commit_1(bar(B_PVDONE) + 8u * (uint32_t)m);
           }
         }
         __syncwarp();
         ++t;
-        if (last) break;
       }
     }
   } else if (warp == 1) {
@@ -370,17 +382,36 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         if (lane == 0) mbar_arrive(bar(B_QROPE));
       }
     }
+  } else if (warp == 2) {
+    // ------------------------------ keys' rope chunk: straight into the operand's place -----------------------
+    // A page holds 64 rows x 16 bytes per unit, which is the unswizzled K-major operand: 1 KB copies of a unit of a page.
+    uint32_t t = 0;
+    bool ok = true;
+    for (Cursor c(p); ok && c.next();) {
+      for (int k = 0; k < c.cnt; ++k, ++t) {
+        const int4 v = __ldg(reinterpret_cast<const int4*>(&p.tiles[c.record(k)]));
+        if (t > 0) ok = wait(B_PVDONE + 3, (t - 1) & 1u, W_PVDONE);  // P^T of the last tile has been read
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        // rows that are not there keep what is in their place: their scores are masked
+        if (lane == 0) mbar_arrive_expect_tx(bar(B_KROPE), v.w > 64 ? 16384u : 8192u);
+        __syncwarp();
+        if (lane < 16 && (lane < 8 || v.w > 64))
+          bulk_load(smem_base + kOffP + (lane & 7) * 2048 + (lane >> 3) * 1024,
+                    p.pages + (int64_t)(lane < 8 ? v.x : v.y) * kCache4PageBytes + (18 + (lane & 7)) * 1024, 1024u, bar(B_KROPE));
+      }
+    }
   } else if (warp < 4) {
     // a warp reaches the tensor memory lanes of its number modulo four: the next role starts at warp 4
   } else if (warp < kSoftWarp0) {
     // ------------------------------ keys: HBM -> registers (4-bit) -> shared memory (bf16) --------------------
     reg_raise<kRegsKeys>();
-    // Two threads per key: thread h has chunk 2 m + h (64 dims, two units) of every 128 dims m, the scale unit h (one word
-    // per chunk) and rope units 4 h .. 4 h + 3.
+    // Two threads per key: thread h has chunk 2 m + h (64 dims, two units) of every 128 dims m and the scale unit h (one word per
+    // chunk).
     const int h = (warp - kKeyWarp0) >> 2;
     const int row = 32 * (warp & 3) + lane;  // a warp reaches the tensor memory lanes of its quarter
-    const uint32_t t_k = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColK;
-    uint32_t code[32], scl[4], rope[16];
+    const uint32_t t_k = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColK + 32u * h;
+    uint32_t code[32], scl[4];
     const uint8_t* src = nullptr;  // this key's first unit in the tile being loaded, null for a row that is not there
     // rows that are not there become zeros (code 8): their scores are masked, and 0 * 0 adds nothing to O
     auto load_pair = [&](int m) {
@@ -393,22 +424,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     auto load_scale = [&]() {
       put(scl, src != nullptr ? __ldg(reinterpret_cast<const uint4*>(src + h * 1024 + 16 * 1024)) : make_uint4(0, 0, 0, 0));
     };
-    auto load_rope = [&]() {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        put(rope + 4 * e, src != nullptr ? __ldg(reinterpret_cast<const uint4*>(src + h * 4096 + (18 + e) * 1024)) : make_uint4(0, 0, 0, 0));
-    };
-    uint32_t u = 0;
+    uint32_t t = 0;
     bool ok = true;
-    // a slot of keys in tensor memory may be overwritten once its last content has been multiplied and copied
-    auto slot_free = [&]() -> bool { return u < 2 || wait(B_KFREE + (u & 1u), ((u >> 1) - 1u) & 1u, W_KFREE); };
-    auto slot_filled = [&]() {
-      tmem_wait_st();
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_KFULL + (u & 1u)));
-      ++u;
-    };
     Cursor c(p);
     bool more = c.next();
     int k = 0;
@@ -433,24 +450,14 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
 #pragma unroll
       for (int m = 0; m < 4; ++m) load_pair(m);
       load_scale();
-      load_rope();
       fetch();
     }
     while (here) {
-      ok = slot_free();
-      if (!ok) break;
-      tc_fence_after_sync();
-      // a group whose scale is NaN (byte 255) makes the whole key NaN: its score then is, and with it every output
-      if ((cache4_nan_bytes(scl[0]) | cache4_nan_bytes(scl[1]) | cache4_nan_bytes(scl[2]) | cache4_nan_bytes(scl[3])) != 0u)
-        rope[0] = 0x7fc07fc0u;
-      tmem_st_x16(t_k + (u & 1u) * 64u + 16u * h, rope);
-      slot_filled();
       const bool next = more;
-      if (next) {
-        open();
-        load_rope();
-      }
-      if (next) fetch();
+      if (next) open();
+      // A group whose scale is NaN (byte 255) makes the key's scores NaN, and with them every output that sees the key; the values
+      // stay numbers, so that rows that do not see it are untouched.
+      const bool nan = (cache4_nan_bytes(scl[0]) | cache4_nan_bytes(scl[1]) | cache4_nan_bytes(scl[2]) | cache4_nan_bytes(scl[3])) != 0u;
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         uint32_t v[32];  // 64 dims of this key
@@ -467,15 +474,24 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         // the next tile's loads go out as the registers become free: they have a whole tile's time to arrive
         if (next) {
           load_pair(m);
-          if (m == 3) load_scale();
+          if (m == 3) {
+            load_scale();
+            fetch();
+          }
         }
-        ok = slot_free();
+        // the slot may be overwritten once its last content has been multiplied and copied
+        ok = m >= 2 ? wait(B_KFREE + m - 2, t & 1u, W_KFREE) : (t == 0 || wait(B_KFREE + m + 2, (t - 1u) & 1u, W_KFREE));
         if (!ok) break;
         tc_fence_after_sync();
-        tmem_st_x32(t_k + (u & 1u) * 64u + 32u * h, v);
-        slot_filled();
+        if (m == 0) smem[kOffNan + (t & 1u) * 256u + (uint32_t)(h * 128 + row)] = nan ? 1 : 0;
+        tmem_st_x32(t_k + (m & 1) * 64u, v);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_KFULL + m));
       }
       if (!ok) break;
+      ++t;
       here = next;
     }
   } else {
@@ -496,34 +512,28 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     volatile int* s_flag = reinterpret_cast<volatile int*>(smem + kOffFlag);
     const int tid = threadIdx.x - 32 * kSoftWarp0;
     const uint32_t max_at = smem_base + kOffMax + 4u * c0;
-    const float scale = p.scale_log2;
-    uint32_t t = 0, u = 0;
+    uint32_t t = 0;
     bool ok = true;
     // The values of tile tv: copied from tensor memory, where the key warps put them for the scores, into shared memory,
     // chunk pair by chunk pair as the previous tile's products release the space.  Here and not in the key warps, which
     // thereby never wait for the value products; the softmax warps have nothing else to do while those run.
     auto copy_values = [&](uint32_t tv) -> bool {
-      if (lane == 0) mbar_arrive(bar(B_KFREE + (u & 1u)));  // the rope piece is not a value
-      ++u;
       uint8_t* const v_row = smem + kOffV + (c0 ? 1 : 0) * kKChunk + key * 128;
 #pragma unroll 1
-      for (int m = 0; m < 4; ++m, ++u) {
-        if (!wait(B_KFULL + (u & 1u), (u >> 1) & 1u, W_KFULL)) return false;
+      for (int m = 0; m < 4; ++m) {
+        if (!wait(B_KFULL + m, tv & 1u, W_KFULL)) return false;
         tc_fence_after_sync();
         uint32_t v[32];
         __syncwarp();
-        tmem_ld_x32(tmem + lane_base + kColK + (u & 1u) * 64u + (c0 ? 32u : 0u), v);
+        tmem_ld_x32(tmem + lane_base + kColK + (m & 1) * 64u + (c0 ? 32u : 0u), v);
         tmem_wait_ld();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_KFREE + (u & 1u)));
+        if (lane == 0) mbar_arrive(bar(B_KFREE + m));
         if (tv > 0 && !wait(B_PVDONE + m, (tv - 1) & 1u, W_PVDONE)) return false;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           *reinterpret_cast<uint4*>(v_row + 2 * m * kKChunk + ((e ^ (key & 7)) << 4)) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_VFULL + m));
       }
       return true;
     };
@@ -540,14 +550,15 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
       float l[NC];
 #pragma unroll
       for (int i = 0; i < NC; ++i) l[i] = 0.f;
+      int2 ahead = *reinterpret_cast<const int2*>(&p.tiles[c.record(0)].base);  // first key position and keys of a tile, fetched a tile ahead
       for (int k = 0; ok && k < c.cnt; ++k, ++t) {
-        const int4 rec = *reinterpret_cast<const int4*>(&p.tiles[c.record(k)]);
-        const bool full = rec.w == kDecodeKeys && pmin - rec.z + 1 >= kDecodeKeys;  // no key of the tile is masked
+        const int2 rec = ahead;
+        const bool full = rec.y == kDecodeKeys && pmin - rec.x + 1 >= kDecodeKeys;  // no key of the tile is masked
         const bool fast = k > 0 && full;
         const uint32_t t_s = t_s0 + (t & 1u) * 64u;
         // p = 2^(score - max), eight rows at a time: added to the sums and written as P^T, one 128-byte row per key,
         // query rows contiguous.  `raised`: with masks, the maxima being final (see below).  Returns the largest exponent.
-        auto write_p = [&](auto raised) -> float {
+        auto write_p = [&](auto raised, float scale) -> float {
           float top = -INFINITY;
           uint8_t* dst = smem + kOffP + key * 128;
 #pragma unroll
@@ -563,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
 #pragma unroll
               for (int n = 0; n < 4; ++n) {
                 float e = fmaf(__uint_as_float(s[j + n]), scale, -mx[n]);
-                if (decltype(raised)::value && (key >= rec.w || rec.z + key > s_pos[c0 + i + j + n])) e = -INFINITY;
+                if (decltype(raised)::value && (key >= rec.y || rec.x + key > s_pos[c0 + i + j + n])) e = -INFINITY;
                 top = fmaxf(top, e);
                 pv[n] = fast_exp2(e);
                 if constexpr (!decltype(raised)::value) l[i + j + n] += pv[n];
@@ -577,15 +588,19 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           fence_proxy_async_smem();
           return top;
         };
-        ok = copy_values(t) && wait(B_SFULL, t & 1u, W_SFULL);
+        ok = copy_values(t);
+        if (k + 1 < c.cnt) ahead = *reinterpret_cast<const int2*>(&p.tiles[c.record(k + 1)].base);
+        ok = ok && wait(B_SFULL, t & 1u, W_SFULL);
         tc_fence_after_sync();
+        const uint8_t* s_nan = smem + kOffNan + (t & 1u) * 256u + key;
+        const float scale = s_nan[0] | s_nan[128] ? NAN : p.scale_log2;
         // First try with the maxima as they are (S of this tile is complete, so P^T of the previous one has been read).
         // A warp that finds an exponent above 8, or that gave up waiting, raises the flag; everyone sees it behind
         // the barrier.  Not tried for the first tile of a group, which has no maxima yet, and for the rare tiles with
         // masked keys, which the longer way below handles.
         const bool all_ok = __all_sync(0xffffffffu, ok);
         float top = INFINITY;
-        if (fast && all_ok) top = write_p(std::false_type());
+        if (fast && all_ok) top = write_p(std::false_type(), scale);
         if (top > 8.f) *s_flag = (int)t + 1;
         tc_fence_before_sync();
         named_barrier_sync(1, kSoftmax);
@@ -600,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
             tmem_wait_ld();
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              const bool masked = !full && (key >= rec.w || rec.z + key > s_pos[c0 + i + j]);
+              const bool masked = !full && (key >= rec.y || rec.x + key > s_pos[c0 + i + j]);
               float v = masked ? -INFINITY : __uint_as_float(s[j]) * scale;
 #pragma unroll
               for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -633,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           // them right for the new one; otherwise this tile's p are added here.
           // Where the maximum rose by more than 2^90 (or there was none) they may have overflowed: there, what was
           // summed up before is below 2^-60 of the new sum and is dropped.
-          write_p(std::true_type());
+          write_p(std::true_type(), scale);
           tc_fence_before_sync();
           named_barrier_sync(1, kSoftmax);
         }
