@@ -66,9 +66,9 @@ constexpr uint32_t kSmemBytes = kSmemUsed;
 constexpr uint32_t kColS = 256, kColK = 384;
 constexpr float kNoMax = -1e30f;     // "no key seen yet": finite, so that differences stay defined
 
-// Registers per thread out of the launch's 640 x 96, by warpgroup: (1 x 56 + 2 x 96 + 2 x 112) x 128 = 60416 of 61440.  Nothing in
+// Registers per thread out of the launch's 640 x 96, by warpgroup: (1 x 64 + 2 x 96 + 2 x 112) x 128 = 61440.  Nothing in
 // the loops may spill: shared memory takes nearly all of L1, so a spilled register comes back from L2.
-constexpr int kRegsIssue = 56, kRegsKeys = 96, kRegsSoftmax = 112;
+constexpr int kRegsIssue = 64, kRegsKeys = 96, kRegsSoftmax = 112;
 template <int N>
 __device__ __forceinline__ void reg_raise() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -123,6 +123,13 @@ struct Cursor {
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// the largest over a warp; NaN is left out
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
 }
 
@@ -224,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
   if (threadIdx.x == 0) {
     store_shared(smem_base + kOffAbort, 0u);
     mbar_init(bar(B_QFULL), 1);
-    mbar_init(bar(B_QROPE), 1);
+    mbar_init(bar(B_QROPE), 2);
     mbar_init(bar(B_KROPE), 1);
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(B_KFULL + i), kKeyWarps);
@@ -327,27 +334,36 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         ++t;
       }
     }
-  } else if (warp == 1) {
+  } else if (warp == 1 || warp == 3) {
     // ------------------------------ queries: latent chunks by TMA, rope chunk turned by R(-delta) -------------
+    // Two warps, eight rows apiece in turn; the rope parts stay in registers for the group, so that a new segment costs
+    // arithmetic and no loads (from memory row by row, a new segment held the scores up for 10000 clk).
     uint32_t t = 0, groups = 0;
     bool ok = true;
-    const int rc = lane & 7;
+    const int rc = lane & 7, r_first = (lane >> 3) + (warp == 3 ? 4 : 0);
     for (Cursor c(p); ok && c.next(); ++groups) {
+      const int row0 = c.b * rows_per_seq + c.rt * kRows;
+      const int valid = min(rows_per_seq - c.rt * kRows, kRows);
+      uint4 raw[kRows / 8];
+      {
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + ((int64_t)row0 + r_first) * kDQK + kDLatent + rc * 8;
+#pragma unroll
+        for (int i = 0; i < kRows / 8; ++i)
+          raw[i] = r_first + 8 * i < valid ? __ldg(reinterpret_cast<const uint4*>(src + (int64_t)(8 * i) * kDQK)) : make_uint4(0, 0, 0, 0);
+      }
       // the previous group's scores are done with the query chunks (its last tile's S is complete)
       if (t > 0) ok = wait(B_SFULL, (t - 1) & 1u, W_SFULL);
+      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      const int row0 = c.b * rows_per_seq + c.rt * kRows;
-      if (elect_one()) {
+      if (warp == 1 && elect_one()) {
         mbar_arrive_expect_tx(bar(B_QFULL), 8 * kRows * 128);
         for (int d = 0; d < 8; ++d) tma_load_2d(smem_base + kOffQ + d * kQChunk, &p.tm_q, bar(B_QFULL), d * 64, row0);
       }
       __syncwarp();
-      int valid = rows_per_seq - c.rt * kRows;
-      if (valid > kRows) valid = kRows;
       int delta = -1;
       for (int k = 0; ok && k < c.cnt; ++k, ++t) {
         const int d = p.tiles[c.record(k)].delta;
-        if (k + 2 < c.cnt && lane < 2) {  // pages of the tile after next into L2, where its loads will find them
+        if (warp == 1 && k + 2 < c.cnt && lane < 2) {  // pages of the tile after next into L2, where its loads will find them
           const int4 v = *reinterpret_cast<const int4*>(&p.tiles[c.record(k + 2)]);
           if (v.w > 64 * lane + 32) prefetch_page(p.pages + (int64_t)(lane == 0 ? v.x : v.y) * kCache4PageBytes);
         }
@@ -358,12 +374,9 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           float cs[4], sn[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) rope_cos_sin(p.rope, d, 4 * rc + e, cs[e], sn[e]);
-          const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + (int64_t)row0 * kDQK + kDLatent + rc * 8;
-#pragma unroll 1
-          for (int r = lane >> 3; r < kRows; r += 4) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < valid) v = *reinterpret_cast<const uint4*>(src + (int64_t)r * kDQK);
-            const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int i = 0; i < kRows / 8; ++i) {
+            const uint32_t in[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
             uint32_t o[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -372,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
               o[e] = pack_bf16(y0, y1);
               lo[e] = pack_bf16(y0 - __uint_as_float(o[e] << 16), y1 - __uint_as_float(o[e] & 0xffff0000u));
             }
-            uint8_t* dst = smem + kOffQ + 8 * kQChunk + sw128_offset((uint32_t)r, (uint32_t)rc);
+            uint8_t* dst = smem + kOffQ + 8 * kQChunk + sw128_offset((uint32_t)(r_first + 8 * i), (uint32_t)rc);
             *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<uint4*>(dst + kQChunk) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           }
@@ -401,8 +414,6 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
                     p.pages + (int64_t)(lane < 8 ? v.x : v.y) * kCache4PageBytes + (18 + (lane & 7)) * 1024, 1024u, bar(B_KROPE));
       }
     }
-  } else if (warp < 4) {
-    // a warp reaches the tensor memory lanes of its number modulo four: the next role starts at warp 4
   } else if (warp < kSoftWarp0) {
     // ------------------------------ keys: HBM -> registers (4-bit) -> shared memory (bf16) --------------------
     reg_raise<kRegsKeys>();
@@ -554,11 +565,14 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
       for (int k = 0; ok && k < c.cnt; ++k, ++t) {
         const int2 rec = ahead;
         const bool full = rec.y == kDecodeKeys && pmin - rec.x + 1 >= kDecodeKeys;  // no key of the tile is masked
-        const bool fast = k > 0 && full;
         const uint32_t t_s = t_s0 + (t & 1u) * 64u;
         // p = 2^(score - max), eight rows at a time: added to the sums and written as P^T, one 128-byte row per key,
-        // query rows contiguous.  `raised`: with masks, the maxima being final (see below).  Returns the largest exponent.
-        auto write_p = [&](auto raised, float scale) -> float {
+        // query rows contiguous.  `masked`: with masks, and with the sums corrected after a raise (see below).  Returns the largest
+        // exponent.
+        auto write_p = [&](auto masked, bool raised, float scale) -> float {
+          constexpr bool kMasked = decltype(masked)::value;
+          const int at = key < rec.y ? rec.x + key : 0x7fffffff;
+          const float add = raised && k > 0 ? 0.f : 1.f;
           float top = -INFINITY;
           uint8_t* dst = smem + kOffP + key * 128;
 #pragma unroll
@@ -568,17 +582,22 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
             tmem_wait_ld();
 #pragma unroll
             for (int j = 0; j < 8; j += 4) {
-              float mx[4], al[4], pv[4];
+              float mx[4], al[4] = {1.f, 1.f, 1.f, 1.f}, pv[4];
+              int4 last = make_int4(0, 0, 0, 0);
               load_shared4(mx, max_at + 4u * (i + j));
-              if constexpr (decltype(raised)::value) load_shared4(al, max_at + (kOffAlpha - kOffMax) + 4u * (i + j));
+              if constexpr (kMasked) {
+                if (raised) load_shared4(al, max_at + (kOffAlpha - kOffMax) + 4u * (i + j));
+                last = *reinterpret_cast<const int4*>(s_pos + c0 + i + j);
+              }
+              const int lasts[4] = {last.x, last.y, last.z, last.w};
 #pragma unroll
               for (int n = 0; n < 4; ++n) {
                 float e = fmaf(__uint_as_float(s[j + n]), scale, -mx[n]);
-                if (decltype(raised)::value && (key >= rec.y || rec.x + key > s_pos[c0 + i + j + n])) e = -INFINITY;
+                if (kMasked && at > lasts[n]) e = -INFINITY;
                 top = fmaxf(top, e);
                 pv[n] = fast_exp2(e);
-                if constexpr (!decltype(raised)::value) l[i + j + n] += pv[n];
-                else l[i + j + n] = al[n] < 1e-27f ? pv[n] : fmaf(l[i + j + n], al[n], fast ? 0.f : pv[n]);
+                if constexpr (!kMasked) l[i + j + n] += pv[n];
+                else l[i + j + n] = al[n] < 1e-27f ? pv[n] : fmaf(l[i + j + n], al[n], add * pv[n]);
               }
               pk[j / 2] = pack_bf16(pv[0], pv[1]);
               pk[j / 2 + 1] = pack_bf16(pv[2], pv[3]);
@@ -596,11 +615,10 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         const float scale = s_nan[0] | s_nan[128] ? NAN : p.scale_log2;
         // First try with the maxima as they are (S of this tile is complete, so P^T of the previous one has been read).
         // A warp that finds an exponent above 8, or that gave up waiting, raises the flag; everyone sees it behind
-        // the barrier.  Not tried for the first tile of a group, which has no maxima yet, and for the rare tiles with
-        // masked keys, which the longer way below handles.
+        // the barrier.  Not tried for the first tile of a group, which has no maxima yet.
         const bool all_ok = __all_sync(0xffffffffu, ok);
         float top = INFINITY;
-        if (fast && all_ok) top = write_p(std::false_type(), scale);
+        if (k > 0 && all_ok) top = full ? write_p(std::false_type(), false, scale) : write_p(std::true_type(), false, scale);
         if (top > 8.f) *s_flag = (int)t + 1;
         tc_fence_before_sync();
         named_barrier_sync(1, kSoftmax);
@@ -615,10 +633,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
             tmem_wait_ld();
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              const bool masked = !full && (key >= rec.y || rec.x + key > s_pos[c0 + i + j]);
-              float v = masked ? -INFINITY : __uint_as_float(s[j]) * scale;
-#pragma unroll
-              for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+              const bool masked = key >= rec.y || rec.x + key > s_pos[c0 + i + j];
+              const float v = warp_max(masked ? -INFINITY : __uint_as_float(s[j]) * scale);
               if (lane == 0) s_red[q * 64 + c0 + i + j] = v;
             }
           }
@@ -648,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           // them right for the new one; otherwise this tile's p are added here.
           // Where the maximum rose by more than 2^90 (or there was none) they may have overflowed: there, what was
           // summed up before is below 2^-60 of the new sum and is dropped.
-          write_p(std::true_type(), scale);
+          write_p(std::true_type(), true, scale);
           tc_fence_before_sync();
           named_barrier_sync(1, kSoftmax);
         }
@@ -687,22 +703,24 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         else if (tid < valid) p.lse[row0 + tid] = lse2 * 0.69314718055994530942f;
       }
       named_barrier_sync(1, kSoftmax);
+      constexpr int kCols = NC < 16 ? NC : 16;
 #pragma unroll 1
-      for (int i0 = 0; i0 < 4 * NC; i0 += 8) {  // 128 dims, then eight rows
+      for (int i0 = 0; i0 < 4 * NC; i0 += kCols) {  // 128 dims, then some rows
         const int m = i0 / NC, r = c0 + i0 % NC;
-        uint32_t o[8];
-        tmem_ld_x8(t_o + (uint32_t)(m * kRows + i0 % NC), o);
+        uint32_t o[kCols];
+        if constexpr (kCols == 8) tmem_ld_x8(t_o + (uint32_t)(m * kRows + i0 % NC), o);
+        else tmem_ld_x16(t_o + (uint32_t)(m * kRows + i0 % NC), o);
         tmem_wait_ld();
         const int dim = 128 * m + key;
         if (whole) {
           __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.O) + (row0 + r) * kDLatent + dim;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < kCols; ++i)
             if (r + i < valid) out[i * kDLatent] = __float2bfloat16_rn(__uint_as_float(o[i]) * s_alpha[r + i]);
         } else {
           float* out = p.part_o + ((int64_t)slot * 64 + r) * kDLatent + dim;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < kCols; ++i)
             if (r + i < valid) out[i * kDLatent] = __uint_as_float(o[i]) * s_alpha[r + i];
         }
       }
