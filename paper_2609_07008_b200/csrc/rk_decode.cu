@@ -59,7 +59,8 @@ constexpr uint32_t kOffPos = kOffMax + 256;          // int [64]: request positi
 constexpr uint32_t kOffRed = kOffPos + 256;          // float [4][64]: per lane quarter
 constexpr uint32_t kOffAlpha = kOffRed + 1024;       // float [64]: factor of the last raise of a row's maximum
 constexpr uint32_t kOffNan = kOffAlpha + 256;         // uint8 [2][2][128]: tile parity, half of the key's groups, key: a scale is NaN
-constexpr uint32_t kSmemUsed = kOffNan + 512;
+constexpr uint32_t kOffGroup = kOffNan + 512;         // int [8]: the softmax warps' group, see there
+constexpr uint32_t kSmemUsed = kOffGroup + 32;
 constexpr uint32_t kSmemBytes = kSmemUsed;
 
 // tensor memory columns: O^T takes 4 x N from 0; two score buffers; two slots of 128 dims of the keys (bf16 pairs)
@@ -92,6 +93,18 @@ struct Cursor {
     rt = s.y;
     tile = s.z;
     cnt = 0;
+  }
+  // put away in shared memory and taken from there
+  __device__ Cursor(const DecodeAttnParams& p_, const volatile int* at)
+      : p(p_), left(at[0]), b(at[1]), rt(at[2]), tile(at[3]), n_b(at[5]), tile0(at[6]), cnt(at[4]) {}
+  __device__ void store(volatile int* at) const {
+    at[0] = left;
+    at[1] = b;
+    at[2] = rt;
+    at[3] = tile;
+    at[4] = cnt;
+    at[5] = n_b;
+    at[6] = tile0;
   }
   // makes the next group current; false when the run is done
   __device__ bool next() {
@@ -126,11 +139,22 @@ __device__ __forceinline__ float fast_exp2(float x) {
   return y;
 }
 
-// the largest over a warp; NaN is left out
-__device__ __forceinline__ float warp_max(float x) {
-  float y;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-  return y;
+// Column results over the lanes of a warp: lane i gets column i mod N of the N (8, 16 or 32) that every lane holds.  Each exchange
+// halves the columns a lane holds, N - 1 of them in all where a reduction per column takes 5 N.
+template <int N, typename Op>
+__device__ __forceinline__ float over_lanes(float (&x)[N], int lane, Op op) {
+#pragma unroll
+  for (int w = N / 2; w >= 1; w /= 2) {
+    const bool upper = (lane & w) != 0;
+#pragma unroll
+    for (int i = 0; i < w; ++i) {
+      const float keep = upper ? x[i + w] : x[i], give = upper ? x[i] : x[i + w];
+      x[i] = op(keep, __shfl_xor_sync(0xffffffffu, give, w));
+    }
+  }
+#pragma unroll
+  for (int w = N; w < 32; w *= 2) x[0] = op(x[0], __shfl_xor_sync(0xffffffffu, x[0], w));
+  return x[0];
 }
 
 __device__ __forceinline__ void prefetch_page(const uint8_t* page) {
@@ -344,6 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     for (Cursor c(p); ok && c.next(); ++groups) {
       const int row0 = c.b * rows_per_seq + c.rt * kRows;
       const int valid = min(rows_per_seq - c.rt * kRows, kRows);
+      int d = __ldg(&p.tiles[c.record(0)].delta);
       uint4 raw[kRows / 8];
       {
         const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) + ((int64_t)row0 + r_first) * kDQK + kDLatent + rc * 8;
@@ -362,11 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
       __syncwarp();
       int delta = -1;
       for (int k = 0; ok && k < c.cnt; ++k, ++t) {
-        const int d = p.tiles[c.record(k)].delta;
-        if (warp == 1 && k + 2 < c.cnt && lane < 2) {  // pages of the tile after next into L2, where its loads will find them
-          const int4 v = *reinterpret_cast<const int4*>(&p.tiles[c.record(k + 2)]);
-          if (v.w > 64 * lane + 32) prefetch_page(p.pages + (int64_t)(lane == 0 ? v.x : v.y) * kCache4PageBytes);
-        }
+        if (k > 0) d = __ldg(&p.tiles[c.record(k)].delta);
         if (k > 0) ok = wait(B_SFULL, (t - 1) & 1u, W_SFULL);
         if (!ok) break;
         if (d != delta) {
@@ -374,9 +395,14 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           float cs[4], sn[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) rope_cos_sin(p.rope, d, 4 * rc + e, cs[e], sn[e]);
+          uint8_t* dst = smem + kOffQ + 8 * kQChunk + sw128_offset((uint32_t)r_first, (uint32_t)rc);
+#pragma unroll 1
+          for (int i = 0; i < kRows / 8; ++i, dst += 1024) {  // the rows go round in the registers: one copy of the code
+            const uint4 now = raw[0];
 #pragma unroll
-          for (int i = 0; i < kRows / 8; ++i) {
-            const uint32_t in[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            for (int n = 0; n + 1 < kRows / 8; ++n) raw[n] = raw[n + 1];
+            raw[kRows / 8 - 1] = now;
+            const uint32_t in[4] = {now.x, now.y, now.z, now.w};
             uint32_t o[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -385,7 +411,6 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
               o[e] = pack_bf16(y0, y1);
               lo[e] = pack_bf16(y0 - __uint_as_float(o[e] << 16), y1 - __uint_as_float(o[e] & 0xffff0000u));
             }
-            uint8_t* dst = smem + kOffQ + 8 * kQChunk + sw128_offset((uint32_t)(r_first + 8 * i), (uint32_t)rc);
             *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
             *reinterpret_cast<uint4*>(dst + kQChunk) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           }
@@ -402,16 +427,29 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     bool ok = true;
     for (Cursor c(p); ok && c.next();) {
       for (int k = 0; k < c.cnt; ++k, ++t) {
+        if (k + 2 < c.cnt && lane < 2) {  // pages of the tile after next into L2, where its loads will find them
+          const int4 v = *reinterpret_cast<const int4*>(&p.tiles[c.record(k + 2)]);
+          if (v.w > 64 * lane + 32) prefetch_page(p.pages + (int64_t)(lane == 0 ? v.x : v.y) * kCache4PageBytes);
+        }
         const int4 v = __ldg(reinterpret_cast<const int4*>(&p.tiles[c.record(k)]));
+        const uint32_t page0 = __reduce_max_sync(0xffffffffu, (uint32_t)v.x), page1 = __reduce_max_sync(0xffffffffu, (uint32_t)v.y);
+        const uint32_t both = __reduce_max_sync(0xffffffffu, v.w > 64 ? 1u : 0u);  // uniform, as the copies' operands have to be
+        const uint8_t* src0 = p.pages + (int64_t)page0 * kCache4PageBytes + 18 * 1024;
+        const uint8_t* src1 = p.pages + (int64_t)page1 * kCache4PageBytes + 18 * 1024;
         if (t > 0) ok = wait(B_PVDONE + 3, (t - 1) & 1u, W_PVDONE);  // P^T of the last tile has been read
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         // rows that are not there keep what is in their place: their scores are masked
-        if (lane == 0) mbar_arrive_expect_tx(bar(B_KROPE), v.w > 64 ? 16384u : 8192u);
+        if (elect_one()) {
+          mbar_arrive_expect_tx(bar(B_KROPE), both != 0u ? 16384u : 8192u);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) bulk_load(smem_base + kOffP + u * 2048, src0 + u * 1024, 1024u, bar(B_KROPE));
+          if (both != 0u) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) bulk_load(smem_base + kOffP + u * 2048 + 1024, src1 + u * 1024, 1024u, bar(B_KROPE));
+          }
+        }
         __syncwarp();
-        if (lane < 16 && (lane < 8 || v.w > 64))
-          bulk_load(smem_base + kOffP + (lane & 7) * 2048 + (lane >> 3) * 1024,
-                    p.pages + (int64_t)(lane < 8 ? v.x : v.y) * kCache4PageBytes + (18 + (lane & 7)) * 1024, 1024u, bar(B_KROPE));
       }
     }
   } else if (warp < kSoftWarp0) {
@@ -447,9 +485,10 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         k = 0;
       }
       if (more) {
-        const int4 v = __ldg(reinterpret_cast<const int4*>(&p.tiles[c.record(k)]));
-        page = row < 64 ? v.x : v.y;
-        n = v.w;
+        // one load per word: choosing among loaded words would wait for them
+        const DecodeTile* tile = &p.tiles[c.record(k)];
+        page = __ldg(&tile->page0 + (row >> 6));
+        n = __ldg(&tile->n);
       }
     };
     auto open = [&]() { src = row < n ? p.pages + (int64_t)page * kCache4PageBytes + (row & 63) * 16 : nullptr; };
@@ -548,21 +587,32 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
       }
       return true;
     };
-    for (Cursor c(p); ok && c.next();) {
+    // The cursor lives in shared memory, moved on by one thread, as the registers are full: tiles left, sequence, row tile, first
+    // tile, its tiles, the sequence's tiles, its first record; the last word says that there is a group.
+    volatile int* s_group = reinterpret_cast<volatile int*>(smem + kOffGroup);
+    if (tid == 0) {
+      Cursor c(p);
+      s_group[7] = c.next();
+      c.store(s_group);
+    }
+    named_barrier_sync(1, kSoftmax);
+    while (ok && s_group[7] != 0) {
       // s_max, s_pos: every warp is done with the previous group (the barrier in its epilogue)
       int pmin = 0x7fffffff;
-      for (int i = 0; i < p.q_len; ++i) pmin = min(pmin, p.pos[c.b * p.q_len + i]);
+      for (int i = 0; i < p.q_len; ++i) pmin = min(pmin, p.pos[s_group[1] * p.q_len + i]);
       if (tid < kRows) {
-        const int r = c.rt * kRows + tid;
+        const int r = s_group[2] * kRows + tid;
         s_max[tid] = kNoMax;
-        s_pos[tid] = r < rows_per_seq ? p.pos[c.b * p.q_len + r / p.n_heads] : -1;
+        s_pos[tid] = r < rows_per_seq ? p.pos[s_group[1] * p.q_len + r / p.n_heads] : -1;
       }
+      const int cnt = s_group[4];
+      const DecodeTile* rec_at = p.tiles + (s_group[6] + s_group[3]);
       named_barrier_sync(1, kSoftmax);
       float l[NC];
 #pragma unroll
       for (int i = 0; i < NC; ++i) l[i] = 0.f;
-      int2 ahead = *reinterpret_cast<const int2*>(&p.tiles[c.record(0)].base);  // first key position and keys of a tile, fetched a tile ahead
-      for (int k = 0; ok && k < c.cnt; ++k, ++t) {
+      int2 ahead = *reinterpret_cast<const int2*>(&rec_at->base);  // first key position and keys of a tile, fetched a tile ahead
+      for (int k = 0; ok && k < cnt; ++k, ++t) {
         const int2 rec = ahead;
         const bool full = rec.y == kDecodeKeys && pmin - rec.x + 1 >= kDecodeKeys;  // no key of the tile is masked
         const uint32_t t_s = t_s0 + (t & 1u) * 64u;
@@ -608,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           return top;
         };
         ok = copy_values(t);
-        if (k + 1 < c.cnt) ahead = *reinterpret_cast<const int2*>(&p.tiles[c.record(k + 1)].base);
+        if (k + 1 < cnt) ahead = *reinterpret_cast<const int2*>(&(++rec_at)->base);
         ok = ok && wait(B_SFULL, t & 1u, W_SFULL);
         tc_fence_after_sync();
         const uint8_t* s_nan = smem + kOffNan + (t & 1u) * 256u + key;
@@ -626,17 +676,22 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           ok = named_barrier_and(2, kSoftmax, ok);  // a warp that gave up must not leave the others in a barrier
           if (!ok) break;
           // exact maxima of the tile; a row's maximum is raised where the tile exceeds it by more than 2^8
-#pragma unroll 1
-          for (int i = 0; i < NC; i += 8) {
-            uint32_t s[8];
-            tmem_ld_x8(t_s + (uint32_t)i, s);
+          {
+            const int at = key < rec.y ? rec.x + key : 0x7fffffff;
+            float v[NC];
+#pragma unroll
+            for (int i = 0; i < NC; i += 8) tmem_ld_x8(t_s + (uint32_t)i, reinterpret_cast<uint32_t*>(v) + i);
             tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const bool masked = key >= rec.y || rec.x + key > s_pos[c0 + i + j];
-              const float v = warp_max(masked ? -INFINITY : __uint_as_float(s[j]) * scale);
-              if (lane == 0) s_red[q * 64 + c0 + i + j] = v;
+            for (int i = 0; i < NC; i += 4) {
+              const int4 last = *reinterpret_cast<const int4*>(s_pos + c0 + i);
+              v[i] = at > last.x ? -INFINITY : v[i] * scale;
+              v[i + 1] = at > last.y ? -INFINITY : v[i + 1] * scale;
+              v[i + 2] = at > last.z ? -INFINITY : v[i + 2] * scale;
+              v[i + 3] = at > last.w ? -INFINITY : v[i + 3] * scale;
             }
+            const float top_of = over_lanes(v, lane, [](float a, float b) { return fmaxf(a, b); });  // leaves NaN out
+            if (lane < NC) s_red[q * 64 + c0 + lane] = top_of;
           }
           named_barrier_sync(1, kSoftmax);
           bool raise = false;
@@ -672,28 +727,18 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
       }
       if (!ok) break;
       // ---- epilogue of the group: sums over the key lanes, then O^T / l ----
-      // (through the value chunks' space, free once the last value product is done: 128 keys x 64 rows in fp32)
       ok = wait(B_PVDONE + 3, (t - 1) & 1u, W_PVDONE);
       ok = named_barrier_and(2, kSoftmax, ok);
       if (!ok) break;
       tc_fence_after_sync();
-      float* const s_sum = reinterpret_cast<float*>(smem + kOffV);
-#pragma unroll
-      for (int i = 0; i < NC; i += 4)
-        *reinterpret_cast<float4*>(s_sum + key * 64 + (((c0 + i) ^ (4 * (key & 7))) & 63)) = make_float4(l[i], l[i + 1], l[i + 2], l[i + 3]);
+      const float sum_of = over_lanes(l, lane, [](float a, float b) { return a + b; });
+      if (lane < NC) s_red[q * 64 + c0 + lane] = sum_of;
       named_barrier_sync(1, kSoftmax);
-      if (tid < 4 * kRows) {  // four threads per row, 32 keys each
-        const int r = tid & (kRows - 1), part = tid / kRows;
-        float v = 0.f;
-#pragma unroll 8
-        for (int j = 0; j < 32; ++j) v += s_sum[(32 * part + j) * 64 + (r ^ (4 * (j & 7)))];
-        s_red[part * 64 + r] = v;
-      }
-      named_barrier_sync(1, kSoftmax);
-      const bool whole = c.whole();
-      const int slot = 2 * blockIdx.x + (c.tile > 0 ? 0 : 1);
-      const int valid = min(rows_per_seq - c.rt * kRows, kRows);
-      const int64_t row0 = (int64_t)c.b * rows_per_seq + c.rt * kRows;
+      const int first_row = s_group[2] * kRows;
+      const bool whole = s_group[4] == s_group[5];
+      const int slot = 2 * blockIdx.x + (s_group[3] > 0 ? 0 : 1);
+      const int valid = min(rows_per_seq - first_row, kRows);
+      const int64_t row0 = (int64_t)s_group[1] * rows_per_seq + first_row;
       if (tid < kRows) {
         // a NaN score makes its row NaN; a row without visible keys has the sum 0
         const float tot = (s_red[tid] + s_red[64 + tid]) + (s_red[128 + tid] + s_red[192 + tid]);
@@ -703,13 +748,14 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         else if (tid < valid) p.lse[row0 + tid] = lse2 * 0.69314718055994530942f;
       }
       named_barrier_sync(1, kSoftmax);
-      constexpr int kCols = NC < 16 ? NC : 16;
+      constexpr int kCols = NC;
 #pragma unroll 1
-      for (int i0 = 0; i0 < 4 * NC; i0 += kCols) {  // 128 dims, then some rows
-        const int m = i0 / NC, r = c0 + i0 % NC;
+      for (int m = 0; m < 4; ++m) {  // 128 dims each
+        const int r = c0;
         uint32_t o[kCols];
-        if constexpr (kCols == 8) tmem_ld_x8(t_o + (uint32_t)(m * kRows + i0 % NC), o);
-        else tmem_ld_x16(t_o + (uint32_t)(m * kRows + i0 % NC), o);
+        if constexpr (kCols == 8) tmem_ld_x8(t_o + (uint32_t)(m * kRows), o);
+        else if constexpr (kCols == 16) tmem_ld_x16(t_o + (uint32_t)(m * kRows), o);
+        else tmem_ld_x32(t_o + (uint32_t)(m * kRows), o);
         tmem_wait_ld();
         const int dim = 128 * m + key;
         if (whole) {
@@ -725,7 +771,13 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         }
       }
       tc_fence_before_sync();
-      named_barrier_sync(1, kSoftmax);  // s_red, s_max and s_pos may be overwritten from here on
+      named_barrier_sync(1, kSoftmax);  // s_group, s_red, s_max and s_pos may be overwritten from here on
+      if (tid == 0) {
+        Cursor c(p, s_group);
+        s_group[7] = c.next();
+        c.store(s_group);
+      }
+      named_barrier_sync(1, kSoftmax);
     }
   }
 
