@@ -38,7 +38,7 @@
 namespace rk {
 namespace {
 
-constexpr int kThreads = 640;      // x 96 registers
+constexpr int kThreads = 640;      // x 96 registers: shared memory takes nearly all of L1, so a spilled register in a loop comes back from L2
 constexpr int kKeyWarps = 8, kKeyWarp0 = 4, kSoftWarp0 = kKeyWarp0 + kKeyWarps;
 constexpr int kSoftWarps = 8, kSoftmax = 32 * kSoftWarps;
 constexpr uint32_t kKChunk = 16384;  // 128 keys x 64 dims bf16
@@ -66,14 +66,6 @@ constexpr uint32_t kSmemBytes = kSmemUsed;
 // tensor memory columns: O^T takes 4 x N from 0; two score buffers; two slots of 128 dims of the keys (bf16 pairs)
 constexpr uint32_t kColS = 256, kColK = 384;
 constexpr float kNoMax = -1e30f;     // "no key seen yet": finite, so that differences stay defined
-
-// Registers per thread out of the launch's 640 x 96, by warpgroup: (1 x 64 + 2 x 96 + 2 x 112) x 128 = 61440.  Nothing in
-// the loops may spill: shared memory takes nearly all of L1, so a spilled register comes back from L2.
-constexpr int kRegsIssue = 64, kRegsKeys = 96, kRegsSoftmax = 112;
-template <int N>
-__device__ __forceinline__ void reg_raise() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void reg_lower() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 enum { W_QFULL = 41, W_QROPE, W_KROPE, W_KFULL, W_KFREE, W_SFULL, W_PREADY, W_PVDONE };
 
@@ -283,7 +275,6 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     if (warp == 0) tmem_dealloc<1>(*tmem_ptr, 512);
     return;
   }
-  if (warp < kKeyWarp0) reg_lower<kRegsIssue>();
   const int rows_per_seq = p.q_len * p.n_heads;
 
   if (warp == 0) {
@@ -454,7 +445,6 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     }
   } else if (warp < kSoftWarp0) {
     // ------------------------------ keys: HBM -> registers (4-bit) -> shared memory (bf16) --------------------
-    reg_raise<kRegsKeys>();
     // Two threads per key: thread h has chunk 2 m + h (64 dims, two units) of every 128 dims m and the scale unit h (one word per
     // chunk).
     const int h = (warp - kKeyWarp0) >> 2;
@@ -546,7 +536,6 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     }
   } else {
     // ------------------------------ softmax, correction, epilogue ---------------------------------------------
-    reg_raise<kRegsSoftmax>();
     // Thread = one key of the tile (TMEM lane) and half of the query rows (columns).
     constexpr int NC = kRows / 2;
     const int q = warp & 3;            // TMEM lane quarter
@@ -623,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           constexpr bool kMasked = decltype(masked)::value;
           const int at = key < rec.y ? rec.x + key : 0x7fffffff;
           const float add = raised && k > 0 ? 0.f : 1.f;
-          float top = -INFINITY;
+          float top = 0.f;
           uint8_t* dst = smem + kOffP + key * 128;
 #pragma unroll
           for (int i = 0; i < NC; i += 8) {
@@ -644,11 +633,11 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
               for (int n = 0; n < 4; ++n) {
                 float e = fmaf(__uint_as_float(s[j + n]), scale, -mx[n]);
                 if (kMasked && at > lasts[n]) e = -INFINITY;
-                top = fmaxf(top, e);
                 pv[n] = fast_exp2(e);
                 if constexpr (!kMasked) l[i + j + n] += pv[n];
                 else l[i + j + n] = al[n] < 1e-27f ? pv[n] : fmaf(l[i + j + n], al[n], add * pv[n]);
               }
+              top = fmaxf(top, fmaxf(fmaxf(pv[0], pv[1]), fmaxf(pv[2], pv[3])));
               pk[j / 2] = pack_bf16(pv[0], pv[1]);
               pk[j / 2 + 1] = pack_bf16(pv[2], pv[3]);
             }
@@ -669,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         const bool all_ok = __all_sync(0xffffffffu, ok);
         float top = INFINITY;
         if (k > 0 && all_ok) top = full ? write_p(std::false_type(), false, scale) : write_p(std::true_type(), false, scale);
-        if (top > 8.f) *s_flag = (int)t + 1;
+        if (top > 256.f) *s_flag = (int)t + 1;
         tc_fence_before_sync();
         named_barrier_sync(1, kSoftmax);
         if (*s_flag == (int)t + 1) {
