@@ -36,25 +36,35 @@ __device__ __forceinline__ int warp_find_segment(const int32_t* __restrict__ off
   return lo;
 }
 
-// Page-relative byte address of row i of a ragged batch (the last off[s+1] - off[s] rows of every segment s), or -1.
-// Rows beyond off[n_segs] are no rows of the batch and are skipped silently; whatever the tables say is bounds
-// checked, a bad entry is reported and its row skipped.
-__device__ __forceinline__ int64_t row_address(const Cache4Table& t, const int32_t* __restrict__ off, int64_t i, int64_t n_pages,
-                                               DeviceStatus* st, int* index_in_segment) {
+// Byte addresses in the pages of up to 32 consecutive rows of a ragged batch (the last off[s+1] - off[s] rows of every segment
+// s), one per lane of the calling warp, and the rows' indexes in their segments; -1 for no row.  Rows beyond off[n_segs] are no
+// rows of the batch and are skipped silently; whatever the tables say is bounds checked, a bad entry is reported and its row
+// skipped.  The segments of the first and the last row are found by the warp together; mostly they are the same.
+__device__ __forceinline__ int64_t row_addresses(const Cache4Table& t, const int32_t* __restrict__ off, int64_t row0, int64_t n_rows,
+                                                 int64_t n_pages, DeviceStatus* st, int* index_in_segment) {
   *index_in_segment = 0;
-  if (t.n_segs == 0 || i >= __ldg(off + t.n_segs)) return -1;
-  const int s = warp_find_segment(off, t.n_segs, (int)i);
+  if (t.n_segs == 0) return -1;
+  const int64_t last = min(min(row0 + 31, n_rows - 1), (int64_t)__ldg(off + t.n_segs) - 1);
+  if (row0 > last) return -1;
+  int s = warp_find_segment(off, t.n_segs, (int)row0), hi = warp_find_segment(off, t.n_segs, (int)last);
+  const int64_t i = row0 + (threadIdx.x & 31);
+  if (i > last) return -1;
+  while (s < hi) {
+    const int mid = (s + hi + 1) >> 1;
+    if (__ldg(off + mid) <= i) s = mid;
+    else hi = mid - 1;
+  }
   const int o0 = __ldg(off + s), o1 = __ldg(off + s + 1), len = __ldg(t.seg_len + s);
   const int p0 = __ldg(t.page_off + s), p1 = __ldg(t.page_off + s + 1);
   const long long j = (long long)len - ((long long)o1 - o0) + (i - o0);
   const long long pi = (long long)p0 + (j >> 6);
   if (i < o0 || j < 0 || j >= len || p0 < 0 || pi >= p1 || pi >= t.n_listed) {
-    if ((threadIdx.x & 31) == 0) report_status(st, 4 /*RK_ERR_ROWS*/, RK_CHK_CACHE_ROW, (int)i);
+    report_status(st, 4 /*RK_ERR_ROWS*/, RK_CHK_CACHE_ROW, (int)i);
     return -1;
   }
   const int page = __ldg(t.page_ids + pi);
   if (page < 0 || page >= n_pages) {
-    if ((threadIdx.x & 31) == 0) report_status(st, 4 /*RK_ERR_ROWS*/, RK_CHK_CACHE_PAGE, page);
+    report_status(st, 4 /*RK_ERR_ROWS*/, RK_CHK_CACHE_PAGE, page);
     return -1;
   }
   *index_in_segment = (int)j;
@@ -64,9 +74,10 @@ __device__ __forceinline__ int64_t row_address(const Cache4Table& t, const int32
 // 32 rows per block.  Lane g of a warp owns scale group g of a row (16 dims, 32 contiguous bytes), so the group's
 // maximum never leaves the lane.  The finished units are staged in shared memory and leave with the row index
 // running fastest: consecutive rows of a page are consecutive 16-byte pieces.
-// Rounding: x * (1 / s) may sit a hair beside a tie; no quotient of an 8-bit and a 4-bit significand lies closer
-// than 2^-9 to a half-integer without being one, so snapping it to multiples of 2^-11 (adding and subtracting
-// 6144) restores exact ties, and the result is round-half-even of the true quotient.
+// Rounding: with approximate reciprocals a quotient may sit a hair beside a tie.  No quotient of an 8-bit and a 4-bit
+// significand lies closer than 2^-9 to a half-integer without being one, so rounding it to multiples of 2^-11 (adding 6144)
+// restores exact ties, and the result is round-half-even of the true quotient.  Likewise max / 7 lies no closer than
+// 2^-11 of itself to the middle between two scales without being on it, so 12 of its 24 bits are kept before it is rounded to 4.
 // Bound by HBM (1152 bytes in, 416 out per row).  Measured: see the table of the decode operators.
 __global__ void __launch_bounds__(256) cache4_append_kernel(uint8_t* __restrict__ pages, int64_t n_pages, Cache4Table tab,
                                                             const __nv_bfloat16* __restrict__ c, int64_t c_stride,
@@ -75,9 +86,10 @@ __global__ void __launch_bounds__(256) cache4_append_kernel(uint8_t* __restrict_
                                                             RopeTurns rope, DeviceStatus* status) {
   __shared__ __align__(16) uint8_t stage[kCache4Units * kUnitStride];
   __shared__ int64_t addr[kRowsPerBlock];
+  __shared__ int index[kRowsPerBlock];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t row0 = (int64_t)blockIdx.x * kRowsPerBlock + warp * 4;
-  // all loads of the warp's four rows first; the segment search runs under them
+  // all loads of the warp's four rows first; the first warp's search runs under them
   uint4 x[4][2];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -91,14 +103,10 @@ __global__ void __launch_bounds__(256) cache4_append_kernel(uint8_t* __restrict_
   const int rr = lane >> 3, rc = lane & 7;  // rope: lane covers 8 dims of one of the four rows
   uint4 xr = make_uint4(0, 0, 0, 0);
   if (row0 + rr < n_new) xr = __ldcs(reinterpret_cast<const uint4*>(kr + (row0 + rr) * r_stride + rc * 8));
-  int my_j = 0;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    int j = 0;
-    int64_t a = -1;
-    if (row0 + r < n_new) a = row_address(tab, new_off, row0 + r, n_pages, status, &j);
-    if (lane == 0) addr[warp * 4 + r] = a;
-    if (rr == r) my_j = j;
+  if (warp == 0) {
+    int j;
+    addr[lane] = row_addresses(tab, new_off, row0, n_new, n_pages, status, &j);
+    index[lane] = j;
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -108,29 +116,28 @@ __global__ void __launch_bounds__(256) cache4_append_kernel(uint8_t* __restrict_
     for (int e = 0; e < 8; ++e) mx = __vmaxu2(mx, w[e] & 0x7fff7fffu);
     const uint32_t top = max(mx & 0xffffu, mx >> 16);
     const bool finite = top < 0x7f80u;
-    const float t = __fdiv_rn(__uint_as_float(top << 16), 7.0f);
-    uint32_t u = __float_as_uint(t);
+    uint32_t u = (__float_as_uint(__uint_as_float(top << 16) * (1.0f / 7.0f)) + 0x800u) & ~0xfffu;
     u += 0x7ffffu + ((u >> 20) & 1u);  // round to four significant bits, ties to even
     int code = (int)(u >> 20) - (107 << 3);
     code = finite ? min(max(code, 0), 254) : 255;
-    const float inv = __fdiv_rn(1.0f, __uint_as_float((uint32_t)(code + (107 << 3)) << 20));
-    float y[16];
+    const float inv = __fdividef(1.0f, __uint_as_float((uint32_t)(code + (107 << 3)) << 20));
+    float y[16];  // 6144 + x / s
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      y[2 * e] = __uint_as_float(w[e] << 16) * inv;
-      y[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u) * inv;
+      y[2 * e] = __fmaf_rn(__uint_as_float(w[e] << 16), inv, 6144.0f);
+      y[2 * e + 1] = __fmaf_rn(__uint_as_float(w[e] & 0xffff0000u), inv, 6144.0f);
     }
     // max|c| / scale is at most 7 * 17 / 16 and rounds to 7, unless the scale was limited or the group is NaN
     if (__any_sync(0xffffffffu, code >= 254)) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = fminf(fmaxf(y[e], -7.0f), 7.0f);
+      for (int e = 0; e < 16; ++e) y[e] = fminf(fmaxf(y[e], 6144.0f - 7.0f), 6144.0f + 7.0f);
     }
     // The float bits of 1.5 * 2^23 + 8 + n are 0x4b400008 + n: eight of them, shifted and summed modulo 2^32, are the
     // packed codes plus a constant.  That keeps the packing on the multiply-add pipe.
     uint2 out = make_uint2(0u, 0u);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float q = __fadd_rn(__fadd_rn(__fadd_rn(y[e], 6144.0f), -6144.0f), 12582920.0f);
+      const float q = __fadd_rn(y[e], 12582920.0f - 6144.0f);
       const uint32_t at = 1u << (4 * ((e & 7) >> 1) + 16 * (e & 1));
       (e < 8 ? out.x : out.y) += (__float_as_uint(q)) * at;
     }
@@ -142,13 +149,14 @@ __global__ void __launch_bounds__(256) cache4_append_kernel(uint8_t* __restrict_
     *reinterpret_cast<uint2*>(stage + (lane >> 1) * kUnitStride + row * 16 + (lane & 1) * 8) = out;
     stage[(16 + ((lane >> 2) & 1)) * kUnitStride + row * 16 + 4 * (lane >> 3) + (lane & 3)] = (uint8_t)code;
   }
+  __syncthreads();
   {  // R(j): the stored key is in the position-zero frame of its segment
     const uint32_t in[4] = {xr.x, xr.y, xr.z, xr.w};
     uint32_t o[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float cs, sn;
-      rope_cos_sin(rope, my_j, 4 * rc + e, cs, sn);
+      rope_cos_sin(rope, index[warp * 4 + rr], 4 * rc + e, cs, sn);
       const float x0 = __uint_as_float(in[e] << 16), x1 = __uint_as_float(in[e] & 0xffff0000u);
       o[e] = pack_bf16(x0 * cs - x1 * sn, x0 * sn + x1 * cs);
     }
@@ -172,12 +180,9 @@ __global__ void __launch_bounds__(256) cache4_read_kernel(const uint8_t* __restr
   __shared__ int64_t addr[kRowsPerBlock];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t row0 = (int64_t)blockIdx.x * kRowsPerBlock;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
+  if (warp == 0) {
     int j;
-    int64_t a = -1;
-    if (row0 + warp * 4 + r < n_rows) a = row_address(tab, row_off, row0 + warp * 4 + r, n_pages, status, &j);
-    if (lane == 0) addr[warp * 4 + r] = a;
+    addr[lane] = row_addresses(tab, row_off, row0, n_rows, n_pages, status, &j);
   }
   __syncthreads();
   {

@@ -122,7 +122,6 @@ struct Cursor {
     return true;
   }
   __device__ int record(int k) const { return tile0 + tile + k; }
-  __device__ bool whole() const { return cnt == n_b; }
 };
 
 __device__ __forceinline__ float fast_exp2(float x) {
