@@ -176,8 +176,7 @@ def _need(t: torch.Tensor, name: str, dtype, shape, contiguous=True) -> torch.Te
     any, else a tuple with -1 for any extent.  Written for speed: a decode step makes a handful of these calls per layer."""
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if shape is not None and t.shape != shape:
-        got = t.shape
+    if shape is not None and (got := t.shape) != shape:
         if len(got) != len(shape):
             raise ValueError(f"{name} must have {len(shape)} dimensions, not {len(got)}")
         for want, have in zip(shape, got):
@@ -439,12 +438,16 @@ class Context:
         _need(c, "c", torch.bfloat16, (-1, 512), contiguous=False)
         _need(k_rope, "k_rope", torch.bfloat16, (n, 64), contiguous=False)
         _need(new_off, "new_off", torch.int32, (table.n_segs + 1,))
-        if n > 0 and (c.stride(1) != 1 or k_rope.stride(1) != 1):
-            raise ValueError("the values of a row of c and k_rope must be contiguous")
-        # a single row's stride is arbitrary and never used
-        self.check(lib.rk_cache4_append(self.handle, _ptr(pages), pages.shape[0], table.ref, c.data_ptr(),
-                                        c.stride(0) if n > 1 else 512, k_rope.data_ptr(), k_rope.stride(0) if n > 1 else 64,
-                                        _ptr(new_off), n, _quick_stream()))
+        c_stride, r_stride = 512, 64  # a single row's stride is arbitrary and never used
+        if not (c.is_contiguous() and k_rope.is_contiguous()) and n > 0:
+            if c.stride(1) != 1 or k_rope.stride(1) != 1:
+                raise ValueError("the values of a row of c and k_rope must be contiguous")
+            if n > 1:
+                c_stride, r_stride = c.stride(0), k_rope.stride(0)
+        s = lib.rk_cache4_append(self.handle, pages.data_ptr(), pages.shape[0], table.ref, c.data_ptr(), c_stride, k_rope.data_ptr(),
+                                 r_stride, new_off.data_ptr(), n, _quick_stream())
+        if s:
+            self.check(s)
 
     def rk_cache4_read(self, pages: torch.Tensor, table: CacheTable, row_off: torch.Tensor, n_rows: int, kv=None) -> torch.Tensor:
         """The last row_off[s+1] - row_off[s] rows of every segment s as packed bf16 rows kv [n_rows, 576]; rows from
@@ -452,10 +455,13 @@ class Context:
         _need(pages, "pages", torch.uint8, (-1, CACHE4_PAGE_BYTES))
         _need(row_off, "row_off", torch.int32, (table.n_segs + 1,))
         if kv is None:
-            kv = _empty((n_rows, 576), dtype=torch.bfloat16, device=pages.device)
-        _need(kv, "kv", torch.bfloat16, (n_rows, 576))
-        self.check(lib.rk_cache4_read(self.handle, _ptr(pages), pages.shape[0], table.ref, _ptr(row_off), n_rows, _ptr(kv),
-                                      _quick_stream()))
+            kv = _empty((n_rows, 576), torch.bfloat16, pages.device)
+        else:
+            _need(kv, "kv", torch.bfloat16, (n_rows, 576))
+        s = lib.rk_cache4_read(self.handle, pages.data_ptr(), pages.shape[0], table.ref, row_off.data_ptr(), n_rows, kv.data_ptr(),
+                               _quick_stream())
+        if s:
+            self.check(s)
         return kv
 
     def rk_decode_plan(self, table: CacheTable, n_pages: int, seq_off: torch.Tensor, item_seg: torch.Tensor,
@@ -483,19 +489,28 @@ class Context:
         rows = plan.rows + (self.n_heads,)
         _need(pages, "pages", torch.uint8, (-1, CACHE4_PAGE_BYTES))
         _need(q, "q", torch.bfloat16, rows + (576,))
+        device = q.device
         if O is None:
-            O = _empty(rows + (512,), dtype=torch.bfloat16, device=q.device)
+            O = _empty(rows + (512,), torch.bfloat16, device)
+        else:
+            _need(O, "O", torch.bfloat16, rows + (512,))
         if lse is None:
-            lse = _empty(rows, dtype=torch.float32, device=q.device)
-        _need(O, "O", torch.bfloat16, rows + (512,))
-        _need(lse, "lse", torch.float32, rows)
+            lse = _empty(rows, torch.float32, device)
+        else:
+            _need(lse, "lse", torch.float32, rows)
         if workspace is None:
             need = C.c_size_t(0)
             self.check(lib.rk_cache4_attn_workspace_bytes(self.handle, plan.ref, C.byref(need)))
-            workspace = _empty(need.value, dtype=torch.uint8, device=q.device)
-        _need(workspace, "workspace", torch.uint8, (-1,))
-        self.check(lib.rk_cache4_attn(self.handle, plan.ref, _ptr(plan.buf), plan.buf.numel(), _ptr(pages), pages.shape[0],
-                                      _ptr(q), _ptr(O), _ptr(lse), _ptr(workspace), workspace.numel(), _quick_stream()))
+            size = need.value
+            workspace = _empty(size, torch.uint8, device)
+        else:
+            _need(workspace, "workspace", torch.uint8, (-1,))
+            size = workspace.numel()
+        buf = plan.buf
+        s = lib.rk_cache4_attn(self.handle, plan.ref, buf.data_ptr(), buf.numel(), pages.data_ptr(), pages.shape[0], q.data_ptr(),
+                               O.data_ptr(), lse.data_ptr(), workspace.data_ptr(), size, _quick_stream())
+        if s:
+            self.check(s)
         return O, lse
 
     def rk_quant4(self, w: torch.Tensor, group: int, w4: Optional[W4] = None) -> W4:
@@ -513,18 +528,24 @@ class Context:
 
     def rk_matvec4(self, w4: W4, x: torch.Tensor, y: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
         """x [n_tok, n_mat, k] bf16 (tokens may be strided) -> y [n_tok, n_mat, n_out], bf16 or float32."""
-        n = x.shape[0]
-        _need(x, "x", torch.bfloat16, (n, w4.n_mat, w4.k), contiguous=False)
+        n, n_mat, n_out, k = x.shape[0], w4.n_mat, w4.n_out, w4.k
+        _need(x, "x", torch.bfloat16, (n, n_mat, k), contiguous=False)
         if y is None:
-            y = _empty((n, w4.n_mat, w4.n_out), dtype=out_dtype, device=x.device)
+            y = _empty((n, n_mat, n_out), out_dtype, x.device)
         else:
-            _need(y, "y", y.dtype, (n, w4.n_mat, w4.n_out), contiguous=False)
-        for t, name in ((x, "x"), (y, "y")):
-            if n > 0 and not t.is_contiguous() and not t[0].is_contiguous():
-                raise ValueError(f"the values of a token of {name} must be contiguous")
-        dt = {torch.bfloat16: 0, torch.float32: 1}[y.dtype]
-        self.check(lib.rk_matvec4(self.handle, w4.ref, x.data_ptr(), x.stride(0) if n > 1 else w4.n_mat * w4.k, n, y.data_ptr(),
-                                  y.stride(0) if n > 1 else w4.n_mat * w4.n_out, dt, _quick_stream()))
+            out_dtype = y.dtype
+            _need(y, "y", out_dtype, (n, n_mat, n_out), contiguous=False)
+        x_stride, y_stride = n_mat * k, n_mat * n_out
+        if not (x.is_contiguous() and y.is_contiguous()) and n > 0:
+            for t, name in ((x, "x"), (y, "y")):
+                if not t[0].is_contiguous():
+                    raise ValueError(f"the values of a token of {name} must be contiguous")
+            if n > 1:
+                x_stride, y_stride = x.stride(0), y.stride(0)
+        dt = 0 if out_dtype is torch.bfloat16 else {torch.float32: 1}[out_dtype]
+        s = lib.rk_matvec4(self.handle, w4.ref, x.data_ptr(), x_stride, n, y.data_ptr(), y_stride, dt, _quick_stream())
+        if s:
+            self.check(s)
         return y
 
     def alloc_layer_buffers(self, req, device) -> dict:
