@@ -167,6 +167,23 @@ def test_append_positions_beyond_float_precision(rk, ctx):
     assert (np.abs(got - want) <= tol).all()
 
 
+def test_append_and_read_with_many_empty_segments(rk, ctx):
+    """A block's rows lie in segments far apart, with runs of empty ones between them."""
+    rng = np.random.default_rng(11)
+    new = rng.choice([0, 0, 0, 0, 0, 1, 2, 40], size=700)
+    new[:100] = 0
+    new[300:400] = 0
+    new[-50:] = 0
+    pool = Pool(rk, list(new), seed=11)
+    c, _ = fill_pool(ctx, pool, 11)
+    off = np.concatenate([[0], np.cumsum(new)])
+    want = np.concatenate([pool.rows(s) for s in range(len(new)) if new[s]])
+    codes, byte = D.quantise_latent(c)
+    assert np.array_equal(want[:, :512], D.latent_values(codes, byte))
+    assert np.array_equal(f64(ctx.rk_cache4_read(pool.pages, pool.table, i32(off), int(off[-1]))), want)
+    ctx.rk_poll_status()
+
+
 def test_read_returns_the_stored_values(rk, ctx):
     pool = Pool(rk, [1, 64, 65, 130, 700, 0, 3], seed=6)
     fill_pool(ctx, pool, 6)
@@ -400,6 +417,31 @@ def test_attention_uniform_scores_and_large_scores(rk, ctx):
     run_attention(ctx, pool, [[(0, 0)]], [[299]], 16, 18, q_std=1e-20)
 
 
+@pytest.mark.parametrize("heads, n, bad", [(16, 2, "c"), (16, 130, "c"), (64, 130, "rope"), (24, 129, "inf c"), (64, 9000, "c"),
+                                           (128, 9000, "rope")])
+def test_attention_bad_key_reaches_only_the_tokens_that_see_it(rk, heads, n, bad):
+    """The last cached row has a non-finite value.  The last query token sees it and is NaN in every head; the token before it
+    and the other request, which ends a row earlier, are what they are without that row."""
+    ctx = make_ctx(rk, heads)
+    pool = Pool(rk, [n], seed=31)
+    rng = np.random.default_rng(32)
+    c, kr = rng.standard_normal((n, 512)), rng.standard_normal((n, 64))
+    if bad == "rope":
+        kr[n - 1, 2:4] = np.nan
+    else:
+        c[n - 1, 200] = np.nan if bad == "c" else np.inf
+    ctx.rk_cache4_append(pool.pages, pool.table, bf(c), bf(kr), i32([0, n]))
+    pool.from_device()
+    items, q_pos = [[(0, 0)], [(0, 0)]], np.array([[n - 2, n - 1], [n - 3, n - 2]])
+    q = bf(rng.standard_normal((2, 2, heads, 576)) * 1.2)
+    O, lse = ctx.rk_cache4_attn(pool.pages, plan_for(ctx, pool, items, q_pos), q)
+    ctx.rk_poll_status()
+    assert torch.isnan(O[0, 1]).all() and torch.isnan(lse[0, 1]).all()
+    pool.lens = [n - 1]                                            # the checker does not see the row either
+    check_attention(ctx, pool, [items[0]], q_pos[:1, :1], q[:1, :1], O[:1, :1], lse[:1, :1], heads)
+    check_attention(ctx, pool, [items[1]], q_pos[1:], q[1:], O[1:], lse[1:], heads)
+
+
 def test_attention_long_offsets_in_a_large_pool(rk, ctx):
     """Pages beyond 4 GiB into the pool, segments at large request offsets."""
     n_pages = (9 << 29) // D.PAGE_BYTES
@@ -626,6 +668,38 @@ def test_matvec_matches_checker(rk, ctx, mats, n_out, k, group, tok):
     ctx.rk_matvec4(w4, x, y=y[:, :mats * n_out].unflatten(1, (mats, n_out)))
     check_matvec(y[:, :mats * n_out].unflatten(1, (mats, n_out)), xs, vals, k, False)
     assert (y[:, mats * n_out:] == 7).all()
+    ctx.rk_poll_status()
+
+
+@pytest.mark.parametrize("mats, n_out, k, group, tok", [
+    (1, 80, 4096, 32, 3), (2, 48, 4160, 64, 9), (1, 32, 8320, 128, 16), (3, 16, 16384, 64, 1), (1, 48, 17024, 128, 5),
+    (1, 16, 33088, 64, 17), (1, 5120, 2112, 64, 12), (1, 9600, 128, 128, 4), (40, 256, 192, 32, 2), (1, 13000 // 16 * 16, 2112, 32, 8)])
+def test_matvec_long_rows_and_many_rows(rk, ctx, mats, n_out, k, group, tok):
+    """k over two, four and eight thread blocks and over several rounds of them, with ragged and empty last slices; several tiles
+    of output rows per thread block, with a short last run."""
+    rng = np.random.default_rng(n_out + k)
+    w = bf(rng.standard_normal((mats, n_out, k)) * 0.02)
+    vals = D.quantise_weights(f64(w), group)
+    x = bf(rng.standard_normal((tok, mats, k)))
+    w4 = ctx.rk_quant4(w, group)
+    y = ctx.rk_matvec4(w4, x, out_dtype=torch.float32)
+    check_matvec(y, f64(x), vals, k, False)
+    assert torch.equal(ctx.rk_matvec4(w4, x, out_dtype=torch.float32), y)
+    ctx.rk_poll_status()
+
+
+def test_matvec_bad_token_stays_alone(rk, ctx):
+    """A token with an infinity and one with a NaN, in the first and in the last block of k: the others are untouched."""
+    rng = np.random.default_rng(41)
+    w = bf(rng.standard_normal((1, 48, 4160)) * 0.02)
+    w4 = ctx.rk_quant4(w, 64)
+    x = bf(rng.standard_normal((11, 1, 4160)))
+    want = ctx.rk_matvec4(w4, x)
+    x[2, 0, 4159], x[9, 0, 0] = float("inf"), float("nan")
+    y = ctx.rk_matvec4(w4, x)
+    good = [t for t in range(11) if t not in (2, 9)]
+    assert torch.equal(y[good], want[good])
+    assert not torch.isfinite(y[2]).any() and torch.isnan(y[9]).all()
     ctx.rk_poll_status()
 
 
