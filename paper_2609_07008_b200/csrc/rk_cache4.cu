@@ -249,7 +249,8 @@ __global__ void __launch_bounds__(kPlanThreads) decode_plan_scan_kernel(DecodePl
         long long seen = (long long)pmax - delta + 1;
         seen = seen < 0 ? 0 : (seen < len ? seen : len);
         const long long np = (seen + 63) >> 6;
-        if (delta < 0 || len < 0 || p0 < 0 || (seen > 0 && (p0 + np > p1 || p0 + np > a.tab.n_listed)) ||
+        // a pool without pages has no row to see (and no page that a tile with a bad entry could stand on)
+        if (delta < 0 || len < 0 || p0 < 0 || (seen > 0 && (p0 + np > p1 || p0 + np > a.tab.n_listed || a.n_pages == 0)) ||
             (long long)delta + len > (1ll << 30)) {
           report_status(a.status, 4, RK_CHK_PLAN_ITEM, i);
         } else {

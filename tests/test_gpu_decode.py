@@ -612,6 +612,25 @@ def test_plan_errors_are_reported(rk, ctx):
     assert ei.value.status == 3
 
 
+def test_pool_without_pages(rk, ctx):
+    """Tables that name rows of a pool without pages: reported, no tile is made, the rows see nothing."""
+    table = rk.CacheTable(i32([100]), i32([0, 2]), i32([0, 1]))
+    pages = torch.empty((0, D.PAGE_BYTES), dtype=torch.uint8, device="cuda")
+    plan = ctx.rk_decode_plan(table, 0, i32([0, 1]), i32([0]), i32([0]), i32([[99]]), max_tiles=1)
+    with pytest.raises(rk.RKError) as ei:
+        ctx.rk_poll_status()
+    assert ei.value.status == 4
+    q = torch.ones((1, 1, 16, 576), dtype=torch.bfloat16, device="cuda")
+    O, lse = ctx.rk_cache4_attn(pages, plan, q)
+    ctx.rk_poll_status()
+    assert (O == 0).all() and torch.isneginf(lse).all()
+    empty = rk.CacheTable(i32([0]), i32([0, 0]), torch.empty(0, dtype=torch.int32, device="cuda"))
+    plan = ctx.rk_decode_plan(empty, 0, i32([0, 1]), i32([0]), i32([0]), i32([[0]]), max_tiles=1)
+    O, lse = ctx.rk_cache4_attn(pages, plan, q)
+    ctx.rk_poll_status()
+    assert (O == 0).all() and torch.isneginf(lse).all()
+
+
 def test_decode_agrees_with_the_online_attention_on_the_same_rows(rk):
     """The last query token of an online request, and the same token over the cache: both attend the same rows."""
     from paper_2609_07008_b200 import synth
