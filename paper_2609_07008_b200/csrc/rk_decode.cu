@@ -195,6 +195,9 @@ __device__ __forceinline__ uint32_t load_shared(uint32_t at) {
 __device__ __forceinline__ void load_shared4(float* r, uint32_t at) {
   asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]) : "r"(at) : "memory");
 }
+__device__ __forceinline__ void store_shared4(uint32_t at, const uint32_t* r) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
 __device__ __forceinline__ void store_shared(uint32_t at, uint32_t v) {
   asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
 }
@@ -450,37 +453,30 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     const int row = 32 * (warp & 3) + lane;  // a warp reaches the tensor memory lanes of its quarter
     const uint32_t t_k = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + kColK + 32u * h;
     uint32_t code[32], scl[4];
-    const uint8_t* src = nullptr;  // this key's first unit in the tile being loaded, null for a row that is not there
-    // rows that are not there become zeros (code 8): their scores are masked, and 0 * 0 adds nothing to O
+    const uint8_t* src = p.pages;  // this key's first unit in the tile being loaded
+    // A row behind the last key of its tile is read like any other (its page is in the pool): whatever it holds becomes finite
+    // values, its scores are masked, and 0 times a value adds nothing to O.
     auto load_pair = [&](int m) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (src != nullptr) put(code + 8 * m + 4 * e, __ldg(reinterpret_cast<const uint4*>(src + h * 2048 + (4 * m + e) * 1024)));
-        else put(code + 8 * m + 4 * e, make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u));
-      }
+      for (int e = 0; e < 2; ++e) put(code + 8 * m + 4 * e, __ldg(reinterpret_cast<const uint4*>(src + h * 2048 + (4 * m + e) * 1024)));
     };
-    auto load_scale = [&]() {
-      put(scl, src != nullptr ? __ldg(reinterpret_cast<const uint4*>(src + h * 1024 + 16 * 1024)) : make_uint4(0, 0, 0, 0));
-    };
+    auto load_scale = [&]() { put(scl, __ldg(reinterpret_cast<const uint4*>(src + h * 1024 + 16 * 1024))); };
     uint32_t t = 0;
     bool ok = true;
     Cursor c(p);
     bool more = c.next();
     int k = 0;
-    int page = 0, n = 0;  // record of the tile after the one in registers, fetched a tile ahead
+    int page = 0;  // of the tile after the one in registers, fetched a tile ahead
     auto fetch = [&]() {  // moves the cursor on and fetches that record
       if (++k >= c.cnt) {
         more = c.next();
         k = 0;
       }
       if (more) {
-        // one load per word: choosing among loaded words would wait for them
-        const DecodeTile* tile = &p.tiles[c.record(k)];
-        page = __ldg(&tile->page0 + (row >> 6));
-        n = __ldg(&tile->n);
+        page = __ldg(&p.tiles[c.record(k)].page0 + (row >> 6));
       }
     };
-    auto open = [&]() { src = row < n ? p.pages + (int64_t)page * kCache4PageBytes + (row & 63) * 16 : nullptr; };
+    auto open = [&]() { src = p.pages + (int64_t)page * kCache4PageBytes + (row & 63) * 16; };
     bool here = more;  // there is a tile in registers
     if (more) {
       k = -1;
@@ -556,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
     // chunk pair by chunk pair as the previous tile's products release the space.  Here and not in the key warps, which
     // thereby never wait for the value products; the softmax warps have nothing else to do while those run.
     auto copy_values = [&](uint32_t tv) -> bool {
-      uint8_t* const v_row = smem + kOffV + (c0 ? 1 : 0) * kKChunk + key * 128;
+      const uint32_t v_row = smem_base + kOffV + (c0 ? 1 : 0) * kKChunk + key * 128 + ((key & 7) << 4);
 #pragma unroll 1
       for (int m = 0; m < 4; ++m) {
         if (!wait(B_KFULL + m, tv & 1u, W_KFULL)) return false;
@@ -571,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         if (tv > 0 && !wait(B_PVDONE + m, (tv - 1) & 1u, W_PVDONE)) return false;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          *reinterpret_cast<uint4*>(v_row + 2 * m * kKChunk + ((e ^ (key & 7)) << 4)) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+          store_shared4((v_row + 2 * m * kKChunk) ^ (e << 4), v + 4 * e);  // rows are 128 bytes apart and aligned
       }
       return true;
     };
@@ -612,7 +608,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           const int at = key < rec.y ? rec.x + key : 0x7fffffff;
           const float add = raised && k > 0 ? 0.f : 1.f;
           float top = 0.f;
-          uint8_t* dst = smem + kOffP + key * 128;
+          const uint32_t dst = smem_base + kOffP + key * 128 + (((c0 / 8) ^ (key & 7)) << 4);
 #pragma unroll
           for (int i = 0; i < NC; i += 8) {
             uint32_t s[8], pk[4];
@@ -640,7 +636,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
               pk[j / 2] = pack_bf16(pv[0], pv[1]);
               pk[j / 2 + 1] = pack_bf16(pv[2], pv[3]);
             }
-            *reinterpret_cast<uint4*>(dst + ((((uint32_t)((c0 + i) / 8)) ^ (uint32_t)(key & 7)) << 4)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            store_shared4(dst ^ (uint32_t)((i / 8) << 4), pk);  // c0 / 8 and i / 8 have no bits in common
           }
           fence_proxy_async_smem();
           return top;
