@@ -7,28 +7,40 @@
 //   O^T[512 dims x N]  += C^T[512 x 128] P^T        4 tiles of 128 dims, A MN-major, B MN-major
 // With the rows in M a 64-row tile would run the tensor cores at half rate (M = 64) and 16 rows at an eighth.
 //
-// Dequantisation happens between the HBM load and the operands: 256 threads, two per key, hold a tile's 13 16-byte
-// units each in registers (53 KB in flight per SM) and turn them into the bf16 values n * s, which are exact.  They go
-// into tensor memory as the A operand of the scores (a lane is a key; 128 dims per slot, two slots); the softmax warps
-// copy them from there into shared memory as the A operand of the values (128 keys x 64 dims per 16 KB chunk, 128-byte
-// swizzle).  An M = 128, N = 64 product takes 33 clk with the keys in tensor memory and 49 with both operands in shared
-// memory (6 KB at 128 B/clk): 2900 clk of products per tile.
+// Dequantisation happens between the HBM load and the operands: 256 threads, two per key, hold the next tile's codes and
+// scales in registers (37 KB in flight per SM) and turn them into the bf16 values n * s, which are exact.  They go into
+// tensor memory as the A operand of the scores (a lane is a key; 128 dims per slot, two slots); the softmax warps copy them
+// from there into shared memory as the A operand of the values (128 keys x 64 dims per 16 KB chunk, 128-byte swizzle).  The
+// keys' rope chunk is bf16 in the pages, whose units of 64 rows x 16 bytes are the unswizzled K-major operand as they are:
+// it is copied into its place by bulk copies, into the space that P^T takes over once the scores are done.
+// An M = 128, N = 64 product takes 33 clk with the keys in tensor memory and 49 with both operands in shared memory
+// (6 KB at 128 B/clk): 3000 clk of products per tile.
 // One tile's values (128 KB), the queries (80 KB) and P^T (16 KB) fill the shared memory, so the value chunks are
 // refilled pair by pair as the products release them.  The scores do not wait for that: the keys of the next pair
-// are already in tensor memory, and the products of the next tile's first pieces run under this tile's softmax.
+// are already in tensor memory, and the products of the next tile's first half run under this tile's softmax.
+//
+// What bounds it: a tile takes some 5000 clk, of which the tensor core works 3000 (37 % of the kernel's cycles with start
+// and end), the ALUs 42 % and the issue slots 46 %.  The rest is the chain from tile to tile: value products -> free chunks
+// -> copied values and free key slots -> last scores -> softmax -> value products, each step at the speed that eight warps
+// get beside the others.  Measured: 64 requests with 64 heads over 440k visible rows 100 us, one request over 262144 rows
+// 62 us (112 MB of pages in: 1.8 TB/s), 16 requests with two tokens of 128 heads 213 us (710 TFLOP/s), 8 tiles 15 us.
+// Tried and slower: the keys through shared memory only (more operand traffic, 1.1x), the key warps writing the values
+// (they then wait for the value products, 1.07x), four key warps of twice the registers (1.25x), the register split of
+// setmaxnreg (its small share spilled, 1.03x to 1.8x), unrolled copies and products (instruction cache, 1.03x to 1.15x).
 //
 // Statistics: running maximum per query row in shared memory, raised only when a tile exceeds it by more than 2^8
 // (then O^T is rescaled in tensor memory, columns = rows of the query); sums per (key lane, row) in registers in
-// fp32, added up over the lanes once per row tile.  P is rounded to bf16 for the tensor cores (relative 2^-9 per
-// key, averaged by the sum); the turned query rope goes in as two bf16 parts, high and low (relative 2^-17 together):
-// the log-sum-exp is an fp32 output, and one part alone moves a logit by 1e-3.
+// fp32, added up over the lanes once per row tile.  P is rounded to bf16 for the tensor cores (at most 2^-8 of each
+// key's, averaged by the sum); the turned query rope goes in as two bf16 parts, high and low (2^-16 together):
+// the log-sum-exp is an fp32 output, and one part alone moves a logit by 1e-3.  A key with a NaN scale has finite values
+// and a NaN flag beside its tile, which the softmax turns into a NaN score: rows whose mask leaves the key out stay clean.
 //
 // Work: the plan lists every (sequence, row tile, key tile) in order and gives each CTA an equal run of them.  A
 // row tile whose keys several CTAs share leaves normalised fp32 partial results and their log-sum-exp, which a
 // second kernel joins in CTA order (no atomics: results do not depend on timing).
 //
-// Warps (640 threads): 0 issues the MMAs, 1 loads the queries (TMA) and turns their rope part, 2 and 3 idle, 4-11 load
-// and dequantise keys, 12-19 softmax, correction and epilogue.
+// Warps (640 threads): 0 issues the MMAs, 1 and 3 load the queries (TMA) and turn their rope part, 2 loads the keys' rope
+// part, 4-11 load and dequantise keys, 12-19 softmax, correction and epilogue.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -446,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
       }
     }
   } else if (warp < kSoftWarp0) {
-    // ------------------------------ keys: HBM -> registers (4-bit) -> shared memory (bf16) --------------------
+    // ------------------------------ keys: HBM -> registers (4-bit) -> tensor memory (bf16) --------------------
     // Two threads per key: thread h has chunk 2 m + h (64 dims, two units) of every 128 dims m and the scale unit h (one word per
     // chunk).
     const int h = (warp - kKeyWarp0) >> 2;
