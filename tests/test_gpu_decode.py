@@ -612,6 +612,18 @@ def test_plan_errors_are_reported(rk, ctx):
     assert ei.value.status == 3
 
 
+@pytest.mark.parametrize("far", [2 ** 30 - 1, 2 ** 30, 2 ** 31 - 1])
+def test_positions_far_behind_the_last_key(rk, ctx, far):
+    """A token at the largest positions sees every key and nothing else (the pages hold NaN behind the last one)."""
+    pool = Pool(rk, [130, 65], seed=51)
+    fill_pool(ctx, pool, 51)
+    items = [[(0, 0), (1, 130)]]
+    run_attention(ctx, pool, items, [[194]], 16, 52)
+    _, _, O, lse = run_attention(ctx, pool, items, [[far]], 16, 52)
+    _, _, near, near_lse = run_attention(ctx, pool, items, [[194]], 16, 52)
+    assert torch.equal(O, near) and torch.equal(lse, near_lse)
+
+
 def test_pool_without_pages(rk, ctx):
     """Tables that name rows of a pool without pages: reported, no tile is made, the rows see nothing."""
     table = rk.CacheTable(i32([100]), i32([0, 2]), i32([0, 1]))
