@@ -324,8 +324,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
 #pragma unroll 1
       for (int k = -1; ok && k < c.cnt; ++k) {
         if (k >= 0) {  // what is left of this tile's scores
-          piece(2, t);
-          piece(3, t);
+#pragma unroll 1
+          for (int i = 2; i < 4; ++i) piece(i, t);
           ok = ok && wait(B_QROPE, t & 1u, W_QROPE) && wait(B_KROPE, t & 1u, W_KROPE);
           if (!ok) break;
           tc_fence_after_sync();
@@ -340,8 +340,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           __syncwarp();
         }
         if (k + 1 < c.cnt) {  // the first half of the next tile's (the next group has other queries)
-          piece(0, k < 0 ? t : t + 1u);
-          piece(1, k < 0 ? t : t + 1u);
+#pragma unroll 1
+          for (int i = 0; i < 2; ++i) piece(i, k < 0 ? t : t + 1u);
         }
         if (k < 0) continue;
         ok = ok && wait(B_PREADY, t & 1u, W_PREADY);
