@@ -397,9 +397,13 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         if (!ok) break;
         if (d != delta) {
           delta = d;
-          float cs[4], sn[4];
+          float cos_of, sin_of, cs[4], sn[4];  // each lane one of the 32 angles, then this lane's four
+          rope_cos_sin(p.rope, d, lane, cos_of, sin_of);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) rope_cos_sin(p.rope, d, 4 * rc + e, cs[e], sn[e]);
+          for (int e = 0; e < 4; ++e) {
+            cs[e] = __shfl_sync(0xffffffffu, cos_of, 4 * rc + e);
+            sn[e] = __shfl_sync(0xffffffffu, sin_of, 4 * rc + e);
+          }
           uint8_t* dst = smem + kOffQ + 8 * kQChunk + sw128_offset((uint32_t)r_first, (uint32_t)rc);
 #pragma unroll 1
           for (int i = 0; i < kRows / 8; ++i, dst += 1024) {  // the rows go round in the registers: one copy of the code
