@@ -1,4 +1,4 @@
-"""Float64 checker of the decode operators: the 4-bit latent cache (format, append, read), attention of single
+"""Float64 oracle of the decode operators: the 4-bit latent cache (format, append, read), attention of single
 tokens over cached segments, and 4-bit weight matrices.  Written from the definitions in include/rk.h."""
 from __future__ import annotations
 

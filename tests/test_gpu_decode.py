@@ -1,4 +1,4 @@
-"""GPU parity of the decode operators through the C ABI against the float64 checker: the 4-bit paged cache (append,
+"""GPU parity of the decode operators through the C ABI against the float64 oracle: the 4-bit paged cache (append,
 read), attention of single tokens over it, 4-bit matrix-vector products, and a run of them together.
 
 Error bounds (derived, per element).  u = 2^-8 is half a bf16 step relative to the value.
@@ -120,7 +120,7 @@ def special_rows(rng, n):
     ([1], [0], 0), ([1, 1, 1], [63, 64, 127], 0), ([0, 5, 0, 200, 0, 1], [3, 60, 0, 1, 64, 5000], 7),
     ([64, 65, 63, 1, 129], [0, 0, 0, 64, 63], 0), ([33] * 40, list(range(40)), 31), ([3, 0, 0], [0, 0, 1], 1),
 ])
-def test_append_matches_checker_and_touches_nothing_else(rk, ctx, new, old, pad):
+def test_append_matches_oracle_and_touches_nothing_else(rk, ctx, new, old, pad):
     rng = np.random.default_rng(sum(new) + pad)
     pool = Pool(rk, [a + b for a, b in zip(new, old)], seed=5, fill=0xA5)
     n = sum(new)
@@ -437,7 +437,7 @@ def test_attention_bad_key_reaches_only_the_tokens_that_see_it(rk, heads, n, bad
     O, lse = ctx.rk_cache4_attn(pool.pages, plan_for(ctx, pool, items, q_pos), q)
     ctx.rk_poll_status()
     assert torch.isnan(O[0, 1]).all() and torch.isnan(lse[0, 1]).all()
-    pool.lens = [n - 1]                                            # the checker does not see the row either
+    pool.lens = [n - 1]                                            # the oracle does not see the row either
     check_attention(ctx, pool, [items[0]], q_pos[:1, :1], q[:1, :1], O[:1, :1], lse[:1, :1], heads)
     check_attention(ctx, pool, [items[1]], q_pos[1:], q[1:], O[1:], lse[1:], heads)
 
@@ -685,7 +685,7 @@ def check_matvec(got, x, vals, k, bf16):
 @pytest.mark.parametrize("tok", [1, 2, 7, 8, 9, 15, 16, 17, 40])
 @pytest.mark.parametrize("mats, n_out, k, group", [(1, 16, 64, 32), (3, 48, 128, 128), (2, 80, 1024, 64), (1, 272, 640, 32),
                                                    (5, 128, 512, 128)])
-def test_matvec_matches_checker(rk, ctx, mats, n_out, k, group, tok):
+def test_matvec_matches_oracle(rk, ctx, mats, n_out, k, group, tok):
     rng = np.random.default_rng(k + tok)
     w = bf(rng.standard_normal((mats, n_out, k)) * 0.02)
     vals = D.quantise_weights(f64(w), group)
@@ -772,7 +772,7 @@ def test_matvec_without_tokens_and_repeats_bit_for_bit(rk, ctx):
 # ------------------------------------------------------------------------------------------------------------
 def test_decode_steps_over_reused_documents(rk):
     """Two requests over three cached documents generate four tokens: append, plan, attention, W_uv, W_a, W_b in
-    4 bits.  Each stage is checked against the checker on that stage's own input."""
+    4 bits.  Each stage is checked against the oracle on that stage's own input."""
     ctx = make_ctx(rk, 16)
     rng = np.random.default_rng(30)
     docs = [200, 333, 64]

@@ -1,5 +1,5 @@
-"""Pins of the decode checker: the cached-row format, its rounding, and attention over cached segments against
-the checkers that already exist or closed forms."""
+"""Pins of the decode oracle: the cached-row format, its rounding, and attention over cached segments against
+the oracles that already exist or closed forms."""
 import numpy as np
 import pytest
 import torch
@@ -56,7 +56,7 @@ def test_scale_and_code_rounding():
     assert (np.abs(D.SCALES[byte] - m) <= m / 16 * (1 + 1e-12)).all()
 
 
-def test_turn_matches_the_online_checker():
+def test_turn_matches_the_online_oracle():
     import oracle
     rng = np.random.default_rng(2)
     x = rng.standard_normal((5, 64))
