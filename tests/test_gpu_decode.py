@@ -352,6 +352,18 @@ def test_attention_heads_and_tokens(rk, heads, q_len):
     run_attention(ctx, pool, items, pos, heads, heads + q_len)
 
 
+@pytest.mark.parametrize("heads, q_len", [(24, 17), (8, 64), (128, 64)])
+def test_attention_many_drafted_tokens(rk, heads, q_len):
+    """Many row tiles per request, the last one short; every token has its own mask, the first ones see only the document."""
+    ctx = make_ctx(rk, heads)
+    lens = [150, q_len + 3, 2]
+    pool = Pool(rk, lens, seed=61)
+    fill_pool(ctx, pool, 61)
+    items = [[(0, 0), (1, 150)], [(2, 0)]]
+    q_pos = np.array([np.arange(q_len) + 150 - 2, np.arange(q_len) - 1])
+    run_attention(ctx, pool, items, q_pos, heads, 62)
+
+
 @pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 127, 128, 129, 191, 192, 193, 255, 256, 257, 1000])
 def test_attention_lengths(rk, ctx, n):
     """One segment of n rows, seen whole, all but the last, one row only, not at all; the rest of its pages is NaN."""
