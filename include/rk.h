@@ -409,7 +409,8 @@ typedef struct rk_decode_shape {
  *   q_pos      device int32 [n_seqs][q_len]: request positions of the query tokens
  *   plan       device, rk_decode_plan_bytes() bytes, 256-byte aligned
  * Row j of an item sits at position item_delta + j; query token t sees it iff item_delta + j <= q_pos[t] (so a
- * padding request is one without items, or with negative positions).  A bad item is left out (RK_ERR_ROWS); more key tiles than
+ * padding request is one without items, or with negative positions, and a padding token has a negative position; any
+ * will do).  A bad item is left out, and so is a key tile whose pages are not in the pool (RK_ERR_ROWS); more key tiles than
  * max_tiles make an empty plan (RK_ERR_WORKSPACE). Both are reported by rk_poll_status(). */
 rk_status rk_decode_plan_bytes(const rk_ctx* ctx, const rk_decode_shape* shape, size_t* out);
 rk_status rk_decode_plan(rk_ctx* ctx, const rk_decode_shape* shape, const rk_cache4_table* table, int64_t n_pages,

@@ -229,8 +229,9 @@ __global__ void __launch_bounds__(kPlanThreads) decode_plan_scan_kernel(DecodePl
   __shared__ long long carry;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) carry = 0;
-  // every key lies below 2^30: a later position sees all there is, and the sums and comparisons behind stay inside 32 bits
-  for (int i = tid; i < a.n_seqs * a.q_len; i += kPlanThreads) a.pos_out[i] = min(a.q_pos[i], 1 << 30);
+  // Every key lies at 0 or above and below 2^30: a later position sees all there is, a negative one nothing, whichever it is.
+  // With both ends limited the sums, differences and comparisons behind stay inside 32 bits.
+  for (int i = tid; i < a.n_seqs * a.q_len; i += kPlanThreads) a.pos_out[i] = max(min(a.q_pos[i], 1 << 30), -1);
   __syncthreads();
   for (int base = 0; base < a.n_items; base += kPlanThreads) {
     const int i = base + tid;

@@ -199,7 +199,7 @@ struct DecodePlanArgs {
   const int32_t* item_delta;  // [n_items]
   const int32_t* q_pos;       // [n_seqs][q_len]
   DecodePlanHeader* header;
-  int32_t* pos_out;    // copy of q_pos
+  int32_t* pos_out;    // copy of q_pos, limited to -1 .. 2^30
   int32_t* item_tile;  // [n_items + 1]
   int32_t* seq_tile;   // [n_seqs + 1]
   int4* cta_start;     // [n_ctas] (sequence, row tile, key tile, used)
