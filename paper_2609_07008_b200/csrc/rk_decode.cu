@@ -646,7 +646,10 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
                 if (kMasked && at > lasts[n]) e = -INFINITY;
                 pv[n] = fast_exp2(e);
                 if constexpr (!kMasked) l[i + j + n] += pv[n];
-                else l[i + j + n] = al[n] < 1e-27f ? pv[n] : fmaf(l[i + j + n], al[n], add * pv[n]);
+                else {
+                  const float old = l[i + j + n];  // a NaN in it stays, see below
+                  l[i + j + n] = al[n] < 1e-27f && old == old ? pv[n] : fmaf(old, al[n], add * pv[n]);
+                }
               }
               top = fmaxf(top, fmaxf(fmaxf(pv[0], pv[1]), fmaxf(pv[2], pv[3])));
               pk[j / 2] = pack_bf16(pv[0], pv[1]);
@@ -718,7 +721,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           // Where the first try was made, the sums already hold this tile's p against the old maximum, and the factor makes
           // them right for the new one; otherwise this tile's p are added here.
           // Where the maximum rose by more than 2^90 (or there was none) they may have overflowed: there, what was
-          // summed up before is below 2^-60 of the new sum and is dropped.
+          // summed up before is below 2^-60 of the new sum and is dropped - unless it is a NaN, which is the row's for good: the
+          // first tiles of a row may hold nothing but NaN scores, which leave the maximum where it was.
           write_p(std::true_type(), true, scale);
           tc_fence_before_sync();
           named_barrier_sync(1, kSoftmax);
