@@ -121,7 +121,17 @@ rk_status rk_set_wait_limit_ms(rk_ctx* ctx, int32_t ms);
  * attention launches of this context use an instantiation whose load warp leaves every ring stage
  * empty, so the consumers' bounded waits expire, the kernel drains and returns, and
  * rk_poll_status() reports RK_ERR_TIMEOUT.  Results are not produced while it is on.  Use it
- * together with a short rk_set_wait_limit_ms. */
+ * together with a short rk_set_wait_limit_ms.
+ * rk_matvec4 likewise issues no copies of the weights, and rk_cache4_attn withholds one of the signals below, whichever `on`
+ * names (any other number counts as RK_STARVE_LOADS); the other calls make no difference between them. */
+#define RK_STARVE_LOADS 1      /* the keys' rope part is not copied */
+#define RK_STARVE_QUERIES 2    /* the queries' latent part is not copied */
+#define RK_STARVE_QUERY_ROPE 3 /* their turned rope part is not announced */
+#define RK_STARVE_KEYS 4       /* nor are unpacked keys */
+#define RK_STARVE_KEYS_FREE 5  /* nor that the scores are done with them */
+#define RK_STARVE_SCORES 6     /* nor the scores */
+#define RK_STARVE_WEIGHTS 7    /* nor the softmax weights */
+#define RK_STARVE_VALUES 8     /* nor the end of the value products */
 rk_status rk_test_starve_loads(rk_ctx* ctx, int32_t on);
 /* The library can be built with -DRK_CHECK (paper_2609_07008_b200/build.py, check=True): its kernels then
  * test every index they derive from a request table (protected-row list, inverse row map, work list,

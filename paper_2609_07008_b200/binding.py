@@ -305,8 +305,8 @@ class Context:
     def rk_check_selftest(self):
         self.check(lib.rk_check_selftest(self.handle, _stream()))
 
-    def rk_test_starve_loads(self, on: bool):
-        self.check(lib.rk_test_starve_loads(self.handle, 1 if on else 0))
+    def rk_test_starve_loads(self, on: int):
+        self.check(lib.rk_test_starve_loads(self.handle, int(on)))
 
     def rk_request_create(self, seg_off, seg_delta, seg_has_artifact, prot_rows) -> "Request":
         return Request(self, seg_off, seg_delta, seg_has_artifact, prot_rows)

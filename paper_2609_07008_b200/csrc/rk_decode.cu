@@ -45,6 +45,7 @@
 
 #include <type_traits>
 
+#include "../../include/rk.h"
 #include "rk_internal.h"
 
 namespace rk {
@@ -222,31 +223,35 @@ __device__ __forceinline__ void put(uint32_t* r, const uint4& v) {
 
 }  // namespace
 
-template <int kRows>
+// kStarve: test instantiation in which the signals of one kind of barrier (p.starve) are withheld, so that whoever waits for them gives
+// up.  Nothing is withheld that memory accesses depend on.
+template <int kRows, bool kStarve>
 __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __grid_constant__ DecodeAttnParams p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t smem_base = smem_u32(smem);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) -> uint32_t { return smem_base + kOffBars + 8u * i; };
+  auto fed = [&](int what) -> bool { return !kStarve || p.starve != what; };
   volatile uint32_t* tmem_ptr = reinterpret_cast<volatile uint32_t*>(smem + kOffTmem);
-  // Bounded wait on one of the barriers, kept short: it is inlined two dozen times, and the kernel's loops have to stay in
-  // the instruction cache.  The word at kOffAbort is the tag of the first wait that ran out (reported once, at the end),
-  // after which everyone gives up.
+  // Bounded wait of a whole warp on one of the barriers, kept short: it is inlined two dozen times, and the kernel's loops have
+  // to stay in the instruction cache.  The word at kOffAbort is the tag of the first wait that ran out (reported once, at the
+  // end), after which everyone gives up.  The lanes look at the barrier, the word and the clock one by one, so the warp votes:
+  // it goes on together or gives up together, as what follows a wait are operations of all its lanes.
   auto wait = [&](int b, uint32_t parity, int where) -> bool {
     const uint32_t at = smem_base + kOffBars + 8u * (uint32_t)b;
     uint32_t t0 = 0u;
+    bool done = true;
 #pragma unroll 1
     for (uint32_t n = 1; !mbar_try_wait(at, parity); ++n) {
       if ((n & 63u) != 0u) continue;
-      if (load_shared(smem_base + kOffAbort) != 0u) return false;
       const uint32_t now = globaltimer_lo();
       if (n == 64u) t0 = now;
-      if (now - t0 > p.wait_ns) {
-        store_shared(smem_base + kOffAbort, (uint32_t)where);
-        return false;
-      }
+      const bool late = now - t0 > p.wait_ns;
+      done = !late && load_shared(smem_base + kOffAbort) == 0u;
+      if (late) store_shared(smem_base + kOffAbort, (uint32_t)where);
+      if (!done) break;
     }
-    return true;
+    return __all_sync(0xffffffffu, done);
   };
 
   {  // the plan has to be the one of this call's shape, heads and pool
@@ -315,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
 #pragma unroll
         for (int s = 0; s < 8; ++s)
           mma_ts(ts, tk + 8u * s, db + (uint32_t)(((s >> 2) * kQChunk + (s & 3) * 32) >> 4), id_qk, s > 0 ? 1u : iu);
-        umma_commit_1(bar(B_KFREE) + 8u * iu);
+        if (fed(RK_STARVE_KEYS_FREE)) umma_commit_1(bar(B_KFREE) + 8u * iu);
       }
       __syncwarp();
     };
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
 #pragma unroll
             for (int s = 0; s < 8; ++s)  // the same 64 dims of the keys against the high and the low part of the turned queries
               mma_ss(ts, da + (uint32_t)(((s & 3) * 4096) >> 4), kDescHiPlain, db + (uint32_t)(((s >> 2) * kQChunk + (s & 3) * 32) >> 4), id_qk, 1u);
-            umma_commit_1(bar(B_SFULL));
+            if (fed(RK_STARVE_SCORES)) umma_commit_1(bar(B_SFULL));
           }
           __syncwarp();
         }
@@ -356,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
             for (int s = 0; s < 8; ++s)
               mma_ss(tmem + (uint32_t)(m * kRows), da + (uint32_t)((s * 2048) >> 4), kDescHi, db + (uint32_t)((s * 2048) >> 4), id_pv,
                      s > 0 ? 1u : (uint32_t)k);
-            umma_commit_1(bar(B_PVDONE) + 8u * (uint32_t)m);
+            if (fed(RK_STARVE_VALUES)) umma_commit_1(bar(B_PVDONE) + 8u * (uint32_t)m);
           }
         }
         __syncwarp();
@@ -383,9 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
       }
       // the previous group's scores are done with the query chunks (its last tile's S is complete)
       if (t > 0) ok = wait(B_SFULL, (t - 1) & 1u, W_SFULL);
-      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (warp == 1 && elect_one()) {
+      if (warp == 1 && fed(RK_STARVE_QUERIES) && elect_one()) {
         mbar_arrive_expect_tx(bar(B_QFULL), 8 * kRows * 128);
         for (int d = 0; d < 8; ++d) tma_load_2d(smem_base + kOffQ + d * kQChunk, &p.tm_q, bar(B_QFULL), d * 64, row0);
       }
@@ -426,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           fence_proxy_async_smem();
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_QROPE));
+        if (lane == 0 && fed(RK_STARVE_QUERY_ROPE)) mbar_arrive(bar(B_QROPE));
       }
     }
   } else if (warp == 2) {
@@ -446,10 +450,9 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         const uint8_t* src0 = p.pages + (int64_t)page0 * kCache4PageBytes + 18 * 1024;
         const uint8_t* src1 = p.pages + (int64_t)page1 * kCache4PageBytes + 18 * 1024;
         if (t > 0) ok = wait(B_PVDONE + 3, (t - 1) & 1u, W_PVDONE);  // P^T of the last tile has been read
-        ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         // rows that are not there keep what is in their place: their scores are masked
-        if (elect_one()) {
+        if (fed(RK_STARVE_LOADS) && elect_one()) {
           mbar_arrive_expect_tx(bar(B_KROPE), both != 0u ? 16384u : 8192u);
 #pragma unroll
           for (int u = 0; u < 8; ++u) bulk_load(smem_base + kOffP + u * 2048, src0 + u * 1024, 1024u, bar(B_KROPE));
@@ -539,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_KFULL + m));
+        if (lane == 0 && fed(RK_STARVE_KEYS)) mbar_arrive(bar(B_KFULL + m));
       }
       if (!ok) break;
       ++t;
@@ -669,9 +672,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         // First try with the maxima as they are (S of this tile is complete, so P^T of the previous one has been read).
         // A warp that finds an exponent above 8, or that gave up waiting, raises the flag; everyone sees it behind
         // the barrier.  Not tried for the first tile of a group, which has no maxima yet.
-        const bool all_ok = __all_sync(0xffffffffu, ok);
         float top = INFINITY;
-        if (k > 0 && all_ok) top = full ? write_p(std::false_type(), false, scale) : write_p(std::true_type(), false, scale);
+        if (k > 0 && ok) top = full ? write_p(std::false_type(), false, scale) : write_p(std::true_type(), false, scale);
         if (top > 256.f) *s_flag = (int)t + 1;
         tc_fence_before_sync();
         named_barrier_sync(1, kSoftmax);
@@ -727,7 +729,7 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
           tc_fence_before_sync();
           named_barrier_sync(1, kSoftmax);
         }
-        if (tid == 0) mbar_arrive(bar(B_PREADY));
+        if (tid == 0 && fed(RK_STARVE_WEIGHTS)) mbar_arrive(bar(B_PREADY));
       }
       if (!ok) break;
       // ---- epilogue of the group: sums over the key lanes, then O^T / l ----
@@ -922,18 +924,26 @@ __global__ void __launch_bounds__(kJoinThreads) rk_decode_join_kernel(const __gr
 
 int decode_row_tile(int rows_per_seq) { return rows_per_seq <= 16 ? 16 : (rows_per_seq <= 32 ? 32 : 64); }
 
+namespace {
+using DecodeKernel = void (*)(const DecodeAttnParams);
+DecodeKernel decode_kernel(int row_tile, bool starve) {
+  if (row_tile == 16) return starve ? rk_decode_attn_kernel<16, true> : rk_decode_attn_kernel<16, false>;
+  if (row_tile == 32) return starve ? rk_decode_attn_kernel<32, true> : rk_decode_attn_kernel<32, false>;
+  return starve ? rk_decode_attn_kernel<64, true> : rk_decode_attn_kernel<64, false>;
+}
+}  // namespace
+
 cudaError_t decode_attn_setup() {
-  cudaError_t e = cudaFuncSetAttribute(rk_decode_attn_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(rk_decode_attn_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(rk_decode_attn_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+  cudaError_t e = cudaSuccess;
+  for (int row_tile = 16; row_tile <= 64 && e == cudaSuccess; row_tile *= 2)
+    for (int starve = 0; starve < 2 && e == cudaSuccess; ++starve)
+      e = cudaFuncSetAttribute(decode_kernel(row_tile, starve != 0), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   return e;
 }
 
 cudaError_t launch_decode_attn(const DecodeAttnParams& p, int row_tile, cudaStream_t stream) {
   const dim3 grid((unsigned)p.n_ctas);
-  if (row_tile == 16) rk_decode_attn_kernel<16><<<grid, kThreads, kSmemBytes, stream>>>(p);
-  else if (row_tile == 32) rk_decode_attn_kernel<32><<<grid, kThreads, kSmemBytes, stream>>>(p);
-  else rk_decode_attn_kernel<64><<<grid, kThreads, kSmemBytes, stream>>>(p);
+  decode_kernel(row_tile, p.starve != 0)<<<grid, kThreads, kSmemBytes, stream>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   rk_decode_join_kernel<<<(unsigned)(2 * p.n_ctas), kJoinThreads, 0, stream>>>(p, row_tile);

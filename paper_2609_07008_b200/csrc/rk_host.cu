@@ -37,7 +37,7 @@ struct rk_ctx {
   bool value_phase = false;  // output-phase variant: the whole stored row is the value, O rows are 576 wide
   int ow = kDLatent;         // width of an attention output row (512, or 576 with value_phase)
   double rope_turns[32];     // theta_j / (2 pi)
-  bool starve_loads = false;  // rk_test_starve_loads: the timeout test's instantiation of the attention kernel
+  int32_t starve_loads = 0;  // rk_test_starve_loads: the timeout tests' instantiations of the attention kernels
   cudaStream_t copy_stream = nullptr;  // rk_layer_host: copies that overlap the kernels
   cudaStream_t copy_out_stream = nullptr;  // rk_layer_stack_host: device->host copies (full duplex with the above)
   cudaEvent_t sev[10] = {nullptr};     // rk_layer_stack_host: kv_ql_in[2], qg_in[2], zoff_in[2], compute_done[2], y_copied[2]
@@ -368,7 +368,7 @@ rk_status rk_check_selftest(rk_ctx* ctx, void* stream) {
 
 rk_status rk_test_starve_loads(rk_ctx* ctx, int32_t on) {
   if (!ctx) return RK_ERR_NULL;
-  ctx->starve_loads = on != 0;
+  ctx->starve_loads = on < 0 || on > RK_STARVE_VALUES ? RK_STARVE_LOADS : on;
   return RK_OK;
 }
 
@@ -668,7 +668,7 @@ static rk_status attn_pass(rk_ctx* ctx, const rk_request* rq, const void* kv, co
   p.row_base = (int32_t)row_base;
   p.n_rows_total = (int32_t)rq->T;
   memcpy(p.rope_turns, ctx->rope_turns, sizeof(p.rope_turns));
-  cudaError_t e = launch_attention(p, n_pairs, ctx->value_phase, ctx->starve_loads, stream);
+  cudaError_t e = launch_attention(p, n_pairs, ctx->value_phase, ctx->starve_loads != 0, stream);
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "attention launch");
 }
 
@@ -1372,6 +1372,7 @@ rk_status rk_cache4_attn(rk_ctx* ctx, const rk_decode_shape* shape, const void* 
   p.n_heads = ctx->prof.n_heads;
   p.n_row_tiles = decode_row_tiles(ctx, shape);
   p.n_ctas = ctx->sm_count;
+  p.starve = ctx->starve_loads;
   cudaError_t e = launch_decode_attn(p, tile, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "decode attention launch");
 }
@@ -1430,6 +1431,7 @@ rk_status rk_matvec4(rk_ctx* ctx, const rk_w4* w4, const void* x, int64_t x_stri
   p.out_f32 = out_dtype;
   p.status = ctx->d_status;
   p.wait_ns = ctx->wait_ns;
+  p.starve = ctx->starve_loads;
   cudaError_t e = launch_matvec4(p, ctx->matvec_slots, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "matrix-vector launch");
 }

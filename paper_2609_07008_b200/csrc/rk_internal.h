@@ -230,6 +230,7 @@ struct DecodeAttnParams {
   int64_t n_pages;
   float scale_log2;
   int32_t n_seqs, q_len, n_items, max_tiles, n_heads, n_row_tiles, n_ctas;
+  int32_t starve;  // rk_test_starve_loads: 0, or which signals the test instantiation withholds
 };
 
 int decode_row_tile(int rows_per_seq);  // 16, 32 or 64 query rows per CTA
@@ -256,6 +257,7 @@ struct Matvec4Params {
   uint32_t stage_bytes, red_bytes;
   DeviceStatus* status;
   unsigned long long wait_ns;
+  int32_t starve;  // rk_test_starve_loads
 };
 cudaError_t launch_quant4(const void* w, int32_t n_mat, int32_t n_out, int32_t k, int32_t group, void* codes, void* scales,
                           cudaStream_t stream);

@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, 2) rk_matvec4_kernel(const __grid_co
   int next_pass = 0, next_batch = 0;  // of the next load
   auto load_next = [&](int s) {
     if (next_pass == p.passes) return;
-    if (threadIdx.x == 0) load(next_pass, next_batch, s);
+    if (threadIdx.x == 0 && p.starve == 0) load(next_pass, next_batch, s);
     if (++next_batch == n_batches) {
       next_batch = 0;
       ++next_pass;
