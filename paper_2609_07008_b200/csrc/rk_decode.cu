@@ -788,14 +788,15 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
   }
 
   // ------------------------------ teardown -------------------------------------------------------------------
-  // after a wait has expired: copies and products in flight get a bounded time to finish
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  // Looked at once every role is done: the epilogue's wait can run out after the other roles have left.  Copies and products in
+  // flight then get a bounded time to finish.
   if (load_shared(smem_base + kOffAbort) != 0u) {
     if (threadIdx.x == 0) report_timeout(p.status, (int)load_shared(smem_base + kOffAbort), 0);
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
   }
-  __syncwarp();
-  tc_fence_before_sync();
-  __syncthreads();
   if (warp == 0) {
     __syncwarp();
     tmem_dealloc<1>(tmem, 512);

@@ -71,3 +71,25 @@ def test_products_give_up_and_the_context_works_on(rk, mats, n_out, k, group, to
     ctx.rk_set_wait_limit_ms(2000)
     check_matvec(ctx.rk_matvec4(w4, x, out_dtype=torch.float32), f64(x), D.quantise_weights(f64(w), group), k, False)
     ctx.rk_poll_status()
+
+
+@pytest.mark.parametrize("heads", [16, 32, 64])
+@pytest.mark.parametrize("tiles", [1, 5])
+def test_wait_that_runs_out_after_the_issuing_warp_has_left_is_reported(rk, heads, tiles):
+    """One key tile per thread block: when the epilogue waits for the end of the value products, the warp that issued them has
+    nothing left to do."""
+    ctx = make_ctx(rk, heads)
+    n = 128 * tiles
+    pool = Pool(rk, [n], seed=94)
+    fill_pool(ctx, pool, 94)
+    plan = plan_for(ctx, pool, [[(0, 0)]], np.array([[n - 1]]))
+    q = bf(np.random.default_rng(95).standard_normal((1, 1, heads, 576)))
+    ctx.rk_set_wait_limit_ms(20)
+    ctx.rk_test_starve_loads(VALUES)
+    ctx.rk_cache4_attn(pool.pages, plan, q)
+    timed_out(rk, ctx)
+    ctx.rk_test_starve_loads(0)
+    ctx.rk_set_wait_limit_ms(2000)
+    O, lse = ctx.rk_cache4_attn(pool.pages, plan, q)
+    ctx.rk_poll_status()
+    check_attention(ctx, pool, [[(0, 0)]], np.array([[n - 1]]), q, O, lse, heads)
