@@ -205,6 +205,12 @@ def _pages(t: torch.Tensor) -> int:
     return shape[0]
 
 
+def _here(kept, name: str):
+    """Tables, plans and weights are kept between calls, and the current device may have changed since they were made."""
+    if kept.index != _current_device():
+        raise ValueError(f"{name} was made on CUDA device {kept.index}, which is not the current one")
+
+
 class CacheTable:
     """Segments of a 4-bit paged cache and their pages: device int32 seg_len [S], page_off [S + 1], page_ids [n].
     The tensors are used as they are at the time of each call; their contents may change between calls."""
@@ -213,7 +219,7 @@ class CacheTable:
         self.seg_len = _need(seg_len, "seg_len", torch.int32, (-1,))
         self.page_off = _need(page_off, "page_off", torch.int32, (seg_len.numel() + 1,))
         self.page_ids = _need(page_ids, "page_ids", torch.int32, (-1,))
-        self.n_segs = seg_len.numel()
+        self.n_segs, self.index = seg_len.numel(), seg_len.get_device()
         self.struct = rk_cache4_table(self.n_segs, page_ids.numel(), _ptr(seg_len), _ptr(page_off), _ptr(page_ids))
         self.ref = C.byref(self.struct)
 
@@ -222,7 +228,8 @@ class DecodePlan:
     """Work list of one decode step (rk_decode_plan): shape, pool size and the device buffer."""
 
     def __init__(self, shape: rk_decode_shape, n_pages: int, buf: torch.Tensor):
-        self.shape, self.n_pages, self.buf = shape, n_pages, buf
+        self.shape, self.n_pages, self.buf = shape, n_pages, _need(buf, "buf", torch.uint8, (-1,))
+        self.index = buf.get_device()
         self.rows = (shape.n_seqs, shape.q_len)
         self.ref = C.byref(shape)
 
@@ -235,6 +242,7 @@ class W4:
         self.codes, self.scales = _need(codes, "codes", torch.uint8, None), _need(scales, "scales", torch.bfloat16, None)
         if codes.numel() < n_mat * n_out * k // 2 or scales.numel() < n_mat * n_out * (k // max(group, 1)):
             raise ValueError("codes or scales are too small for the shape")
+        self.index = codes.get_device()
         self.struct = rk_w4(n_mat, n_out, k, group, _ptr(codes), _ptr(scales))
         self.ref = C.byref(self.struct)
 
@@ -451,6 +459,7 @@ class Context:
         segment s; table.seg_len already counts them.  pages: uint8 [n_pages, 26624].  Rows may be strided."""
         n = c.shape[0]
         n_pages = _pages(pages)
+        _here(table, "table")
         _need(c, "c", torch.bfloat16, (-1, 512), contiguous=False)
         _need(k_rope, "k_rope", torch.bfloat16, (n, 64), contiguous=False)
         _need(new_off, "new_off", torch.int32, (table.n_segs + 1,))
@@ -469,6 +478,7 @@ class Context:
         """The last row_off[s+1] - row_off[s] rows of every segment s as packed bf16 rows kv [n_rows, 576]; rows from
         row_off[n_segs] on are left as they were."""
         n_pages = _pages(pages)
+        _here(table, "table")
         _need(row_off, "row_off", torch.int32, (table.n_segs + 1,))
         if kv is None:
             kv = _empty((n_rows, 576), torch.bfloat16, pages.device)
@@ -485,6 +495,9 @@ class Context:
         """Work list of a decode step: request b sees the segments item_seg[seq_off[b]:seq_off[b+1]] at the request offsets
         item_delta; q_pos [n_seqs, q_len] are its query tokens' positions.  max_tiles bounds the sum over the items of
         ceil(rows / 128).  With plan= its buffer is filled anew (a captured graph keeps using it)."""
+        _here(table, "table")
+        if plan is not None:
+            _here(plan, "plan")
         _need(q_pos, "q_pos", torch.int32, (-1, -1))
         _need(seq_off, "seq_off", torch.int32, (q_pos.shape[0] + 1,))
         _need(item_seg, "item_seg", torch.int32, (-1,))
@@ -495,7 +508,7 @@ class Context:
         if plan is None:
             plan = DecodePlan(shape, int(n_pages), _empty(need.value, dtype=torch.uint8, device=q_pos.device))
         else:
-            plan.__init__(shape, int(n_pages), _need(plan.buf, "plan.buf", torch.uint8, (-1,)))
+            plan.__init__(shape, int(n_pages), plan.buf)
         self.check(lib.rk_decode_plan(self.handle, C.byref(shape), table.ref, int(n_pages), _ptr(seq_off), _ptr(item_seg),
                                       _ptr(item_delta), _ptr(q_pos), _ptr(plan.buf), plan.buf.numel(), _quick_stream()))
         return plan
@@ -504,6 +517,7 @@ class Context:
         """q [n_seqs, q_len, n_heads, 576] -> (O [n_seqs, q_len, n_heads, 512] bf16, lse fp32)."""
         rows = plan.rows + (self.n_heads,)
         n_pages = _pages(pages)
+        _here(plan, "plan")
         _need(q, "q", torch.bfloat16, rows + (576,))
         device = q.device
         if O is None:
@@ -539,12 +553,14 @@ class Context:
                     _empty(max(n // max(int(group), 1), 8), dtype=torch.bfloat16, device=w.device))
         elif (w4.n_mat, w4.n_out, w4.k, w4.group) != (n_mat, n_out, k, int(group)):
             raise ValueError("w4 has another shape")
+        _here(w4, "w4")
         self.check(lib.rk_quant4(self.handle, _ptr(w), w4.ref, _quick_stream()))
         return w4
 
     def rk_matvec4(self, w4: W4, x: torch.Tensor, y: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
         """x [n_tok, n_mat, k] bf16 (tokens may be strided) -> y [n_tok, n_mat, n_out], bf16 or float32."""
         n, n_mat, n_out, k = x.shape[0], w4.n_mat, w4.n_out, w4.k
+        _here(w4, "w4")
         _need(x, "x", torch.bfloat16, (n, n_mat, k), contiguous=False)
         if y is None:
             y = _empty((n, n_mat, n_out), out_dtype, x.device)
