@@ -170,7 +170,9 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
-_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+# torch's own short ways to the current device and stream, which a torch without CUDA or a later one may not have
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 _empty_strided = torch.empty_strided
 
 

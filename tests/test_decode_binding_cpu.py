@@ -1,5 +1,8 @@
 """Argument checks of the binding's decode calls that need no device: tensors are stand-ins that answer what the checks ask."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -100,3 +103,23 @@ def test_plan_buffer_has_to_be_bytes_in_a_row(on):
         binding.DecodePlan(shape, 4, FakeTensor(0, torch.int32, 1024))
     with pytest.raises(ValueError):
         binding.DecodePlan(shape, 4, FakeTensor(0, torch.uint8, 4, 1024))
+
+
+def test_import_needs_no_private_function_of_torch():
+    """A torch without the two private look-ups (one built without CUDA has neither): the binding imports, and the public
+    functions take their place."""
+    code = """
+import torch
+for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+class Stream:
+    cuda_stream = 77
+torch.cuda.current_device = lambda: 3
+torch.cuda.current_stream = lambda device=None: Stream() if device == 3 else None
+from paper_2609_07008_b200 import binding
+assert binding._current_device() == 3 and binding._quick_stream() == 77
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
