@@ -564,10 +564,13 @@ class Context:
         n, n_mat, n_out, k = x.shape[0], w4.n_mat, w4.n_out, w4.k
         _here(w4, "w4")
         _need(x, "x", torch.bfloat16, (n, n_mat, k), contiguous=False)
+        if y is not None:
+            out_dtype = y.dtype
+        if out_dtype is not torch.bfloat16 and out_dtype is not torch.float32:
+            raise TypeError(f"the products' outputs are bfloat16 or float32, not {out_dtype}")
         if y is None:
             y = _empty((n, n_mat, n_out), out_dtype, x.device)
         else:
-            out_dtype = y.dtype
             _need(y, "y", out_dtype, (n, n_mat, n_out), contiguous=False)
         x_stride, y_stride = n_mat * k, n_mat * n_out
         if not (x.is_contiguous() and y.is_contiguous()) and n > 0:
@@ -576,7 +579,7 @@ class Context:
                     raise ValueError(f"the values of a token of {name} must be contiguous")
             if n > 1:
                 x_stride, y_stride = x.stride(0), y.stride(0)
-        dt = 0 if out_dtype is torch.bfloat16 else {torch.float32: 1}[out_dtype]
+        dt = 0 if out_dtype is torch.bfloat16 else 1
         s = lib.rk_matvec4(self.handle, w4.ref, x.data_ptr(), x_stride, n, y.data_ptr(), y_stride, dt, _quick_stream())
         if s:
             self.check(s)

@@ -123,3 +123,14 @@ assert binding._current_device() == 3 and binding._quick_stream() == 77
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64, torch.int32])
+def test_products_refuse_output_types_they_do_not_have(on, dtype):
+    binding, ctx, _ = on
+    w4 = kept(binding, 0)[2]
+    x = FakeTensor(0, torch.bfloat16, 1, 1, 64)
+    with pytest.raises(TypeError, match="bfloat16 or float32"):
+        ctx.rk_matvec4(w4, x, out_dtype=dtype)
+    with pytest.raises(TypeError, match="bfloat16 or float32"):
+        ctx.rk_matvec4(w4, x, y=FakeTensor(0, dtype, 1, 1, 16))
