@@ -937,14 +937,18 @@ DecodeKernel decode_kernel(int row_tile, bool starve) {
 cudaError_t decode_attn_setup() {
   cudaError_t e = cudaSuccess;
   for (int row_tile = 16; row_tile <= 64 && e == cudaSuccess; row_tile *= 2)
-    for (int starve = 0; starve < 2 && e == cudaSuccess; ++starve)
-      e = cudaFuncSetAttribute(decode_kernel(row_tile, starve != 0), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+    e = cudaFuncSetAttribute(decode_kernel(row_tile, false), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   return e;
 }
 
 cudaError_t launch_decode_attn(const DecodeAttnParams& p, int row_tile, cudaStream_t stream) {
   const dim3 grid((unsigned)p.n_ctas);
-  decode_kernel(row_tile, p.starve != 0)<<<grid, kThreads, kSmemBytes, stream>>>(p);
+  const DecodeKernel kernel = decode_kernel(row_tile, p.starve != 0);
+  if (p.starve != 0) {  // set up here, so that creating a context does not load the test's instantiations
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<grid, kThreads, kSmemBytes, stream>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   rk_decode_join_kernel<<<(unsigned)(2 * p.n_ctas), kJoinThreads, 0, stream>>>(p, row_tile);
