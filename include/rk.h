@@ -415,7 +415,7 @@ typedef struct rk_decode_shape {
 /* The work list of a decode step, for all layers whose caches share the tables: made once per step, on the device.
  *   seq_off    device int32 [n_seqs + 1]: request b sees items seq_off[b] .. seq_off[b+1] - 1
  *   item_seg   device int32 [n_items]: the segment; one segment may be an item of several requests
- *   item_delta device int32 [n_items]: the request position of its row 0, >= 0
+ *   item_delta device int32 [n_items]: the request position of its row 0, >= 0; item_delta + seg_len <= 2^30
  *   q_pos      device int32 [n_seqs][q_len]: request positions of the query tokens
  *   plan       device, rk_decode_plan_bytes() bytes, 256-byte aligned
  * Row j of an item sits at position item_delta + j; query token t sees it iff item_delta + j <= q_pos[t] (so a

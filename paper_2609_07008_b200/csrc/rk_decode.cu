@@ -22,8 +22,10 @@
 // What bounds it: a tile takes some 5000 clk, of which the tensor core works 3000 (37 % of the kernel's cycles with start
 // and end), the ALUs 42 % and the issue slots 46 %.  The rest is the chain from tile to tile: value products -> free chunks
 // -> copied values and free key slots -> last scores -> softmax -> value products, each step at the speed that eight warps
-// get beside the others.  Measured: 64 requests with 64 heads over 440k visible rows 100 us, one request over 262144 rows
-// 62 us (112 MB of pages in: 1.8 TB/s), 16 requests with two tokens of 128 heads 213 us (710 TFLOP/s), 8 tiles 15 us.
+// get beside the others.  Measured: 64 requests with 64 heads over 440k visible rows 101 us, one request over 262144 rows
+// 62 us (112 MB of pages in: 1.8 TB/s), 16 requests with two tokens of 128 heads 218 us (694 TFLOP/s), 8 tiles 15 us.
+// Rows that do not fill their row tile are slower, see write_p: one request over 262144 rows 64 us with 24 heads, 54 with 32, 78
+// with 48, 61 with 64, 133 with 72, 104 with 128.
 // Tried and slower: the keys through shared memory only (more operand traffic, 1.1x), the key warps writing the values
 // (they then wait for the value products, 1.07x), four key warps of twice the registers (1.25x), the register split of
 // setmaxnreg (its small share spilled, 1.03x to 1.8x), unrolled copies and products (instruction cache, 1.03x to 1.15x).
@@ -236,7 +238,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
   // Bounded wait of a whole warp on one of the barriers, kept short: it is inlined two dozen times, and the kernel's loops have
   // to stay in the instruction cache.  The word at kOffAbort is the tag of the first wait that ran out (reported once, at the
   // end), after which everyone gives up.  The lanes look at the barrier, the word and the clock one by one, so the warp votes:
-  // it goes on together or gives up together, as what follows a wait are operations of all its lanes.
+  // it goes on together or gives up together, as what follows a wait are operations of all its lanes.  The votes cost 2 % (64
+  // requests 98.7 -> 100.8 us); fewer of them, with the roles going on to the end of a tile on unfinished data, won 1 % back.
   auto wait = [&](int b, uint32_t parity, int where) -> bool {
     const uint32_t at = smem_base + kOffBars + 8u * (uint32_t)b;
     uint32_t t0 = 0u;
@@ -671,7 +674,8 @@ __global__ void __launch_bounds__(kThreads, 1) rk_decode_attn_kernel(const __gri
         const float scale = s_nan[0] | s_nan[128] ? NAN : p.scale_log2;
         // First try with the maxima as they are (S of this tile is complete, so P^T of the previous one has been read).
         // A warp that finds an exponent above 8, or that gave up waiting, raises the flag; everyone sees it behind
-        // the barrier.  Not tried for the first tile of a group, which has no maxima yet.
+        // the barrier.  Not tried for the first tile of a group, which has no maxima yet.  A column without a query row never gets
+        // one: unmasked, its p are infinite (nobody reads them), and every full tile of a short row tile is gone over twice.
         float top = INFINITY;
         if (k > 0 && ok) top = full ? write_p(std::false_type(), false, scale) : write_p(std::true_type(), false, scale);
         if (top > 256.f) *s_flag = (int)t + 1;
