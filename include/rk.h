@@ -433,7 +433,8 @@ rk_status rk_decode_plan(rk_ctx* ctx, const rk_decode_shape* shape, const rk_cac
  * A row that sees no key gets O = 0, lse = -inf.  `plan` must come from rk_decode_plan with this shape, head count and
  * n_pages (else RK_ERR_LAYOUT from rk_poll_status, O and lse left as they were) and the pages it names must still hold the rows; the plan
  * and the pages are only read, so concurrent calls may share them.  The workspace may not be shared by calls that overlap. A cached
- * row that holds a NaN makes the query rows that see it NaN, and only those.
+ * row that holds a NaN makes the query rows that see it NaN, O and lse, and only those; an infinity in its rope part may do
+ * the same (the turned query is multiplied in two parts).
  * The result does not depend on timing: partial results are joined in a fixed order. */
 rk_status rk_cache4_attn_workspace_bytes(const rk_ctx* ctx, const rk_decode_shape* shape, size_t* out);
 rk_status rk_cache4_attn(rk_ctx* ctx, const rk_decode_shape* shape, const void* plan, size_t plan_bytes, const void* pages,
