@@ -18,7 +18,7 @@
  *    pos[r] = seg_delta[i] + (r - seg_off[i]).  Row t sees key k iff pos[k] <= pos[t].
  *  - `stream` is a cudaStream_t (0 = default stream).  Calls enqueue work and return; the
  *    only blocking calls are rk_create / rk_request_create / rk_poll_status / *_destroy and
- *    rk_layer_host.  The decode calls can be captured into a CUDA graph.
+ *    rk_layer_host.  The decode calls and those behind them can be captured into a CUDA graph.
  *  - The library allocates device memory only inside rk_create and rk_request_create (small
  *    tables) and frees it in the matching destroy.  kv, weights and z_off are never written.
  *  - No kernel traps: a device-side wait that expires records RK_ERR_TIMEOUT in a status
@@ -112,7 +112,7 @@ rk_status rk_destroy(rk_ctx* ctx);
 /* Message of the last failing call on this context (valid until the next call). */
 const char* rk_last_error(const rk_ctx* ctx);
 /* Synchronises `stream`, returns the device status word and clears it: RK_OK, RK_ERR_TIMEOUT, RK_ERR_ROWS (a bad
- * entry in the tables of a decode call, or a report of the bounds-checked build), RK_ERR_WORKSPACE or RK_ERR_LAYOUT
+ * entry in the tables of a decode call or of the experts' products, or a report of the bounds-checked build), RK_ERR_WORKSPACE or RK_ERR_LAYOUT
  * (a decode plan that is too small, or made for another call).  The first report wins. */
 rk_status rk_poll_status(rk_ctx* ctx, void* stream);
 /* Per-wait time limit of device-side waits, in milliseconds (default 2000). */
@@ -459,6 +459,96 @@ rk_status rk_quant4(rk_ctx* ctx, const void* w, const rk_w4* w4, void* stream);
  *   y  device bf16 (out_dtype 0) or fp32 (out_dtype 1): token t at y + t * y_stride, [n_mat][n_out] (>= n_mat * n_out) */
 rk_status rk_matvec4(rk_ctx* ctx, const rk_w4* w4, const void* x, int64_t x_stride, int64_t n_tok, void* y,
                      int64_t y_stride, int32_t out_dtype, void* stream);
+
+/* ---- Behind the attention: experts and tokens ---------------------------------------------------------------
+ *
+ * The rest of a generating step: which experts a token goes to (the weights are what rk_moe_fanout takes), the experts'
+ * products, the large products of prompts in 8-bit integers, and the token out of the logits.  These calls need the
+ * context's device to be the current one (RK_ERR_CUDA otherwise), read only the tensors that they are given, keep nothing
+ * and can be captured into a CUDA graph; calls on different streams may overlap as long as their outputs differ.
+ * n = 0 is allowed everywhere and does nothing. */
+
+#define RK_SCORE_SOFTMAX 0
+#define RK_SCORE_SIGMOID 1
+typedef struct rk_route {
+  int32_t n_experts;   /* E, at most 1024, a multiple of n_groups */
+  int32_t k;           /* experts per token, 1..16 and at most top_groups * E / n_groups */
+  int32_t n_groups;    /* groups of E / n_groups consecutive experts, 1..32 */
+  int32_t top_groups;  /* groups that a token's experts may come from, 1..n_groups */
+  int32_t group_top;   /* 1 or 2: a group is ranked by the sum of that many of its best experts */
+  int32_t score;       /* RK_SCORE_SOFTMAX (over all experts) or RK_SCORE_SIGMOID */
+  int32_t renorm;      /* non-zero: the weights of a token are divided by their sum */
+  float scale;         /* factor of the weights, finite */
+} rk_route;
+
+/* Routes n tokens.  s = the scores of the token's logits, c = s + bias.  The top_groups groups of the highest rank take
+ * part (equal: the lower group), and the k experts of the largest c in them are chosen (equal: the lower index), in
+ * descending order.  Their weights are their s (without bias), divided by their sum with `renorm` (0 where that is 0),
+ * times scale.  Scores are compared and weighted in 64 bits; the weights are rounded to fp32.
+ *   logits  device [n][E], bf16 (logits_dtype 0) or fp32 (1), rows `stride` elements apart (stride >= E)
+ *   bias    device fp32 [E], or NULL
+ *   ids     device int32 [n][k];  weights  device fp32 [n][k]
+ * An expert whose logit or bias is -inf is never chosen; a group is ranked by the experts that it has left, and slots without
+ * an expert get id -1 and weight 0.  A token with a NaN among its scores (a NaN logit or bias, +inf with softmax) gets
+ * ids -1 and weights NaN. */
+rk_status rk_moe_route(rk_ctx* ctx, const rk_route* route, const void* logits, int32_t logits_dtype, int64_t stride,
+                       const float* bias, int64_t n, int32_t* ids, float* weights, void* stream);
+
+/* Lists the pairs p = t * k + s of a routing by expert.
+ *   ids      device int32 [n][k]; a pair whose id is outside 0 .. n_experts - 1 is not listed
+ *   keep     device uint8 [n]: bit s set = slot s of the token stays (rk_moe_fanout's keep_out); NULL = all stay.  k <= 8 with it
+ *   row_off  device int32 [n_experts + 1];  rows  device int32 [n * k]
+ * rows[row_off[e]] .. rows[row_off[e + 1] - 1] are the pairs of expert e, ascending; the places from row_off[n_experts] on
+ * hold -1.  n * k < 2^30; n_experts <= 1024. With n = 0 row_off is all 0. */
+rk_status rk_moe_group(rk_ctx* ctx, const int32_t* ids, const uint8_t* keep, int64_t n, int32_t k, int32_t n_experts,
+                       int32_t* row_off, int32_t* rows, void* stream);
+
+/* Rows in 8 bits: n_mat * n_rows rows of k values, codes -127..127 times the row's scale. */
+typedef struct rk_q8 {
+  int32_t n_mat;      /* matrices (experts); 1 for tokens and dense weights; at most 1024 */
+  int64_t n_rows;     /* rows of a matrix: output channels, or tokens */
+  int32_t k;          /* 1 .. 131072 */
+  void* codes;        /* device int8 [n_mat][n_rows][k rounded up to a multiple of 16], zeros behind k; 16-byte aligned */
+  float* scales;      /* device fp32 [n_mat][n_rows] */
+} rk_q8;
+
+/* Quantises rows: scale = fp32(max|x| / 127), codes = x / scale rounded half to even (exactly) and limited to -127..127.  A
+ * row of zeros has scale 0; a row with an infinity or a NaN has the scale NaN and codes 0, and makes NaN what it is
+ * multiplied with.
+ *   x  device bf16: row i at x + i * x_stride (in elements, >= k, of any alignment to 2 bytes; multiples of 16 bytes are faster) */
+rk_status rk_quant8(rk_ctx* ctx, const void* x, int64_t x_stride, const rk_q8* q8, void* stream);
+
+/* y[t][o] = x.scales[t] w.scales[o] * sum_j x.codes[t][j] w.codes[o][j]; the sums are exact, the result is rounded to fp32
+ * and, for out_dtype 0, to bf16.  w.n_mat = x.n_mat = 1, w.k = x.k.
+ *   y  device bf16 (out_dtype 0) or fp32 (1): token t at y + t * y_stride, w.n_rows values (y_stride >= w.n_rows) */
+rk_status rk_matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, void* y, int64_t y_stride, int32_t out_dtype, void* stream);
+
+/* The experts' products over the lists of rk_moe_group: y[p] = W_e x[p / per] for every pair p of expert e, W_e = matrix e of w.
+ *   row_off  device int32 [w.n_mat + 1];  rows  device int32 [n_pairs]
+ *   per      the slots per token where x has a row per token (first products), 1 where it has a row per pair (second
+ *            products); x.n_rows * per >= n_pairs
+ *   y        device, n_pairs rows; rows that no list names are left as they were
+ * The tables are bounds-checked on the device: an expert whose bounds are not 0 <= row_off[e] <= row_off[e + 1] <= n_pairs,
+ * and a listed pair outside 0 .. n_pairs - 1, is skipped and rk_poll_status() returns RK_ERR_ROWS.  A pair listed twice gets,
+ * element by element, the product of one of its experts. */
+rk_status rk_matmul8_experts(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int32_t* row_off, const int32_t* rows,
+                             int64_t n_pairs, int32_t per, void* y, int64_t y_stride, int32_t out_dtype, void* stream);
+
+/* Samples a token from each row of logits.  p_i = exp((l_i - max l) / temperature).  In the order of falling logits (equal:
+ * the lower index first; -0.0 equals +0.0) a token stays if
+ *   its rank is below top_k,   the p in front of it sum to less than top_p * (the sum over the top_k),   p_i >= min_p;
+ * the first one always stays.  The token is the first that stayed, by index, whose cumulated p (over those that stayed, by
+ * index) exceeds u times their sum.
+ *   logits  device [n][vocab], bf16 (logits_dtype 0) or fp32 (1), rows `stride` elements apart; -inf is never drawn
+ *   u       device fp32 [n]: uniform random numbers in [0, 1); values outside count as the nearest inside, NaN as 0
+ *   temperature, top_k, top_p, min_p  device [n] (top_k int32, the others fp32), each NULL where all rows leave it off.
+ *     temperature <= 0 or NaN: the largest logit; top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN: off
+ *   tokens  device int32 [n];  probs  device fp32 [n], the token's p over the sum of those that stayed, or NULL
+ * A row with a NaN, and a row of nothing but -inf, gets token -1 and prob NaN.  +inf: only those are drawn, each alike.  p is rounded to multiples of
+ * 2^-42: a token below 2^-43 of the largest is not drawn.  1 <= vocab <= 2^20, n * 8 < 2^31. */
+rk_status rk_sample(rk_ctx* ctx, const void* logits, int32_t logits_dtype, int64_t stride, int64_t n, int32_t vocab, const float* u,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens,
+                    float* probs, void* stream);
 
 #ifdef __cplusplus
 }

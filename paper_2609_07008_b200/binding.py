@@ -67,6 +67,15 @@ class rk_w4(C.Structure):
                 ("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
+class rk_route(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_experts", "k", "n_groups", "top_groups", "group_top", "score", "renorm")] + [
+        ("scale", C.c_float)]
+
+
+class rk_q8(C.Structure):
+    _fields_ = [("n_mat", C.c_int32), ("n_rows", C.c_int64), ("k", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
 CACHE4_PAGE_ROWS = 64
 CACHE4_PAGE_BYTES = 26624
 
@@ -77,7 +86,8 @@ EXPORTS = ["rk_version", "rk_status_string", "rk_create", "rk_destroy", "rk_last
            "rk_layer_host", "rk_layer_stack_host", "rk_mla_off_workspace_bytes", "rk_mla_off_build",
            "rk_protected_rows_workspace_bytes", "rk_protected_rows", "rk_moe_fanout",
            "rk_cache4_append", "rk_cache4_read", "rk_decode_plan_bytes", "rk_decode_plan",
-           "rk_cache4_attn_workspace_bytes", "rk_cache4_attn", "rk_quant4", "rk_matvec4"]
+           "rk_cache4_attn_workspace_bytes", "rk_cache4_attn", "rk_quant4", "rk_matvec4",
+           "rk_moe_route", "rk_moe_group", "rk_quant8", "rk_matmul8", "rk_matmul8_experts", "rk_sample"]
 
 
 def _load() -> C.CDLL:
@@ -130,6 +140,13 @@ def _load() -> C.CDLL:
     lib.rk_cache4_attn.argtypes = [vp, pshape, vp, C.c_size_t, vp, i64, vp, vp, vp, vp, C.c_size_t, vp]
     lib.rk_quant4.argtypes = [vp, vp, pw4, vp]
     lib.rk_matvec4.argtypes = [vp, pw4, vp, i64, i64, vp, i64, i32, vp]
+    pq8 = C.POINTER(rk_q8)
+    lib.rk_moe_route.argtypes = [vp, C.POINTER(rk_route), vp, i32, i64, vp, i64, vp, vp, vp]
+    lib.rk_moe_group.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, vp]
+    lib.rk_quant8.argtypes = [vp, vp, i64, pq8, vp]
+    lib.rk_matmul8.argtypes = [vp, pq8, pq8, vp, i64, i32, vp]
+    lib.rk_matmul8_experts.argtypes = [vp, pq8, pq8, vp, vp, i64, i32, vp, i64, i32, vp]
+    lib.rk_sample.argtypes = [vp, vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is C.c_int:  # default restype: rk_status
@@ -247,6 +264,40 @@ class W4:
         self.index = codes.get_device()
         self.struct = rk_w4(n_mat, n_out, k, group, _ptr(codes), _ptr(scales))
         self.ref = C.byref(self.struct)
+
+
+class Q8:
+    """Rows in 8 bits (rk_quant8's result, or codes and scales that a program keeps): codes int8 [n_mat, n_rows, k rounded
+    up to a multiple of 16] (or [n_rows, ...] for one matrix), zeros behind k; scales float32 [n_mat, n_rows] or [n_rows]."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, k: int):
+        shape = codes.shape
+        if len(shape) not in (2, 3) or shape[-1] != (k + 15) // 16 * 16:
+            raise ValueError(f"codes of k = {k} must be [n_mat, n_rows, {(k + 15) // 16 * 16}], not {tuple(shape)}")
+        self.codes = _need(codes, "codes", torch.int8, None)
+        self.scales = _need(scales, "scales", torch.float32, shape[:-1])
+        self.n_mat, self.n_rows, self.k = (shape[0] if len(shape) == 3 else 1), shape[-2], int(k)
+        self.index = codes.get_device()
+        self.struct = rk_q8(self.n_mat, self.n_rows, self.k, _ptr(codes), _ptr(scales))
+        self.ref = C.byref(self.struct)
+
+
+def _rows(t: torch.Tensor, name: str, dtypes, width: int = -1) -> int:
+    """Checks a matrix whose rows may be strided; the row stride in elements."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    _need(t, name, t.dtype, (-1, width), contiguous=False)
+    if t.is_contiguous():
+        return t.shape[1]
+    if t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"the values of a row of {name} must be contiguous")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"the rows of {name} overlap")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+_FLOATS = (torch.bfloat16, torch.float32)
+_SCORES = {"softmax": 0, "sigmoid": 1}
 
 
 def make_layout_struct(seg_off, seg_delta, seg_has_artifact):
@@ -584,6 +635,138 @@ class Context:
         if s:
             self.check(s)
         return y
+
+    # -- behind the attention: experts and tokens -----------------------------------------------
+    def rk_moe_route(self, logits: torch.Tensor, k: int, *, bias: Optional[torch.Tensor] = None, score: str = "softmax",
+                     n_groups: int = 1, top_groups: int = 1, group_top: int = 1, renorm: bool = False, scale: float = 1.0,
+                     ids=None, weights=None):
+        """logits [n, E] bf16 or float32 (rows may be strided) -> (ids [n, k] int32, weights [n, k] float32): the k experts of
+        the largest score + bias among those of the top_groups best groups, in descending order."""
+        stride = _rows(logits, "logits", _FLOATS)
+        n, n_experts = logits.shape
+        if score not in _SCORES:
+            raise ValueError(f"score must be 'softmax' or 'sigmoid', not {score!r}")
+        if bias is not None:
+            _need(bias, "bias", torch.float32, (n_experts,))
+        if ids is None:
+            ids = _empty((n, k), torch.int32, logits.device)
+        else:
+            _need(ids, "ids", torch.int32, (n, k))
+        if weights is None:
+            weights = _empty((n, k), torch.float32, logits.device)
+        else:
+            _need(weights, "weights", torch.float32, (n, k))
+        route = rk_route(n_experts, k, n_groups, top_groups, group_top, _SCORES[score], 1 if renorm else 0, scale)
+        s = lib.rk_moe_route(self.handle, C.byref(route), logits.data_ptr(), 0 if logits.dtype is torch.bfloat16 else 1, stride,
+                             None if bias is None else bias.data_ptr(), n, ids.data_ptr(), weights.data_ptr(), _quick_stream())
+        if s:
+            self.check(s)
+        return ids, weights
+
+    def rk_moe_group(self, ids: torch.Tensor, n_experts: int, keep: Optional[torch.Tensor] = None, row_off=None, rows=None):
+        """ids [n, k] int32 (and keep [n] uint8, rk_moe_fanout's masks) -> (row_off [n_experts + 1], rows [n * k]) int32: the
+        pairs t * k + s by expert; the places behind the last listed pair hold -1."""
+        _need(ids, "ids", torch.int32, (-1, -1))
+        n, k = ids.shape
+        if keep is not None:
+            _need(keep, "keep", torch.uint8, (n,))
+        if row_off is None:
+            row_off = _empty(n_experts + 1, torch.int32, ids.device)
+        else:
+            _need(row_off, "row_off", torch.int32, (n_experts + 1,))
+        if rows is None:
+            rows = _empty(n * k, torch.int32, ids.device)
+        else:
+            _need(rows, "rows", torch.int32, (n * k,))
+        s = lib.rk_moe_group(self.handle, ids.data_ptr(), None if keep is None else keep.data_ptr(), n, k, n_experts,
+                             row_off.data_ptr(), rows.data_ptr(), _quick_stream())
+        if s:
+            self.check(s)
+        return row_off, rows
+
+    def rk_quant8(self, x: torch.Tensor, q8: Optional[Q8] = None) -> Q8:
+        """Rows of x in 8 bits with a scale each: x [n, k] bf16 (rows may be strided), or [n_mat, n, k] contiguous (weights)."""
+        if x.dim() == 3:
+            _need(x, "x", torch.bfloat16, (-1, -1, -1))
+            stride = x.shape[2]
+        else:
+            stride = _rows(x, "x", (torch.bfloat16,))
+        k = x.shape[-1]
+        if q8 is None:
+            shape = tuple(x.shape[:-1])
+            q8 = Q8(_empty(shape + ((k + 15) // 16 * 16,), torch.int8, x.device), _empty(shape, torch.float32, x.device), k)
+        else:
+            _here(q8, "q8")
+            if (q8.n_mat, q8.n_rows, q8.k) != (x.shape[0] if x.dim() == 3 else 1, x.shape[-2], k):
+                raise ValueError("q8 has another shape")
+        s = lib.rk_quant8(self.handle, x.data_ptr(), stride, q8.ref, _quick_stream())
+        if s:
+            self.check(s)
+        return q8
+
+    def _out8(self, w: Q8, x: Q8, n: int, y, out_dtype):
+        """Output of an 8-bit product: tensor, row stride, type number."""
+        _here(w, "w")
+        _here(x, "x")
+        if y is not None:
+            out_dtype = y.dtype
+        if out_dtype is not torch.bfloat16 and out_dtype is not torch.float32:
+            raise TypeError(f"the products' outputs are bfloat16 or float32, not {out_dtype}")
+        stride = w.n_rows
+        if y is None:
+            y = _empty((n, stride), out_dtype, x.codes.device)
+        else:
+            stride = _rows(y, "y", _FLOATS, w.n_rows)
+            if y.shape[0] != n:
+                raise ValueError(f"y must have {n} rows, not {y.shape[0]}")
+        return y, stride, 0 if out_dtype is torch.bfloat16 else 1
+
+    def rk_matmul8(self, w: Q8, x: Q8, y: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
+        """y [n, n_out] = x w^T of 8-bit rows, bf16 or float32 (rows of y may be strided)."""
+        y, stride, dt = self._out8(w, x, x.n_rows, y, out_dtype)
+        s = lib.rk_matmul8(self.handle, w.ref, x.ref, y.data_ptr(), stride, dt, _quick_stream())
+        if s:
+            self.check(s)
+        return y
+
+    def rk_matmul8_experts(self, w: Q8, x: Q8, row_off: torch.Tensor, rows: torch.Tensor, per: int,
+                           y: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16) -> torch.Tensor:
+        """y[p] = w[e] x[p // per] for the pairs p = rows[row_off[e]:row_off[e + 1]] of every expert e (rk_moe_group's lists);
+        rows of y that no list names are left as they were."""
+        _need(row_off, "row_off", torch.int32, (w.n_mat + 1,))
+        _need(rows, "rows", torch.int32, (-1,))
+        n = rows.shape[0]
+        y, stride, dt = self._out8(w, x, n, y, out_dtype)
+        s = lib.rk_matmul8_experts(self.handle, w.ref, x.ref, row_off.data_ptr(), rows.data_ptr(), n, per, y.data_ptr(), stride, dt,
+                                   _quick_stream())
+        if s:
+            self.check(s)
+        return y
+
+    def rk_sample(self, logits: torch.Tensor, u: torch.Tensor, *, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None,
+                  probs=None):
+        """One token per row of logits [n, vocab] (bf16 or float32, rows may be strided) from the uniform random numbers u [n];
+        temperature, top_p, min_p float32 [n], top_k int32 [n], each None for off.  Returns (tokens [n] int32, probs [n])."""
+        stride = _rows(logits, "logits", _FLOATS)
+        n, vocab = logits.shape
+        _need(u, "u", torch.float32, (n,))
+        ptrs = []
+        for t, name, dtype in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                               (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+            ptrs.append(None if t is None else _need(t, name, dtype, (n,)).data_ptr())
+        if tokens is None:
+            tokens = _empty((n,), torch.int32, logits.device)
+        else:
+            _need(tokens, "tokens", torch.int32, (n,))
+        if probs is None:
+            probs = _empty((n,), torch.float32, logits.device)
+        else:
+            _need(probs, "probs", torch.float32, (n,))
+        s = lib.rk_sample(self.handle, logits.data_ptr(), 0 if logits.dtype is torch.bfloat16 else 1, stride, n, vocab, u.data_ptr(),
+                          *ptrs, tokens.data_ptr(), probs.data_ptr(), _quick_stream())
+        if s:
+            self.check(s)
+        return tokens, probs
 
     def alloc_layer_buffers(self, req, device) -> dict:
         G, L, T, A = self.n_groups, self.n_local, req.T, req.A

@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "librk.so")
 CHECK_LIB_PATH = os.path.join(LIB_DIR, "librk_check.so")   # the same sources with -DRK_CHECK (device index checks)
-SOURCES = ["rk_host.cu", "rk_attn.cu", "rk_gemm.cu", "rk_stream.cu", "rk_policy.cu", "rk_cache4.cu", "rk_decode.cu", "rk_matvec4.cu"]
+SOURCES = ["rk_host.cu", "rk_attn.cu", "rk_gemm.cu", "rk_stream.cu", "rk_policy.cu", "rk_cache4.cu", "rk_decode.cu", "rk_matvec4.cu",
+           "rk_experts.cu", "rk_matmul8.cu", "rk_sample.cu"]
 HEADERS = ["rk_ptx.cuh", "rk_internal.h", os.path.join("..", "..", "include", "rk.h")]
 
 

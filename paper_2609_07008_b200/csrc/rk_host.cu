@@ -275,6 +275,8 @@ rk_status rk_create_ex(const rk_profile* prof, uint32_t flags, rk_ctx** out) {
   if (e == cudaSuccess) e = proj_fused_setup();
   if (e == cudaSuccess) e = decode_attn_setup();
   if (e == cudaSuccess) e = matvec4_setup(ctx->matvec_slots, ctx->sm_count);
+  if (e == cudaSuccess) e = experts_setup();
+  if (e == cudaSuccess) e = matmul8_setup();
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&ctx->d_status), sizeof(DeviceStatus));
   if (e == cudaSuccess) e = cudaMemset(ctx->d_status, 0, sizeof(DeviceStatus));
   if (e != cudaSuccess) {
@@ -392,6 +394,8 @@ rk_status rk_poll_status(rk_ctx* ctx, void* stream) {
         return fail(ctx, RK_ERR_ROWS, "decode plan: entry %d is invalid", h.aux);
       case RK_CHK_PLAN_MATCH:
         return fail(ctx, RK_ERR_LAYOUT, "the plan was not made by rk_decode_plan for this shape, head count and number of pages");
+      case RK_CHK_EXPERT_OFF: return fail(ctx, RK_ERR_ROWS, "row_off: the bounds of expert %d are not inside the list", h.aux);
+      case RK_CHK_EXPERT_ROW: return fail(ctx, RK_ERR_ROWS, "rows: pair %d does not exist", h.aux);
     }
     return fail(ctx, RK_ERR_TIMEOUT, "device wait expired: tag %d, block %d, aux %d", h.where, h.block, h.aux);
   }
@@ -1434,6 +1438,203 @@ rk_status rk_matvec4(rk_ctx* ctx, const rk_w4* w4, const void* x, int64_t x_stri
   p.starve = ctx->starve_loads;
   cudaError_t e = launch_matvec4(p, ctx->matvec_slots, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "matrix-vector launch");
+}
+
+// ------------------------------------------------------------------------------------------
+// Behind the attention: routing to experts, products in 8-bit integers, sampling
+
+static rk_status device_check(rk_ctx* ctx) {
+  int device = -1;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "cudaGetDevice");
+  if (device != ctx->device) return fail(ctx, RK_ERR_CUDA, "the context's device is not current");
+  return RK_OK;
+}
+static bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+rk_status rk_moe_route(rk_ctx* ctx, const rk_route* rt, const void* logits, int32_t logits_dtype, int64_t stride, const float* bias,
+                       int64_t n, int32_t* ids, float* weights, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  if (!rt) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (rt->n_groups < 1 || rt->n_groups > kMaxGroups || rt->n_experts < 1 || rt->n_experts > kMaxExperts || rt->n_experts % rt->n_groups != 0)
+    return fail(ctx, RK_ERR_UNSUPPORTED, "%d experts in %d groups: at most %d experts, a multiple of at most %d groups", rt->n_experts,
+                rt->n_groups, kMaxExperts, kMaxGroups);
+  const int size = rt->n_experts / rt->n_groups;
+  if (rt->top_groups < 1 || rt->top_groups > rt->n_groups) return fail(ctx, RK_ERR_PROFILE, "top_groups must be 1 .. n_groups");
+  if (rt->k < 1 || rt->k > kMaxSlots || rt->k > rt->top_groups * size)
+    return fail(ctx, RK_ERR_PROFILE, "k must be 1 .. %d and at most the experts of top_groups groups", kMaxSlots);
+  if (rt->group_top != 1 && rt->group_top != 2) return fail(ctx, RK_ERR_UNSUPPORTED, "group_top must be 1 or 2");
+  if (rt->score != RK_SCORE_SOFTMAX && rt->score != RK_SCORE_SIGMOID) return fail(ctx, RK_ERR_UNSUPPORTED, "unknown score");
+  if (!std::isfinite(rt->scale)) return fail(ctx, RK_ERR_PROFILE, "scale is not finite");
+  if (logits_dtype != 0 && logits_dtype != 1) return fail(ctx, RK_ERR_UNSUPPORTED, "logits_dtype must be 0 (bf16) or 1 (fp32)");
+  if (n < 0 || n >= ((int64_t)1 << 31) / kMaxSlots) return fail(ctx, RK_ERR_ROWS, "n out of range");
+  if (n > 0 && (!logits || !ids || !weights)) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (n > 1 && stride < rt->n_experts) return fail(ctx, RK_ERR_LAYOUT, "rows of logits overlap");
+  if (!aligned_to(logits, logits_dtype ? 4 : 2) || !aligned_to(bias, 4) || !aligned_to(ids, 4) || !aligned_to(weights, 4))
+    return fail(ctx, RK_ERR_ALIGN, "tensors must be aligned to their types");
+  rk_status s = device_check(ctx);
+  if (s != RK_OK || n == 0) return s;
+  RouteParams p = {};
+  p.logits = logits;
+  p.bias = bias;
+  p.ids = ids;
+  p.weights = weights;
+  p.n = n;
+  p.stride = stride;
+  p.bf16 = logits_dtype == 0;
+  p.softmax = rt->score == RK_SCORE_SOFTMAX;
+  p.renorm = rt->renorm != 0;
+  p.k = rt->k;
+  p.n_groups = rt->n_groups;
+  p.group_size = size;
+  p.top_groups = rt->top_groups;
+  p.group_top = rt->group_top;
+  p.scale = rt->scale;
+  cudaError_t e = launch_moe_route(p, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "routing launch");
+}
+
+rk_status rk_moe_group(rk_ctx* ctx, const int32_t* ids, const uint8_t* keep, int64_t n, int32_t k, int32_t n_experts, int32_t* row_off,
+                       int32_t* rows, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  if (n_experts < 1 || n_experts > kMaxExperts) return fail(ctx, RK_ERR_UNSUPPORTED, "n_experts must be 1 .. %d", kMaxExperts);
+  if (k < 1 || k > kMaxSlots) return fail(ctx, RK_ERR_UNSUPPORTED, "k must be 1 .. %d", kMaxSlots);
+  if (keep && k > 8) return fail(ctx, RK_ERR_UNSUPPORTED, "a keep mask has 8 bits: k must be at most 8 with it");
+  if (n < 0 || n * k >= ((int64_t)1 << 30)) return fail(ctx, RK_ERR_ROWS, "n out of range");
+  if (!row_off || (n > 0 && (!ids || !rows))) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (!aligned_to(ids, 4) || !aligned_to(row_off, 4) || !aligned_to(rows, 4)) return fail(ctx, RK_ERR_ALIGN, "tensors must be aligned to their types");
+  rk_status s = device_check(ctx);
+  if (s != RK_OK) return s;
+  GroupParams p = {ids, keep, row_off, rows, n, k, n_experts};
+  cudaError_t e = launch_moe_group(p, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "expert list launch");
+}
+
+static rk_status q8_check(rk_ctx* ctx, const rk_q8* q) {
+  if (!q) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (q->n_mat < 1 || q->n_mat > kMaxExperts || q->k < 1 || q->k > kMaxK8)
+    return fail(ctx, RK_ERR_UNSUPPORTED, "n_mat must be 1 .. %d and k 1 .. %d", kMaxExperts, kMaxK8);
+  if (q->n_rows < 0 || (int64_t)q->n_rows >= ((int64_t)1 << 31) / q->n_mat - 1024) return fail(ctx, RK_ERR_ROWS, "too many rows");
+  if (q->n_rows > 0 && (!q->codes || !q->scales)) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (!aligned16(q->codes) || !aligned_to(q->scales, 4)) return fail(ctx, RK_ERR_ALIGN, "codes must be 16-byte aligned, scales to their type");
+  return RK_OK;
+}
+
+rk_status rk_quant8(rk_ctx* ctx, const void* x, int64_t x_stride, const rk_q8* q8, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  rk_status s = q8_check(ctx, q8);
+  if (s != RK_OK) return s;
+  const int64_t rows = q8->n_rows * q8->n_mat;
+  if (rows > 0 && !x) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (rows > 1 && x_stride < q8->k) return fail(ctx, RK_ERR_LAYOUT, "x_stride is smaller than a row");
+  if (!aligned_to(x, 2)) return fail(ctx, RK_ERR_ALIGN, "x must be aligned to its type");
+  s = device_check(ctx);
+  if (s != RK_OK || rows == 0) return s;
+  cudaError_t e = launch_quant8(x, x_stride, rows, q8->k, q8->codes, q8->scales, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "quantisation launch");
+}
+
+// 2-D tensor map of bytes with 128-byte swizzle, 128 columns x box_rows
+static rk_status make_tmap8(const rk_ctx* ctx, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+  cuuint64_t dims[2] = {cols, rows};
+  cuuint64_t strides[1] = {cols};
+  cuuint32_t box[2] = {128, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = ctx->encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS)
+    return fail(ctx, RK_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d) rows=%llu cols=%llu", (int)r, (unsigned long long)rows,
+                (unsigned long long)cols);
+  return RK_OK;
+}
+
+static rk_status matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int32_t* row_off, const int32_t* rows, int64_t n_tok,
+                         int32_t per, void* y, int64_t y_stride, int32_t out_dtype, void* stream) {
+  rk_status s = q8_check(ctx, w);
+  if (s == RK_OK) s = q8_check(ctx, x);
+  if (s != RK_OK) return s;
+  if (x->n_mat != 1) return fail(ctx, RK_ERR_LAYOUT, "the token rows are one matrix");
+  if (w->k != x->k) return fail(ctx, RK_ERR_LAYOUT, "weights have k = %d, tokens %d", w->k, x->k);
+  if (w->n_rows < 1) return fail(ctx, RK_ERR_LAYOUT, "weights without rows");
+  if (out_dtype != 0 && out_dtype != 1) return fail(ctx, RK_ERR_UNSUPPORTED, "out_dtype must be 0 (bf16) or 1 (fp32)");
+  if (n_tok > 0 && !y) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (n_tok > 1 && y_stride < w->n_rows) return fail(ctx, RK_ERR_LAYOUT, "rows of y overlap");
+  if (!aligned_to(y, out_dtype ? 4 : 2)) return fail(ctx, RK_ERR_ALIGN, "y must be aligned to its type");
+  s = device_check(ctx);
+  if (s != RK_OK || n_tok == 0) return s;
+  Matmul8Params p;
+  memset(&p, 0, sizeof(p));
+  p.k_pad = (w->k + 15) / 16 * 16;
+  s = make_tmap8(ctx, &p.tm_w, w->codes, (uint64_t)w->n_mat * w->n_rows, p.k_pad, 128);
+  if (s == RK_OK) s = make_tmap8(ctx, &p.tm_x, x->codes, (uint64_t)x->n_rows, p.k_pad, rows ? 1 : 128);
+  if (s != RK_OK) return s;
+  p.sw = w->scales;
+  p.sx = x->scales;
+  p.row_off = row_off;
+  p.rows = rows;
+  p.y = y;
+  p.y_stride = y_stride;
+  p.status = ctx->d_status;
+  p.wait_ns = ctx->wait_ns;
+  p.n_tok = (int32_t)n_tok;
+  p.n_out = (int32_t)w->n_rows;
+  p.n_mat = w->n_mat;
+  p.per = per;
+  p.out_f32 = out_dtype;
+  cudaError_t e = launch_matmul8(p, ctx->sm_count, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "8-bit product launch");
+}
+
+rk_status rk_matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, void* y, int64_t y_stride, int32_t out_dtype, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  if (!w || !x) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (w->n_mat != 1) return fail(ctx, RK_ERR_LAYOUT, "the dense product takes one matrix");
+  return matmul8(ctx, w, x, nullptr, nullptr, x->n_rows, 1, y, y_stride, out_dtype, stream);
+}
+
+rk_status rk_matmul8_experts(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int32_t* row_off, const int32_t* rows, int64_t n_pairs,
+                             int32_t per, void* y, int64_t y_stride, int32_t out_dtype, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  if (!w || !x) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (n_pairs < 0 || n_pairs >= ((int64_t)1 << 30)) return fail(ctx, RK_ERR_ROWS, "n_pairs out of range");
+  if (n_pairs > 0 && (!row_off || !rows)) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (per < 1 || per > kMaxSlots) return fail(ctx, RK_ERR_UNSUPPORTED, "per must be 1 .. %d", kMaxSlots);
+  if (x->n_rows < (n_pairs + per - 1) / per)
+    return fail(ctx, RK_ERR_LAYOUT, "%lld token rows for %lld pairs, %d per token", (long long)x->n_rows, (long long)n_pairs, per);
+  if (!aligned_to(row_off, 4) || !aligned_to(rows, 4)) return fail(ctx, RK_ERR_ALIGN, "tables must be aligned to their types");
+  return matmul8(ctx, w, x, row_off, rows, n_pairs, per, y, y_stride, out_dtype, stream);
+}
+
+rk_status rk_sample(rk_ctx* ctx, const void* logits, int32_t logits_dtype, int64_t stride, int64_t n, int32_t vocab, const float* u,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens,
+                    float* probs, void* stream) {
+  if (!ctx) return RK_ERR_NULL;
+  if (vocab < 1 || vocab > kMaxVocab) return fail(ctx, RK_ERR_UNSUPPORTED, "vocab must be 1 .. %d", kMaxVocab);
+  if (logits_dtype != 0 && logits_dtype != 1) return fail(ctx, RK_ERR_UNSUPPORTED, "logits_dtype must be 0 (bf16) or 1 (fp32)");
+  if (n < 0 || n >= (((int64_t)1 << 31) - 1) / 8) return fail(ctx, RK_ERR_ROWS, "n out of range");
+  if (n > 0 && (!logits || !u || !tokens)) return fail(ctx, RK_ERR_NULL, "null argument");
+  if (n > 1 && stride < vocab) return fail(ctx, RK_ERR_LAYOUT, "rows of logits overlap");
+  if (!aligned_to(logits, logits_dtype ? 4 : 2) || !aligned_to(u, 4) || !aligned_to(temperature, 4) || !aligned_to(top_k, 4) ||
+      !aligned_to(top_p, 4) || !aligned_to(min_p, 4) || !aligned_to(tokens, 4) || !aligned_to(probs, 4))
+    return fail(ctx, RK_ERR_ALIGN, "tensors must be aligned to their types");
+  rk_status s = device_check(ctx);
+  if (s != RK_OK || n == 0) return s;
+  SampleParams p = {};
+  p.logits = logits;
+  p.u = u;
+  p.temperature = temperature;
+  p.top_k = top_k;
+  p.top_p = top_p;
+  p.min_p = min_p;
+  p.tokens = tokens;
+  p.probs = probs;
+  p.n = n;
+  p.stride = stride;
+  p.vocab = vocab;
+  p.bf16 = logits_dtype == 0;
+  cudaError_t e = launch_sample(p, ctx->sm_count, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "sampling launch");
 }
 
 }  // extern "C"

@@ -265,6 +265,66 @@ cudaError_t launch_quant4(const void* w, int32_t n_mat, int32_t n_out, int32_t k
 cudaError_t matvec4_setup(int32_t* slots, int sm_count);
 cudaError_t launch_matvec4(Matvec4Params p, const int32_t* slots, cudaStream_t stream);
 
+// ---- routing to experts, products in 8-bit integers, sampling --------------------------------------
+constexpr int kMaxExperts = 1024;
+constexpr int kMaxSlots = 16;      // experts per token
+constexpr int kMaxGroups = 32;
+constexpr int kMaxVocab = 1 << 20;
+constexpr int kMaxK8 = 131072;     // 127^2 k stays below 2^31
+
+struct RouteParams {
+  const void* logits;  // [n][n_groups * group_size], rows `stride` elements apart
+  const float* bias;   // [n_groups * group_size] or null
+  int32_t* ids;        // [n][k]
+  float* weights;      // [n][k]
+  int64_t n, stride;
+  int32_t bf16, softmax, renorm, k, n_groups, group_size, top_groups, group_top;
+  float scale;
+  int32_t lanes_log2;  // set by the launcher: lanes of a warp per group
+};
+cudaError_t launch_moe_route(RouteParams p, cudaStream_t stream);
+
+struct GroupParams {
+  const int32_t* ids;   // [n][k]
+  const uint8_t* keep;  // [n] bit s = slot s stays, or null
+  int32_t* row_off;     // [n_experts + 1]
+  int32_t* rows;        // [n * k]
+  int64_t n;
+  int32_t k, n_experts;
+};
+cudaError_t experts_setup();
+cudaError_t launch_moe_group(const GroupParams& p, cudaStream_t stream);
+
+struct Matmul8Params {
+  CUtensorMap tm_w;      // [n_mat * n_out][k_pad] bytes, box 128 x 128
+  CUtensorMap tm_x;      // [token rows][k_pad] bytes, box 128 x 128, by expert 128 x 1
+  const float* sw;       // [n_mat * n_out]
+  const float* sx;       // [token rows]
+  const int32_t* row_off;  // by expert: [n_mat + 1] into rows
+  const int32_t* rows;     // by expert: [n_tok] pairs; null: dense
+  void* y;
+  int64_t y_stride;
+  DeviceStatus* status;
+  unsigned long long wait_ns;
+  int32_t n_tok;  // token rows; by expert: pairs (places of the list, rows of y)
+  int32_t n_out, k_pad, n_mat, per, out_f32;
+};
+cudaError_t matmul8_setup();
+cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32_t k, void* codes, float* scales, cudaStream_t stream);
+cudaError_t launch_matmul8(const Matmul8Params& p, int sm_count, cudaStream_t stream);
+
+struct SampleParams {
+  const void* logits;  // [n][vocab], rows `stride` elements apart
+  const float *u, *temperature, *top_p, *min_p;  // [n]; all but u may be null
+  const int32_t* top_k;
+  int32_t* tokens;  // [n]
+  float* probs;     // [n] or null
+  int64_t n, stride;
+  int32_t vocab, bf16;
+  int32_t blocks;  // set by the launcher: thread blocks per row (a cluster)
+};
+cudaError_t launch_sample(SampleParams p, int sm_count, cudaStream_t stream);
+
 #ifdef __CUDACC__
 // scale byte -> the bf16 value in both halves: 2^((b >> 3) - 20) (1 + (b & 7) / 8); 255 is NaN
 __device__ __forceinline__ uint32_t cache4_scale(uint32_t b) {

@@ -1,0 +1,467 @@
+// Products in 8-bit integers: y[t][o] = sx[t] sw[o] sum_j X[t][j] W[o][j], codes X, W in -127 .. 127, scales in fp32.
+//
+// Rows (of weights and of tokens alike) are quantised by themselves: scale = fp32(max|x| / 127), code = x / scale rounded
+// half to even.  The sums are exact (int32; k <= 131072 keeps |sum| < 2^31) and meet the scales once, in fp32, in the
+// epilogue; rounding to bf16, where asked for, is the last step.
+//
+// rk_matmul8_pair_kernel: a pair of CTAs (cta_group::2) owns 256 output channels x up to 256 token rows.  The channels
+// are the rows of the accumulator (M = 256) and the tokens its columns, because the number of tokens is what varies:
+// N follows the rows that a tile really has, in steps of 32, down to the one or two rows an expert gets in a decode step.
+// Each CTA streams its 128 channels of W and its half of the token rows in 128-byte steps of k (16 + up to 16 KB per
+// stage); W is read once per 256 tokens, and with N = 256 an SM draws 64 bytes per clock from L2 at the full rate of the
+// tensor cores, below the 76 that it can.  Persistent: the accumulator is double buffered in tensor memory, so that the
+// scales and stores of one tile run under the products of the next.
+//
+// By expert, the token rows of a tile are a gather (the tokens that chose the expert), four rows per TMA instruction, so
+// that no sorted copy of the activations is made; the outputs go straight to the pairs' rows of y.
+#include <cuda_bf16.h>
+
+#include "rk_internal.h"
+
+namespace rk {
+namespace {
+
+// ------------------------------------------------------------------------------------------------------------
+// quantisation of rows
+// ------------------------------------------------------------------------------------------------------------
+constexpr int kQuantHeld = 4;  // 8-value chunks that a thread keeps in registers between the maximum and the codes
+
+// round(x / scale), half to even, exactly: the quick product decides unless it lands within 1e-4 of the middle between two
+// codes (its error is below 127 * 2^-23); there the sign of |x| - scale (m + 1/2), one double-precision fused product whose
+// result is rounded once, tells the side.
+__device__ __forceinline__ int quant8_code(float x, float scale, float inv) {
+  const float t = fabsf(x * inv);
+  float m = floorf(t);
+  const float f = t - m;
+  if (f > 0.4999f) {
+    if (f < 0.5001f) {
+      const double r = fma(-(double)scale, (double)(m + 0.5f), (double)fabsf(x));
+      if (r > 0.0 || (r == 0.0 && ((int)m & 1))) m += 1.f;
+    } else {
+      m += 1.f;
+    }
+  }
+  const int c = min((int)m, 127);
+  return x < 0.f ? -c : c;
+}
+// the same where 1 / scale has left the range of fp32 (rows whose largest value is below 1e-28)
+__device__ __noinline__ int quant8_code_tiny(float x, float scale) {
+  const double t = fabs((double)x) / (double)scale;
+  const int c = (int)fmin(rint(t), 127.0);
+  return x < 0.f ? -c : c;
+}
+
+template <bool kVec>
+__device__ __forceinline__ uint4 load_chunk(const __nv_bfloat16* row, int at, int k) {
+  if constexpr (kVec) {
+    if (at + 8 <= k) return __ldcs(reinterpret_cast<const uint4*>(row + at));
+  }
+  uint32_t v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = at + 2 * i < k ? (uint32_t)__bfloat16_as_ushort(row[at + 2 * i]) : 0u;
+    const uint32_t hi = at + 2 * i + 1 < k ? (uint32_t)__bfloat16_as_ushort(row[at + 2 * i + 1]) : 0u;
+    v[i] = lo | (hi << 16);
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// the largest magnitude of eight bf16 values, as its 15 bits (an order of magnitudes: infinities and NaN come last)
+__device__ __forceinline__ uint32_t chunk_top(const uint4& c) {
+  uint32_t t = __vmaxu2(__vmaxu2(c.x & 0x7fff7fffu, c.y & 0x7fff7fffu), __vmaxu2(c.z & 0x7fff7fffu, c.w & 0x7fff7fffu));
+  return max(t & 0xffffu, t >> 16);
+}
+__device__ __forceinline__ uint2 chunk_codes(const uint4& c, float scale, float inv, bool tiny) {
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+  uint32_t out[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    const int q = tiny ? quant8_code_tiny(x, scale) : quant8_code(x, scale, inv);
+    out[i >> 2] |= ((uint32_t)q & 0xffu) << (8 * (i & 3));
+  }
+  return make_uint2(out[0], out[1]);
+}
+
+// One row per thread block.  A row of up to 32 values per thread is read once; longer ones a second time out of L2.  HBM
+// bound: two bytes in, one out per value.
+template <bool kVec>
+__global__ void __launch_bounds__(512) quant8_kernel(const __nv_bfloat16* __restrict__ x, int64_t x_stride, int k, int k_pad,
+                                                     uint8_t* __restrict__ codes, float* __restrict__ scales) {
+  const int64_t row = blockIdx.x;
+  const __nv_bfloat16* src = x + row * x_stride;
+  const int n_chunks = k_pad >> 3, nt = blockDim.x;  // k_pad is a multiple of 16
+  uint4 held[kQuantHeld];
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < kQuantHeld; ++i) {
+    const int c = threadIdx.x + i * nt;
+    held[i] = c < n_chunks ? load_chunk<kVec>(src, 8 * c, k) : make_uint4(0u, 0u, 0u, 0u);
+  }
+#pragma unroll
+  for (int i = 0; i < kQuantHeld; ++i) top = max(top, chunk_top(held[i]));
+  for (int c = threadIdx.x + kQuantHeld * nt; c < n_chunks; c += nt) top = max(top, chunk_top(load_chunk<kVec>(src, 8 * c, k)));
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (nt > 32) {
+    __shared__ uint32_t tops[16];
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+    __syncthreads();
+    for (int w = 0; w < nt >> 5; ++w) top = max(top, tops[w]);
+  }
+  const bool finite = top < 0x7f80u;
+  const float scale = finite ? __fdiv_rn(__uint_as_float(top << 16), 127.f) : __uint_as_float(0x7fc00000u);
+  const bool blank = !finite || scale == 0.f, tiny = scale < 1e-30f;
+  const float inv = blank ? 0.f : __fdiv_rn(1.f, scale);
+  uint2* dst = reinterpret_cast<uint2*>(codes + row * k_pad);
+#pragma unroll
+  for (int i = 0; i < kQuantHeld; ++i) {
+    const int c = threadIdx.x + i * nt;
+    if (c < n_chunks) dst[c] = blank ? make_uint2(0u, 0u) : chunk_codes(held[i], scale, inv, tiny);
+  }
+  for (int c = threadIdx.x + kQuantHeld * nt; c < n_chunks; c += nt)
+    dst[c] = blank ? make_uint2(0u, 0u) : chunk_codes(load_chunk<kVec>(src, 8 * c, k), scale, inv, tiny);
+  if (threadIdx.x == 0) scales[row] = scale;
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// products
+// ------------------------------------------------------------------------------------------------------------
+constexpr int kThreads8 = 384;  // warp 0 loads, warp 1 issues, warps 4-11 scale and store
+constexpr int kStages8 = 6;
+constexpr int kStep = 128;      // bytes (= values) of k per stage
+constexpr int kTileM = 256, kTileN = 256;
+constexpr int kBandTok = 8;     // token tiles of a band: W streams past them together
+
+struct Smem8 {
+  static constexpr uint32_t kABytes = 128 * kStep, kBBytes = 128 * kStep, kStageBytes = kABytes + kBBytes;
+  static constexpr uint32_t kOffBars = kStages8 * kStageBytes;  // full[stages], empty[stages], acc_full[2], acc_empty[2]
+  static constexpr uint32_t kOffTmemPtr = kOffBars + (2 * kStages8 + 4) * 8;
+  static constexpr uint32_t kOffAbort = kOffTmemPtr + 8;
+  static constexpr uint32_t kOffScan = kOffAbort + 8;               // 32 words of the block's scan
+  static constexpr uint32_t kOffTok = kOffScan + 128;               // [2][256] token scale, [2][256] output row
+  static constexpr uint32_t kOffFirst = kOffTok + 2 * 256 * 8;      // by expert: first tile of each, [n_mat + 1]; then row_off
+  static constexpr uint32_t kBytes = kOffFirst + 2 * (kMaxExperts + 1) * 4 + 1024 + 16;
+};
+enum { WM_EMPTY = 61, WM_FULL, WM_ACC_EMPTY, WM_ACC_FULL };
+
+// D[tmem] (+)= A B^T in int8 -> int32, both operands in shared memory, by a CTA pair
+__device__ __forceinline__ void umma_i8_pair(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
+      "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// signed 8-bit operands, both K-major, int32 sums
+__device__ __forceinline__ uint32_t umma_idesc_i8(int m, int n) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+// four rows r of a tensor whose map has one-row boxes, side by side in shared memory (512 bytes)
+__device__ __forceinline__ void tma_gather4_pair(uint32_t dst, const CUtensorMap* m, uint32_t cluster_bar, int c0, const int4& r) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, "
+      "%5, %6, %7}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(cluster_bar), "r"(c0), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w)
+      : "memory");
+}
+
+struct Tile8 {
+  int mat, chan, tok, n;  // matrix, first channel, first token row (by expert: place in the list), token rows
+};
+
+template <bool kExperts>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
+  using S = Smem8;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t crank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  auto full_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * s; };
+  auto empty_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * (kStages8 + s); };
+  auto acc_full_bar = [&](int b) -> uint32_t { return smem_base + S::kOffBars + 8u * (2 * kStages8 + b); };
+  auto acc_empty_bar = [&](int b) -> uint32_t { return smem_base + S::kOffBars + 8u * (2 * kStages8 + 2 + b); };
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffAbort);
+  volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + S::kOffTmemPtr);
+  int* first = reinterpret_cast<int*>(smem + S::kOffFirst);
+  int* offs = first + kMaxExperts + 1;
+  const uint64_t limit = p.wait_ns;
+  const int n_chan = (p.n_out + kTileM - 1) / kTileM;
+  const int k_chunks = (p.k_pad + kStep - 1) / kStep;
+
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int s = 0; s < kStages8; ++s) {
+      mbar_init(full_bar(s), 1);   // leader's: one arrival (its own expect_tx) + the bytes of both CTAs
+      mbar_init(empty_bar(s), 1);  // each CTA's: the pair's commit arrives on both
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(acc_full_bar(b), 1);    // each CTA's: the pair's commit arrives on both
+      mbar_init(acc_empty_bar(b), 16);  // leader's: the eight epilogue warps of both CTAs
+    }
+    fence_mbar_init_cluster();
+  }
+  if (warp == 0) {
+    __syncwarp();
+    tmem_alloc<2>(smem_base + S::kOffTmemPtr, 512);
+    tmem_relinquish<2>();
+  }
+  int n_tiles;
+  if constexpr (kExperts) {
+    // the list's bounds, made safe: an expert's rows lie inside the list and behind the previous expert's
+    int* scan = reinterpret_cast<int*>(smem + S::kOffScan);
+    for (int e = threadIdx.x; e <= p.n_mat; e += kThreads8) offs[e] = p.row_off[e];
+    __syncthreads();
+    int base = 0;
+    for (int e0 = 0; e0 < p.n_mat; e0 += kThreads8) {
+      const int e = e0 + (int)threadIdx.x;
+      int tiles = 0;
+      if (e < p.n_mat) {
+        const int lo = offs[e], hi = offs[e + 1];
+        if (lo >= 0 && lo <= hi && hi <= p.n_tok)
+          tiles = ((hi - lo + kTileN - 1) / kTileN) * n_chan;
+        else if (blockIdx.x == 0)
+          report_status(p.status, 4 /*RK_ERR_ROWS*/, RK_CHK_EXPERT_OFF, e);
+      }
+      int sum = tiles;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, d);
+        if (lane >= d) sum += v;
+      }
+      if (lane == 31) scan[warp] = sum;
+      __syncthreads();
+      int before = base;
+      for (int w = 0; w < kThreads8 / 32; ++w) {
+        if (w < warp) before += scan[w];
+        base += scan[w];
+      }
+      if (e < p.n_mat) first[e] = before + sum - tiles;
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) first[p.n_mat] = base;
+    n_tiles = base;
+  } else {
+    n_tiles = n_chan * ((p.n_tok + kTileN - 1) / kTileN);
+  }
+  // Tile t of the pair's sequence.  `e` walks up the experts as t grows.
+  auto tile_at = [&](int t, int& e) -> Tile8 {
+    Tile8 r;
+    if constexpr (kExperts) {
+      while (t >= first[e + 1]) ++e;
+      const int i = t - first[e], tt = i / n_chan;
+      r.mat = e;
+      r.chan = (i - tt * n_chan) * kTileM;
+      r.tok = offs[e] + tt * kTileN;
+      r.n = min(kTileN, offs[e + 1] - r.tok);
+    } else {
+      const int n_tok_tiles = (p.n_tok + kTileN - 1) / kTileN, per_band = kBandTok * n_chan;
+      const int band = t / per_band, here = min(kBandTok, n_tok_tiles - band * kBandTok), rem = t - band * per_band;
+      const int cb = rem / here;
+      r.mat = 0;
+      r.chan = cb * kTileM;
+      r.tok = (band * kBandTok + rem - cb * here) * kTileN;
+      r.n = min(kTileN, p.n_tok - r.tok);
+    }
+    return r;
+  };
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_ptr_smem;
+
+  if (warp == 0) {
+    // ---- loads: this CTA's 128 channels and its half of the token rows; bytes are counted on the leader's barrier ----
+    if (lane == 0) {
+      tma_prefetch_desc(&p.tm_w);
+      tma_prefetch_desc(&p.tm_x);
+    }
+    uint32_t it = 0;
+    int e = 0;
+    bool ok = true;
+    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+      const Tile8 tile = tile_at(t, e);
+      const int half = ((tile.n + 31) >> 5) << 4;  // token rows of this CTA, a multiple of 16
+      const int w_row = tile.mat * p.n_out + tile.chan + (int)crank * 128;
+      int4 src = make_int4(0, 0, 0, 0);
+      if constexpr (kExperts) {
+        // lane l gathers rows 4 l .. 4 l + 3 of the half; places behind the last row repeat it (their sums are not stored)
+        int r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = tile.tok + min((int)crank * half + 4 * lane + i, tile.n - 1);
+          const int pr = p.rows[at];
+          r[i] = (unsigned)pr < (unsigned)p.n_tok ? (int)((unsigned)pr / (unsigned)p.per) : 0;
+        }
+        src = make_int4(r[0], r[1], r[2], r[3]);
+      }
+      const uint32_t b_bytes = kExperts ? (uint32_t)half * kStep : S::kBBytes;
+      for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
+        const uint32_t s = it % kStages8;
+        if (it >= (uint32_t)kStages8)
+          ok = mbar_wait_bounded<false>(empty_bar(s), ((it / kStages8) & 1u) ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t full_remote = mapa_shared(full_bar(s), 0);
+        const uint32_t a_dst = smem_base + s * S::kStageBytes;
+        if (elect_one()) {
+          if (crank == 0) mbar_arrive_expect_tx(full_bar(s), 2 * (S::kABytes + b_bytes));
+          tma_load_2d_pair(a_dst, &p.tm_w, full_remote, kc * kStep, w_row);
+          if constexpr (!kExperts) tma_load_2d_pair(a_dst + S::kABytes, &p.tm_x, full_remote, kc * kStep, tile.tok + (int)crank * half);
+        }
+        if constexpr (kExperts) {
+          if (4 * lane < half) tma_gather4_pair(a_dst + S::kABytes + 512u * lane, &p.tm_x, full_remote, kc * kStep, src);
+        }
+        __syncwarp();
+      }
+    }
+    for (uint32_t back = 1; back <= (uint32_t)kStages8 && ok; ++back) {
+      if (it >= back) {
+        const uint32_t u = it - back;
+        ok = mbar_wait_bounded<false>(empty_bar(u % kStages8), (u / kStages8) & 1u, limit, abort_flag, p.status, WM_EMPTY, -1);
+        ok = __all_sync(0xffffffffu, ok);
+      }
+    }
+  } else if (warp == 1) {
+    // ---- products (leader CTA only) ----
+    if (crank == 0) {
+      uint32_t it = 0, tile_i = 0;
+      int e = 0;
+      bool ok = true;
+      for (int t = pair; t < n_tiles && ok; t += n_pairs, ++tile_i) {
+        const Tile8 tile = tile_at(t, e);
+        const uint32_t idesc = umma_idesc_i8(kTileM, ((tile.n + 31) >> 5) << 5);
+        const uint32_t b = tile_i & 1u;
+        if (tile_i >= 2) {
+          ok = mbar_wait_bounded<true>(acc_empty_bar(b), ((tile_i >> 1) & 1u) ^ 1u, limit, abort_flag, p.status, WM_ACC_EMPTY, t);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after_sync();
+        }
+        const uint32_t acc = tmem_base + b * kTileN;
+        for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
+          const uint32_t s = it % kStages8;
+          ok = mbar_wait_bounded<false>(full_bar(s), (it / kStages8) & 1u, limit, abort_flag, p.status, WM_FULL, t);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          const uint32_t a_addr = smem_base + s * S::kStageBytes;
+          if (elect_one()) {
+            const uint64_t da = umma_desc_sw128(a_addr, 16, 1024), db = umma_desc_sw128(a_addr + S::kABytes, 16, 1024);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              umma_i8_pair(acc, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc, (kc > 0 || k > 0) ? 1u : 0u);
+            umma_commit_2_mc(empty_bar(s), 3);
+            if (kc == k_chunks - 1) umma_commit_2_mc(acc_full_bar(b), 3);
+          }
+          __syncwarp();
+        }
+      }
+    }
+  } else if (warp >= 4) {
+    // ---- scales and stores: lane = channel, columns = token rows; the two groups of four warps take 32 columns in turn ----
+    const int group = (warp - 4) >> 2, quad = warp & 3;
+    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+    const uint32_t acc_empty_remote = mapa_shared(acc_empty_bar(0), 0);
+    float* tok_scale = reinterpret_cast<float*>(smem + S::kOffTok);
+    int* tok_row = reinterpret_cast<int*>(smem + S::kOffTok) + 512;
+    uint32_t tile_i = 0;
+    int e = 0;
+    bool ok = true;
+    for (int t = pair; t < n_tiles && ok; t += n_pairs, ++tile_i) {
+      const Tile8 tile = tile_at(t, e);
+      const uint32_t b = tile_i & 1u;
+      {  // scale and output row of every token row of the tile (two sets: the other one may still be in use)
+        const int i = (int)threadIdx.x - 128;
+        float sc = 0.f;
+        int row = -1;
+        if (i < tile.n) {
+          if constexpr (kExperts) {
+            const int pr = p.rows[tile.tok + i];
+            if ((unsigned)pr < (unsigned)p.n_tok) {
+              row = pr;
+              sc = p.sx[(unsigned)pr / (unsigned)p.per];
+            } else {
+              report_status(p.status, 4 /*RK_ERR_ROWS*/, RK_CHK_EXPERT_ROW, pr);
+            }
+          } else {
+            row = tile.tok + i;
+            sc = p.sx[row];
+          }
+        }
+        tok_scale[256 * b + i] = sc;
+        tok_row[256 * b + i] = row;
+      }
+      const int chan = tile.chan + (int)crank * 128 + quad * 32 + lane;
+      const bool mine = chan < p.n_out;
+      const float sw = mine ? p.sw[(int64_t)tile.mat * p.n_out + chan] : 0.f;
+      ok = mbar_wait_bounded<false>(acc_full_bar(b), (tile_i >> 1) & 1u, limit, abort_flag, p.status, WM_ACC_FULL, t);
+      ok = named_barrier_and(1, 256, ok);
+      if (!ok) break;
+      tc_fence_after_sync();
+      for (int c0 = 32 * group; c0 < tile.n; c0 += 64) {
+        uint32_t o[32];
+        tmem_ld_x32(tmem_base + lane_base + b * kTileN + c0, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const int row = tok_row[256 * b + c0 + i];
+          if (row < 0 || !mine) continue;
+          const float v = (float)(int)o[i] * tok_scale[256 * b + c0 + i] * sw;
+          if (p.out_f32)
+            static_cast<float*>(p.y)[(int64_t)row * p.y_stride + chan] = v;
+          else
+            static_cast<__nv_bfloat16*>(p.y)[(int64_t)row * p.y_stride + chan] = __float2bfloat16_rn(v);
+        }
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(acc_empty_remote + 8u * b);
+    }
+  }
+  if (*abort_flag != 0) {
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
+  }
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 0) {
+    __syncwarp();
+    tmem_dealloc<2>(tmem_base, 512);
+  }
+}
+
+}  // namespace
+
+cudaError_t matmul8_setup() {
+  cudaError_t e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
+  return e;
+}
+
+cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32_t k, void* codes, float* scales, cudaStream_t stream) {
+  const int k_pad = (k + 15) / 16 * 16, want = (k_pad / 8 + kQuantHeld - 1) / kQuantHeld;
+  int nt = 32;
+  while (nt < want && nt < 512) nt *= 2;
+  const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && x_stride % 8 == 0;
+  auto kernel = vec ? quant8_kernel<true> : quant8_kernel<false>;
+  kernel<<<(unsigned)n_rows, nt, 0, stream>>>(static_cast<const __nv_bfloat16*>(x), x_stride, k, k_pad, static_cast<uint8_t*>(codes), scales);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_matmul8(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
+  const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
+  // by expert the number of tiles is known on the device only: at most one part-filled tile per expert more than full ones
+  const int64_t tok_tiles = (p.n_tok + kTileN - 1) / kTileN + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
+  const int64_t tiles = n_chan * tok_tiles;
+  const int n_pairs = (int)(tiles < sm_count / 2 ? tiles : sm_count / 2);
+  auto kernel = p.rows ? rk_matmul8_pair_kernel<true> : rk_matmul8_pair_kernel<false>;
+  kernel<<<2 * n_pairs, kThreads8, Smem8::kBytes, stream>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace rk

@@ -46,7 +46,8 @@ __device__ __forceinline__ void report_status(DeviceStatus* st, int code, int wh
 // table, `aux` holds the value) and the access is skipped.  Nothing traps.  In the ordinary build the
 // function is the constant true and the test disappears.
 enum { RK_CHK_PROT_ROW = 101, RK_CHK_WORK_TILE = 102, RK_CHK_INV_MAP = 103, RK_CHK_COMPACT = 104, RK_CHK_SELFTEST = 199,
-       RK_CHK_CACHE_ROW = 201, RK_CHK_CACHE_PAGE = 202, RK_CHK_PLAN_ITEM = 203, RK_CHK_PLAN_MATCH = 204 };
+       RK_CHK_CACHE_ROW = 201, RK_CHK_CACHE_PAGE = 202, RK_CHK_PLAN_ITEM = 203, RK_CHK_PLAN_MATCH = 204,
+       RK_CHK_EXPERT_OFF = 211, RK_CHK_EXPERT_ROW = 212 };
 #ifdef RK_CHECK
 __device__ __forceinline__ bool rk_index_ok(bool ok, DeviceStatus* st, int where, long long value) {
   if (!ok && st != nullptr && atomicCAS(&st->code, 0, 4 /*RK_ERR_ROWS*/) == 0) {
