@@ -277,6 +277,7 @@ rk_status rk_create_ex(const rk_profile* prof, uint32_t flags, rk_ctx** out) {
   if (e == cudaSuccess) e = matvec4_setup(ctx->matvec_slots, ctx->sm_count);
   if (e == cudaSuccess) e = experts_setup();
   if (e == cudaSuccess) e = matmul8_setup();
+  if (e == cudaSuccess) e = sample_setup();
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&ctx->d_status), sizeof(DeviceStatus));
   if (e == cudaSuccess) e = cudaMemset(ctx->d_status, 0, sizeof(DeviceStatus));
   if (e != cudaSuccess) {

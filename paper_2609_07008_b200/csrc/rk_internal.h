@@ -323,6 +323,7 @@ struct SampleParams {
   int32_t vocab, bf16;
   int32_t blocks;  // set by the launcher: thread blocks per row (a cluster)
 };
+cudaError_t sample_setup();
 cudaError_t launch_sample(SampleParams p, int sm_count, cudaStream_t stream);
 
 #ifdef __CUDACC__
