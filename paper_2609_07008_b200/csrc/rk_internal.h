@@ -297,7 +297,8 @@ cudaError_t launch_moe_group(const GroupParams& p, cudaStream_t stream);
 
 struct Matmul8Params {
   CUtensorMap tm_w;      // [n_mat * n_out][k_pad] bytes, box 128 x 128
-  CUtensorMap tm_x;      // [token rows][k_pad] bytes, box 128 x 128, by expert 128 x 1
+  CUtensorMap tm_x;      // dense: [token rows][k_pad] bytes, box 128 x 128
+  const uint8_t* x;      // by expert: the same rows
   const float* sw;       // [n_mat * n_out]
   const float* sx;       // [token rows]
   const int32_t* row_off;  // by expert: [n_mat + 1] into rows

@@ -12,8 +12,10 @@
 // tensor cores, below the 76 that it can.  Persistent: the accumulator is double buffered in tensor memory, so that the
 // scales and stores of one tile run under the products of the next.
 //
-// By expert, the token rows of a tile are a gather (the tokens that chose the expert), four rows per TMA instruction, so
-// that no sorted copy of the activations is made; the outputs go straight to the pairs' rows of y.
+// By expert, the token rows of a tile are a gather (the tokens that chose the expert): four warps copy them with 16-byte
+// asynchronous loads into the swizzled operand layout, so that no sorted copy of the activations is made; the outputs go
+// straight to the pairs' rows of y.  (TMA's gather of four rows took 72 clocks of each SM's copy engine per instruction,
+// 2300 per 128 rows; a stage has 512.)
 #include <cuda_bf16.h>
 
 #include "rk_internal.h"
@@ -125,7 +127,9 @@ __global__ void __launch_bounds__(512) quant8_kernel(const __nv_bfloat16* __rest
 // ------------------------------------------------------------------------------------------------------------
 // products
 // ------------------------------------------------------------------------------------------------------------
-constexpr int kThreads8 = 384;  // warp 0 loads, warp 1 issues, warps 4-11 scale and store
+constexpr int kThreads8 = 384;          // warp 0 loads, warp 1 issues, warps 4-11 scale and store
+constexpr int kGatherWarps = 4;         // by expert: warps 12-15 gather token rows
+constexpr int kGatherLag = 3;           // stages whose copies a gather warp has under way before it announces the oldest
 constexpr int kStages8 = 6;
 constexpr int kStep = 128;      // bytes (= values) of k per stage
 constexpr int kTileM = 256, kTileN = 256;
@@ -156,13 +160,14 @@ __device__ __forceinline__ void umma_i8_pair(uint32_t tmem_d, uint64_t desc_a, u
 __device__ __forceinline__ uint32_t umma_idesc_i8(int m, int n) {
   return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
-// four rows r of a tensor whose map has one-row boxes, side by side in shared memory (512 bytes)
-__device__ __forceinline__ void tma_gather4_pair(uint32_t dst, const CUtensorMap* m, uint32_t cluster_bar, int c0, const int4& r) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, "
-      "%5, %6, %7}], [%2];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(m)), "r"(cluster_bar), "r"(c0), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w)
-      : "memory");
+// 16 bytes from global to shared memory, or 16 zeros
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src, bool real) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 struct Tile8 {
@@ -170,7 +175,8 @@ struct Tile8 {
 };
 
 template <bool kExperts>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8, 1)
+    rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
   using S = Smem8;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -193,7 +199,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_mat
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int s = 0; s < kStages8; ++s) {
-      mbar_init(full_bar(s), 1);   // leader's: one arrival (its own expect_tx) + the bytes of both CTAs
+      // leader's: one arrival (its own expect_tx) + the bytes of both CTAs, and both CTAs' gather warps
+      mbar_init(full_bar(s), kExperts ? 1 + 2 * kGatherWarps : 1);
       mbar_init(empty_bar(s), 1);  // each CTA's: the pair's commit arrives on both
     }
     for (int b = 0; b < 2; ++b) {
@@ -211,10 +218,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_mat
   if constexpr (kExperts) {
     // the list's bounds, made safe: an expert's rows lie inside the list and behind the previous expert's
     int* scan = reinterpret_cast<int*>(smem + S::kOffScan);
-    for (int e = threadIdx.x; e <= p.n_mat; e += kThreads8) offs[e] = p.row_off[e];
+    for (int e = threadIdx.x; e <= p.n_mat; e += blockDim.x) offs[e] = p.row_off[e];
     __syncthreads();
     int base = 0;
-    for (int e0 = 0; e0 < p.n_mat; e0 += kThreads8) {
+    for (int e0 = 0; e0 < p.n_mat; e0 += blockDim.x) {
       const int e = e0 + (int)threadIdx.x;
       int tiles = 0;
       if (e < p.n_mat) {
@@ -232,7 +239,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_mat
       if (lane == 31) scan[warp] = sum;
       __syncthreads();
       int before = base;
-      for (int w = 0; w < kThreads8 / 32; ++w) {
+      for (int w = 0; w < (int)blockDim.x / 32; ++w) {
         if (w < warp) before += scan[w];
         base += scan[w];
       }
@@ -276,7 +283,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_mat
     // ---- loads: this CTA's 128 channels and its half of the token rows; bytes are counted on the leader's barrier ----
     if (lane == 0) {
       tma_prefetch_desc(&p.tm_w);
-      tma_prefetch_desc(&p.tm_x);
+      if (!kExperts) tma_prefetch_desc(&p.tm_x);
     }
     uint32_t it = 0;
     int e = 0;
@@ -285,19 +292,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_mat
       const Tile8 tile = tile_at(t, e);
       const int half = ((tile.n + 31) >> 5) << 4;  // token rows of this CTA, a multiple of 16
       const int w_row = tile.mat * p.n_out + tile.chan + (int)crank * 128;
-      int4 src = make_int4(0, 0, 0, 0);
-      if constexpr (kExperts) {
-        // lane l gathers rows 4 l .. 4 l + 3 of the half; places behind the last row repeat it (their sums are not stored)
-        int r[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = tile.tok + min((int)crank * half + 4 * lane + i, tile.n - 1);
-          const int pr = p.rows[at];
-          r[i] = (unsigned)pr < (unsigned)p.n_tok ? (int)((unsigned)pr / (unsigned)p.per) : 0;
-        }
-        src = make_int4(r[0], r[1], r[2], r[3]);
-      }
-      const uint32_t b_bytes = kExperts ? (uint32_t)half * kStep : S::kBBytes;
+      constexpr uint32_t kBytes = S::kABytes + (kExperts ? 0u : S::kBBytes);
       for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
         const uint32_t s = it % kStages8;
         if (it >= (uint32_t)kStages8)
@@ -307,12 +302,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_mat
         const uint32_t full_remote = mapa_shared(full_bar(s), 0);
         const uint32_t a_dst = smem_base + s * S::kStageBytes;
         if (elect_one()) {
-          if (crank == 0) mbar_arrive_expect_tx(full_bar(s), 2 * (S::kABytes + b_bytes));
+          if (crank == 0) mbar_arrive_expect_tx(full_bar(s), 2 * kBytes);
           tma_load_2d_pair(a_dst, &p.tm_w, full_remote, kc * kStep, w_row);
           if constexpr (!kExperts) tma_load_2d_pair(a_dst + S::kABytes, &p.tm_x, full_remote, kc * kStep, tile.tok + (int)crank * half);
-        }
-        if constexpr (kExperts) {
-          if (4 * lane < half) tma_gather4_pair(a_dst + S::kABytes + 512u * lane, &p.tm_x, full_remote, kc * kStep, src);
         }
         __syncwarp();
       }
@@ -359,6 +351,48 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1) rk_mat
         }
       }
     }
+  } else if (kExperts && warp >= 12) {
+    // ---- gather (by expert): rows of the half in steps of 16, four of them per warp, eight lanes to a row of 128 bytes ----
+    const int sub = (warp - 12) * 4 + (lane >> 3), chunk = lane & 7;
+    uint32_t it = 0;
+    int e = 0;
+    bool ok = true;
+    auto announce = [&](uint32_t i) {  // the copies of stage use i have landed: show them to the tensor cores
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(mapa_shared(full_bar(i % kStages8), 0));
+    };
+    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
+      const Tile8 tile = tile_at(t, e);
+      const int half = ((tile.n + 31) >> 5) << 4;
+      const uint8_t* src[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // places behind the last row repeat it (their sums are not stored)
+        const int pr = p.rows[tile.tok + min((int)crank * half + 16 * i + sub, tile.n - 1)];
+        const uint32_t row = (unsigned)pr < (unsigned)p.n_tok ? (unsigned)pr / (unsigned)p.per : 0u;
+        src[i] = p.x + (int64_t)row * p.k_pad + 16 * chunk;
+      }
+      for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
+        const uint32_t s = it % kStages8;
+        if (it >= (uint32_t)kStages8)
+          ok = mbar_wait_bounded<false>(empty_bar(s), ((it / kStages8) & 1u) ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t dst = smem_base + s * S::kStageBytes + S::kABytes;
+        const bool real = kc * kStep + 16 * chunk < p.k_pad;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (16 * i < half) copy16_async(dst + sw128_offset(16 * i + sub, chunk), real ? src[i] + kc * kStep : src[i], real);
+        copies_commit();
+        if (it >= (uint32_t)kGatherLag) {
+          copies_wait<kGatherLag>();
+          announce(it - kGatherLag);
+        }
+      }
+    }
+    copies_wait<0>();
+    for (uint32_t i = it > (uint32_t)kGatherLag ? it - kGatherLag : 0u; i < it && ok; ++i) announce(i);
   } else if (warp >= 4) {
     // ---- scales and stores: lane = channel, columns = token rows; the two groups of four warps take 32 columns in turn ----
     const int group = (warp - 4) >> 2, quad = warp & 3;
@@ -459,8 +493,10 @@ cudaError_t launch_matmul8(const Matmul8Params& p, int sm_count, cudaStream_t st
   const int64_t tok_tiles = (p.n_tok + kTileN - 1) / kTileN + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
   const int64_t tiles = n_chan * tok_tiles;
   const int n_pairs = (int)(tiles < sm_count / 2 ? tiles : sm_count / 2);
-  auto kernel = p.rows ? rk_matmul8_pair_kernel<true> : rk_matmul8_pair_kernel<false>;
-  kernel<<<2 * n_pairs, kThreads8, Smem8::kBytes, stream>>>(p);
+  if (p.rows)
+    rk_matmul8_pair_kernel<true><<<2 * n_pairs, kThreads8 + 32 * kGatherWarps, Smem8::kBytes, stream>>>(p);
+  else
+    rk_matmul8_pair_kernel<false><<<2 * n_pairs, kThreads8, Smem8::kBytes, stream>>>(p);
   return cudaGetLastError();
 }
 
