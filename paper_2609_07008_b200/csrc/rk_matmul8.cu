@@ -27,29 +27,18 @@ namespace {
 // quantisation of rows
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kQuantHeld = 4;  // 8-value chunks that a thread keeps in registers between the maximum and the codes
+constexpr int kQuantRows = 8;  // rows of a thread block where a warp has a row to itself
 
-// round(x / scale), half to even, exactly: the quick product decides unless it lands within 1e-4 of the middle between two
-// codes (its error is below 127 * 2^-23); there the sign of |x| - scale (m + 1/2), one double-precision fused product whose
-// result is rounded once, tells the side.
+constexpr float kQuantNear = 0.49998f;
+
+// round(x / scale), half to even, exactly, and limited to -127 .. 127.  The quick quotient t tells the two codes; the sign of
+// |x| - scale (m + 1/2), one fused product in double that is rounded once, the side of the middle between them.  Where 1 / scale
+// is beyond fp32 (inv = 0), the quotient is taken in double.
 __device__ __forceinline__ int quant8_code(float x, float scale, float inv) {
-  const float t = fabsf(x * inv);
-  float m = floorf(t);
-  const float f = t - m;
-  if (f > 0.4999f) {
-    if (f < 0.5001f) {
-      const double r = fma(-(double)scale, (double)(m + 0.5f), (double)fabsf(x));
-      if (r > 0.0 || (r == 0.0 && ((int)m & 1))) m += 1.f;
-    } else {
-      m += 1.f;
-    }
-  }
-  const int c = min((int)m, 127);
-  return x < 0.f ? -c : c;
-}
-// the same where 1 / scale has left the range of fp32 (rows whose largest value is below 1e-28)
-__device__ __noinline__ int quant8_code_tiny(float x, float scale) {
-  const double t = fabs((double)x) / (double)scale;
-  const int c = (int)fmin(rint(t), 127.0);
+  const double a = fabs((double)x), m = inv == 0.f ? floor(a / (double)scale) : (double)floorf(fabsf(x * inv));
+  const double r = fma(-(double)scale, m + 0.5, a);
+  int c = (int)fmin(m, 127.0);
+  if (c < 127 && (r > 0.0 || (r == 0.0 && (c & 1)))) ++c;
   return x < 0.f ? -c : c;
 }
 
@@ -72,56 +61,98 @@ __device__ __forceinline__ uint32_t chunk_top(const uint4& c) {
   uint32_t t = __vmaxu2(__vmaxu2(c.x & 0x7fff7fffu, c.y & 0x7fff7fffu), __vmaxu2(c.z & 0x7fff7fffu, c.w & 0x7fff7fffu));
   return max(t & 0xffffu, t >> 16);
 }
-__device__ __forceinline__ uint2 chunk_codes(const uint4& c, float scale, float inv, bool tiny) {
+// Codes of eight values.  x * inv + 1.5 * 2^23 is rounded to a whole number, half to even, whose two's complement is in the
+// low byte.  `off` collects the largest distance from a whole number: inv is off by 2^-24 of itself, the quotient by less than
+// 1e-5, so that up to 0.49998 the code is right.
+__device__ __forceinline__ uint2 chunk_codes(const uint4& c, float inv, float& off) {
+  constexpr float kMagic = 12582912.f;
   const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-  uint32_t out[2] = {0u, 0u};
+  uint32_t y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float x = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
-    const int q = tiny ? quant8_code_tiny(x, scale) : quant8_code(x, scale, inv);
-    out[i >> 2] |= ((uint32_t)q & 0xffu) << (8 * (i & 3));
+    const float x = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16), r = fmaf(x, inv, kMagic);
+    off = fmaxf(off, fabsf(fmaf(x, inv, kMagic - r)));
+    y[i] = __float_as_uint(r);
   }
-  return make_uint2(out[0], out[1]);
+  return make_uint2(__byte_perm(__byte_perm(y[0], y[1], 0x0040), __byte_perm(y[2], y[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(y[4], y[5], 0x0040), __byte_perm(y[6], y[7], 0x0040), 0x5410));
 }
 
-// One row per thread block.  A row of up to 32 values per thread is read once; longer ones a second time out of L2.  HBM
-// bound: two bytes in, one out per value.
+// The values near the middle between two codes again (all values for inv = 0) of the threads `who` of the warp, each of which
+// has the chunks thread, thread + step, ... of n_chunks.  A few threads' values are spread over the lanes, a thread's 32 at a
+// time (2 us less than its walk over them); many threads walk side by side.
 template <bool kVec>
-__global__ void __launch_bounds__(512) quant8_kernel(const __nv_bfloat16* __restrict__ x, int64_t x_stride, int k, int k_pad,
-                                                     uint8_t* __restrict__ codes, float* __restrict__ scales) {
-  const int64_t row = blockIdx.x;
+__device__ __noinline__ void quant8_exact(unsigned who, const __nv_bfloat16* row, int k, int warp_first, int step, int n_chunks,
+                                          float scale, float inv, uint8_t* codes) {
+  const int lane = threadIdx.x & 31;
+  auto fix = [&](int i, float x) {
+    const float t = x * inv;
+    if (inv == 0.f || fabsf(t - rintf(t)) >= kQuantNear - 1e-5f) codes[i] = (uint8_t)quant8_code(x, scale, inv);
+  };
+  __syncwarp();
+  if (__popc(who) <= 4) {
+    for (; who != 0u; who &= who - 1u)
+      for (int c = warp_first + __ffs(who) - 1 + (lane >> 3) * step; c < n_chunks; c += 4 * step) {
+        const int i = 8 * c + (lane & 7);
+        if (i < k) fix(i, __bfloat162float(row[i]));
+      }
+  } else if ((who >> lane) & 1u) {
+    for (int c = warp_first + lane; c < n_chunks; c += step) {
+      const uint4 v = load_chunk<kVec>(row, 8 * c, k);
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t w = i < 4 ? (i < 2 ? v.x : v.y) : (i < 6 ? v.z : v.w);
+        fix(8 * c + i, __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16));
+      }
+    }
+  }
+}
+
+// A row per thread block, or per warp (kWarp: up to 1024 values).  A row of up to 32 values per thread is read once; longer
+// ones a second time out of L2.  HBM bound: two bytes in, one out per value.
+template <bool kVec, bool kWarp>
+__global__ void __launch_bounds__(512, 3) quant8_kernel(const __nv_bfloat16* __restrict__ x, int64_t x_stride, int64_t n_rows, int k,
+                                                        int k_pad, uint8_t* __restrict__ codes, float* __restrict__ scales) {
+  const int64_t row = kWarp ? (int64_t)blockIdx.x * kQuantRows + (threadIdx.x >> 5) : blockIdx.x;
+  if (kWarp && row >= n_rows) return;
   const __nv_bfloat16* src = x + row * x_stride;
-  const int n_chunks = k_pad >> 3, nt = blockDim.x;  // k_pad is a multiple of 16
+  const int n_chunks = k_pad >> 3, nt = kWarp ? 32 : blockDim.x, tid = kWarp ? threadIdx.x & 31 : threadIdx.x;  // k_pad is a multiple of 16
   uint4 held[kQuantHeld];
   uint32_t top = 0u;
 #pragma unroll
   for (int i = 0; i < kQuantHeld; ++i) {
-    const int c = threadIdx.x + i * nt;
+    const int c = tid + i * nt;
     held[i] = c < n_chunks ? load_chunk<kVec>(src, 8 * c, k) : make_uint4(0u, 0u, 0u, 0u);
   }
 #pragma unroll
   for (int i = 0; i < kQuantHeld; ++i) top = max(top, chunk_top(held[i]));
-  for (int c = threadIdx.x + kQuantHeld * nt; c < n_chunks; c += nt) top = max(top, chunk_top(load_chunk<kVec>(src, 8 * c, k)));
+  for (int c = tid + kQuantHeld * nt; c < n_chunks; c += nt) top = max(top, chunk_top(load_chunk<kVec>(src, 8 * c, k)));
   top = __reduce_max_sync(0xffffffffu, top);
-  if (nt > 32) {
+  if constexpr (!kWarp) {
     __shared__ uint32_t tops[16];
-    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+    if ((tid & 31) == 0) tops[tid >> 5] = top;
     __syncthreads();
     for (int w = 0; w < nt >> 5; ++w) top = max(top, tops[w]);
   }
   const bool finite = top < 0x7f80u;
   const float scale = finite ? __fdiv_rn(__uint_as_float(top << 16), 127.f) : __uint_as_float(0x7fc00000u);
-  const bool blank = !finite || scale == 0.f, tiny = scale < 1e-30f;
-  const float inv = blank ? 0.f : __fdiv_rn(1.f, scale);
-  uint2* dst = reinterpret_cast<uint2*>(codes + row * k_pad);
+  const bool blank = !finite || scale == 0.f;
+  // 0 in place of the reciprocal makes codes of 0, and, for rows of tiny values, has all of them done exactly
+  const float inv = blank || scale < 1e-30f ? 0.f : __fdiv_rn(1.f, scale);
+  float off = !blank && inv == 0.f ? 1.f : 0.f;
+  uint8_t* to = codes + row * k_pad;
+  uint2* dst = reinterpret_cast<uint2*>(to);
 #pragma unroll
   for (int i = 0; i < kQuantHeld; ++i) {
-    const int c = threadIdx.x + i * nt;
-    if (c < n_chunks) dst[c] = blank ? make_uint2(0u, 0u) : chunk_codes(held[i], scale, inv, tiny);
+    const int c = tid + i * nt;
+    if (c < n_chunks) dst[c] = finite ? chunk_codes(held[i], inv, off) : make_uint2(0u, 0u);
   }
-  for (int c = threadIdx.x + kQuantHeld * nt; c < n_chunks; c += nt)
-    dst[c] = blank ? make_uint2(0u, 0u) : chunk_codes(load_chunk<kVec>(src, 8 * c, k), scale, inv, tiny);
-  if (threadIdx.x == 0) scales[row] = scale;
+  for (int c = tid + kQuantHeld * nt; c < n_chunks; c += nt)
+    dst[c] = finite ? chunk_codes(load_chunk<kVec>(src, 8 * c, k), inv, off) : make_uint2(0u, 0u);
+  // (with a power of two for a scale, one row in 128, the quick quotient is the quotient, and ties are many)
+  const unsigned near = __ballot_sync(0xffffffffu, off >= kQuantNear && (inv == 0.f || (__float_as_uint(scale) & 0x7fffffu) != 0u));
+  if (near != 0u) quant8_exact<kVec>(near, src, k, tid & ~31, nt, n_chunks, scale, inv, to);
+  if (tid == 0) scales[row] = scale;
 }
 
 // ------------------------------------------------------------------------------------------------------------
@@ -479,11 +510,18 @@ cudaError_t matmul8_setup() {
 
 cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32_t k, void* codes, float* scales, cudaStream_t stream) {
   const int k_pad = (k + 15) / 16 * 16, want = (k_pad / 8 + kQuantHeld - 1) / kQuantHeld;
-  int nt = 32;
-  while (nt < want && nt < 512) nt *= 2;
   const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && x_stride % 8 == 0;
-  auto kernel = vec ? quant8_kernel<true> : quant8_kernel<false>;
-  kernel<<<(unsigned)n_rows, nt, 0, stream>>>(static_cast<const __nv_bfloat16*>(x), x_stride, k, k_pad, static_cast<uint8_t*>(codes), scales);
+  const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(x);
+  uint8_t* dst = static_cast<uint8_t*>(codes);
+  if (want <= 32) {
+    auto kernel = vec ? quant8_kernel<true, true> : quant8_kernel<false, true>;
+    kernel<<<(unsigned)((n_rows + kQuantRows - 1) / kQuantRows), 32 * kQuantRows, 0, stream>>>(src, x_stride, n_rows, k, k_pad, dst, scales);
+  } else {
+    int nt = 64;
+    while (nt < want && nt < 512) nt *= 2;
+    auto kernel = vec ? quant8_kernel<true, false> : quant8_kernel<false, false>;
+    kernel<<<(unsigned)n_rows, nt, 0, stream>>>(src, x_stride, n_rows, k, k_pad, dst, scales);
+  }
   return cudaGetLastError();
 }
 
