@@ -172,8 +172,8 @@ struct Smem8 {
   static constexpr uint32_t kOffTmemPtr = kOffBars + (2 * kStages8 + 4) * 8;
   static constexpr uint32_t kOffAbort = kOffTmemPtr + 8;
   static constexpr uint32_t kOffScan = kOffAbort + 8;               // 32 words of the block's scan
-  static constexpr uint32_t kOffTok = kOffScan + 128;               // [2][256] token scale, [2][256] output row
-  static constexpr uint32_t kOffFirst = kOffTok + 2 * 256 * 8;      // by expert: first tile of each, [n_mat + 1]; then row_off
+  static constexpr uint32_t kOffTok = (kOffScan + 128 + 15) / 16 * 16;  // [2][256] TokenOut
+  static constexpr uint32_t kOffFirst = kOffTok + 2 * 256 * 16;     // by expert: first tile of each, [n_mat + 1]; then row_off
   static constexpr uint32_t kBytes = kOffFirst + 2 * (kMaxExperts + 1) * 4 + 1024 + 16;
 };
 enum { WM_EMPTY = 61, WM_FULL, WM_ACC_EMPTY, WM_ACC_FULL };
@@ -204,6 +204,29 @@ __device__ __forceinline__ void copies_wait() {
 struct Tile8 {
   int mat, chan, tok, n;  // matrix, first channel, first token row (by expert: place in the list), token rows
 };
+
+struct __align__(16) TokenOut {  // an output row of a tile
+  long long at;  // bytes from y, negative: not stored
+  float scale;
+  int pad;
+};
+
+// 32 columns of the accumulator: lane = channel, register i = token i.  `to` is y at the lane's channel.
+template <class T>
+__device__ __forceinline__ void store_columns(const uint32_t (&o)[32], const TokenOut* tok, uint8_t* to, float sw, bool mine) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const int4 raw = *reinterpret_cast<const int4*>(tok + i);
+    const long long at = ((long long)raw.y << 32) | (uint32_t)raw.x;
+    const float v = (float)(int)o[i] * __int_as_float(raw.z) * sw;
+    if (mine && raw.y >= 0) {
+      if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<float*>(to + at) = v;
+      else
+        *reinterpret_cast<__nv_bfloat16*>(to + at) = __float2bfloat16_rn(v);
+    }
+  }
+}
 
 template <bool kExperts>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8, 1)
@@ -429,8 +452,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
     const int group = (warp - 4) >> 2, quad = warp & 3;
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t acc_empty_remote = mapa_shared(acc_empty_bar(0), 0);
-    float* tok_scale = reinterpret_cast<float*>(smem + S::kOffTok);
-    int* tok_row = reinterpret_cast<int*>(smem + S::kOffTok) + 512;
+    TokenOut* toks = reinterpret_cast<TokenOut*>(smem + S::kOffTok);
     uint32_t tile_i = 0;
     int e = 0;
     bool ok = true;
@@ -455,8 +477,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
             sc = p.sx[row];
           }
         }
-        tok_scale[256 * b + i] = sc;
-        tok_row[256 * b + i] = row;
+        TokenOut out;
+        out.at = row < 0 ? -1 : (long long)row * p.y_stride * (p.out_f32 ? 4 : 2);
+        out.scale = sc;
+        out.pad = 0;
+        toks[256 * b + i] = out;
       }
       const int chan = tile.chan + (int)crank * 128 + quad * 32 + lane;
       const bool mine = chan < p.n_out;
@@ -469,16 +494,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
         uint32_t o[32];
         tmem_ld_x32(tmem_base + lane_base + b * kTileN + c0, o);
         tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const int row = tok_row[256 * b + c0 + i];
-          if (row < 0 || !mine) continue;
-          const float v = (float)(int)o[i] * tok_scale[256 * b + c0 + i] * sw;
-          if (p.out_f32)
-            static_cast<float*>(p.y)[(int64_t)row * p.y_stride + chan] = v;
-          else
-            static_cast<__nv_bfloat16*>(p.y)[(int64_t)row * p.y_stride + chan] = __float2bfloat16_rn(v);
-        }
+        if (p.out_f32)
+          store_columns<float>(o, toks + 256 * b + c0, static_cast<uint8_t*>(p.y) + (int64_t)chan * 4, sw, mine);
+        else
+          store_columns<__nv_bfloat16>(o, toks + 256 * b + c0, static_cast<uint8_t*>(p.y) + (int64_t)chan * 2, sw, mine);
       }
       tc_fence_before_sync();
       __syncwarp();
