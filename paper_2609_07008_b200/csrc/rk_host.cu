@@ -1604,6 +1604,7 @@ rk_status rk_matmul8_experts(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const 
   if (per < 1 || per > kMaxSlots) return fail(ctx, RK_ERR_UNSUPPORTED, "per must be 1 .. %d", kMaxSlots);
   if (x->n_rows < (n_pairs + per - 1) / per)
     return fail(ctx, RK_ERR_LAYOUT, "%lld token rows for %lld pairs, %d per token", (long long)x->n_rows, (long long)n_pairs, per);
+  if (x->k > 0 && x->n_rows > ((int64_t)1 << 32) / ((x->k + 15) / 16) - 1) return fail(ctx, RK_ERR_ROWS, "the token rows exceed 64 GiB");
   if (!aligned_to(row_off, 4) || !aligned_to(rows, 4)) return fail(ctx, RK_ERR_ALIGN, "tables must be aligned to their types");
   return matmul8(ctx, w, x, row_off, rows, n_pairs, per, y, y_stride, out_dtype, stream);
 }

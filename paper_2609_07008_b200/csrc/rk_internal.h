@@ -309,10 +309,11 @@ struct Matmul8Params {
   unsigned long long wait_ns;
   int32_t n_tok;  // token rows; by expert: pairs (places of the list, rows of y)
   int32_t n_out, k_pad, n_mat, per, out_f32;
+  int32_t paired;  // set by the launcher: rows and channels allow 4-byte stores of bf16 pairs
 };
 cudaError_t matmul8_setup();
 cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32_t k, void* codes, float* scales, cudaStream_t stream);
-cudaError_t launch_matmul8(const Matmul8Params& p, int sm_count, cudaStream_t stream);
+cudaError_t launch_matmul8(Matmul8Params p, int sm_count, cudaStream_t stream);
 
 struct SampleParams {
   const void* logits;  // [n][vocab], rows `stride` elements apart

@@ -159,8 +159,7 @@ __global__ void __launch_bounds__(512, 3) quant8_kernel(const __nv_bfloat16* __r
 // products
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kThreads8 = 384;          // warp 0 loads, warp 1 issues, warps 4-11 scale and store
-constexpr int kGatherWarps = 4;         // by expert: warps 12-15 gather token rows
-constexpr int kGatherLag = 3;           // stages whose copies a gather warp has under way before it announces the oldest
+constexpr int kGatherWarps = 4;         // by expert: warps 12-15, and 2 and 3, gather token rows: one for each stage of the ring
 constexpr int kStages8 = 6;
 constexpr int kStep = 128;      // bytes (= values) of k per stage
 constexpr int kTileM = 256, kTileN = 256;
@@ -201,6 +200,11 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// token rows are cut into as few tiles as they need, of equal size (a multiple of 32): a short rest would cost nearly a full
+// tile's loads of W
+__device__ __forceinline__ int token_tiles(int n) { return (n + kTileN - 1) / kTileN; }
+__device__ __forceinline__ int token_tile_rows(int n, int tiles) { return ((n + tiles - 1) / tiles + 31) & ~31; }
+
 struct Tile8 {
   int mat, chan, tok, n;  // matrix, first channel, first token row (by expert: place in the list), token rows
 };
@@ -225,6 +229,21 @@ __device__ __forceinline__ void store_columns(const uint32_t (&o)[32], const Tok
       else
         *reinterpret_cast<__nv_bfloat16*>(to + at) = __float2bfloat16_rn(v);
     }
+  }
+}
+// The same for bf16 where rows and channels allow 4-byte stores: neighbouring lanes trade one of two tokens, after which the
+// even lane has both channels of the first and the odd lane both of the second.  `to` is y at the even lane's channel.
+__device__ __forceinline__ void store_columns_paired(const uint32_t (&o)[32], const TokenOut* tok, uint8_t* to, float sw, bool mine) {
+  const bool odd = threadIdx.x & 1;
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    const int4 a = *reinterpret_cast<const int4*>(tok + i), b = *reinterpret_cast<const int4*>(tok + i + 1);
+    const float va = (float)(int)o[i] * __int_as_float(a.z) * sw, vb = (float)(int)o[i + 1] * __int_as_float(b.z) * sw;
+    const float got = __shfl_xor_sync(0xffffffffu, odd ? va : vb, 1);
+    const int hi = odd ? b.y : a.y;
+    const long long at = ((long long)hi << 32) | (uint32_t)(odd ? b.x : a.x);
+    const uint32_t v = odd ? pack_bf16(got, vb) : pack_bf16(va, got);
+    if (mine && hi >= 0) *reinterpret_cast<uint32_t*>(to + at) = v;
   }
 }
 
@@ -253,8 +272,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int s = 0; s < kStages8; ++s) {
-      // leader's: one arrival (its own expect_tx) + the bytes of both CTAs, and both CTAs' gather warps
-      mbar_init(full_bar(s), kExperts ? 1 + 2 * kGatherWarps : 1);
+      // leader's: one arrival (its own expect_tx) + the bytes of both CTAs, and both CTAs' gather warp of the stage
+      mbar_init(full_bar(s), kExperts ? 1 + 2 : 1);
       mbar_init(empty_bar(s), 1);  // each CTA's: the pair's commit arrives on both
     }
     for (int b = 0; b < 2; ++b) {
@@ -281,7 +300,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
       if (e < p.n_mat) {
         const int lo = offs[e], hi = offs[e + 1];
         if (lo >= 0 && lo <= hi && hi <= p.n_tok)
-          tiles = ((hi - lo + kTileN - 1) / kTileN) * n_chan;
+          tiles = token_tiles(hi - lo) * n_chan;
         else if (blockIdx.x == 0)
           report_status(p.status, 4 /*RK_ERR_ROWS*/, RK_CHK_EXPERT_OFF, e);
       }
@@ -303,7 +322,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
     if (threadIdx.x == 0) first[p.n_mat] = base;
     n_tiles = base;
   } else {
-    n_tiles = n_chan * ((p.n_tok + kTileN - 1) / kTileN);
+    n_tiles = n_chan * token_tiles(p.n_tok);
   }
   // Tile t of the pair's sequence.  `e` walks up the experts as t grows.
   auto tile_at = [&](int t, int& e) -> Tile8 {
@@ -311,18 +330,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
     if constexpr (kExperts) {
       while (t >= first[e + 1]) ++e;
       const int i = t - first[e], tt = i / n_chan;
+      const int n = offs[e + 1] - offs[e], rows = token_tile_rows(n, token_tiles(n));
       r.mat = e;
       r.chan = (i - tt * n_chan) * kTileM;
-      r.tok = offs[e] + tt * kTileN;
-      r.n = min(kTileN, offs[e + 1] - r.tok);
+      r.tok = offs[e] + tt * rows;
+      r.n = min(rows, offs[e + 1] - r.tok);
     } else {
-      const int n_tok_tiles = (p.n_tok + kTileN - 1) / kTileN, per_band = kBandTok * n_chan;
+      const int n_tok_tiles = token_tiles(p.n_tok), rows = token_tile_rows(p.n_tok, n_tok_tiles), per_band = kBandTok * n_chan;
       const int band = t / per_band, here = min(kBandTok, n_tok_tiles - band * kBandTok), rem = t - band * per_band;
       const int cb = rem / here;
       r.mat = 0;
       r.chan = cb * kTileM;
-      r.tok = (band * kBandTok + rem - cb * here) * kTileN;
-      r.n = min(kTileN, p.n_tok - r.tok);
+      r.tok = (band * kBandTok + rem - cb * here) * rows;
+      r.n = min(rows, p.n_tok - r.tok);
     }
     return r;
   };
@@ -405,48 +425,47 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
         }
       }
     }
-  } else if (kExperts && warp >= 12) {
-    // ---- gather (by expert): rows of the half in steps of 16, four of them per warp, eight lanes to a row of 128 bytes ----
-    const int sub = (warp - 12) * 4 + (lane >> 3), chunk = lane & 7;
-    uint32_t it = 0;
-    int e = 0;
-    bool ok = true;
-    auto announce = [&](uint32_t i) {  // the copies of stage use i have landed: show them to the tensor cores
+  } else if (kExperts && (warp >= 12 || warp == 2 || warp == 3)) {
+    // ---- gather (by expert): a warp fills one stage of the ring over and over, so that all six may be under way.  Four rows
+    // per instruction, eight lanes to a row of 128 bytes ----
+    static_assert(kStages8 == kGatherWarps + 2, "one warp per stage");
+    const uint32_t s = warp >= 12 ? warp - 12 : warp + 2;
+    const int sub = lane >> 3, chunk = lane & 7;
+    const uint32_t dst = smem_base + s * S::kStageBytes + S::kABytes;
+    const uint32_t full_remote = mapa_shared(full_bar(s), 0);
+    int e = 0, t = pair, known = -1, half = 0, kc = (int)s;
+    uint32_t from[32];  // this lane's rows of the half, in units of 16 bytes from x
+    for (uint32_t use = 0;; ++use, kc += kStages8) {
+      for (; kc >= k_chunks; kc -= k_chunks) t += n_pairs;
+      if (t >= n_tiles) break;
+      if (t != known) {
+        const Tile8 tile = tile_at(t, e);
+        known = t;
+        half = ((tile.n + 31) >> 5) << 4;
+        uint32_t row[4];  // lane l has rows l, l + 32, ...; places behind the last repeat it (their sums are not stored)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int pr = p.rows[tile.tok + min((int)crank * half + 32 * j + lane, tile.n - 1)];
+          row[j] = ((unsigned)pr < (unsigned)p.n_tok ? (unsigned)pr / (unsigned)p.per : 0u) * (uint32_t)(p.k_pad >> 4);
+        }
+        // rows x k_pad / 16 stays below 2^32
+#pragma unroll
+        for (int i = 0; i < 32; ++i) from[i] = __shfl_sync(0xffffffffu, row[i >> 3], ((4 * i) & 31) + sub) + chunk;
+      }
+      bool ok = use == 0 || mbar_wait_bounded<false>(empty_bar(s), (use & 1u) ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const bool real = kc * kStep + 16 * chunk < p.k_pad;
+      const uint8_t* src = p.x + (real ? kc * kStep : 0);
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (4 * i < half) copy16_async(dst + sw128_offset(4 * i + sub, chunk), src + (uint64_t)from[i] * 16, real);
+      copies_commit();
+      copies_wait<0>();
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_remote(mapa_shared(full_bar(i % kStages8), 0));
-    };
-    for (int t = pair; t < n_tiles && ok; t += n_pairs) {
-      const Tile8 tile = tile_at(t, e);
-      const int half = ((tile.n + 31) >> 5) << 4;
-      const uint8_t* src[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        // places behind the last row repeat it (their sums are not stored)
-        const int pr = p.rows[tile.tok + min((int)crank * half + 16 * i + sub, tile.n - 1)];
-        const uint32_t row = (unsigned)pr < (unsigned)p.n_tok ? (unsigned)pr / (unsigned)p.per : 0u;
-        src[i] = p.x + (int64_t)row * p.k_pad + 16 * chunk;
-      }
-      for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
-        const uint32_t s = it % kStages8;
-        if (it >= (uint32_t)kStages8)
-          ok = mbar_wait_bounded<false>(empty_bar(s), ((it / kStages8) & 1u) ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        const uint32_t dst = smem_base + s * S::kStageBytes + S::kABytes;
-        const bool real = kc * kStep + 16 * chunk < p.k_pad;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (16 * i < half) copy16_async(dst + sw128_offset(16 * i + sub, chunk), real ? src[i] + kc * kStep : src[i], real);
-        copies_commit();
-        if (it >= (uint32_t)kGatherLag) {
-          copies_wait<kGatherLag>();
-          announce(it - kGatherLag);
-        }
-      }
+      if (lane == 0) mbar_arrive_remote(full_remote);
     }
-    copies_wait<0>();
-    for (uint32_t i = it > (uint32_t)kGatherLag ? it - kGatherLag : 0u; i < it && ok; ++i) announce(i);
   } else if (warp >= 4) {
     // ---- scales and stores: lane = channel, columns = token rows; the two groups of four warps take 32 columns in turn ----
     const int group = (warp - 4) >> 2, quad = warp & 3;
@@ -496,6 +515,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
         tmem_wait_ld();
         if (p.out_f32)
           store_columns<float>(o, toks + 256 * b + c0, static_cast<uint8_t*>(p.y) + (int64_t)chan * 4, sw, mine);
+        else if (p.paired)
+          store_columns_paired(o, toks + 256 * b + c0, static_cast<uint8_t*>(p.y) + (int64_t)(chan & ~1) * 2, sw, mine);
         else
           store_columns<__nv_bfloat16>(o, toks + 256 * b + c0, static_cast<uint8_t*>(p.y) + (int64_t)chan * 2, sw, mine);
       }
@@ -544,7 +565,8 @@ cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32
   return cudaGetLastError();
 }
 
-cudaError_t launch_matmul8(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
+cudaError_t launch_matmul8(Matmul8Params p, int sm_count, cudaStream_t stream) {
+  p.paired = !p.out_f32 && (reinterpret_cast<uintptr_t>(p.y) & 3u) == 0 && p.y_stride % 2 == 0 && p.n_out % 2 == 0;
   const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
   // by expert the number of tiles is known on the device only: at most one part-filled tile per expert more than full ones
   const int64_t tok_tiles = (p.n_tok + kTileN - 1) / kTileN + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
