@@ -30,6 +30,7 @@ struct rk_ctx {
   int sm_count = 0;
   int n_pairs = 0;
   int32_t matvec_slots[4] = {};
+  int32_t matmul8_slots[2] = {};
   DeviceStatus* d_status = nullptr;
   GemmBatch* d_batches = nullptr;  // [uv_g: G][uv_l: L][wa_g: G][wa_l: G][wb: 1]
   int off_uv_g = 0, off_uv_l = 0, off_wa_g = 0, off_wa_l = 0, off_wb = 0;
@@ -276,7 +277,7 @@ rk_status rk_create_ex(const rk_profile* prof, uint32_t flags, rk_ctx** out) {
   if (e == cudaSuccess) e = decode_attn_setup();
   if (e == cudaSuccess) e = matvec4_setup(ctx->matvec_slots, ctx->sm_count);
   if (e == cudaSuccess) e = experts_setup();
-  if (e == cudaSuccess) e = matmul8_setup();
+  if (e == cudaSuccess) e = matmul8_setup(ctx->matmul8_slots);
   if (e == cudaSuccess) e = sample_setup();
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&ctx->d_status), sizeof(DeviceStatus));
   if (e == cudaSuccess) e = cudaMemset(ctx->d_status, 0, sizeof(DeviceStatus));
@@ -1562,6 +1563,7 @@ static rk_status matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int3
   if (n_tok > 0 && !y) return fail(ctx, RK_ERR_NULL, "null argument");
   if (n_tok > 1 && y_stride < w->n_rows) return fail(ctx, RK_ERR_LAYOUT, "rows of y overlap");
   if (!aligned_to(y, out_dtype ? 4 : 2)) return fail(ctx, RK_ERR_ALIGN, "y must be aligned to its type");
+  if ((n_tok / 256 + w->n_mat + 1) * (w->n_rows / 256 + 1) > ((int64_t)1 << 30)) return fail(ctx, RK_ERR_ROWS, "too many tiles");
   s = device_check(ctx);
   if (s != RK_OK || n_tok == 0) return s;
   Matmul8Params p;
@@ -1584,7 +1586,7 @@ static rk_status matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int3
   p.n_mat = w->n_mat;
   p.per = per;
   p.out_f32 = out_dtype;
-  cudaError_t e = launch_matmul8(p, ctx->sm_count, static_cast<cudaStream_t>(stream));
+  cudaError_t e = launch_matmul8(p, ctx->sm_count, ctx->matmul8_slots, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "8-bit product launch");
 }
 

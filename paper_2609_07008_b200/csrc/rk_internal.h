@@ -309,11 +309,13 @@ struct Matmul8Params {
   unsigned long long wait_ns;
   int32_t n_tok;  // token rows; by expert: pairs (places of the list, rows of y)
   int32_t n_out, k_pad, n_mat, per, out_f32;
-  int32_t paired;  // set by the launcher: rows and channels allow 4-byte stores of bf16 pairs
+  // set by the launcher: rows and channels allow 4-byte stores of bf16 pairs; pairs of CTAs that share the k of a tile
+  int32_t paired, split;
 };
-cudaError_t matmul8_setup();
+// split_slots[i]: clusters of 4 << i thread blocks that run at the same time on the current device
+cudaError_t matmul8_setup(int32_t* split_slots);
 cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32_t k, void* codes, float* scales, cudaStream_t stream);
-cudaError_t launch_matmul8(Matmul8Params p, int sm_count, cudaStream_t stream);
+cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_slots, cudaStream_t stream);
 
 struct SampleParams {
   const void* logits;  // [n][vocab], rows `stride` elements apart

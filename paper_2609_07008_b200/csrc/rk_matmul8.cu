@@ -170,7 +170,7 @@ struct Smem8 {
   static constexpr uint32_t kOffBars = kStages8 * kStageBytes;  // full[stages], empty[stages], acc_full[2], acc_empty[2]
   static constexpr uint32_t kOffTmemPtr = kOffBars + (2 * kStages8 + 4) * 8;
   static constexpr uint32_t kOffAbort = kOffTmemPtr + 8;
-  static constexpr uint32_t kOffScan = kOffAbort + 8;               // 32 words of the block's scan
+  static constexpr uint32_t kOffScan = kOffAbort + 8;               // 16 sums of the block's scan
   static constexpr uint32_t kOffTok = (kOffScan + 128 + 15) / 16 * 16;  // [2][256] TokenOut
   static constexpr uint32_t kOffFirst = kOffTok + 2 * 256 * 16;     // by expert: first tile of each, [n_mat + 1]; then row_off
   static constexpr uint32_t kBytes = kOffFirst + 2 * (kMaxExperts + 1) * 4 + 1024 + 16;
@@ -247,16 +247,19 @@ __device__ __forceinline__ void store_columns_paired(const uint32_t (&o)[32], co
   }
 }
 
-template <bool kExperts>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8, 1)
+// kSplit: p.split pairs of a cluster share the k of one tile (a cluster has one tile then), and a CTA joins the sums of its
+// share of the token columns out of the others' shared memory.
+template <bool kExperts, bool kSplit>
+__global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8, 1)
     rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
   using S = Smem8;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t crank = cluster_ctarank();
-  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const uint32_t cluster_rank = cluster_ctarank(), crank = cluster_rank & 1u, lead = cluster_rank & ~1u;  // place in the pair; the pair's leader
+  const int split = kSplit ? p.split : 1;
+  const int pair = (int)blockIdx.x / (2 * split), n_pairs = (int)gridDim.x / (2 * split);
   auto full_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * s; };
   auto empty_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * (kStages8 + s); };
   auto acc_full_bar = [&](int b) -> uint32_t { return smem_base + S::kOffBars + 8u * (2 * kStages8 + b); };
@@ -267,7 +270,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
   int* offs = first + kMaxExperts + 1;
   const uint64_t limit = p.wait_ns;
   const int n_chan = (p.n_out + kTileM - 1) / kTileM;
-  const int k_chunks = (p.k_pad + kStep - 1) / kStep;
+  const int all_chunks = (p.k_pad + kStep - 1) / kStep;
+  const int k_first = kSplit ? all_chunks * (int)(cluster_rank >> 1) / split : 0;  // in steps of k
+  const int k_chunks = kSplit ? all_chunks * (int)((cluster_rank >> 1) + 1) / split - k_first : all_chunks;
 
   if (threadIdx.x == 0) {
     *abort_flag = 0;
@@ -290,37 +295,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
   int n_tiles;
   if constexpr (kExperts) {
     // the list's bounds, made safe: an expert's rows lie inside the list and behind the previous expert's
-    int* scan = reinterpret_cast<int*>(smem + S::kOffScan);
+    long long* scan = reinterpret_cast<long long*>(smem + S::kOffScan);
     for (int e = threadIdx.x; e <= p.n_mat; e += blockDim.x) offs[e] = p.row_off[e];
     __syncthreads();
-    int base = 0;
+    long long base = 0;
     for (int e0 = 0; e0 < p.n_mat; e0 += blockDim.x) {
       const int e = e0 + (int)threadIdx.x;
-      int tiles = 0;
+      long long tiles = 0;
       if (e < p.n_mat) {
         const int lo = offs[e], hi = offs[e + 1];
         if (lo >= 0 && lo <= hi && hi <= p.n_tok)
-          tiles = token_tiles(hi - lo) * n_chan;
+          tiles = (long long)token_tiles(hi - lo) * n_chan;
         else if (blockIdx.x == 0)
           report_status(p.status, 4 /*RK_ERR_ROWS*/, RK_CHK_EXPERT_OFF, e);
       }
-      int sum = tiles;
+      long long sum = tiles;
       for (int d = 1; d < 32; d <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, sum, d);
+        const long long v = __shfl_up_sync(0xffffffffu, sum, d);
         if (lane >= d) sum += v;
       }
       if (lane == 31) scan[warp] = sum;
       __syncthreads();
-      int before = base;
+      long long before = base;
       for (int w = 0; w < (int)blockDim.x / 32; ++w) {
         if (w < warp) before += scan[w];
         base += scan[w];
       }
-      if (e < p.n_mat) first[e] = before + sum - tiles;
+      if (e < p.n_mat) first[e] = (int)(before + sum - tiles);
       __syncthreads();
     }
-    if (threadIdx.x == 0) first[p.n_mat] = base;
-    n_tiles = base;
+    if (threadIdx.x == 0) first[p.n_mat] = (int)base;
+    // bounds that fall and rise again may name more rows than the list has; what 32 bits cannot count is left alone
+    n_tiles = base <= (1 << 30) ? (int)base : 0;
+    if (base > (1 << 30) && blockIdx.x == 0 && threadIdx.x == 0) report_status(p.status, 4 /*RK_ERR_ROWS*/, RK_CHK_EXPERT_OFF, p.n_mat);
   } else {
     n_tiles = n_chan * token_tiles(p.n_tok);
   }
@@ -373,12 +380,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
           ok = mbar_wait_bounded<false>(empty_bar(s), ((it / kStages8) & 1u) ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        const uint32_t full_remote = mapa_shared(full_bar(s), 0);
+        const uint32_t full_remote = mapa_shared(full_bar(s), lead);
         const uint32_t a_dst = smem_base + s * S::kStageBytes;
         if (elect_one()) {
           if (crank == 0) mbar_arrive_expect_tx(full_bar(s), 2 * kBytes);
-          tma_load_2d_pair(a_dst, &p.tm_w, full_remote, kc * kStep, w_row);
-          if constexpr (!kExperts) tma_load_2d_pair(a_dst + S::kABytes, &p.tm_x, full_remote, kc * kStep, tile.tok + (int)crank * half);
+          tma_load_2d_pair(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row);
+          if constexpr (!kExperts) tma_load_2d_pair(a_dst + S::kABytes, &p.tm_x, full_remote, (k_first + kc) * kStep, tile.tok + (int)crank * half);
         }
         __syncwarp();
       }
@@ -418,8 +425,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
 #pragma unroll
             for (int k = 0; k < 4; ++k)
               umma_i8_pair(acc, da + (uint64_t)(2 * k), db + (uint64_t)(2 * k), idesc, (kc > 0 || k > 0) ? 1u : 0u);
-            umma_commit_2_mc(empty_bar(s), 3);
-            if (kc == k_chunks - 1) umma_commit_2_mc(acc_full_bar(b), 3);
+            umma_commit_2_mc(empty_bar(s), (uint16_t)(3u << lead));
+            if (kc == k_chunks - 1) umma_commit_2_mc(acc_full_bar(b), (uint16_t)(3u << lead));
           }
           __syncwarp();
         }
@@ -432,7 +439,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
     const uint32_t s = warp >= 12 ? warp - 12 : warp + 2;
     const int sub = lane >> 3, chunk = lane & 7;
     const uint32_t dst = smem_base + s * S::kStageBytes + S::kABytes;
-    const uint32_t full_remote = mapa_shared(full_bar(s), 0);
+    const uint32_t full_remote = mapa_shared(full_bar(s), lead);
     int e = 0, t = pair, known = -1, half = 0, kc = (int)s;
     uint32_t from[32];  // this lane's rows of the half, in units of 16 bytes from x
     for (uint32_t use = 0;; ++use, kc += kStages8) {
@@ -470,7 +477,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
     // ---- scales and stores: lane = channel, columns = token rows; the two groups of four warps take 32 columns in turn ----
     const int group = (warp - 4) >> 2, quad = warp & 3;
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-    const uint32_t acc_empty_remote = mapa_shared(acc_empty_bar(0), 0);
+    const uint32_t acc_empty_remote = mapa_shared(acc_empty_bar(0), lead);
     TokenOut* toks = reinterpret_cast<TokenOut*>(smem + S::kOffTok);
     uint32_t tile_i = 0;
     int e = 0;
@@ -513,6 +520,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
         uint32_t o[32];
         tmem_ld_x32(tmem_base + lane_base + b * kTileN + c0, o);
         tmem_wait_ld();
+        if constexpr (kSplit) {  // into the ring, whose products are done: [token][channel]
+          uint32_t* part = reinterpret_cast<uint32_t*>(smem) + c0 * 128 + quad * 32 + lane;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) part[i * 128] = o[i];
+          continue;
+        }
         if (p.out_f32)
           store_columns<float>(o, toks + 256 * b + c0, static_cast<uint8_t*>(p.y) + (int64_t)chan * 4, sw, mine);
         else if (p.paired)
@@ -528,6 +541,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
   if (*abort_flag != 0) {
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
   }
+  if constexpr (kSplit) {
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();  // all partial sums are in shared memory
+    if (warp >= 4) {
+      int e = 0;
+      const Tile8 tile = tile_at(pair, e);
+      const int part = (((tile.n + 31) >> 5) << 5) / split;  // token columns of this CTA: a multiple of 8
+      const int begin = (int)(cluster_rank >> 1) * part, end = min(begin + part, tile.n);
+      const int quad = warp & 3, chan = tile.chan + (int)crank * 128 + quad * 32 + lane;
+      const bool mine = chan < p.n_out;
+      const float sw = mine ? p.sw[chan] : 0.f;
+      const TokenOut* toks = reinterpret_cast<const TokenOut*>(smem + S::kOffTok);
+      for (int c = begin + 4 * ((warp - 4) >> 2); c < end; c += 8) {
+        int sum[4] = {0, 0, 0, 0};
+        const uint32_t at = smem_base + (uint32_t)(c * 128 + quad * 32 + lane) * 4u;
+        for (int r = 0; r < split; ++r) {
+          const uint32_t from = mapa_shared(at, 2 * r + crank);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            int v;
+            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(from + 512u * i) : "memory");
+            sum[i] += v;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const TokenOut out = toks[c + i];
+          const float v = (float)sum[i] * out.scale * sw;
+          if (!mine || out.at < 0) continue;
+          if (p.out_f32)
+            *reinterpret_cast<float*>(static_cast<uint8_t*>(p.y) + out.at + (int64_t)chan * 4) = v;
+          else
+            *reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(p.y) + out.at + (int64_t)chan * 2) = __float2bfloat16_rn(v);
+        }
+      }
+    }
+  }
   __syncwarp();
   tc_fence_before_sync();
   __syncthreads();
@@ -539,12 +590,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kExperts ? kThreads8
   }
 }
 
+template <bool kExperts, bool kSplit>
+cudaLaunchConfig_t pair_config(int n_blocks, int cluster, cudaLaunchAttribute* attr, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(n_blocks);
+  cfg.blockDim = dim3(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8);
+  cfg.dynamicSmemBytes = Smem8::kBytes;
+  cfg.stream = stream;
+  attr->id = cudaLaunchAttributeClusterDimension;
+  attr->val.clusterDim.x = cluster;
+  attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cfg;
+}
+
 }  // namespace
 
-cudaError_t matmul8_setup() {
-  cudaError_t e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
+cudaError_t matmul8_setup(int32_t* split_slots) {
+  cudaError_t e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
+    e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
+  for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = pair_config<false, true>(4 << i, 4 << i, &attr, nullptr);
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, true>, &cfg);
+    split_slots[i] = n;
+  }
   return e;
 }
 
@@ -565,18 +640,29 @@ cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32
   return cudaGetLastError();
 }
 
-cudaError_t launch_matmul8(Matmul8Params p, int sm_count, cudaStream_t stream) {
+cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_slots, cudaStream_t stream) {
   p.paired = !p.out_f32 && (reinterpret_cast<uintptr_t>(p.y) & 3u) == 0 && p.y_stride % 2 == 0 && p.n_out % 2 == 0;
   const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
   // by expert the number of tiles is known on the device only: at most one part-filled tile per expert more than full ones
   const int64_t tok_tiles = (p.n_tok + kTileN - 1) / kTileN + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
   const int64_t tiles = n_chan * tok_tiles;
+  cudaLaunchAttribute attr;
+  if (!p.rows) {
+    // few tiles: k is shared by the pairs of a cluster, as long as all tiles run at once and a pair keeps eight steps of k
+    const int k_chunks = (p.k_pad + kStep - 1) / kStep;
+    p.split = tiles <= split_slots[1] && k_chunks >= 32 ? 4 : tiles <= split_slots[0] && k_chunks >= 16 ? 2 : 1;
+    if (p.split > 1) {
+      const cudaLaunchConfig_t cfg = pair_config<false, true>((int)tiles * 2 * p.split, 2 * p.split, &attr, stream);
+      return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, true>, p);
+    }
+  }
   const int n_pairs = (int)(tiles < sm_count / 2 ? tiles : sm_count / 2);
-  if (p.rows)
-    rk_matmul8_pair_kernel<true><<<2 * n_pairs, kThreads8 + 32 * kGatherWarps, Smem8::kBytes, stream>>>(p);
-  else
-    rk_matmul8_pair_kernel<false><<<2 * n_pairs, kThreads8, Smem8::kBytes, stream>>>(p);
-  return cudaGetLastError();
+  if (p.rows) {
+    const cudaLaunchConfig_t cfg = pair_config<true, false>(2 * n_pairs, 2, &attr, stream);
+    return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<true, false>, p);
+  }
+  const cudaLaunchConfig_t cfg = pair_config<false, false>(2 * n_pairs, 2, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false>, p);
 }
 
 }  // namespace rk
