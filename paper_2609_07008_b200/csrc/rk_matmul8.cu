@@ -247,9 +247,9 @@ __device__ __forceinline__ void store_columns_paired(const uint32_t (&o)[32], co
   }
 }
 
-// kSplit: p.split pairs of a cluster share the k of one tile (a cluster has one tile then), and a CTA joins the sums of its
+// kSplit > 1: that many pairs of a cluster share the k of one tile (a cluster has one tile then), and a CTA joins the sums of its
 // share of the token columns out of the others' shared memory.
-template <bool kExperts, bool kSplit>
+template <bool kExperts, int kSplit>
 __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8, 1)
     rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
   using S = Smem8;
@@ -258,8 +258,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t cluster_rank = cluster_ctarank(), crank = cluster_rank & 1u, lead = cluster_rank & ~1u;  // place in the pair; the pair's leader
-  const int split = kSplit ? p.split : 1;
-  const int pair = (int)blockIdx.x / (2 * split), n_pairs = (int)gridDim.x / (2 * split);
+  const int pair = (int)blockIdx.x / (2 * kSplit), n_pairs = (int)gridDim.x / (2 * kSplit);
   auto full_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * s; };
   auto empty_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * (kStages8 + s); };
   auto acc_full_bar = [&](int b) -> uint32_t { return smem_base + S::kOffBars + 8u * (2 * kStages8 + b); };
@@ -271,8 +270,8 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   const uint64_t limit = p.wait_ns;
   const int n_chan = (p.n_out + kTileM - 1) / kTileM;
   const int all_chunks = (p.k_pad + kStep - 1) / kStep;
-  const int k_first = kSplit ? all_chunks * (int)(cluster_rank >> 1) / split : 0;  // in steps of k
-  const int k_chunks = kSplit ? all_chunks * (int)((cluster_rank >> 1) + 1) / split - k_first : all_chunks;
+  const int k_first = kSplit > 1 ? all_chunks * (int)(cluster_rank >> 1) / kSplit : 0;  // in steps of k
+  const int k_chunks = kSplit > 1 ? all_chunks * (int)((cluster_rank >> 1) + 1) / kSplit - k_first : all_chunks;
 
   if (threadIdx.x == 0) {
     *abort_flag = 0;
@@ -366,28 +365,30 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
       tma_prefetch_desc(&p.tm_w);
       if (!kExperts) tma_prefetch_desc(&p.tm_x);
     }
-    uint32_t it = 0;
+    uint32_t it = 0, s = 0, turn = 0;  // uses of stages; the stage of this one, and its place among the stage's uses (mod 2)
     int e = 0;
     bool ok = true;
+    constexpr uint32_t kBytes = 2u * (S::kABytes + (kExperts ? 0u : S::kBBytes));
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const Tile8 tile = tile_at(t, e);
       const int half = ((tile.n + 31) >> 5) << 4;  // token rows of this CTA, a multiple of 16
       const int w_row = tile.mat * p.n_out + tile.chan + (int)crank * 128;
-      constexpr uint32_t kBytes = S::kABytes + (kExperts ? 0u : S::kBBytes);
       for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
-        const uint32_t s = it % kStages8;
-        if (it >= (uint32_t)kStages8)
-          ok = mbar_wait_bounded<false>(empty_bar(s), ((it / kStages8) & 1u) ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
+        if (it >= (uint32_t)kStages8) ok = mbar_wait_bounded<false>(empty_bar(s), turn ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         const uint32_t full_remote = mapa_shared(full_bar(s), lead);
         const uint32_t a_dst = smem_base + s * S::kStageBytes;
         if (elect_one()) {
-          if (crank == 0) mbar_arrive_expect_tx(full_bar(s), 2 * kBytes);
+          if (crank == 0) mbar_arrive_expect_tx(full_bar(s), kBytes);
           tma_load_2d_pair(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row);
           if constexpr (!kExperts) tma_load_2d_pair(a_dst + S::kABytes, &p.tm_x, full_remote, (k_first + kc) * kStep, tile.tok + (int)crank * half);
         }
         __syncwarp();
+        if (++s == (uint32_t)kStages8) {
+          s = 0;
+          turn ^= 1u;
+        }
       }
     }
     for (uint32_t back = 1; back <= (uint32_t)kStages8 && ok; ++back) {
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   } else if (warp == 1) {
     // ---- products (leader CTA only) ----
     if (crank == 0) {
-      uint32_t it = 0, tile_i = 0;
+      uint32_t s = 0, turn = 0, tile_i = 0;
       int e = 0;
       bool ok = true;
       for (int t = pair; t < n_tiles && ok; t += n_pairs, ++tile_i) {
@@ -414,9 +415,8 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
           tc_fence_after_sync();
         }
         const uint32_t acc = tmem_base + b * kTileN;
-        for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
-          const uint32_t s = it % kStages8;
-          ok = mbar_wait_bounded<false>(full_bar(s), (it / kStages8) & 1u, limit, abort_flag, p.status, WM_FULL, t);
+        for (int kc = 0; kc < k_chunks && ok; ++kc) {
+          ok = mbar_wait_bounded<false>(full_bar(s), turn, limit, abort_flag, p.status, WM_FULL, t);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           const uint32_t a_addr = smem_base + s * S::kStageBytes;
@@ -429,6 +429,10 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
             if (kc == k_chunks - 1) umma_commit_2_mc(acc_full_bar(b), (uint16_t)(3u << lead));
           }
           __syncwarp();
+          if (++s == (uint32_t)kStages8) {
+            s = 0;
+            turn ^= 1u;
+          }
         }
       }
     }
@@ -520,7 +524,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
         uint32_t o[32];
         tmem_ld_x32(tmem_base + lane_base + b * kTileN + c0, o);
         tmem_wait_ld();
-        if constexpr (kSplit) {  // into the ring, whose products are done: [token][channel]
+        if constexpr (kSplit > 1) {  // into the ring, whose products are done: [token][channel]
           uint32_t* part = reinterpret_cast<uint32_t*>(smem) + c0 * 128 + quad * 32 + lane;
 #pragma unroll
           for (int i = 0; i < 32; ++i) part[i * 128] = o[i];
@@ -541,40 +545,41 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   if (*abort_flag != 0) {
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
   }
-  if constexpr (kSplit) {
+  if constexpr (kSplit > 1) {
     __syncwarp();
     cluster_arrive();
     cluster_wait();  // all partial sums are in shared memory
     if (warp >= 4) {
       int e = 0;
       const Tile8 tile = tile_at(pair, e);
-      const int part = (((tile.n + 31) >> 5) << 5) / split;  // token columns of this CTA: a multiple of 8
+      const int part = (((tile.n + 31) >> 5) << 5) / kSplit;  // token columns of this CTA: a multiple of 8
       const int begin = (int)(cluster_rank >> 1) * part, end = min(begin + part, tile.n);
       const int quad = warp & 3, chan = tile.chan + (int)crank * 128 + quad * 32 + lane;
       const bool mine = chan < p.n_out;
       const float sw = mine ? p.sw[chan] : 0.f;
       const TokenOut* toks = reinterpret_cast<const TokenOut*>(smem + S::kOffTok);
-      for (int c = begin + 4 * ((warp - 4) >> 2); c < end; c += 8) {
-        int sum[4] = {0, 0, 0, 0};
+      constexpr int kCols = 4;  // columns at a time: all their loads (a trip to another SM each) are under way together
+      for (int c = begin + kCols * ((warp - 4) >> 2); c < end; c += 2 * kCols) {
+        int v[kSplit][kCols];
         const uint32_t at = smem_base + (uint32_t)(c * 128 + quad * 32 + lane) * 4u;
-        for (int r = 0; r < split; ++r) {
+#pragma unroll
+        for (int r = 0; r < kSplit; ++r) {
           const uint32_t from = mapa_shared(at, 2 * r + crank);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            int v;
-            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(from + 512u * i) : "memory");
-            sum[i] += v;
-          }
+          for (int i = 0; i < kCols; ++i) asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v[r][i]) : "r"(from + 512u * i));
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < kCols; ++i) {
+          int sum = v[0][i];
+#pragma unroll
+          for (int r = 1; r < kSplit; ++r) sum += v[r][i];
           const TokenOut out = toks[c + i];
-          const float v = (float)sum[i] * out.scale * sw;
+          const float f = (float)sum * out.scale * sw;
           if (!mine || out.at < 0) continue;
           if (p.out_f32)
-            *reinterpret_cast<float*>(static_cast<uint8_t*>(p.y) + out.at + (int64_t)chan * 4) = v;
+            *reinterpret_cast<float*>(static_cast<uint8_t*>(p.y) + out.at + (int64_t)chan * 4) = f;
           else
-            *reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(p.y) + out.at + (int64_t)chan * 2) = __float2bfloat16_rn(v);
+            *reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(p.y) + out.at + (int64_t)chan * 2) = __float2bfloat16_rn(f);
         }
       }
     }
@@ -590,7 +595,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   }
 }
 
-template <bool kExperts, bool kSplit>
+template <bool kExperts>
 cudaLaunchConfig_t pair_config(int n_blocks, int cluster, cudaLaunchAttribute* attr, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n_blocks);
@@ -608,16 +613,15 @@ cudaLaunchConfig_t pair_config(int n_blocks, int cluster, cudaLaunchAttribute* a
 }  // namespace
 
 cudaError_t matmul8_setup(int32_t* split_slots) {
-  cudaError_t e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(rk_matmul8_pair_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
+  cudaError_t e = cudaSuccess;
+  for (auto kernel : {rk_matmul8_pair_kernel<false, 1>, rk_matmul8_pair_kernel<true, 1>, rk_matmul8_pair_kernel<false, 2>, rk_matmul8_pair_kernel<false, 4>})
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
   for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = pair_config<false, true>(4 << i, 4 << i, &attr, nullptr);
+    const cudaLaunchConfig_t cfg = pair_config<false>(4 << i, 4 << i, &attr, nullptr);
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, true>, &cfg);
+    e = i == 0 ? cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, 2>, &cfg)
+               : cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, 4>, &cfg);
     split_slots[i] = n;
   }
   return e;
@@ -650,19 +654,19 @@ cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_s
   if (!p.rows) {
     // few tiles: k is shared by the pairs of a cluster, as long as all tiles run at once and a pair keeps eight steps of k
     const int k_chunks = (p.k_pad + kStep - 1) / kStep;
-    p.split = tiles <= split_slots[1] && k_chunks >= 32 ? 4 : tiles <= split_slots[0] && k_chunks >= 16 ? 2 : 1;
-    if (p.split > 1) {
-      const cudaLaunchConfig_t cfg = pair_config<false, true>((int)tiles * 2 * p.split, 2 * p.split, &attr, stream);
-      return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, true>, p);
+    const int split = tiles <= split_slots[1] && k_chunks >= 32 ? 4 : tiles <= split_slots[0] && k_chunks >= 16 ? 2 : 1;
+    if (split > 1) {
+      const cudaLaunchConfig_t cfg = pair_config<false>((int)tiles * 2 * split, 2 * split, &attr, stream);
+      return split == 4 ? cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, 4>, p) : cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, 2>, p);
     }
   }
   const int n_pairs = (int)(tiles < sm_count / 2 ? tiles : sm_count / 2);
   if (p.rows) {
-    const cudaLaunchConfig_t cfg = pair_config<true, false>(2 * n_pairs, 2, &attr, stream);
-    return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<true, false>, p);
+    const cudaLaunchConfig_t cfg = pair_config<true>(2 * n_pairs, 2, &attr, stream);
+    return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<true, 1>, p);
   }
-  const cudaLaunchConfig_t cfg = pair_config<false, false>(2 * n_pairs, 2, &attr, stream);
-  return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false>, p);
+  const cudaLaunchConfig_t cfg = pair_config<false>(2 * n_pairs, 2, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, 1>, p);
 }
 
 }  // namespace rk
