@@ -1,18 +1,19 @@
 // Sampling a token from each row of logits: temperature, top-k, top-p, min-p, and one given random number per row.
 //
-// p_i = exp((l_i - max) / T), as whole numbers of 2^-42 (a token below 2^-43 of the largest weighs nothing).  Whole numbers
+// p_i = exp((l_i - max) / T), as whole numbers of 2^-42 (a token below 2^-42 of the largest weighs nothing).  Whole numbers
 // add up to the same sum in any order, so that sums, cuts and the chosen token depend on the inputs alone, and their error
-// (2^-43 per token) is far below the distance at which two neighbouring tokens' borders could be confused.  The
-// exponential is taken in double: x = n + j / 64 + r, 2^-j/64 from a table, 2^-r by its Taylor series to degree 4
-// (|r| <= 1/128: 4e-14).
+// (2^-42 per token) is far below the distance at which two neighbouring tokens' borders could be confused.  The
+// exponential is taken in double: 256 x = i + r with i whole, 2^-i/256 from a table and a shift, 2^-r/256 by its Taylor
+// series to degree 3 (|r| <= 1/2: 1.4e-13).  A token costs eleven double-precision instructions that way, which bounds the
+// passes that need every token's weight; 64-bit conversions, four times as slow, are done in integers.
 //
 // The three filters each keep a prefix of one order, falling logit and then rising index, so together they keep the tokens
 // not below one (logit, index) pair, the cut.  A row belongs to a cluster of thread blocks, each with a run of consecutive tokens.
 //   1. the largest logit (and whether there is a NaN)
-//   2. where top-k or top-p is on: counts and sums in 2048 bins of (max - l) / T, joined in the first block; the tokens of
-//      the bin that holds a cut (some hundred of 128 K) go to the first block too, which sorts them and finds the cut.
+//   2. where top-k or top-p is on: counts and sums in bins of i, joined in the first block; the tokens of the bins that hold
+//      a cut (some hundred of 128 K) go to the first block too, which ranks them and finds the cut.
 //      Where they are too many (thousands of equal logits), the bin is taken apart by 11 bits of (logit, index) at a time.
-//   3. sums of what stays, by block and by warp; the warp that holds u * total walks its run
+//   3. sums of what stays, by block and by warp; the block that holds u * total shares out the warp's run that holds it
 // The row is read again by each step: it comes out of L2 after the first.
 #include <cuda_bf16.h>
 
@@ -21,13 +22,17 @@
 namespace rk {
 namespace {
 
+#ifndef SAMPLE_MAX
+#define SAMPLE_MAX 8
+#define SAMPLE_MIN 4096
+#endif
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kBinsPer = kBins / kThreads;
-constexpr int kList = 2048;                      // tokens of a cut's bin that are sorted in shared memory
+constexpr int kList = 2048, kListPer = kList / kThreads;  // tokens of a cut's bins that are ranked in shared memory
 constexpr int kUnitLog2 = 42;                    // weights are multiples of 2^-42
-constexpr float kOctaves = 43.f;                 // weights below 2^-43 round to nothing
+constexpr int kSteps = 256;                      // i counts 256ths of an octave below the largest
+constexpr int kEnd = kUnitLog2 * kSteps;         // from here on tokens weigh nothing
 constexpr int kIndexBits = 20, kDigitBits = 11, kKeyBits = 32 + kIndexBits, kDigits = (kKeyBits + kDigitBits - 1) / kDigitBits;
-constexpr int kUnroll = 4;                       // 16-byte loads that a thread has under way
 typedef unsigned long long u64;
 
 struct Found {           // what the first block of a row's cluster tells the others
@@ -41,21 +46,22 @@ struct Found {           // what the first block of a row's cluster tells the ot
 };
 
 struct Shared {
-  double table[64];              // 2^(-j/64)
+  double table[kSteps];          // 2^(42 - j/256)
   u64 list[2][kList];            // (key, index) of the tokens in bin_k and in bin_lo .. bin_hi
+  u64 mass[kThreads];            // weights of a short list
   uint32_t listed[2];
   uint32_t count[kBins], lo[kBins], hi[kBins];
-  u64 slot64[8];                 // one word per block of the cluster
-  u64 slot64b[8];
+  u64 slot64b[8];                // one word per block of the cluster
+  u64 slot_part[kWarps];
   u64 warp64[kWarps];
   uint32_t warp32[kWarps];
-  uint32_t nan[8];
+  float top[8];
+  uint32_t first[8];
   Found found;
   int pick_bin;
   uint32_t pick_count;           // tokens in front of the picked bin
   u64 pick_mass;                 // and their sum
   u64 pick_own;                  // sum of the picked bin
-  uint32_t picked;
 };
 
 // order of logits: larger key, larger logit; both zeros are one
@@ -89,22 +95,48 @@ __device__ __forceinline__ void cluster_sync() {
   cluster_wait();
 }
 
+// fp32 -> fp64 for finite numbers, in integers; below fp32's normal numbers it is off by up to 2^-126
+__device__ __forceinline__ double widen(float f) {
+  const uint32_t b = __float_as_uint(f);
+  return __hiloint2double((int)((((b & 0x7fffffffu) >> 3) + 0x38000000u) | (b & 0x80000000u)), (int)(b << 29));
+}
+
 struct Weights {
-  float top;       // the largest logit
-  double rate;     // log2(e) / T
+  double top, rate;     // the largest logit; 256 log2(e) / T
   const double* table;
-  // octaves below the largest: log2(p_max / p)
-  __device__ __forceinline__ double octaves(float l) const { return l == top ? 0.0 : ((double)top - (double)l) * rate; }
-  __device__ __forceinline__ double weight(double x) const {  // 2^-x for 0 <= x < 44
-    const double s = rint(x * 64.0);
-    const double r = fma(s, -0x1p-6, x) * -0.69314718055994530942;
-    const double e = fma(fma(fma(fma(r, 1.0 / 24.0, 1.0 / 6.0), r, 0.5), r, 1.0), r, 1.0);
-    const int i = (int)s;
-    return __hiloint2double((1023 - (i >> 6)) << 20, 0) * (table[i & 63] * e);
+  // Place i of a logit on the scale of 256ths of an octave below the largest, and the rest; only for logits down to kEnd.
+  __device__ __forceinline__ int place(float l, double& rest) const {
+    constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum has the nearest whole number in its low word
+    const double s = (top - widen(l)) * rate, t = s + kMagic;
+    rest = s - (t - kMagic);
+    return __double2loint(t);
+  }
+  // 2^(42 - (i mod 256 + rest) / 256)
+  __device__ __forceinline__ double scaled(int i, double r) const {
+    constexpr double c1 = -0.69314718055994530942 / kSteps, c2 = c1 * c1 / 2.0, c3 = c1 * c1 * c1 / 6.0;
+    const double t = table[i & (kSteps - 1)];
+    return fma(t, r * fma(fma(c3, r, c2), r, c1), t);
+  }
+  __device__ __forceinline__ u64 units(double v, int i) const {  // scaled() as the whole number of 2^-42 that the token weighs
+    return (u64)(__double_as_longlong(v + 0x1p52) & ((1ll << 52) - 1)) >> (i >> 8);
+  }
+  __device__ __forceinline__ u64 units(float l) const {
+    double r;
+    const int i = place(l, r);
+    return units(scaled(i, r), i);
   }
 };
-__device__ __forceinline__ u64 units(double weight) { return (u64)__double2ll_rn(weight * (double)(1ull << kUnitLog2)); }
-__device__ __forceinline__ int coarse_bin(double x) { return min((int)((float)x * ((float)kBins / kOctaves)), kBins - 1); }
+// bins of i: 64 to an octave for the first 16 octaves, then 32
+constexpr int kFine = 16 * kSteps;
+__device__ __forceinline__ int bin_of(int i) { return i < kFine ? i >> 2 : (kFine >> 2) + ((i - kFine) >> 3); }
+__device__ __forceinline__ int bin_begin(int b) { return b < kFine >> 2 ? b << 2 : kFine + ((b - (kFine >> 2)) << 3); }
+static_assert((kFine >> 2) + ((kEnd - kFine) >> 3) <= kBins, "bins");
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 
 // A thread block's run of a row.  A warp has consecutive 16-byte units of it, one per lane and step; units that reach over
 // an end of the row are put together from single loads.
@@ -144,29 +176,63 @@ struct Run {
     if constexpr (kBf16) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
     return __uint_as_float(w[e]);
   }
-  // f(logit, index) for every token of the warp, ascending within a lane
-  template <class F>
-  __device__ __forceinline__ void each(F f) const {
+  // f(logit, index) for every token of the warp with a logit of at least `least`, ascending within a lane; kAhead units are
+  // loaded together
+  template <int kAhead, class F>
+  __device__ __forceinline__ void each(float least, F f) const {
     const int lane = threadIdx.x & 31;
-    for (int u0 = first + lane; u0 < last; u0 += 32 * kUnroll) {
-      uint4 v[kUnroll];
+    for (int u0 = first + lane; u0 < last; u0 += 32 * kAhead) {
+      uint4 v[kAhead];
 #pragma unroll
-      for (int j = 0; j < kUnroll; ++j)
+      for (int j = 0; j < kAhead; ++j)
         if (u0 + 32 * j < last) v[j] = load(u0 + 32 * j);
 #pragma unroll
-      for (int j = 0; j < kUnroll; ++j) {
+      for (int j = 0; j < kAhead; ++j) {
         if (u0 + 32 * j >= last) break;
         const int i = index(u0 + 32 * j);
 #pragma unroll
-        for (int e = 0; e < kUnit; ++e)
-          if ((unsigned)(i + e) < (unsigned)vocab) f(value(v[j], e), i + e);
+        for (int e = 0; e < kUnit; ++e) {
+          const float l = value(v[j], e);
+          if (l >= least && (unsigned)(i + e) < (unsigned)vocab) f(l, i + e);
+        }
       }
     }
+  }
+  // the largest logit, NaN if there is one (in this lane)
+  __device__ __forceinline__ float top() const {
+    constexpr int kAhead = 4;
+    const int lane = threadIdx.x & 31;
+    const float none = -__int_as_float(0x7f800000);
+    float m = none;
+    for (int u0 = first + lane; u0 < last; u0 += 32 * kAhead) {
+      uint4 v[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) v[j] = u0 + 32 * j < last ? load(u0 + 32 * j) : load(u0);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int u = u0 + 32 * j < last ? u0 + 32 * j : u0;
+        if (whole(u)) {
+          if constexpr (kBf16) {
+            uint32_t a, b;
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v[j].x), "r"(v[j].y));
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v[j].z), "r"(v[j].w));
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+            m = max_nan(m, max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u)));
+          } else {
+            m = max_nan(max_nan(m, max_nan(__uint_as_float(v[j].x), __uint_as_float(v[j].y))), max_nan(__uint_as_float(v[j].z), __uint_as_float(v[j].w)));
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < kUnit; ++e) m = max_nan(m, (unsigned)(index(u) + e) < (unsigned)vocab ? value(v[j], e) : none);
+        }
+      }
+    }
+    return m;
   }
 };
 
 // Sorts list[0 .. n) descending; n <= kList.  All threads of the block; ends with a barrier.
-__device__ __forceinline__ void sort_list(u64* list, int n) {
+__device__ __noinline__ void sort_list(u64* list, int n) {
   int size = 2;
   while (size < n) size *= 2;
   for (int i = n + (int)threadIdx.x; i < size; i += kThreads) list[i] = 0ull;
@@ -194,97 +260,82 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const int n_blocks = p.blocks, rank = (int)cluster_ctarank();
   const int64_t row = blockIdx.x / n_blocks;
   const unsigned all = 0xffffffffu;
+  const float inf = __int_as_float(0x7f800000);
   const Run<kBf16> run(p.logits, row * p.stride, p.vocab, rank, n_blocks, warp);
   auto peer = [&](const void* at, int r) -> uint32_t { return mapa_shared(smem_u32(at), r); };
   auto clear_bins = [&] {
     for (int b = tid; b < kBins; b += kThreads) sh.count[b] = sh.lo[b] = sh.hi[b] = 0u;
   };
 
-  if (tid < 64) sh.table[tid] = exp2(-(double)tid / 64.0);
   if (tid < 2) sh.listed[tid] = 0u;
+  for (int j = tid; j < kSteps; j += kThreads) sh.table[j] = exp2((double)kUnitLog2 - (double)j / kSteps);
   clear_bins();
 
-  // ---- 1. the largest logit and the lowest index that has it ----
-  u64 best = 0;
-  {
-    float top = -__int_as_float(0x7f800000);
-    int at = 0;
-    bool nan = false;
-    run.each([&](float l, int i) {
-      nan |= l != l;
-      if (l > top) {
-        top = l;
-        at = i;
-      }
-    });
-    best = ((u64)key_of(top) << 32) | (uint32_t)~at;
+  // ---- 1. the largest logit ----
+  float top = run.top();
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      const u64 o = __shfl_xor_sync(all, best, d);
-      best = o > best ? o : best;
-    }
-    if (lane == 0) sh.warp64[warp] = best;
-    const int any_nan = __syncthreads_or(nan);
-    if (tid == 0) {
-      for (int w = 1; w < kWarps; ++w) best = sh.warp64[w] > best ? sh.warp64[w] : best;
-      sh.slot64[rank] = best;
-      sh.nan[rank] = any_nan;
-    }
+  for (int d = 16; d > 0; d >>= 1) top = max_nan(top, __shfl_xor_sync(all, top, d));
+  if (lane == 0) sh.warp32[warp] = __float_as_uint(top);
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < kWarps; ++w) top = max_nan(top, __uint_as_float(sh.warp32[w]));
+    sh.top[rank] = top;
   }
   cluster_sync();
-  uint32_t nan_all = 0;
-  best = 0;
-  for (int r = 0; r < n_blocks; ++r) {
-    const u64 o = ld_cluster_u64(peer(&sh.slot64[r], r));
-    nan_all |= ld_cluster_u32(peer(&sh.nan[r], r));
-    best = o > best ? o : best;
-  }
-  const float top = logit_of((uint32_t)(best >> 32));
-  const int first = (int)~(uint32_t)best;
+  top = -inf;
+  for (int r = 0; r < n_blocks; ++r) top = max_nan(top, __uint_as_float(ld_cluster_u32(peer(&sh.top[r], r))));
   const float temp = p.temperature ? p.temperature[row] : 1.f;
-  const bool dead = nan_all || !(top > -__int_as_float(0x7f800000));
-  if (dead || !(temp > 0.f)) {
+  const int top_k = p.top_k ? p.top_k[row] : 0;
+  const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
+  const bool dead = !(top > -inf);
+  const bool one = !(temp > 0.f) || top_p <= 0.f || min_p > 1.f || top_k == 1;  // the first token only
+  if (dead || one) {
+    uint32_t at = 0xffffffffu;
+    if (!dead) run.template each<2>(top, [&](float, int i) { at = min(at, (uint32_t)i); });
+    at = __reduce_min_sync(all, at);
+    __syncthreads();
+    if (lane == 0) sh.warp32[warp] = at;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kWarps; ++w) at = min(at, sh.warp32[w]);
+      sh.first[rank] = at;
+    }
+    cluster_sync();
     if (rank == 0 && tid == 0) {
-      p.tokens[row] = dead ? -1 : first;
+      for (int r = 1; r < n_blocks; ++r) at = min(at, ld_cluster_u32(peer(&sh.first[r], r)));
+      p.tokens[row] = dead ? -1 : (int)at;
       if (p.probs) p.probs[row] = dead ? __int_as_float(0x7fc00000) : 1.f;
     }
-    cluster_sync();  // the others may still be reading this block's slots
+    cluster_sync();  // no block leaves while the first one reads
     return;
   }
   Weights w;
-  w.top = top;
-  w.rate = 1.44269504088896340736 / (double)temp;
+  w.top = widen(top);
+  w.rate = (double)kSteps * 1.44269504088896340736 / (double)temp;
   w.table = sh.table;
 
-  const int top_k = p.top_k ? p.top_k[row] : 0;
-  const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
   u64 cut = 0;  // tokens whose composite is at least this stay
-  if (top_p <= 0.f || min_p > 1.f || top_k == 1) cut = composite(top, first);
-  const bool by_mass = cut == 0 && top_p < 1.f;
-  const bool by_count = cut == 0 && top_k > 1 && top_k < p.vocab;
-  // logits below this weigh nothing (a little lower than exactly, rounding included): a cheap test in front of the double one
-  const float floor_all = top == __int_as_float(0x7f800000) ? top : (float)((double)top - 43.01 / w.rate - 1e-6 * fabs((double)top));
+  const bool by_mass = top_p < 1.f, by_count = top_k > 1 && top_k < p.vocab;
+  // A logit that is at least `steps` 256ths of an octave below the largest, or a little less (rounding included): a cheap
+  // test in front of the double one.  -inf is never above it, and next to +inf nothing else is.
+  auto below = [&](double steps) -> float {
+    if (top == inf) return top;
+    return fmaxf((float)((double)top - steps / w.rate - 1e-6 * fabs((double)top)), -3.402823466e38f);
+  };
+  const float floor_all = below((double)kEnd + 4.0);
 
   // ---- 2. the cut ----
-  // Adds a token to a bin.
-  auto add_bin = [&](int b, bool mass, double x) {
+  auto add_bin = [&](int b, bool mass, int i, double rest) {
     atomicAdd(&sh.count[b], 1u);
     if (mass) {
-      const u64 u = units(w.weight(x));
+      const u64 u = w.units(w.scaled(i, rest), i);
       const uint32_t add = (uint32_t)u, old = atomicAdd(&sh.lo[b], add);
       const uint32_t carry = (uint32_t)(u >> 32) + (old + add < old ? 1u : 0u);
       if (carry) atomicAdd(&sh.hi[b], carry);
     }
   };
-  // This thread's bins kBinsPer * tid ...: exclusive sums over the block (its own bins only, no other blocks').
-  auto scan_bins = [&](const uint32_t (&c)[kBinsPer], const u64 (&m)[kBinsPer], uint32_t& cb, u64& mb) {
-    uint32_t csum = 0;
-    u64 msum = 0;
-#pragma unroll
-    for (int j = 0; j < kBinsPer; ++j) {
-      csum += c[j];
-      msum += m[j];
-    }
+  // Exclusive sums over the block's threads, added to cb and mb.
+  auto scan_bins = [&](uint32_t csum, u64 msum, uint32_t& cb, u64& mb) {
     uint32_t cx = csum;
     u64 mx = msum;
 #pragma unroll
@@ -309,78 +360,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       mb += sh.warp64[v];
     }
   };
-  // ---- by digits: for bins too full to be sorted.  Counts and sums over the tokens for which digit(l, x, i) is a bin ----
-  auto histogram = [&](auto digit) {
-    clear_bins();
-    __syncthreads();
-    run.each([&](float l, int i) {
-      if (l < floor_all) return;
-      const double x = w.octaves(l);
-      if (!(x < (double)kOctaves)) return;
-      const int b = digit(l, x, i);
-      if (b >= 0) add_bin(b, true, x);
-    });
-    cluster_sync();
-  };
-  // The bin with before < want <= before + its own, in counts (want_count) or sums (want_mass).  base_*: in front of bin 0.
-  auto pick = [&](bool by_sum, uint32_t base_count, u64 base_mass, uint32_t want_count, double want_mass) {
-    uint32_t c[kBinsPer];
-    u64 m[kBinsPer];
-#pragma unroll
-    for (int j = 0; j < kBinsPer; ++j) {
-      const int b = tid * kBinsPer + j;
-      c[j] = 0;
-      m[j] = 0;
-      for (int r = 0; r < n_blocks; ++r) {
-        c[j] += ld_cluster_u32(peer(&sh.count[b], r));
-        m[j] += ((u64)ld_cluster_u32(peer(&sh.hi[b], r)) << 32) + ld_cluster_u32(peer(&sh.lo[b], r));
-      }
-    }
-    uint32_t cb = base_count;
-    u64 mb = base_mass;
-    scan_bins(c, m, cb, mb);
-#pragma unroll
-    for (int j = 0; j < kBinsPer; ++j) {
-      if (c[j] != 0u && (by_sum ? (double)mb < want_mass && !((double)(mb + m[j]) < want_mass) : cb < want_count && want_count <= cb + c[j])) {
-        sh.pick_bin = tid * kBinsPer + j;
-        sh.pick_count = cb;
-        sh.pick_mass = mb;
-        sh.pick_own = m[j];
-      }
-      cb += c[j];
-      mb += m[j];
-    }
-    cluster_sync();  // nobody clears its bins before all have read them
-  };
-  // The last token in the order with before < want; sets `cut` and returns the sum up to and with it.
-  auto search = [&](bool by_sum, uint32_t want_count, double want_mass) -> u64 {
-    histogram([&](float, double x, int) -> int { return coarse_bin(x); });
-    pick(by_sum, 0u, 0ull, want_count, want_mass);
-    const int bin = sh.pick_bin;
-    uint32_t base_count = sh.pick_count;
-    u64 base_mass = sh.pick_mass, prefix = 0;
-    for (int d = kDigits - 1; d >= 0; --d) {
-      const int shift = d * kDigitBits;
-      histogram([&](float l, double x, int i) -> int {
-        if (coarse_bin(x) != bin) return -1;
-        const u64 c = composite(l, i);
-        if (d < kDigits - 1 && c >> (shift + kDigitBits) != prefix) return -1;
-        return kBins - 1 - (int)((c >> shift) & (kBins - 1));  // the largest first
-      });
-      pick(by_sum, base_count, base_mass, want_count, want_mass);
-      prefix = (prefix << kDigitBits) | (u64)(kBins - 1 - sh.pick_bin);
-      base_count = sh.pick_count;
-      base_mass = sh.pick_mass;
-    }
-    cut = prefix > cut ? prefix : cut;
-    return base_mass + sh.pick_own;
-  };
 
   if (by_count || by_mass) {
-    run.each([&](float l, int) {
-      if (l < floor_all) return;
-      const double x = w.octaves(l);
-      if (x < (double)kOctaves) add_bin(coarse_bin(x), by_mass, x);
+    run.template each<2>(floor_all, [&](float l, int) {
+      double rest;
+      const int i = w.place(l, rest);
+      if (i < kEnd) add_bin(bin_of(i), by_mass, i, rest);
     });
     __syncthreads();
     if (rank != 0) {
@@ -396,22 +381,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     cluster_sync();
     if (rank == 0) {
-      uint32_t c[kBinsPer], cb0 = 0;
-      u64 m[kBinsPer], mb0 = 0;
+      uint32_t c[kBinsPer], csum = 0, cb0 = 0;
+      u64 m[kBinsPer], msum = 0, mb0 = 0;
 #pragma unroll
       for (int j = 0; j < kBinsPer; ++j) {
-        c[j] = sh.count[tid * kBinsPer + j];
-        m[j] = ((u64)sh.hi[tid * kBinsPer + j] << 32) + sh.lo[tid * kBinsPer + j];
+        csum += c[j] = sh.count[tid * kBinsPer + j];
+        msum += m[j] = ((u64)sh.hi[tid * kBinsPer + j] << 32) + sh.lo[tid * kBinsPer + j];
       }
-      scan_bins(c, m, cb0, mb0);
+      scan_bins(csum, msum, cb0, mb0);
       if (tid == 0) {
         sh.found.bin_k = sh.found.bin_lo = sh.found.bin_hi = -1;
         sh.found.slow = 0;
         sh.found.mass_lo = 0;
-        u64 t = 0;
-        for (int v = 0; v < kWarps; ++v) t += sh.warp64[v];
-        sh.found.total = t;
+        sh.found.cut = 0;
       }
+      if (tid == kThreads - 1) sh.found.total = mb0 + msum;
       __syncthreads();
       uint32_t cb = cb0;
       u64 mb = mb0;
@@ -449,112 +433,192 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     cluster_sync();
     const int bin_k = (int)ld_cluster_u32(peer(&sh.found.bin_k, 0));
     const int bin_lo = (int)ld_cluster_u32(peer(&sh.found.bin_lo, 0)), bin_hi = (int)ld_cluster_u32(peer(&sh.found.bin_hi, 0));
-    run.each([&](float l, int i) {
-      if (l < floor_all) return;
-      const double x = w.octaves(l);
-      if (!(x < (double)kOctaves)) return;
-      const int b = coarse_bin(x);
-      if (b == bin_k) {
-        const uint32_t at = add_cluster_u32(peer(&sh.listed[0], 0), 1u);
-        if (at < kList) st_cluster_u64(peer(&sh.list[0][at], 0), composite(l, i));
+    {
+      // one window of logits around the bins; the doubles decide inside it
+      int from = kBins, to = -1;
+      if (bin_k >= 0) from = to = bin_k;
+      if (by_mass) {
+        from = min(from, bin_lo);
+        to = max(to, bin_hi);
       }
-      if (by_mass && b >= bin_lo && b <= bin_hi) {
-        const uint32_t at = add_cluster_u32(peer(&sh.listed[1], 0), 1u);
-        if (at < kList) st_cluster_u64(peer(&sh.list[1][at], 0), composite(l, i));
-      }
-    });
+      const float high = from <= 0 || top == inf ? inf : (float)((double)top - (double)(bin_begin(from) - 2) / w.rate + 1e-6 * fabs((double)top));
+      const float low = fmaxf(floor_all, below((double)bin_begin(to + 1) + 2.0));
+      run.template each<2>(low, [&](float l, int at) {
+        if (l > high) return;
+        double rest;
+        const int i = w.place(l, rest), b = bin_of(i);
+        if (i >= kEnd) return;
+        if (b == bin_k) {
+          const uint32_t slot = add_cluster_u32(peer(&sh.listed[0], 0), 1u);
+          if (slot < kList) st_cluster_u64(peer(&sh.list[0][slot], 0), composite(l, at));
+        }
+        if (by_mass && b >= bin_lo && b <= bin_hi) {
+          const uint32_t slot = add_cluster_u32(peer(&sh.listed[1], 0), 1u);
+          if (slot < kList) st_cluster_u64(peer(&sh.list[1][slot], 0), composite(l, at));
+        }
+      });
+    }
     cluster_sync();
     if (rank == 0) {
       const uint32_t n_k = bin_k >= 0 ? sh.listed[0] : 0u, n_p = by_mass ? sh.listed[1] : 0u;
       if (n_k > kList || n_p > kList) {
         if (tid == 0) sh.found.slow = 1;
       } else {
-        // a list in order, `per` consecutive places per thread: the sum in front of this thread's places
-        auto sum_in_front = [&](const u64* list, uint32_t n, u64 base) -> u64 {
-          const uint32_t lo = tid * (kList / kThreads);
-          u64 mine = 0;
-          for (uint32_t j = lo; j < lo + kList / kThreads && j < n; ++j) mine += units(w.weight(w.octaves(logit_of((uint32_t)(list[j] >> kIndexBits)))));
-          u64 x = mine;
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) {
-            const u64 v = __shfl_up_sync(all, x, d);
-            if (lane >= d) x += v;
-          }
-          __syncthreads();
-          if (lane == 31) sh.warp64[warp] = x;
-          __syncthreads();
-          x += base - mine;
-          for (int v = 0; v < warp; ++v) x += sh.warp64[v];
-          return x;
-        };
-        if (tid == 0) sh.found.cut = 0;
-        u64 total = sh.found.total;
-        if (bin_k >= 0) {
-          sort_list(sh.list[0], (int)n_k);
-          const uint32_t at = (uint32_t)top_k - sh.found.count_k - 1;  // place of the k-th token
-          if (tid == 0) sh.found.cut = sh.list[0][at];
-          if (by_mass) {
-            u64 front = sum_in_front(sh.list[0], n_k, sh.found.mass_k);
-            for (uint32_t j = tid * (kList / kThreads); j < (tid + 1) * (kList / kThreads) && j <= at; ++j) {
-              front += units(w.weight(w.octaves(logit_of((uint32_t)(sh.list[0][j] >> kIndexBits)))));
-              if (j == at) sh.pick_mass = front;
-            }
+        auto mass_of = [&](u64 c) -> u64 { return w.units(logit_of((uint32_t)(c >> kIndexBits))); };
+        // The last token of list[0 .. n) in the order with fewer than want_count in front of it, or (by sum) with less than
+        // want_mass; base_*: in front of the list.  Leaves it in pick_own, and the sum up to and with it in pick_mass.
+        // Up to one token per thread, a thread counts what is in front of its own; longer lists are sorted.
+        auto last_of = [&](u64* list, uint32_t n, bool by_sum, uint32_t base_count, u64 base_mass, uint32_t want_count, double want_mass) {
+          if (n <= kThreads) {
+            const u64 mine = tid < (int)n ? list[tid] : 0ull, own = tid < (int)n ? mass_of(mine) : 0ull;
+            sh.mass[tid] = own;
             __syncthreads();
-            total = sh.pick_mass;
+            if (tid < (int)n) {
+              uint32_t front = base_count;
+              u64 sum = base_mass;
+              for (uint32_t j = 0; j < n; ++j) {
+                const bool before = list[j] > mine;
+                front += before;
+                sum += before ? sh.mass[j] : 0ull;
+              }
+              const bool last = front + 1 == base_count + n;
+              if (by_sum ? (double)sum < want_mass && (last || !((double)(sum + own) < want_mass)) : front + 1 == want_count) {
+                sh.pick_own = mine;
+                sh.pick_mass = sum + own;
+              }
+            }
+          } else {
+            sort_list(list, (int)n);
+            const uint32_t lo = tid * kListPer, hi = min(lo + kListPer, n);
+            u64 mine = 0, sum = base_mass;
+            for (uint32_t j = lo; j < hi; ++j) mine += mass_of(list[j]);
+            uint32_t unused = 0;
+            scan_bins(0u, mine, unused, sum);
+            for (uint32_t j = lo; j < hi; ++j) {
+              const u64 next = sum + mass_of(list[j]);
+              if (by_sum ? (double)sum < want_mass && (j + 1 == n || !((double)next < want_mass)) : base_count + j + 1 == want_count) {
+                sh.pick_own = list[j];
+                sh.pick_mass = next;
+              }
+              sum = next;
+            }
           }
+          __syncthreads();
+        };
+        u64 total = sh.found.total, found = 0;
+        if (bin_k >= 0) {
+          last_of(sh.list[0], n_k, false, sh.found.count_k, sh.found.mass_k, (uint32_t)top_k, 0.0);
+          total = sh.pick_mass;
+          found = sh.pick_own;
+          __syncthreads();
         }
         if (by_mass) {
-          sort_list(sh.list[1], (int)n_p);
-          const double want = (double)top_p * (double)total;
-          u64 front = sum_in_front(sh.list[1], n_p, sh.found.mass_lo);
-          for (uint32_t j = tid * (kList / kThreads); j < (tid + 1) * (kList / kThreads) && j < n_p; ++j) {
-            const u64 next = front + units(w.weight(w.octaves(logit_of((uint32_t)(sh.list[1][j] >> kIndexBits)))));
-            // the last one with less than `want` in front of it
-            if ((double)front < want && (!((double)next < want) || j + 1 == n_p)) sh.pick_own = sh.list[1][j];
-            front = next;
-          }
-          __syncthreads();
-          if (tid == 0 && sh.pick_own > sh.found.cut) sh.found.cut = sh.pick_own;
+          last_of(sh.list[1], n_p, true, 0u, sh.found.mass_lo, 0u, (double)top_p * (double)total);
+          found = sh.pick_own > found ? sh.pick_own : found;
         }
+        if (tid == 0) sh.found.cut = found;
       }
     }
     cluster_sync();
     if (ld_cluster_u32(peer(&sh.found.slow, 0)) == 0u) {
       cut = ld_cluster_u64(peer(&sh.found.cut, 0));
     } else {
+      // by digits: counts and sums over the tokens of a bin that share a prefix, 11 bits of (logit, index) further each time
       u64 total = ld_cluster_u64(peer(&sh.found.total, 0));
-      if (bin_k >= 0) total = search(false, (uint32_t)top_k, 0.0);
-      if (by_mass) search(true, 0u, (double)top_p * (double)total);
+#pragma unroll 1
+      for (int task = 0; task < 2; ++task) {
+        const bool by_sum = task == 1;
+        if (by_sum ? !by_mass : bin_k < 0) continue;
+        const double want_mass = (double)top_p * (double)total;
+        int bin = 0;
+        uint32_t base_count = 0;
+        u64 base_mass = 0, prefix = 0;
+#pragma unroll 1
+        for (int d = kDigits; d >= 0; --d) {  // the first time over the bins
+          const int shift = d * kDigitBits;
+          clear_bins();
+          __syncthreads();
+          run.template each<1>(floor_all, [&](float l, int at) {
+            double rest;
+            const int i = w.place(l, rest);
+            if (i >= kEnd) return;
+            int b = bin_of(i);
+            if (d < kDigits) {
+              if (b != bin) return;
+              const u64 c = composite(l, at);
+              if (d < kDigits - 1 && c >> (shift + kDigitBits) != prefix) return;
+              b = kBins - 1 - (int)((c >> shift) & (kBins - 1));  // the largest first
+            }
+            add_bin(b, true, i, rest);
+          });
+          cluster_sync();
+          // the bin with before < want <= before + its own
+          uint32_t c[kBinsPer], csum = 0, cb = base_count;
+          u64 m[kBinsPer], msum = 0, mb = base_mass;
+#pragma unroll
+          for (int j = 0; j < kBinsPer; ++j) {
+            const int b = tid * kBinsPer + j;
+            c[j] = 0;
+            m[j] = 0;
+            for (int r = 0; r < n_blocks; ++r) {
+              c[j] += ld_cluster_u32(peer(&sh.count[b], r));
+              m[j] += ((u64)ld_cluster_u32(peer(&sh.hi[b], r)) << 32) + ld_cluster_u32(peer(&sh.lo[b], r));
+            }
+            csum += c[j];
+            msum += m[j];
+          }
+          scan_bins(csum, msum, cb, mb);
+#pragma unroll
+          for (int j = 0; j < kBinsPer; ++j) {
+            if (c[j] != 0u && (by_sum ? (double)mb < want_mass && !((double)(mb + m[j]) < want_mass) : cb < (uint32_t)top_k && (uint32_t)top_k <= cb + c[j])) {
+              sh.pick_bin = tid * kBinsPer + j;
+              sh.pick_count = cb;
+              sh.pick_mass = mb;
+              sh.pick_own = m[j];
+            }
+            cb += c[j];
+            mb += m[j];
+          }
+          cluster_sync();  // nobody clears its bins before all have read them
+          if (d == kDigits)
+            bin = sh.pick_bin;
+          else
+            prefix = (prefix << kDigitBits) | (u64)(kBins - 1 - sh.pick_bin);
+          base_count = sh.pick_count;
+          base_mass = sh.pick_mass;
+        }
+        cut = prefix > cut ? prefix : cut;
+        total = base_mass + sh.pick_own;
+        __syncthreads();
+      }
     }
   }
 
   // ---- 3. the token ----
-  const double least = min_p > 1.f ? 1.0 : (double)min_p;  // above 1: the cut has decided; NaN compares false: off
-  float floor_kept = fmaxf(floor_all, logit_of(max((uint32_t)(cut >> kIndexBits), key_of(-__int_as_float(0x7f800000)))));
-  if (min_p > 0.f && top < __int_as_float(0x7f800000))
-    floor_kept = fmaxf(floor_kept, (float)((double)top - (0.01 - (double)log2f((float)least)) / w.rate - 1e-6 * fabs((double)top)));
-  auto stays = [&](float l, int i, double& weight) -> u64 {
-    if (l < floor_kept) return 0ull;
-    const double x = w.octaves(l);
-    if (!(x < (double)kOctaves)) return 0ull;
-    const double mine = w.weight(x);
-    if (mine < least || composite(l, i) < cut) return 0ull;
+  const double least = (double)min_p;  // NaN compares false: off
+  float floor_kept = floor_all;
+  if (cut != 0) floor_kept = fmaxf(floor_kept, logit_of((uint32_t)(cut >> kIndexBits)));
+  if (min_p > 0.f) floor_kept = fmaxf(floor_kept, below((double)kSteps * -(double)log2f(min_p) + 4.0));
+  auto stays = [&](float l, int at, double& weight) -> u64 {
+    double rest;
+    const int i = w.place(l, rest);
+    if (i >= kEnd || composite(l, at) < cut) return 0ull;
+    const double v = w.scaled(i, rest), mine = __hiloint2double(__double2hiint(v) - (((i >> 8) + kUnitLog2) << 20), __double2loint(v));
+    if (mine < least) return 0ull;
     weight = mine;
-    return units(mine);
+    return w.units(v, i);
   };
   u64 sum = 0;
   double weight = 0.0;
-  run.each([&](float l, int i) { sum += stays(l, i, weight); });
+  run.template each<2>(floor_kept, [&](float l, int at) { sum += stays(l, at, weight); });
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(all, sum, d);
   __syncthreads();
   if (lane == 0) sh.warp64[warp] = sum;
   __syncthreads();
-  if (tid == 0) {
-    u64 t = 0;
-    for (int v = 0; v < kWarps; ++v) t += sh.warp64[v];
-    sh.slot64b[rank] = t;
-  }
+  u64 mine = 0;
+  for (int v = 0; v < kWarps; ++v) mine += sh.warp64[v];
+  if (tid == 0) sh.slot64b[rank] = mine;
   cluster_sync();
   u64 before = 0, total = 0;
   for (int r = 0; r < n_blocks; ++r) {
@@ -563,45 +627,64 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     total += t;
   }
   cluster_arrive();
-  for (int v = 0; v < warp; ++v) before += sh.warp64[v];
   const float u = p.u[row];
   u64 want = u > 0.f ? (u64)((double)u * (double)total) : 0ull;
   want = want < total ? want : total - 1;
-  if (before <= want && want < before + sum) {
-    for (int u0 = run.first; u0 < run.last; u0 += 32) {
-      const int unit = u0 + lane;
-      u64 mine = 0;
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (unit < run.last) {
-        v = run.load(unit);
+  if (before <= want && want < before + mine) {  // this block has it
+    int holder = 0;
+    for (; before + sh.warp64[holder] <= want; ++holder) before += sh.warp64[holder];
+    // that warp's run in equal parts over all warps
+    const Run<kBf16> held(p.logits, row * p.stride, p.vocab, rank, n_blocks, holder);
+    const int part = (held.last - held.first + kThreads - 1) / kThreads * 32;
+    const int u_first = min(held.first + warp * part, held.last), u_last = min(u_first + part, held.last);
+    auto unit_sum = [&](const uint4& v, int unit) -> u64 {
+      u64 t = 0;
 #pragma unroll
-        for (int e = 0; e < Run<kBf16>::kUnit; ++e)
-          if ((unsigned)(run.index(unit) + e) < (unsigned)p.vocab) mine += stays(run.value(v, e), run.index(unit) + e, weight);
+      for (int e = 0; e < Run<kBf16>::kUnit; ++e) {
+        const float l = run.value(v, e);
+        const int at = run.index(unit) + e;
+        if (l >= floor_kept && (unsigned)at < (unsigned)p.vocab) t += stays(l, at, weight);
       }
-      u64 x = mine;
+      return t;
+    };
+    sum = 0;
+    for (int unit = u_first + lane; unit < u_last; unit += 32) sum += unit_sum(run.load(unit), unit);
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const u64 o = __shfl_up_sync(all, x, d);
-        if (lane >= d) x += o;
-      }
-      const unsigned over = __ballot_sync(all, before + x > want);
-      if (over != 0u) {
-        if (lane == __ffs(over) - 1) {
-          u64 front = before + x - mine;
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(all, sum, d);
+    if (lane == 0) sh.slot_part[warp] = sum;
+    __syncthreads();
+    for (int v = 0; v < warp; ++v) before += sh.slot_part[v];
+    if (before <= want && want < before + sum) {
+      for (int u0 = u_first; u0 < u_last; u0 += 32) {
+        const int unit = u0 + lane;
+        const uint4 v = unit < u_last ? run.load(unit) : make_uint4(0u, 0u, 0u, 0u);
+        const u64 own = unit < u_last ? unit_sum(v, unit) : 0ull;
+        u64 x = own;
 #pragma unroll
-          for (int e = 0; e < Run<kBf16>::kUnit; ++e) {
-            const int i = run.index(unit) + e;
-            if ((unsigned)i >= (unsigned)p.vocab || front > want) continue;
-            front += stays(run.value(v, e), i, weight);
-            if (front > want) {
-              p.tokens[row] = i;
-              if (p.probs) p.probs[row] = (float)(weight * (double)(1ull << kUnitLog2) / (double)total);
+        for (int d = 1; d < 32; d <<= 1) {
+          const u64 o = __shfl_up_sync(all, x, d);
+          if (lane >= d) x += o;
+        }
+        const unsigned over = __ballot_sync(all, before + x > want);
+        if (over != 0u) {
+          if (lane == __ffs(over) - 1) {
+            u64 front = before + x - own;
+#pragma unroll
+            for (int e = 0; e < Run<kBf16>::kUnit; ++e) {
+              const float l = run.value(v, e);
+              const int at = run.index(unit) + e;
+              if (!(l >= floor_kept) || (unsigned)at >= (unsigned)p.vocab || front > want) continue;
+              front += stays(l, at, weight);
+              if (front > want) {
+                p.tokens[row] = at;
+                if (p.probs) p.probs[row] = (float)(weight * (double)(1ull << kUnitLog2) / (double)total);
+              }
             }
           }
+          break;
         }
-        break;
+        before += __shfl_sync(all, x, 31);
       }
-      before += __shfl_sync(all, x, 31);
     }
   }
   cluster_wait();
@@ -618,7 +701,7 @@ cudaError_t sample_setup() {
 cudaError_t launch_sample(SampleParams p, int sm_count, cudaStream_t stream) {
   // more blocks per row while the device has places for them (two per SM) and each keeps 2048 tokens
   int blocks = 1;
-  while (blocks < 8 && p.n * blocks * 2 <= 2 * sm_count && p.vocab > 4096 * blocks) blocks *= 2;
+  while (blocks < SAMPLE_MAX && p.n * blocks * 2 <= 2 * sm_count && p.vocab > SAMPLE_MIN * blocks) blocks *= 2;
   p.blocks = blocks;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.n * blocks));
