@@ -98,34 +98,45 @@ __device__ __forceinline__ void cluster_sync() {
 // fp32 -> fp64 for finite numbers, in integers; below fp32's normal numbers it is off by up to 2^-126
 __device__ __forceinline__ double widen(float f) {
   const uint32_t b = __float_as_uint(f);
-  return __hiloint2double((int)((((b & 0x7fffffffu) >> 3) + 0x38000000u) | (b & 0x80000000u)), (int)(b << 29));
+  return __hiloint2double((((int)b >> 3) & (int)0x8fffffffu) + 0x38000000, (int)(b << 29));
 }
 
 struct Weights {
   double top, rate;     // the largest logit; 256 log2(e) / T
   const double* table;
-  // Place i of a logit on the scale of 256ths of an octave below the largest, and the rest; only for logits down to kEnd.
+  // 256ths of an octave below the largest
+  __device__ __forceinline__ double depth(float l) const { return (top - widen(l)) * rate; }
+  // the same as a whole number and a rest; any number comes out for logits beyond kEnd
   __device__ __forceinline__ int place(float l, double& rest) const {
     constexpr double kMagic = 6755399441055744.0;  // 1.5 * 2^52: the sum has the nearest whole number in its low word
-    const double s = (top - widen(l)) * rate, t = s + kMagic;
+    const double s = depth(l), t = s + kMagic;
     rest = s - (t - kMagic);
     return __double2loint(t);
   }
-  // 2^(42 - (i mod 256 + rest) / 256)
+  // 2^(42 - (i + rest) / 256)
   __device__ __forceinline__ double scaled(int i, double r) const {
     constexpr double c1 = -0.69314718055994530942 / kSteps, c2 = c1 * c1 / 2.0, c3 = c1 * c1 * c1 / 6.0;
-    const double t = table[i & (kSteps - 1)];
-    return fma(t, r * fma(fma(c3, r, c2), r, c1), t);
+    const double t = table[i & (kSteps - 1)], v = fma(t, r * fma(fma(c3, r, c2), r, c1), t);
+    return __hiloint2double(__double2hiint(v) - ((i & ~(kSteps - 1)) << 12), __double2loint(v));
   }
-  __device__ __forceinline__ u64 units(double v, int i) const {  // scaled() as the whole number of 2^-42 that the token weighs
-    return (u64)(__double_as_longlong(v + 0x1p52) & ((1ll << 52) - 1)) >> (i >> 8);
-  }
+  // what a token weighs, as a whole number in the low 52 bits
+  static constexpr double kWhole = 0x1p52;
+  static __device__ __forceinline__ u64 units(double scaled_) { return (u64)(__double_as_longlong(scaled_ + kWhole) & ((1ll << 52) - 1)); }
   __device__ __forceinline__ u64 units(float l) const {
     double r;
     const int i = place(l, r);
-    return units(scaled(i, r), i);
+    return units(scaled(i, r));
   }
 };
+// The lowest logit for which `in` holds; it holds for all larger ones up to `top`, and `guess` is within a few roundings of it.
+template <class F>
+__device__ __forceinline__ float lowest(float guess, float top, F in) {
+  constexpr float kLowest = -3.402823466e38f;
+  float x = fminf(fmaxf(guess, kLowest), top);
+  while (x < top && !in(x)) x = nextafterf(x, top);
+  while (x > kLowest && in(nextafterf(x, kLowest))) x = nextafterf(x, kLowest);
+  return x;
+}
 // bins of i: 64 to an octave for the first 16 octaves, then 32
 constexpr int kFine = 16 * kSteps;
 __device__ __forceinline__ int bin_of(int i) { return i < kFine ? i >> 2 : (kFine >> 2) + ((i - kFine) >> 3); }
@@ -160,14 +171,16 @@ struct Run {
   __device__ __forceinline__ uint4 load(int unit) const {
     const uint8_t* p = base + (int64_t)unit * 16;
     if (whole(unit)) return __ldg(reinterpret_cast<const uint4*>(p));
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    uint32_t w[4];  // -inf beyond the row
 #pragma unroll
-    for (int e = 0; e < kUnit; ++e) {
-      if ((unsigned)(index(unit) + e) >= (unsigned)vocab) continue;
-      if constexpr (kBf16)
-        w[e >> 1] |= (uint32_t) * (reinterpret_cast<const uint16_t*>(p) + e) << (16 * (e & 1));
-      else
-        w[e] = *(reinterpret_cast<const uint32_t*>(p) + e);
+    for (int j = 0; j < 4; ++j) {
+      auto inside = [&](int e) { return (unsigned)(index(unit) + e) < (unsigned)vocab; };
+      if constexpr (kBf16) {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + 2 * j;
+        w[j] = (inside(2 * j) ? (uint32_t)h[0] : 0xff80u) | (inside(2 * j + 1) ? (uint32_t)h[1] : 0xff80u) << 16;
+      } else {
+        w[j] = inside(j) ? *(reinterpret_cast<const uint32_t*>(p) + j) : 0xff800000u;
+      }
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
@@ -176,10 +189,10 @@ struct Run {
     if constexpr (kBf16) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
     return __uint_as_float(w[e]);
   }
-  // f(logit, index) for every token of the warp with a logit of at least `least`, ascending within a lane; kAhead units are
-  // loaded together
+  // f(logits, index) for four neighbouring tokens at a time, ascending within a lane, where one has a logit of at least `least`
+  // (more than -inf, which stands beyond the row's ends); kAhead units are loaded together
   template <int kAhead, class F>
-  __device__ __forceinline__ void each(float least, F f) const {
+  __device__ __forceinline__ void each4(float least, F f) const {
     const int lane = threadIdx.x & 31;
     for (int u0 = first + lane; u0 < last; u0 += 32 * kAhead) {
       uint4 v[kAhead];
@@ -189,13 +202,16 @@ struct Run {
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         if (u0 + 32 * j >= last) break;
-        const int i = index(u0 + 32 * j);
-#pragma unroll
-        for (int e = 0; e < kUnit; ++e) {
-          const float l = value(v[j], e);
-          if (l >= least && (unsigned)(i + e) < (unsigned)vocab) f(l, i + e);
-        }
+        four(v[j], u0 + 32 * j, least, f);
       }
+    }
+  }
+  template <class F>
+  __device__ __forceinline__ void four(const uint4& v, int unit, float least, F f) const {
+#pragma unroll
+    for (int q = 0; q < kUnit; q += 4) {
+      const float l[4] = {value(v, q), value(v, q + 1), value(v, q + 2), value(v, q + 3)};
+      if (fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= least) f(l, index(unit) + q);
     }
   }
   // the largest logit, NaN if there is one (in this lane)
@@ -210,20 +226,14 @@ struct Run {
       for (int j = 0; j < kAhead; ++j) v[j] = u0 + 32 * j < last ? load(u0 + 32 * j) : load(u0);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const int u = u0 + 32 * j < last ? u0 + 32 * j : u0;
-        if (whole(u)) {
-          if constexpr (kBf16) {
-            uint32_t a, b;
-            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v[j].x), "r"(v[j].y));
-            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v[j].z), "r"(v[j].w));
-            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
-            m = max_nan(m, max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u)));
-          } else {
-            m = max_nan(max_nan(m, max_nan(__uint_as_float(v[j].x), __uint_as_float(v[j].y))), max_nan(__uint_as_float(v[j].z), __uint_as_float(v[j].w)));
-          }
+        if constexpr (kBf16) {
+          uint32_t a, b;
+          asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v[j].x), "r"(v[j].y));
+          asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v[j].z), "r"(v[j].w));
+          asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+          m = max_nan(m, max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u)));
         } else {
-#pragma unroll
-          for (int e = 0; e < kUnit; ++e) m = max_nan(m, (unsigned)(index(u) + e) < (unsigned)vocab ? value(v[j], e) : none);
+          m = max_nan(max_nan(m, max_nan(__uint_as_float(v[j].x), __uint_as_float(v[j].y))), max_nan(__uint_as_float(v[j].z), __uint_as_float(v[j].w)));
         }
       }
     }
@@ -291,7 +301,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const bool one = !(temp > 0.f) || top_p <= 0.f || min_p > 1.f || top_k == 1;  // the first token only
   if (dead || one) {
     uint32_t at = 0xffffffffu;
-    if (!dead) run.template each<2>(top, [&](float, int i) { at = min(at, (uint32_t)i); });
+    if (!dead)
+      run.template each4<4>(top, [&](const float(&l)[4], int i) { at = min(at, (uint32_t)(i + (l[0] == top ? 0 : l[1] == top ? 1 : l[2] == top ? 2 : 3))); });
     at = __reduce_min_sync(all, at);
     __syncthreads();
     if (lane == 0) sh.warp32[warp] = at;
@@ -316,19 +327,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
   u64 cut = 0;  // tokens whose composite is at least this stay
   const bool by_mass = top_p < 1.f, by_count = top_k > 1 && top_k < p.vocab;
-  // A logit that is at least `steps` 256ths of an octave below the largest, or a little less (rounding included): a cheap
-  // test in front of the double one.  -inf is never above it, and next to +inf nothing else is.
+  // The logit `steps` 256ths of an octave below the largest, a little lower (rounding included), but above -inf; next to
+  // +inf nothing else counts.
   auto below = [&](double steps) -> float {
     if (top == inf) return top;
     return fmaxf((float)((double)top - steps / w.rate - 1e-6 * fabs((double)top)), -3.402823466e38f);
   };
-  const float floor_all = below((double)kEnd + 4.0);
+  const float floor_all = top == inf ? top : lowest((float)((double)top - ((double)kEnd - 0.5) / w.rate), top, [&](float l) {
+    double rest;
+    return w.depth(l) < (double)kEnd + 1.0 && w.place(l, rest) < kEnd;
+  });  // tokens from here on up weigh something
 
   // ---- 2. the cut ----
-  auto add_bin = [&](int b, bool mass, int i, double rest) {
-    atomicAdd(&sh.count[b], 1u);
+  auto add_bin = [&](int b, bool count, bool mass, u64 u) {
+    if (count) atomicAdd(&sh.count[b], 1u);
     if (mass) {
-      const u64 u = w.units(w.scaled(i, rest), i);
       const uint32_t add = (uint32_t)u, old = atomicAdd(&sh.lo[b], add);
       const uint32_t carry = (uint32_t)(u >> 32) + (old + add < old ? 1u : 0u);
       if (carry) atomicAdd(&sh.hi[b], carry);
@@ -362,17 +375,24 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   };
 
   if (by_count || by_mass) {
-    run.template each<2>(floor_all, [&](float l, int) {
-      double rest;
-      const int i = w.place(l, rest);
-      if (i < kEnd) add_bin(bin_of(i), by_mass, i, rest);
+    run.template each4<2>(floor_all, [&](const float(&l)[4], int) {
+      int i[4];
+      u64 u[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        double rest;
+        i[e] = w.place(l[e], rest);
+        u[e] = by_mass ? w.units(w.scaled(i[e], rest)) : 0ull;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (l[e] >= floor_all) add_bin(bin_of(i[e]), by_count, by_mass, u[e]);
     });
     __syncthreads();
     if (rank != 0) {
       for (int b = tid; b < kBins; b += kThreads) {
-        if (sh.count[b] == 0u) continue;
-        add_cluster_u32(peer(&sh.count[b], 0), sh.count[b]);
-        if (by_mass) {
+        if (by_count && sh.count[b] != 0u) add_cluster_u32(peer(&sh.count[b], 0), sh.count[b]);
+        if (by_mass && (sh.lo[b] | sh.hi[b]) != 0u) {
           const uint32_t add = sh.lo[b], old = add_cluster_u32(peer(&sh.lo[b], 0), add);
           const uint32_t carry = sh.hi[b] + (old + add < old ? 1u : 0u);
           if (carry) add_cluster_u32(peer(&sh.hi[b], 0), carry);
@@ -443,18 +463,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       }
       const float high = from <= 0 || top == inf ? inf : (float)((double)top - (double)(bin_begin(from) - 2) / w.rate + 1e-6 * fabs((double)top));
       const float low = fmaxf(floor_all, below((double)bin_begin(to + 1) + 2.0));
-      run.template each<2>(low, [&](float l, int at) {
-        if (l > high) return;
-        double rest;
-        const int i = w.place(l, rest), b = bin_of(i);
-        if (i >= kEnd) return;
-        if (b == bin_k) {
-          const uint32_t slot = add_cluster_u32(peer(&sh.listed[0], 0), 1u);
-          if (slot < kList) st_cluster_u64(peer(&sh.list[0][slot], 0), composite(l, at));
-        }
-        if (by_mass && b >= bin_lo && b <= bin_hi) {
-          const uint32_t slot = add_cluster_u32(peer(&sh.listed[1], 0), 1u);
-          if (slot < kList) st_cluster_u64(peer(&sh.list[1][slot], 0), composite(l, at));
+      run.template each4<4>(low, [&](const float(&l)[4], int at) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (!(l[e] >= low && l[e] <= high)) continue;
+          double rest;
+          const int b = bin_of(w.place(l[e], rest));
+          if (b == bin_k) {
+            const uint32_t slot = add_cluster_u32(peer(&sh.listed[0], 0), 1u);
+            if (slot < kList) st_cluster_u64(peer(&sh.list[0][slot], 0), composite(l[e], at + e));
+          }
+          if (by_mass && b >= bin_lo && b <= bin_hi) {
+            const uint32_t slot = add_cluster_u32(peer(&sh.listed[1], 0), 1u);
+            if (slot < kList) st_cluster_u64(peer(&sh.list[1][slot], 0), composite(l[e], at + e));
+          }
         }
       });
     }
@@ -538,18 +560,22 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           const int shift = d * kDigitBits;
           clear_bins();
           __syncthreads();
-          run.template each<1>(floor_all, [&](float l, int at) {
-            double rest;
-            const int i = w.place(l, rest);
-            if (i >= kEnd) return;
-            int b = bin_of(i);
-            if (d < kDigits) {
-              if (b != bin) return;
-              const u64 c = composite(l, at);
-              if (d < kDigits - 1 && c >> (shift + kDigitBits) != prefix) return;
-              b = kBins - 1 - (int)((c >> shift) & (kBins - 1));  // the largest first
+          run.template each4<1>(floor_all, [&](const float(&l)[4], int at) {
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {
+              const float x = e < 2 ? (e == 0 ? l[0] : l[1]) : (e == 2 ? l[2] : l[3]);
+              if (!(x >= floor_all)) continue;
+              double rest;
+              const int i = w.place(x, rest);
+              int b = bin_of(i);
+              if (d < kDigits) {
+                if (b != bin) continue;
+                const u64 c = composite(x, at + e);
+                if (d < kDigits - 1 && c >> (shift + kDigitBits) != prefix) continue;
+                b = kBins - 1 - (int)((c >> shift) & (kBins - 1));  // the largest first
+              }
+              add_bin(b, true, true, w.units(w.scaled(i, rest)));
             }
-            add_bin(b, true, i, rest);
           });
           cluster_sync();
           // the bin with before < want <= before + its own
@@ -595,22 +621,32 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   }
 
   // ---- 3. the token ----
-  const double least = (double)min_p;  // NaN compares false: off
-  float floor_kept = floor_all;
-  if (cut != 0) floor_kept = fmaxf(floor_kept, logit_of((uint32_t)(cut >> kIndexBits)));
-  if (min_p > 0.f) floor_kept = fmaxf(floor_kept, below((double)kSteps * -(double)log2f(min_p) + 4.0));
-  auto stays = [&](float l, int at, double& weight) -> u64 {
-    double rest;
-    const int i = w.place(l, rest);
-    if (i >= kEnd || composite(l, at) < cut) return 0ull;
-    const double v = w.scaled(i, rest), mine = __hiloint2double(__double2hiint(v) - (((i >> 8) + kUnitLog2) << 20), __double2loint(v));
-    if (mine < least) return 0ull;
-    weight = mine;
-    return w.units(v, i);
+  // what stays: the logits above floor_kept, and of those that equal cut_logit the tokens up to cut_at
+  float floor_kept = floor_all, cut_logit = -inf;
+  int cut_at = 0;
+  if (cut != 0) {
+    cut_logit = logit_of((uint32_t)(cut >> kIndexBits));
+    cut_at = (1 << kIndexBits) - 1 - (int)(cut & ((1u << kIndexBits) - 1));
+    floor_kept = fmaxf(floor_kept, cut_logit);
+  }
+  if (min_p > 0.f && top < inf) {  // (NaN: off)
+    const double most = -(double)kSteps * log2((double)min_p);
+    floor_kept = fmaxf(floor_kept, lowest((float)((double)top - most / w.rate), top, [&](float l) { return w.depth(l) <= most; }));
+  }
+  auto stays = [&](float l, int at) { return l >= floor_kept && (l > cut_logit || at <= cut_at); };
+  // the weights of four tokens: whole numbers, so that a thread's sum (little more than 2^10 tokens of up to 2^42) is exact in double
+  auto sum4 = [&](const float(&l)[4], int at, double& sum) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      double rest;
+      const int i = w.place(l[e], rest);
+      const double u = (w.scaled(i, rest) + w.kWhole) - w.kWhole;
+      if (stays(l[e], at + e)) sum += u;
+    }
   };
-  u64 sum = 0;
-  double weight = 0.0;
-  run.template each<2>(floor_kept, [&](float l, int at) { sum += stays(l, at, weight); });
+  double thread_sum = 0.0;
+  run.template each4<2>(floor_kept, [&](const float(&l)[4], int at) { sum4(l, at, thread_sum); });
+  u64 sum = (u64)thread_sum;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(all, sum, d);
   __syncthreads();
@@ -638,14 +674,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const int part = (held.last - held.first + kThreads - 1) / kThreads * 32;
     const int u_first = min(held.first + warp * part, held.last), u_last = min(u_first + part, held.last);
     auto unit_sum = [&](const uint4& v, int unit) -> u64 {
-      u64 t = 0;
-#pragma unroll
-      for (int e = 0; e < Run<kBf16>::kUnit; ++e) {
-        const float l = run.value(v, e);
-        const int at = run.index(unit) + e;
-        if (l >= floor_kept && (unsigned)at < (unsigned)p.vocab) t += stays(l, at, weight);
-      }
-      return t;
+      double t = 0.0;
+      run.four(v, unit, floor_kept, [&](const float(&l)[4], int at) { sum4(l, at, t); });
+      return (u64)t;
     };
     sum = 0;
     for (int unit = u_first + lane; unit < u_last; unit += 32) sum += unit_sum(run.load(unit), unit);
@@ -669,15 +700,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         if (over != 0u) {
           if (lane == __ffs(over) - 1) {
             u64 front = before + x - own;
-#pragma unroll
-            for (int e = 0; e < Run<kBf16>::kUnit; ++e) {
-              const float l = run.value(v, e);
+#pragma unroll 1
+            for (int e = 0; e < Run<kBf16>::kUnit && front <= want; ++e) {
               const int at = run.index(unit) + e;
-              if (!(l >= floor_kept) || (unsigned)at >= (unsigned)p.vocab || front > want) continue;
-              front += stays(l, at, weight);
+              if ((unsigned)at >= (unsigned)p.vocab) continue;
+              const float l = kBf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.logits)[row * p.stride + at])
+                                    : static_cast<const float*>(p.logits)[row * p.stride + at];
+              if (!stays(l, at)) continue;
+              double rest;
+              const int i = w.place(l, rest);
+              const double v = w.scaled(i, rest);
+              front += w.units(v);
               if (front > want) {
                 p.tokens[row] = at;
-                if (p.probs) p.probs[row] = (float)(weight * (double)(1ull << kUnitLog2) / (double)total);
+                if (p.probs) p.probs[row] = (float)(v / (double)total);
               }
             }
           }
@@ -702,6 +738,7 @@ cudaError_t launch_sample(SampleParams p, int sm_count, cudaStream_t stream) {
   // more blocks per row while the device has places for them (two per SM) and each keeps 2048 tokens
   int blocks = 1;
   while (blocks < SAMPLE_MAX && p.n * blocks * 2 <= 2 * sm_count && p.vocab > SAMPLE_MIN * blocks) blocks *= 2;
+  if (p.vocab > (1 << 19) && blocks == 1) blocks = 2;  // at most 2^10 tokens per thread (and a unit): sums exact in double
   p.blocks = blocks;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.n * blocks));
