@@ -10,9 +10,13 @@
 // The three filters each keep a prefix of one order, falling logit and then rising index, so together they keep the tokens
 // not below one (logit, index) pair, the cut.  A row belongs to a cluster of thread blocks, each with a run of consecutive tokens.
 //   1. the largest logit (and whether there is a NaN)
-//   2. where top-k or top-p is on: counts and sums in bins of i, joined in the first block; the tokens of the bins that hold
-//      a cut (some hundred of 128 K) go to the first block too, which ranks them and finds the cut.
-//      Where they are too many (thousands of equal logits), the bin is taken apart by 11 bits of (logit, index) at a time.
+//   2. up to 256 for top-k: the tokens that reach a logit which at least k tokens do (step 1 found one on its way) go to the
+//      first block, which sorts them and needs nothing more.
+//      Otherwise, where top-k or top-p is on: counts, and estimates of the weights, in bins of 1/64 octave in fp32, joined in the first
+//      block, which picks the bins around the cuts; then exact sums of what is in front of them, while their tokens (some
+//      hundred of 128 K) go to the first block's lists, which ranks them, finds the cuts and checks the estimate.
+//      Where that fails or a list is too short (thousands of equal logits), the cut is searched for by exact counts and sums,
+//      11 bits of (logit, index) at a time.
 //   3. sums of what stays, by block and by warp; the block that holds u * total shares out the warp's run that holds it
 // The row is read again by each step: it comes out of L2 after the first.
 #include <cuda_bf16.h>
@@ -29,6 +33,7 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kBinsPer = kBins / kThreads;
 constexpr int kList = 2048, kListPer = kList / kThreads;  // tokens of a cut's bins that are ranked in shared memory
+constexpr int kQuick = 256;                      // up to here the top k are found without bins
 constexpr int kUnitLog2 = 42;                    // weights are multiples of 2^-42
 constexpr int kSteps = 256;                      // i counts 256ths of an octave below the largest
 constexpr int kEnd = kUnitLog2 * kSteps;         // from here on tokens weigh nothing
@@ -37,10 +42,9 @@ typedef unsigned long long u64;
 
 struct Found {           // what the first block of a row's cluster tells the others
   int bin_k;             // bin of the top-k cut, or -1
-  int bin_lo, bin_hi;    // bins that may hold the top-p cut; empty if bin_lo > bin_hi
-  int slow;              // the lists overflowed
+  int bin_lo, bin_hi;    // bins around the top-p cut
+  int slow;              // a list overflowed, or the cut is outside the bins
   uint32_t count_k;      // tokens in front of bin_k
-  u64 mass_k, mass_lo;   // sums in front of bin_k and of bin_lo
   u64 total;             // sum of all tokens
   u64 cut;
 };
@@ -52,10 +56,12 @@ struct Shared {
   uint32_t listed[2];
   uint32_t count[kBins], lo[kBins], hi[kBins];
   u64 slot64b[8];                // one word per block of the cluster
+  u64 slot_all[8], slot_above[8];
   u64 slot_part[kWarps];
+  uint32_t extra_lo[8 * kWarps], extra_hi[8 * kWarps];  // by warp of the cluster: weights of the listed tokens that stay
   u64 warp64[kWarps];
   uint32_t warp32[kWarps];
-  float top[8];
+  float top[8], low[8];
   uint32_t first[8];
   Found found;
   int pick_bin;
@@ -128,19 +134,44 @@ struct Weights {
     return units(scaled(i, r));
   }
 };
-// The lowest logit for which `in` holds; it holds for all larger ones up to `top`, and `guess` is within a few roundings of it.
+// The lowest logit for which `in` holds; it holds for `top` and everything down from there to the one looked for.  The lanes
+// of a warp (all of them) first test 32 numbers around the guess, four apart, then 32 places of what is left of the order
+// of fp32 numbers: two rounds where the guess is good, eight at most.
 template <class F>
-__device__ __forceinline__ float lowest(float guess, float top, F in) {
-  constexpr float kLowest = -3.402823466e38f;
-  float x = fminf(fmaxf(guess, kLowest), top);
-  while (x < top && !in(x)) x = nextafterf(x, top);
-  while (x > kLowest && in(nextafterf(x, kLowest))) x = nextafterf(x, kLowest);
-  return x;
+__device__ __forceinline__ float lowest(float top, float guess, F in) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t out = key_of(-3.402823466e38f) - 1u, hit = key_of(top);  // `in` does not hold (or nothing is there) / holds
+  const uint32_t mid = min(max(key_of(guess), out + 65u), hit);  // (a guess that is no number is as good as any)
+  bool near = hit - out > 256u;
+  while (hit - out > 1u) {
+    const uint32_t at = near ? min(mid - 64u + 4u * lane, hit) : out + 1u + (uint32_t)(((u64)(hit - out - 1u) * lane) >> 5);  // ascending
+    near = false;
+    const unsigned holds = __ballot_sync(0xffffffffu, in(logit_of(at)));
+    const int first = holds != 0u ? __ffs(holds) - 1 : 32;
+    const uint32_t at_first = __shfl_sync(0xffffffffu, at, first & 31), at_before = __shfl_sync(0xffffffffu, at, (first + 31) & 31);
+    if (first < 32) hit = at_first;
+    if (first > 0) out = at_before;
+  }
+  return logit_of(hit);
 }
+// Where tokens gather around a cut is first estimated in fp32: bins of 1/64 octave (or any other size: all that is asked of
+// them is to follow the order of the logits), the last one without an end.
+struct Coarse {
+  float top, scale;   // scale = 64 log2(e) / T
+  float one;          // units of a bin's largest weight, so that a bin's 32-bit sum holds a whole row
+  __device__ __forceinline__ int bin(float l) const {
+    return (int)(__float_as_uint(fminf((top - l) * scale, (float)(kBins - 1)) + 8388608.f) & 0x7fffffu);
+  }
+  // and the weight next to the bin's middle, in units of 1 / one: a linear step is off by 1.5e-5
+  __device__ __forceinline__ int bin(float l, uint32_t& weight) const {
+    const float q = fminf((top - l) * scale, (float)(kBins - 1)), t = q + 8388608.f;
+    weight = __float_as_uint(fmaf(one * -0.01083042f, q - (t - 8388608.f), one) + 8388608.f) & 0x7fffffu;
+    return (int)(__float_as_uint(t) & 0x7fffffu);
+  }
+};
 // bins of i: 64 to an octave for the first 16 octaves, then 32
 constexpr int kFine = 16 * kSteps;
 __device__ __forceinline__ int bin_of(int i) { return i < kFine ? i >> 2 : (kFine >> 2) + ((i - kFine) >> 3); }
-__device__ __forceinline__ int bin_begin(int b) { return b < kFine >> 2 ? b << 2 : kFine + ((b - (kFine >> 2)) << 3); }
 static_assert((kFine >> 2) + ((kEnd - kFine) >> 3) <= kBins, "bins");
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -157,12 +188,15 @@ struct Run {
   const uint8_t* base;  // 16-byte aligned, at or in front of the row
   int head, vocab;      // elements between base and the row
   int first, last;      // units of this warp
+  int per, warps;       // units of a warp; warps of the cluster that have some
 
   __device__ __forceinline__ Run(const void* logits, int64_t at, int vocab_, int block, int n_blocks, int warp) : vocab(vocab_) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(logits) + at * (kBf16 ? 2 : 4);
     base = reinterpret_cast<const uint8_t*>(a & ~(uintptr_t)15);
     head = (int)(a & 15) / (kBf16 ? 2 : 4);
-    const int n = (head + vocab + kUnit - 1) / kUnit, per = (n + n_blocks * kWarps * 32 - 1) / (n_blocks * kWarps * 32) * 32;
+    const int n = (head + vocab + kUnit - 1) / kUnit;
+    per = (n + n_blocks * kWarps * 32 - 1) / (n_blocks * kWarps * 32) * 32;
+    warps = (n + per - 1) / per;
     first = min((block * kWarps + warp) * per, n);
     last = min(first + per, n);
   }
@@ -277,26 +311,65 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     for (int b = tid; b < kBins; b += kThreads) sh.count[b] = sh.lo[b] = sh.hi[b] = 0u;
   };
 
-  if (tid < 2) sh.listed[tid] = 0u;
-  for (int j = tid; j < kSteps; j += kThreads) sh.table[j] = exp2((double)kUnitLog2 - (double)j / kSteps);
-  clear_bins();
-
-  // ---- 1. the largest logit ----
-  float top = run.top();
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) top = max_nan(top, __shfl_xor_sync(all, top, d));
-  if (lane == 0) sh.warp32[warp] = __float_as_uint(top);
-  __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kWarps; ++w) top = max_nan(top, __uint_as_float(sh.warp32[w]));
-    sh.top[rank] = top;
-  }
-  cluster_sync();
-  top = -inf;
-  for (int r = 0; r < n_blocks; ++r) top = max_nan(top, __uint_as_float(ld_cluster_u32(peer(&sh.top[r], r))));
   const float temp = p.temperature ? p.temperature[row] : 1.f;
   const int top_k = p.top_k ? p.top_k[row] : 0;
   const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
+  if (tid < 2) sh.listed[tid] = 0u;
+  if (tid < 8 * kWarps) sh.extra_lo[tid] = sh.extra_hi[tid] = 0u;
+  for (int j = tid; j < kSteps; j += kThreads) sh.table[j] = exp2((double)kUnitLog2 - (double)j / kSteps);
+  clear_bins();
+
+  // ---- 1. the largest logit, and a logit that at least top_k tokens reach: the smallest of the largest logits of that many
+  // groups of threads that have tokens ----
+  float top = run.top(), reached = top;
+  int group = kThreads;  // threads; the last warp's lanes may be without tokens
+  while (group > 1 && (group >= 32 ? run.warps * 32 / group : (run.warps - 1) * (32 / group)) < top_k) group >>= 1;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    top = max_nan(top, __shfl_xor_sync(all, top, d));
+    const float o = __shfl_xor_sync(all, reached, d);
+    if (d < group) reached = fmaxf(reached, o);
+  }
+  int groups = __popc(__ballot_sync(all, reached > -inf)) / min(group, 32);
+  if (group < 32) {
+    reached = reached > -inf ? reached : inf;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) reached = fminf(reached, __shfl_xor_sync(all, reached, d));
+  }
+  if (lane == 0) {
+    sh.warp32[warp] = __float_as_uint(top);
+    sh.warp64[warp] = ((u64)groups << 32) | __float_as_uint(reached);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    float best = -inf;  // of several warps that are a group
+    reached = inf;
+    groups = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      const float o = __uint_as_float((uint32_t)sh.warp64[w]);
+      top = max_nan(top, __uint_as_float(sh.warp32[w]));
+      best = group <= 32 ? o : fmaxf(best, o);
+      if (((w + 1) * 32) % group != 0) continue;
+      if (best > -inf) {
+        reached = fminf(reached, best);
+        groups += group <= 32 ? (int)(sh.warp64[w] >> 32) : 1;
+      }
+      best = -inf;
+    }
+    sh.top[rank] = top;
+    sh.low[rank] = reached;
+    sh.first[rank] = (uint32_t)groups;
+  }
+  cluster_sync();
+  top = -inf;
+  reached = inf;
+  groups = 0;
+  for (int r = 0; r < n_blocks; ++r) {
+    top = max_nan(top, __uint_as_float(ld_cluster_u32(peer(&sh.top[r], r))));
+    reached = fminf(reached, __uint_as_float(ld_cluster_u32(peer(&sh.low[r], r))));
+    groups += (int)ld_cluster_u32(peer(&sh.first[r], r));
+  }
+  if (groups < top_k) reached = -inf;
   const bool dead = !(top > -inf);
   const bool one = !(temp > 0.f) || top_p <= 0.f || min_p > 1.f || top_k == 1;  // the first token only
   if (dead || one) {
@@ -304,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     if (!dead)
       run.template each4<4>(top, [&](const float(&l)[4], int i) { at = min(at, (uint32_t)(i + (l[0] == top ? 0 : l[1] == top ? 1 : l[2] == top ? 2 : 3))); });
     at = __reduce_min_sync(all, at);
-    __syncthreads();
+    cluster_sync();  // (the slots have been read)
     if (lane == 0) sh.warp32[warp] = at;
     __syncthreads();
     if (tid == 0) {
@@ -327,26 +400,29 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
   u64 cut = 0;  // tokens whose composite is at least this stay
   const bool by_mass = top_p < 1.f, by_count = top_k > 1 && top_k < p.vocab;
-  // The logit `steps` 256ths of an octave below the largest, a little lower (rounding included), but above -inf; next to
-  // +inf nothing else counts.
-  auto below = [&](double steps) -> float {
-    if (top == inf) return top;
-    return fmaxf((float)((double)top - steps / w.rate - 1e-6 * fabs((double)top)), -3.402823466e38f);
-  };
-  const float floor_all = top == inf ? top : lowest((float)((double)top - ((double)kEnd - 0.5) / w.rate), top, [&](float l) {
+  // tokens from here on up weigh something (next to +inf nothing else does), and reach min_p
+  const float floor_all = top == inf ? top : lowest(top, (float)((double)top - ((double)kEnd - 0.5) / w.rate), [&](float l) {
     double rest;
     return w.depth(l) < (double)kEnd + 1.0 && w.place(l, rest) < kEnd;
-  });  // tokens from here on up weigh something
+  });
+  float floor_min = floor_all;
+  if (min_p > 0.f && top < inf) {  // (NaN: off)
+    const double most = -(double)kSteps * log2((double)min_p);
+    floor_min = fmaxf(floor_all, lowest(top, (float)((double)top - most / w.rate), [&](float l) { return w.depth(l) <= most; }));
+  }
+  const float u = p.u[row];
+  auto place_of = [&](u64 total) -> u64 {  // u times a sum of weights, below the sum
+    const u64 want = u > 0.f ? (u64)((double)u * (double)total) : 0ull;
+    return want < total ? want : total - 1;
+  };
 
   // ---- 2. the cut ----
-  auto add_bin = [&](int b, bool count, bool mass, u64 u) {
-    if (count) atomicAdd(&sh.count[b], 1u);
-    if (mass) {
-      const uint32_t add = (uint32_t)u, old = atomicAdd(&sh.lo[b], add);
-      const uint32_t carry = (uint32_t)(u >> 32) + (old + add < old ? 1u : 0u);
-      if (carry) atomicAdd(&sh.hi[b], carry);
-    }
+  // puts a token on one of the first block's lists
+  auto keep = [&](int list, float l, int at) {
+    const uint32_t slot = add_cluster_u32(peer(&sh.listed[list], 0), 1u);
+    if (slot < kList) st_cluster_u64(peer(&sh.list[list][slot], 0), composite(l, at));
   };
+  auto mass_of = [&](u64 c) -> u64 { return w.units(logit_of((uint32_t)(c >> kIndexBits))); };
   // Exclusive sums over the block's threads, added to cb and mb.
   auto scan_bins = [&](uint32_t csum, u64 msum, uint32_t& cb, u64& mb) {
     uint32_t cx = csum;
@@ -374,48 +450,111 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
   };
 
-  if (by_count || by_mass) {
-    run.template each4<2>(floor_all, [&](const float(&l)[4], int) {
-      int i[4];
-      u64 u[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        double rest;
-        i[e] = w.place(l[e], rest);
-        u[e] = by_mass ? w.units(w.scaled(i[e], rest)) : 0ull;
-      }
+  if (by_count && top_k <= kQuick) {
+    // The tokens that reach `reached` (some hundred) hold the top k: the first block sorts them and goes through with it.
+    const float from = fmaxf(reached, floor_all);
+    run.template each4<4>(from, [&](const float(&l)[4], int at) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (l[e] >= floor_all) add_bin(bin_of(i[e]), by_count, by_mass, u[e]);
+        if (l[e] >= from) keep(0, l[e], at + e);
+    });
+    cluster_sync();
+    const int n = (int)min(ld_cluster_u32(peer(&sh.listed[0], 0)), (uint32_t)kList + 1u);
+    if (n <= kList) {
+      cluster_arrive();
+      if (rank == 0) {
+        u64* sorted = sh.list[0];
+        if (n <= kThreads) {
+          const u64 mine = tid < n ? sorted[tid] : 0ull;
+          int front = 0;
+#pragma unroll 8
+          for (int j = 0; j < n; ++j) front += sh.list[0][j] > mine;
+          sorted = sh.list[1];
+          if (tid < n) sorted[front] = mine;
+          __syncthreads();
+        } else {
+          sort_list(sorted, n);
+        }
+        const int k = min(top_k, n);
+        const u64 mine = tid < k ? sorted[tid] : 0ull, own = tid < k ? mass_of(mine) : 0ull;
+        u64 front = 0;
+        uint32_t unused = 0;
+        scan_bins(0u, own, unused, front);
+        if (tid == k - 1) sh.pick_mass = front + own;
+        __syncthreads();
+        const double most = (double)top_p * (double)sh.pick_mass;
+        const bool stays = tid < k && (tid == 0 || ((!(top_p < 1.f) || (double)front < most) && logit_of((uint32_t)(mine >> kIndexBits)) >= floor_min));
+        const int stay = __syncthreads_count(stays);  // the first ones
+        const uint32_t at = (1u << kIndexBits) - 1u - (uint32_t)(mine & ((1u << kIndexBits) - 1u));
+        if (tid == stay - 1) sh.pick_own = front + own;
+        sh.mass[tid] = own;
+        sh.count[tid] = at;
+        __syncthreads();
+        const u64 total = sh.pick_own, want = place_of(total);
+        if (stays) {
+          u64 upto = 0;
+#pragma unroll 8
+          for (int j = 0; j < stay; ++j) upto += sh.count[j] <= at ? sh.mass[j] : 0ull;
+          if (upto > want && upto - own <= want) {
+            p.tokens[row] = (int)at;
+            double rest;
+            const int i = w.place(logit_of((uint32_t)(mine >> kIndexBits)), rest);
+            if (p.probs) p.probs[row] = (float)(w.scaled(i, rest) / (double)total);
+          }
+        }
+      }
+      cluster_wait();
+      return;
+    }
+    cluster_sync();  // everyone has seen the number: too many (equal logits, or falling ones); the bins sort it out
+    if (rank == 0 && tid == 0) sh.listed[0] = 0u;
+    clear_bins();
+    __syncthreads();
+  }
+  bool summed = false;  // the sums of what stays are there already: sh.slot_part, and the first block's extra_*
+  if (by_count || by_mass) {
+    Coarse bins;
+    float p_high = __int_as_float(0x7fc00000);
+    bins.top = top;
+    bins.scale = fminf((float)(w.rate * (64.0 / kSteps)), 1e30f);
+    const int one_log2 = min(21, __clz(p.vocab) - 2);  // x the tokens of a row: below 2^31
+    bins.one = (float)(1 << one_log2);
+    run.template each4<2>(floor_all, [&](const float(&l)[4], int) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t weight;
+        const int b = bins.bin(l[e], weight);
+        if (l[e] >= floor_all) {
+          if (by_count) atomicAdd(&sh.count[b], 1u);
+          if (by_mass) atomicAdd(&sh.lo[b], weight);
+        }
+      }
     });
     __syncthreads();
     if (rank != 0) {
       for (int b = tid; b < kBins; b += kThreads) {
         if (by_count && sh.count[b] != 0u) add_cluster_u32(peer(&sh.count[b], 0), sh.count[b]);
-        if (by_mass && (sh.lo[b] | sh.hi[b]) != 0u) {
-          const uint32_t add = sh.lo[b], old = add_cluster_u32(peer(&sh.lo[b], 0), add);
-          const uint32_t carry = sh.hi[b] + (old + add < old ? 1u : 0u);
-          if (carry) add_cluster_u32(peer(&sh.hi[b], 0), carry);
-        }
+        if (by_mass && sh.lo[b] != 0u) add_cluster_u32(peer(&sh.lo[b], 0), sh.lo[b]);
       }
     }
     cluster_sync();
     if (rank == 0) {
-      uint32_t c[kBinsPer], csum = 0, cb0 = 0;
+      uint32_t c[kBinsPer], n[kBinsPer], csum = 0, cb0 = 0;  // tokens (exact, for top-k), and their estimated weight below
       u64 m[kBinsPer], msum = 0, mb0 = 0;
 #pragma unroll
       for (int j = 0; j < kBinsPer; ++j) {
-        csum += c[j] = sh.count[tid * kBinsPer + j];
-        msum += m[j] = ((u64)sh.hi[tid * kBinsPer + j] << 32) + sh.lo[tid * kBinsPer + j];
+        const int b = tid * kBinsPer + j;
+        n[j] = sh.lo[b];
+        csum += c[j] = by_count ? sh.count[b] : n[j] >> one_log2;
+        msum += m[j] = (u64)((double)n[j] * (double)exp2f(30.f - (float)b * (1.f / 64.f)));
       }
       scan_bins(csum, msum, cb0, mb0);
       if (tid == 0) {
         sh.found.bin_k = sh.found.bin_lo = sh.found.bin_hi = -1;
         sh.found.slow = 0;
-        sh.found.mass_lo = 0;
         sh.found.cut = 0;
       }
-      if (tid == kThreads - 1) sh.found.total = mb0 + msum;
+      if (tid == kThreads - 1) sh.pick_mass = mb0 + msum;
       __syncthreads();
       uint32_t cb = cb0;
       u64 mb = mb0;
@@ -424,69 +563,136 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         if (by_count && cb < (uint32_t)top_k && (uint32_t)top_k <= cb + c[j]) {
           sh.found.bin_k = tid * kBinsPer + j;
           sh.found.count_k = cb;
-          sh.found.mass_k = mb;
-          sh.pick_own = m[j];
+          sh.pick_mass = mb + (u64)((double)m[j] * (double)((uint32_t)top_k - cb) / (double)c[j]);
         }
         cb += c[j];
         mb += m[j];
       }
       __syncthreads();
       if (by_mass) {
-        // the sum over the top k is known up to what bin_k holds
-        const bool limited = sh.found.bin_k >= 0;
-        const double least = (double)top_p * (double)(limited ? sh.found.mass_k : sh.found.total);
-        const double most = (double)top_p * (double)(limited ? sh.found.mass_k + sh.pick_own : sh.found.total);
+        // the bin that the estimate points to, and its neighbours as far as the estimate may be off (a weight is rounded to
+        // half a unit of 1 / one, in either direction), up to kAround tokens to either side
+        constexpr uint32_t kAround = 96;
+        const int last = sh.found.bin_k >= 0 ? sh.found.bin_k : kBins - 1;
+        const double want = (double)top_p * (double)sh.pick_mass;
+        cb = cb0;
         mb = mb0;
 #pragma unroll
         for (int j = 0; j < kBinsPer; ++j) {
-          if ((double)mb < least && !((double)(mb + m[j]) < least)) {
+          if (m[j] != 0ull && (double)mb < want && !((double)(mb + m[j]) < want)) {
+            sh.pick_bin = tid * kBinsPer + j;
+            sh.pick_count = cb;
+            sh.pick_own = cb + c[j];
             sh.found.bin_lo = tid * kBinsPer + j;
-            sh.found.mass_lo = mb;
+            sh.pick_mass = mb;
+            sh.found.total = mb + m[j];
           }
-          if ((double)mb < most && !((double)(mb + m[j]) < most)) sh.found.bin_hi = tid * kBinsPer + j;
+          cb += c[j];
           mb += m[j];
         }
         __syncthreads();
-        if (tid == 0 && sh.found.bin_lo < 0) sh.found.bin_lo = 0;  // the top k lie in the first bin
+        if (sh.found.bin_lo >= 0) {
+          const int center = min(sh.pick_bin, last);
+          const uint32_t front = sh.pick_count, behind = (uint32_t)sh.pick_own;
+          const u64 off = (u64)(want / (double)bins.one) + 1ull, mass_front = sh.pick_mass, mass_behind = sh.found.total;
+          __syncthreads();
+          if (tid == 0) {
+            sh.found.bin_lo = center;
+            sh.found.bin_hi = center;
+          }
+          __syncthreads();
+          cb = cb0;
+          mb = mb0;
+#pragma unroll
+          for (int j = 0; j < kBinsPer; ++j) {
+            const int b = tid * kBinsPer + j;
+            const bool near = b < center ? mass_front - (mb + m[j]) <= off : mb - mass_behind <= off;
+            if (near && b < center && front - cb <= kAround) atomicMin(&sh.found.bin_lo, b);
+            cb += c[j];
+            mb += m[j];
+            if (near && b > center && b <= last && cb - behind <= kAround) atomicMax(&sh.found.bin_hi, b);
+          }
+        } else if (tid == 0) {
+          sh.found.slow = 1;  // the estimate went wrong (weights beyond the bins)
+        }
       }
     }
     cluster_sync();
     const int bin_k = (int)ld_cluster_u32(peer(&sh.found.bin_k, 0));
     const int bin_lo = (int)ld_cluster_u32(peer(&sh.found.bin_lo, 0)), bin_hi = (int)ld_cluster_u32(peer(&sh.found.bin_hi, 0));
     {
-      // one window of logits around the bins; the doubles decide inside it
-      int from = kBins, to = -1;
-      if (bin_k >= 0) from = to = bin_k;
+      // the tokens of those bins go to the lists; with top-p, the exact sums of what is in front of them and of everything
+      // (with top-k, of what is in front of its bin).  From here on the bins are ranges of logits.
+      auto edge = [&](int b) {  // the lowest logit of bin b
+        return lowest(top, top - ((float)b + 0.5f) / bins.scale, [&](float l) { return bins.bin(l) <= b; });
+      };
+      const float none = __int_as_float(0x7fc00000);  // no logit is at least that
+      const int best = bins.bin(top);
+      const float k_low = bin_k >= 0 ? fmaxf(edge(bin_k), floor_all) : floor_all, k_high = bin_k > best ? edge(bin_k - 1) : none;
       if (by_mass) {
-        from = min(from, bin_lo);
-        to = max(to, bin_hi);
-      }
-      const float high = from <= 0 || top == inf ? inf : (float)((double)top - (double)(bin_begin(from) - 2) / w.rate + 1e-6 * fabs((double)top));
-      const float low = fmaxf(floor_all, below((double)bin_begin(to + 1) + 2.0));
-      run.template each4<4>(low, [&](const float(&l)[4], int at) {
+        const float p_low = fmaxf(edge(bin_hi), k_low);
+        if (bin_lo > best) p_high = edge(bin_lo - 1);
+        const float all_low = bin_k >= 0 ? k_high : floor_all;
+        double above = 0.0, everything = 0.0;
+        run.template each4<2>(k_low, [&](const float(&l)[4], int at) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (!(l[e] >= low && l[e] <= high)) continue;
-          double rest;
-          const int b = bin_of(w.place(l[e], rest));
-          if (b == bin_k) {
-            const uint32_t slot = add_cluster_u32(peer(&sh.listed[0], 0), 1u);
-            if (slot < kList) st_cluster_u64(peer(&sh.list[0][slot], 0), composite(l[e], at + e));
+          for (int e = 0; e < 4; ++e) {
+            double rest;
+            const int i = w.place(l[e], rest);
+            const double u = (w.scaled(i, rest) + w.kWhole) - w.kWhole;
+            if (l[e] >= all_low) everything += u;
+            if (l[e] >= p_high) above += u;
           }
-          if (by_mass && b >= bin_lo && b <= bin_hi) {
-            const uint32_t slot = add_cluster_u32(peer(&sh.listed[1], 0), 1u);
-            if (slot < kList) st_cluster_u64(peer(&sh.list[1][slot], 0), composite(l[e], at + e));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (l[e] >= p_low && !(l[e] >= p_high)) keep(1, l[e], at + e);
+            if (bin_k >= 0 && l[e] >= k_low && !(l[e] >= k_high)) keep(0, l[e], at + e);
           }
+        });
+        u64 s0 = (u64)everything, s1 = (u64)above;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+          s0 += __shfl_xor_sync(all, s0, d);
+          s1 += __shfl_xor_sync(all, s1, d);
         }
-      });
+        if (lane == 0) {
+          sh.warp64[warp] = s0;
+          sh.slot_part[warp] = s1;
+        }
+        __syncthreads();
+        if (tid == 0) {
+          for (int v = 1; v < kWarps; ++v) {
+            s0 += sh.warp64[v];
+            s1 += sh.slot_part[v];
+          }
+          st_cluster_u64(peer(&sh.slot_all[rank], 0), s0);
+          st_cluster_u64(peer(&sh.slot_above[rank], 0), s1);
+        }
+      } else {
+        run.template each4<4>(k_low, [&](const float(&l)[4], int at) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (l[e] >= k_low && !(l[e] >= k_high)) keep(0, l[e], at + e);
+        });
+      }
     }
     cluster_sync();
     if (rank == 0) {
       const uint32_t n_k = bin_k >= 0 ? sh.listed[0] : 0u, n_p = by_mass ? sh.listed[1] : 0u;
-      if (n_k > kList || n_p > kList) {
-        if (tid == 0) sh.found.slow = 1;
-      } else {
-        auto mass_of = [&](u64 c) -> u64 { return w.units(logit_of((uint32_t)(c >> kIndexBits))); };
+      u64 total = 0, above = 0;
+      if (by_mass) {
+        for (int r = 0; r < n_blocks; ++r) {
+          total += sh.slot_all[r];
+          above += sh.slot_above[r];
+        }
+      }
+      __syncthreads();
+      if (tid == 0) {
+        sh.found.total = total;  // (with top-k: made whole by the search by digits, where that is needed)
+        if (n_k > kList || n_p > kList) sh.found.slow = 1;
+      }
+      __syncthreads();
+      if (sh.found.slow == 0) {
         // The last token of list[0 .. n) in the order with fewer than want_count in front of it, or (by sum) with less than
         // want_mass; base_*: in front of the list.  Leaves it in pick_own, and the sum up to and with it in pick_mass.
         // Up to one token per thread, a thread counts what is in front of its own; longer lists are sorted.
@@ -498,6 +704,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             if (tid < (int)n) {
               uint32_t front = base_count;
               u64 sum = base_mass;
+#pragma unroll 8
               for (uint32_t j = 0; j < n; ++j) {
                 const bool before = list[j] > mine;
                 front += before;
@@ -527,16 +734,30 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           }
           __syncthreads();
         };
-        u64 total = sh.found.total, found = 0;
+        u64 found = 0;
         if (bin_k >= 0) {
-          last_of(sh.list[0], n_k, false, sh.found.count_k, sh.found.mass_k, (uint32_t)top_k, 0.0);
+          last_of(sh.list[0], n_k, false, sh.found.count_k, total, (uint32_t)top_k, 0.0);
           total = sh.pick_mass;
           found = sh.pick_own;
           __syncthreads();
         }
         if (by_mass) {
-          last_of(sh.list[1], n_p, true, 0u, sh.found.mass_lo, 0u, (double)top_p * (double)total);
+          const double want = (double)top_p * (double)total;
+          if (tid == 0) sh.pick_mass = 0;
+          __syncthreads();
+          last_of(sh.list[1], n_p, true, 0u, above, 0u, want);
+          // the cut is where the estimate said if less than `want` lies in front of the list and no less than that up to its end
+          if (tid == 0 && (!((double)above < want) || (double)sh.pick_mass < want)) sh.found.slow = 1;
           found = sh.pick_own > found ? sh.pick_own : found;
+          for (uint32_t j = tid; j < n_p; j += kThreads) {
+            const u64 c = sh.list[1][j];
+            if (c < found || !(logit_of((uint32_t)(c >> kIndexBits)) >= floor_min)) continue;
+            const int at = (1 << kIndexBits) - 1 - (int)(c & ((1u << kIndexBits) - 1u)), owner = (at + run.head) / Run<kBf16>::kUnit / run.per;
+            const u64 u = mass_of(c);
+            const uint32_t add = (uint32_t)u, old = atomicAdd(&sh.extra_lo[owner], add);
+            const uint32_t carry = (uint32_t)(u >> 32) + (old + add < old ? 1u : 0u);
+            if (carry) atomicAdd(&sh.extra_hi[owner], carry);
+          }
         }
         if (tid == 0) sh.found.cut = found;
       }
@@ -544,6 +765,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     cluster_sync();
     if (ld_cluster_u32(peer(&sh.found.slow, 0)) == 0u) {
       cut = ld_cluster_u64(peer(&sh.found.cut, 0));
+      summed = by_mass && !(floor_min > p_high);  // min_p leaves what is in front of the listed bins
     } else {
       // by digits: counts and sums over the tokens of a bin that share a prefix, 11 bits of (logit, index) further each time
       u64 total = ld_cluster_u64(peer(&sh.found.total, 0));
@@ -574,7 +796,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
                 if (d < kDigits - 1 && c >> (shift + kDigitBits) != prefix) continue;
                 b = kBins - 1 - (int)((c >> shift) & (kBins - 1));  // the largest first
               }
-              add_bin(b, true, true, w.units(w.scaled(i, rest)));
+              const u64 u = w.units(w.scaled(i, rest));
+              const uint32_t add = (uint32_t)u, old = atomicAdd(&sh.lo[b], add);
+              const uint32_t carry = (uint32_t)(u >> 32) + (old + add < old ? 1u : 0u);
+              if (carry) atomicAdd(&sh.hi[b], carry);
+              atomicAdd(&sh.count[b], 1u);
             }
           });
           cluster_sync();
@@ -622,16 +848,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
   // ---- 3. the token ----
   // what stays: the logits above floor_kept, and of those that equal cut_logit the tokens up to cut_at
-  float floor_kept = floor_all, cut_logit = -inf;
+  float floor_kept = floor_min, cut_logit = -inf;
   int cut_at = 0;
   if (cut != 0) {
     cut_logit = logit_of((uint32_t)(cut >> kIndexBits));
     cut_at = (1 << kIndexBits) - 1 - (int)(cut & ((1u << kIndexBits) - 1));
     floor_kept = fmaxf(floor_kept, cut_logit);
-  }
-  if (min_p > 0.f && top < inf) {  // (NaN: off)
-    const double most = -(double)kSteps * log2((double)min_p);
-    floor_kept = fmaxf(floor_kept, lowest((float)((double)top - most / w.rate), top, [&](float l) { return w.depth(l) <= most; }));
   }
   auto stays = [&](float l, int at) { return l >= floor_kept && (l > cut_logit || at <= cut_at); };
   // the weights of four tokens: whole numbers, so that a thread's sum (little more than 2^10 tokens of up to 2^42) is exact in double
@@ -644,11 +866,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       if (stays(l[e], at + e)) sum += u;
     }
   };
-  double thread_sum = 0.0;
-  run.template each4<2>(floor_kept, [&](const float(&l)[4], int at) { sum4(l, at, thread_sum); });
-  u64 sum = (u64)thread_sum;
+  u64 sum;
+  if (summed) {
+    const int owner = rank * kWarps + warp;
+    sum = sh.slot_part[warp] + ((u64)ld_cluster_u32(peer(&sh.extra_hi[owner], 0)) << 32) + ld_cluster_u32(peer(&sh.extra_lo[owner], 0));
+  } else {
+    double thread_sum = 0.0;
+    run.template each4<2>(floor_kept, [&](const float(&l)[4], int at) { sum4(l, at, thread_sum); });
+    sum = (u64)thread_sum;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(all, sum, d);
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(all, sum, d);
+  }
   __syncthreads();
   if (lane == 0) sh.warp64[warp] = sum;
   __syncthreads();
@@ -663,9 +891,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     total += t;
   }
   cluster_arrive();
-  const float u = p.u[row];
-  u64 want = u > 0.f ? (u64)((double)u * (double)total) : 0ull;
-  want = want < total ? want : total - 1;
+  const u64 want = place_of(total);
   if (before <= want && want < before + mine) {  // this block has it
     int holder = 0;
     for (; before + sh.warp64[holder] <= want; ++holder) before += sh.warp64[holder];
