@@ -26,10 +26,6 @@
 namespace rk {
 namespace {
 
-#ifndef SAMPLE_MAX
-#define SAMPLE_MAX 8
-#define SAMPLE_MIN 4096
-#endif
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kBinsPer = kBins / kThreads;
 constexpr int kList = 2048, kListPer = kList / kThreads;  // tokens of a cut's bins that are ranked in shared memory
@@ -963,7 +959,7 @@ cudaError_t sample_setup() {
 cudaError_t launch_sample(SampleParams p, int sm_count, cudaStream_t stream) {
   // more blocks per row while the device has places for them (two per SM) and each keeps 2048 tokens
   int blocks = 1;
-  while (blocks < SAMPLE_MAX && p.n * blocks * 2 <= 2 * sm_count && p.vocab > SAMPLE_MIN * blocks) blocks *= 2;
+  while (blocks < 8 && p.n * blocks * 2 <= 2 * sm_count && p.vocab > 4096 * blocks) blocks *= 2;
   if (p.vocab > (1 << 19) && blocks == 1) blocks = 2;  // at most 2^10 tokens per thread (and a unit): sums exact in double
   p.blocks = blocks;
   cudaLaunchConfig_t cfg = {};
