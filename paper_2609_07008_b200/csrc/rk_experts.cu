@@ -8,94 +8,80 @@ namespace rk {
 namespace {
 
 // ------------------------------------------------------------------------------------------------------------
-// rk_moe_route: one token per warp.  The lanes are split evenly over the groups (L lanes per group, L a power of two), lane
-// `sub` of group g holds experts sub, sub + L, ... of the group, so that a group's rank is a reduction over L neighbours.
+// rk_moe_route: a warp per token, a few tokens in turn.  The lanes are split evenly over the groups (L lanes per group, L a
+// power of two), and a lane holds neighbouring experts of its group, so that a group's rank is a reduction over L lanes and
+// the order of lanes and places is the experts' own.
+//
 // Scores are compared in 64 bits: with a few hundred experts the k-th and the next score of a token are closer than fp32
-// rounding about once in 10^4 tokens, and the choice would depend on the instruction that computed them.
+// rounding about once in 10^4 tokens, and the choice would depend on the instruction that computed them.  Hence the order
+// is first taken in fp32, and kept where every decision in it (k + 1 neighbouring scores, all pairs of group ranks) is
+// clearer than the error of the fp32 scores, bounded below; one token in a hundred or two is done again in 64 bits.
+// The weights of the chosen experts are computed in 64 bits, for the tokens of a warp together.
+//
+// A warp's cost is instructions, not the logits' bytes: every lane sorts its keys once, and the k rounds of "largest key of
+// the warp, its lane moves up" are about 20 each.
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kRouteWarps = 8;
 constexpr double kNone = -__builtin_huge_val();
+constexpr unsigned kAll = 0xffffffffu;
 
 __device__ __forceinline__ double max_f64(double a, double b) { return a > b ? a : b; }
 
+template <bool kBf16>
+__device__ __forceinline__ float route_logit(const RouteParams& p, int64_t token, int expert) {
+  const int64_t at = token * p.stride + expert;
+  return kBf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.logits)[at]) : static_cast<const float*>(p.logits)[at];
+}
+
+// The chosen experts in 64 bits: lane q's is returned, -1 where none is left, -2 for a token with a NaN among its scores.
 template <int kPer, bool kBf16>
-__global__ void __launch_bounds__(32 * kRouteWarps) moe_route_kernel(const RouteParams p) {
-  const int64_t token = (int64_t)blockIdx.x * kRouteWarps + (threadIdx.x >> 5);
-  if (token >= p.n) return;
-  const int lane = threadIdx.x & 31;
-  const int width = 1 << p.lanes_log2;  // lanes per group
-  const int g = lane >> p.lanes_log2, sub = lane & (width - 1);
-  const unsigned all = 0xffffffffu;
-  double s[kPer], c[kPer];
+__device__ __noinline__ int route_exact(const RouteParams& p, int64_t token) {
+  const int lane = threadIdx.x & 31, width = 1 << p.lanes_log2, g = lane >> p.lanes_log2, sub = lane & (width - 1);
+  const int begin = g * p.group_size + sub * p.per, count = g < p.n_groups ? max(0, min(p.per, p.group_size - sub * p.per)) : 0;
+  double c[kPer];
   bool bad = false;
   double top = kNone;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int j = sub + i * width;
-    float x = -__int_as_float(0x7f800000);
-    if (g < p.n_groups && j < p.group_size) {
-      const int64_t at = token * p.stride + g * p.group_size + j;
-      x = kBf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p.logits)[at]) : static_cast<const float*>(p.logits)[at];
-    }
+    const float x = i < count ? route_logit<kBf16>(p, token, begin + i) : -__int_as_float(0x7f800000);
     bad |= x != x;
-    s[i] = (double)x;
-    top = max_f64(top, s[i]);
+    c[i] = (double)x;
+    top = max_f64(top, c[i]);
   }
+  double sum = 0.0;
   if (p.softmax) {
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = max_f64(top, __shfl_xor_sync(all, top, d));
-    double sum = 0.0;
+    for (int d = 16; d > 0; d >>= 1) top = max_f64(top, __shfl_xor_sync(kAll, top, d));
+#pragma unroll 1
+    for (int i = 0; i < kPer; ++i) sum += c[i] == kNone ? 0.0 : exp(c[i] - top);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      c[i] = s[i] == kNone ? kNone : 0.0;
-      s[i] = s[i] == kNone ? 0.0 : exp(s[i] - top);
-      sum += s[i];
-    }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(all, sum, d);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) s[i] /= sum;
-  } else {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      c[i] = s[i] == kNone ? kNone : 0.0;
-      s[i] = s[i] == kNone ? 0.0 : 1.0 / (1.0 + exp(-s[i]));
-    }
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(kAll, sum, d);
   }
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int j = sub + i * width;
     if (c[i] == kNone) continue;
-    c[i] = s[i];
-    if (p.bias) c[i] += (double)p.bias[g * p.group_size + j];
+    const double e = exp(p.softmax ? c[i] - top : -c[i]);
+    c[i] = p.softmax ? e / sum : 1.0 / (1.0 + e);
+    if (p.bias) c[i] += (double)p.bias[begin + i];
     bad |= c[i] != c[i];
   }
-  int32_t* ids = p.ids + token * p.k;
-  float* weights = p.weights + token * p.k;
-  if (__any_sync(all, bad)) {
-    if (lane < p.k) {
-      ids[lane] = -1;
-      weights[lane] = __int_as_float(0x7fc00000);
-    }
-    return;
-  }
+  if (__any_sync(kAll, bad)) return -2;
   if (p.n_groups > 1) {
-    // the two largest of the group
-    double a = kNone, b = kNone;
+    double a = kNone, b = kNone;  // the two largest of the group
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       b = max_f64(b, a < c[i] ? a : c[i]);
       a = max_f64(a, c[i]);
     }
     for (int d = width >> 1; d > 0; d >>= 1) {
-      const double a2 = __shfl_xor_sync(all, a, d), b2 = __shfl_xor_sync(all, b, d);
+      const double a2 = __shfl_xor_sync(kAll, a, d), b2 = __shfl_xor_sync(kAll, b, d);
       b = max_f64(max_f64(b, b2), a < a2 ? a : a2);
       a = max_f64(a, a2);
     }
     const double rank = p.group_top == 2 && b != kNone ? a + b : a;
     int better = 0;
     for (int h = 0; h < p.n_groups; ++h) {
-      const double r = __shfl_sync(all, rank, h << p.lanes_log2);
+      const double r = __shfl_sync(kAll, rank, h << p.lanes_log2);
       better += r > rank || (r == rank && h < g);
     }
     if (better >= p.top_groups) {
@@ -103,28 +89,24 @@ __global__ void __launch_bounds__(32 * kRouteWarps) moe_route_kernel(const Route
       for (int i = 0; i < kPer; ++i) c[i] = kNone;
     }
   }
-  // the k best, one after another
-  double w = 0.0, sum = 0.0;
   int id = -1;
   for (int q = 0; q < p.k; ++q) {
-    double best = kNone, score = 0.0;
+    double best = kNone;
     int at = 0x7fffffff;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       if (c[i] > best) {
         best = c[i];
-        score = s[i];
-        at = g * p.group_size + sub + i * width;
+        at = begin + i;
       }
     }
     const int mine = at;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
-      const double b2 = __shfl_xor_sync(all, best, d), s2 = __shfl_xor_sync(all, score, d);
-      const int a2 = __shfl_xor_sync(all, at, d);
+      const double b2 = __shfl_xor_sync(kAll, best, d);
+      const int a2 = __shfl_xor_sync(kAll, at, d);
       if (b2 > best || (b2 == best && a2 < at)) {
         best = b2;
-        score = s2;
         at = a2;
       }
     }
@@ -132,28 +114,284 @@ __global__ void __launch_bounds__(32 * kRouteWarps) moe_route_kernel(const Route
     if (mine == at) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
-        if (g * p.group_size + sub + i * width == at) c[i] = kNone;
+        if (begin + i == at) c[i] = kNone;
     }
-    sum += score;
-    if (lane == q) {
-      w = score;
-      id = at;
+    if (lane == q) id = at;
+  }
+  return id;
+}
+
+// fp32 scores.  exp2 and the reciprocal are right to 2^-22 of their values, the exponent is off by 2^-23.5 |x|:
+//   sigmoid  s (1 - s) (2^-22 + |x| 2^-23.5) + 2^-22.5 s  <  2^-21
+//   softmax  s (2^-21 + |x - top| 2^-23.5 + 2^-21)        <  2^-17 s   up to |x - top| = 80; what is left below that is 0
+// A score plus bias is rounded once (2^-24 of it), and its last bits are the place that it has in its lane.  Without a bias
+// the logits themselves are the order, and equal logits are equal scores; only where scores of different logits could round
+// to the same 64-bit number (logits closer than 2^-45, sigmoid above 15, softmax 600 below the largest) is it left open.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float reciprocal_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+// numbers as integers of the same order; the transformation is its own inverse
+__device__ __forceinline__ int ordered(int bits) { return bits ^ ((bits >> 31) & 0x7fffffff); }
+constexpr float kLog2e = 1.44269504088896340736f;
+// e^d for d <= 0, right to 2^-31: 2^n times the Taylor series of 2^r to degree 8 (|r| <= 1/2)
+__device__ __forceinline__ double exp_31(double d) {
+  const double x = d * 1.44269504088896340736, n = rint(x), r = (x - n) * 0.69314718055994530942;
+  double e = 1.0 / 40320.0;
+  const double c[8] = {1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e = fma(e, r, c[i]);
+  return x < -1000.0 ? 0.0 : __hiloint2double(__double2hiint(e) + ((int)n << 20), __double2loint(e));
+}
+// Batcher's odd-even merge sort, descending; the loops unroll into a fixed network
+template <int kN>
+__device__ __forceinline__ void sort_down(int (&v)[kN]) {
+#pragma unroll
+  for (int p = 1; p < kN; p *= 2) {
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2) {
+#pragma unroll
+      for (int j = k % p; j + k < kN; j += 2 * k) {
+#pragma unroll
+        for (int i = 0; i < k; ++i) {
+          if (i + j + k < kN && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            const int lo = min(v[i + j], v[i + j + k]), hi = max(v[i + j], v[i + j + k]);
+            v[i + j] = hi;
+            v[i + j + k] = lo;
+          }
+        }
+      }
     }
   }
-  if (lane < p.k) {
-    if (p.renorm) w = sum > 0.0 ? w / sum : 0.0;
-    ids[lane] = id;
-    weights[lane] = (float)(w * (double)p.scale);
+}
+
+template <int kPer, bool kBf16>
+__global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 3 : 1) moe_route_kernel(const RouteParams p) {
+  constexpr int kPlace = kPer <= 2 ? 1 : kPer <= 8 ? 7 : kPer <= 16 ? 15 : kPer <= 32 ? 31 : 63;  // bits of a key for its place
+  constexpr float kKeyStep = (float)(kPlace + 2) * 0x1p-23f;                                     // ... and what that and the sum cost
+  constexpr int kNoKey = (int)0x80800000;  // no finite number comes below it
+  const int lane = threadIdx.x & 31, width = 1 << p.lanes_log2, g = lane >> p.lanes_log2, sub = lane & (width - 1);
+  const int span = p.k <= 8 ? 8 : 16, turns = p.turns;  // lanes for a token's choice; tokens of a warp
+  const int64_t first = ((int64_t)blockIdx.x * kRouteWarps + (threadIdx.x >> 5)) * turns;
+  if (first >= p.n) return;
+  const float inf = __int_as_float(0x7f800000);
+  // this lane's experts: `count` from `begin` on
+  const int begin = g * p.group_size + sub * p.per;
+  const int count = g < p.n_groups ? max(0, min(p.per, p.group_size - sub * p.per)) : 0;
+  float bias[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) bias[i] = p.bias && i < count ? p.bias[begin + i] : 0.f;
+  auto load = [&](int64_t token, float (&x)[kPer]) {
+    if constexpr (!kBf16 && kPer % 4 == 0) {
+      if (p.whole) {  // every lane has kPer experts, 16-byte aligned
+        const float4* src = reinterpret_cast<const float4*>(static_cast<const float*>(p.logits) + token * p.stride + begin);
+#pragma unroll
+        for (int i = 0; i < kPer / 4; ++i) {
+          const float4 v = src[i];
+          x[4 * i] = v.x;
+          x[4 * i + 1] = v.y;
+          x[4 * i + 2] = v.z;
+          x[4 * i + 3] = v.w;
+        }
+        return;
+      }
+    }
+    if constexpr (kBf16 && kPer % 8 == 0) {
+      if (p.whole) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p.logits) + token * p.stride + begin);
+#pragma unroll
+        for (int i = 0; i < kPer / 8; ++i) {
+          const uint4 v = src[i];
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[8 * i + j] = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = i < count ? route_logit<kBf16>(p, token, begin + i) : -inf;
+  };
+  float ahead[kPer];
+  load(first, ahead);
+  int id = -1;  // lane turn * span + q: choice q of the token
+  double sum = 1.0, top_mine = 0.0;  // of the softmax (that of renormalised weights drops out)
+#pragma unroll 1
+  for (int turn = 0; turn < turns && first + turn < p.n; ++turn) {
+    const int64_t token = first + turn;
+    float x[kPer], top = -inf, scale = 1.f;
+    int key[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = ahead[i];
+    if (turn + 1 < turns && token + 1 < p.n) load(token + 1, ahead);
+    if (p.softmax) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) top = fmaxf(top, x[i]);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, d));
+      if (p.bias || p.n_groups > 1) {
+        float all = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) all += exp2_fast((x[i] - top) * kLog2e);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) all += __shfl_xor_sync(kAll, all, d);
+        scale = reciprocal_fast(all);
+      }
+    }
+    float worst = 0.f;  // NaN or +inf where a score is: those tokens go the exact way
+    bool clear = true, closed = false;
+    if (p.bias || p.n_groups > 1) {
+      float s[kPer], a = -inf, b = -inf, largest = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        s[i] = p.softmax ? exp2_fast((x[i] - top) * kLog2e) * scale : reciprocal_fast(1.f + exp2_fast(-x[i] * kLog2e));
+        s[i] = x[i] == -inf ? -inf : s[i] + bias[i];
+        worst = max_nan(worst, s[i]);
+      }
+      if (p.n_groups > 1) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          b = fmaxf(b, fminf(a, s[i]));
+          a = fmaxf(a, s[i]);
+          largest = fmaxf(largest, s[i] == -inf ? 0.f : fabsf(s[i]));
+        }
+        const bool plain = !p.bias && p.group_top == 1;  // the largest logits are the order of the ranks
+        if (plain) {
+          a = -inf;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) a = fmaxf(a, x[i]);
+        }
+        for (int d = width >> 1; d > 0; d >>= 1) {
+          const float a2 = __shfl_xor_sync(kAll, a, d), b2 = __shfl_xor_sync(kAll, b, d);
+          b = fmaxf(fmaxf(b, b2), fminf(a, a2));
+          a = fmaxf(a, a2);
+          largest = fmaxf(largest, __shfl_xor_sync(kAll, largest, d));
+        }
+        const float rank = p.group_top == 2 && b != -inf ? a + b : a;
+        // twice the error of a sum of two scores, twice that for two sums, and the sum's own rounding
+        const float near = (p.softmax ? 0x1p-14f * scale : 0x1p-18f) + 4.f * kKeyStep * largest + 0x1p-100f;
+        int better = 0;
+        for (int h = 0; h < p.n_groups; ++h) {
+          const float r = __shfl_sync(kAll, rank, h << p.lanes_log2);
+          better += r > rank || (r == rank && h < g);
+          clear &= h == g || g >= p.n_groups || (r == -inf && rank == -inf) || (plain ? r == rank || fabsf(r - rank) > 0x1p-45f : fabsf(r - rank) > near);
+        }
+        if (plain && g < p.n_groups && rank != -inf) clear &= p.softmax ? rank - top > -600.f : rank < 15.f;
+        closed = better >= p.top_groups;
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) key[i] = __float_as_int(p.bias ? s[i] : x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) key[i] = __float_as_int(x[i]);
+    }
+    if (!p.bias) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) worst = max_nan(worst, x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      key[i] = (ordered(key[i]) & ~kPlace) | (kPlace - i);
+      if (closed) key[i] = (int)0x80000000;
+    }
+    sort_down(key);
+    // k rounds and one more: the largest key of the warp, equal ones by their lane (the experts of a lane, and the lanes, are in
+    // order); its lane moves up
+    int won = (int)0x80000000, from = 0, last = won;  // choice q of the token: its key, and the lane that had it
+    const int q_mine = lane - turn * span;
+    for (int q = 0; q <= p.k; ++q) {
+      const int v = __reduce_max_sync(kAll, key[0] & ~kPlace);
+      last = v;
+      if (v < kNoKey) break;
+      const int owner = __ffs(__ballot_sync(kAll, (key[0] & ~kPlace) == v)) - 1;
+      const int whole = __shfl_sync(kAll, key[0], owner);
+      won = q_mine == q ? whole : won;
+      from = q_mine == q ? owner : from;
+      const bool up = lane == owner;
+#pragma unroll
+      for (int i = 0; i + 1 < kPer; ++i) key[i] = up ? key[i + 1] : key[i];
+      key[kPer - 1] = up ? (int)0x80000000 : key[kPer - 1];
+    }
+    const bool has = q_mine >= 0 && q_mine < p.k && won >= kNoKey;
+    const int chosen = has ? (from >> p.lanes_log2) * p.group_size + (from & (width - 1)) * p.per + kPlace - (won & kPlace) : -1;
+    won &= ~kPlace;
+    // neighbours of the order have to be further apart than both may be off
+    {
+      int next = __shfl_down_sync(kAll, won, 1);
+      const int other = __shfl_down_sync(kAll, chosen, 1);
+      if (q_mine == p.k - 1) next = last;
+      if (has && next >= kNoKey) {
+        const float c = __int_as_float(ordered(won)), c2 = __int_as_float(ordered(next));
+        bool apart;
+        if (p.bias) {
+          apart = c - c2 > (p.softmax ? 0x1p-16f * scale : 0x1p-20f) + kKeyStep * (fabsf(c) + fabsf(c2)) + 0x1p-100f;
+        } else {
+          apart = c - c2 > kKeyStep * (fabsf(c) + fabsf(c2)) + 0x1p-45f;
+          // equal logits are in order already (but those at the end of the list: which of them is out is not known here)
+          if (!apart && q_mine < p.k - 1) apart = route_logit<kBf16>(p, token, chosen) == route_logit<kBf16>(p, token, other);
+          apart &= p.softmax ? c2 - top > -600.f : c < 15.f;
+        }
+        clear &= apart;
+      }
+    }
+    int mine = chosen;
+    if (!__all_sync(kAll, clear && worst < inf)) {
+      const int e = route_exact<kPer, kBf16>(p, token);
+      mine = __shfl_sync(kAll, e, q_mine & 31);
+    }
+    const bool here = q_mine >= 0 && q_mine < p.k;
+    if (here) {
+      id = mine;
+      top_mine = (double)top;
+    }
+    if (p.softmax && !p.renorm) {  // the sum in 64 bits, to which the weights are held
+      double all = 0.0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) all += x[i] == -inf ? 0.0 : exp_31((double)x[i] - (double)top);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) all += __shfl_xor_sync(kAll, all, d);
+      if (here) sum = all;
+    }
+  }
+  // ---- weights ----
+  const int turn = lane / span, q = lane - turn * span;
+  const int64_t token = first + turn;
+  const bool out = q < p.k && turn < turns && token < p.n;
+  double w = 0.0;
+  if (out && id >= 0) {
+    const double x = (double)route_logit<kBf16>(p, token, id);
+    w = p.softmax ? exp(x - top_mine) / sum : 1.0 / (1.0 + exp(-x));
+  }
+  if (p.renorm) {
+    double all = w;
+    for (int d = span >> 1; d > 0; d >>= 1) all += __shfl_xor_sync(kAll, all, d);
+    w = all > 0.0 ? w / all : 0.0;
+  }
+  if (out) {
+    p.ids[token * p.k + q] = id < 0 ? -1 : id;
+    p.weights[token * p.k + q] = id == -2 ? __int_as_float(0x7fc00000) : (float)(w * (double)p.scale);
   }
 }
 
 // ------------------------------------------------------------------------------------------------------------
-// rk_moe_group: a stable counting sort of the pairs by expert, by one cluster, without atomics and without a workspace.
-// Every warp owns a run of consecutive pairs and a count per expert in shared memory; lanes with the same expert find one
-// another by match.any, the lowest of them adds their number.  Scans over warps, over the cluster's blocks (through
-// distributed shared memory) and over experts turn the counts into places; a second walk over the same run writes the list.
+// rk_moe_group: a stable counting sort of the pairs by expert, by one cluster, without a workspace.
+// Every warp owns a run of consecutive pairs and a count per expert in shared memory.  Scans over warps, over the cluster's blocks (through
+// distributed shared memory) and over experts turn the counts into places; a second walk over the same run writes the list:
+// lanes with the same expert find one another by votes on the bits of its number (match.any takes an SM 70 clocks).
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kGroupThreads = 1024, kGroupWarps = kGroupThreads / 32;
+constexpr int kGroupAhead = 8;  // steps whose ids a warp loads together
 
 __device__ __forceinline__ int ld_cluster_s32(uint32_t addr) {
   int v;
@@ -161,6 +399,8 @@ __device__ __forceinline__ int ld_cluster_s32(uint32_t addr) {
   return v;
 }
 
+// kBits: of an expert's number
+template <int kBits>
 __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const GroupParams p) {
   extern __shared__ int group_smem[];
   int* count = group_smem;                        // [warps][experts]
@@ -180,24 +420,28 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
     const int e = p.ids[i];
     if ((unsigned)e >= (unsigned)n_e) return -1;
     if (p.keep != nullptr) {
-      const int64_t t = i / p.k;
-      if (!((p.keep[t] >> (int)(i - t * p.k)) & 1)) return -1;
+      const uint32_t t = (uint32_t)i / (uint32_t)p.k;
+      if (!((p.keep[t] >> ((uint32_t)i - t * (uint32_t)p.k)) & 1)) return -1;
     }
     return e;
   };
-  for (int64_t i = lo; i < hi; i += 32) {
-    const int e = expert_of(i + lane);
-    const unsigned same = __match_any_sync(0xffffffffu, e);
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
-    __syncwarp();
+  for (int64_t i = lo; i < hi; i += 32 * kGroupAhead) {
+    int e[kGroupAhead];
+#pragma unroll
+    for (int j = 0; j < kGroupAhead; ++j) e[j] = expert_of(i + 32 * j + lane);
+#pragma unroll
+    for (int j = 0; j < kGroupAhead; ++j)
+      if (e[j] >= 0) atomicAdd(mine + e[j], 1);
   }
   __syncthreads();
   for (int e = threadIdx.x; e < n_e; e += kGroupThreads) {
-    int sum = 0;
+    int v[kGroupWarps], sum = 0;
+#pragma unroll
+    for (int w = 0; w < kGroupWarps; ++w) v[w] = count[w * n_e + e];
+#pragma unroll
     for (int w = 0; w < kGroupWarps; ++w) {
-      const int v = count[w * n_e + e];
       count[w * n_e + e] = sum;
-      sum += v;
+      sum += v[w];
     }
     total[e] = sum;
   }
@@ -233,18 +477,31 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
   }
   __syncthreads();
   cluster_arrive();  // no block leaves before the others have read its counts
-  for (int64_t i = lo; i < hi; i += 32) {
-    const int e = expert_of(i + lane);
-    const unsigned same = __match_any_sync(0xffffffffu, e);
-    const unsigned below = same & ((1u << lane) - 1u);
-    int at = 0;
-    if (e >= 0) at = mine[e];
-    __syncwarp();
-    if (e >= 0) {
-      p.rows[base[e] + at + __popc(below)] = (int32_t)(i + lane);
-      if (below == 0u) mine[e] = at + __popc(same);
+  auto same_expert = [&](int e) -> unsigned {  // lanes with the same expert; whatever for those without
+    unsigned same = __ballot_sync(kAll, e >= 0);
+#pragma unroll
+    for (int b = 0; b < kBits; ++b) {
+      const unsigned not_mine = (unsigned)((int)((unsigned)e << (31 - b)) >> 31);
+      same &= ~(__ballot_sync(kAll, (e >> b) & 1) ^ not_mine);
     }
-    __syncwarp();
+    return same;
+  };
+  for (int64_t i = lo; i < hi; i += 32 * kGroupAhead) {
+    int e[kGroupAhead];
+#pragma unroll
+    for (int j = 0; j < kGroupAhead; ++j) e[j] = expert_of(i + 32 * j + lane);
+#pragma unroll
+    for (int j = 0; j < kGroupAhead; ++j) {
+      const unsigned same = same_expert(e[j]), below = same & ((1u << lane) - 1u);
+      int at = 0;
+      if (e[j] >= 0) at = mine[e[j]];
+      __syncwarp();
+      if (e[j] >= 0) {
+        p.rows[base[e[j]] + at + __popc(below)] = (int32_t)(i + 32 * j + lane);
+        if (below == 0u) mine[e[j]] = at + __popc(same);
+      }
+      __syncwarp();
+    }
   }
   for (int64_t i = (int64_t)sum_all + (int64_t)rank * kGroupThreads + threadIdx.x; i < n; i += (int64_t)n_blocks * kGroupThreads) p.rows[i] = -1;
   cluster_wait();
@@ -252,7 +509,8 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
 
 template <bool kBf16>
 cudaError_t route_dispatch(const RouteParams& p, int per, cudaStream_t stream) {
-  const unsigned grid = (unsigned)((p.n + kRouteWarps - 1) / kRouteWarps);
+  const int64_t tokens = kRouteWarps * p.turns;  // of a thread block
+  const unsigned grid = (unsigned)((p.n + tokens - 1) / tokens);
   if (per <= 2)
     moe_route_kernel<2, kBf16><<<grid, 32 * kRouteWarps, 0, stream>>>(p);
   else if (per <= 8)
@@ -268,32 +526,66 @@ cudaError_t route_dispatch(const RouteParams& p, int per, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t experts_setup() {
-  return cudaFuncSetAttribute(moe_group_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kGroupWarps + 2) * kMaxExperts * 4);
+namespace {
+typedef void (*GroupKernel)(const GroupParams);
+const GroupKernel kGroupKernels[10] = {moe_group_kernel<1>, moe_group_kernel<2>, moe_group_kernel<3>, moe_group_kernel<4>, moe_group_kernel<5>,
+                                       moe_group_kernel<6>, moe_group_kernel<7>, moe_group_kernel<8>, moe_group_kernel<9>, moe_group_kernel<10>};
+GroupKernel group_kernel(int n_experts) {
+  int bits = 1;
+  while (1 << bits < n_experts) ++bits;
+  return kGroupKernels[bits - 1];
 }
-
-cudaError_t launch_moe_route(RouteParams p, cudaStream_t stream) {
-  p.lanes_log2 = 5;
-  while (p.lanes_log2 > 0 && (32 >> p.lanes_log2) < p.n_groups) --p.lanes_log2;  // 32 / lanes per group >= groups
-  const int per = (p.group_size + (1 << p.lanes_log2) - 1) >> p.lanes_log2;
-  return p.bf16 ? route_dispatch<true>(p, per, stream) : route_dispatch<false>(p, per, stream);
-}
-
-cudaError_t launch_moe_group(const GroupParams& p, cudaStream_t stream) {
-  // eight blocks where their walks (32 pairs per warp and step) are longer than the cluster's two barriers
-  const int n_blocks = p.n * p.k > 4 * kGroupThreads ? 8 : 1;
+cudaLaunchConfig_t group_config(int n_blocks, int n_experts, cudaLaunchAttribute* attr, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n_blocks);
   cfg.blockDim = dim3(kGroupThreads);
-  cfg.dynamicSmemBytes = (size_t)(kGroupWarps + 2) * p.n_experts * 4;
+  cfg.dynamicSmemBytes = (size_t)(kGroupWarps + 2) * n_experts * 4;
   cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = n_blocks;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
+  attr->id = cudaLaunchAttributeClusterDimension;
+  attr->val.clusterDim.x = n_blocks;
+  attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
+  cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, moe_group_kernel, p);
+  return cfg;
+}
+}  // namespace
+
+cudaError_t experts_setup(int32_t* group_blocks) {
+  cudaError_t e = cudaSuccess;
+  for (GroupKernel kernel : kGroupKernels) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kGroupWarps + 2) * kMaxExperts * 4);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  }
+  if (e != cudaSuccess) return e;
+  // 16 blocks where the device has room for such a cluster
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = group_config(16, kMaxExperts, &attr, nullptr);
+  int n = 0;
+  *group_blocks = cudaOccupancyMaxActiveClusters(&n, kGroupKernels[9], &cfg) == cudaSuccess && n > 0 ? 16 : 8;
+  cudaGetLastError();
+  return cudaSuccess;
+}
+
+cudaError_t launch_moe_route(RouteParams p, int sm_count, cudaStream_t stream) {
+  p.lanes_log2 = 5;
+  while (p.lanes_log2 > 0 && (32 >> p.lanes_log2) < p.n_groups) --p.lanes_log2;  // 32 / lanes per group >= groups
+  const int per = (p.group_size + (1 << p.lanes_log2) - 1) >> p.lanes_log2;
+  // a warp takes several tokens (their weights are computed together) once every SM has 32 warps at work
+  const int span = p.k <= 8 ? 8 : 16;
+  const int64_t turns = p.n / (32 * (int64_t)sm_count);
+  p.turns = turns < 1 ? 1 : turns > 32 / span ? 32 / span : (int32_t)turns;
+  p.per = per;
+  const int64_t in_16 = p.bf16 ? 8 : 4;
+  p.whole = (per == 8 || per == 16 || per == 32) && (per << p.lanes_log2) == p.group_size && (p.n_groups << p.lanes_log2) == 32 &&
+            (reinterpret_cast<uintptr_t>(p.logits) & 15u) == 0 && p.stride % in_16 == 0;
+  return p.bf16 ? route_dispatch<true>(p, per, stream) : route_dispatch<false>(p, per, stream);
+}
+
+cudaError_t launch_moe_group(const GroupParams& p, int32_t group_blocks, cudaStream_t stream) {
+  // several blocks where their walks (32 pairs per warp and step) are longer than the cluster's two barriers
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = group_config(p.n * p.k > 4 * kGroupThreads ? group_blocks : 1, p.n_experts, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, group_kernel(p.n_experts), p);
 }
 
 }  // namespace rk

@@ -31,6 +31,7 @@ struct rk_ctx {
   int n_pairs = 0;
   int32_t matvec_slots[4] = {};
   int32_t matmul8_slots[2] = {};
+  int32_t group_blocks = 8;
   DeviceStatus* d_status = nullptr;
   GemmBatch* d_batches = nullptr;  // [uv_g: G][uv_l: L][wa_g: G][wa_l: G][wb: 1]
   int off_uv_g = 0, off_uv_l = 0, off_wa_g = 0, off_wa_l = 0, off_wb = 0;
@@ -276,7 +277,7 @@ rk_status rk_create_ex(const rk_profile* prof, uint32_t flags, rk_ctx** out) {
   if (e == cudaSuccess) e = proj_fused_setup();
   if (e == cudaSuccess) e = decode_attn_setup();
   if (e == cudaSuccess) e = matvec4_setup(ctx->matvec_slots, ctx->sm_count);
-  if (e == cudaSuccess) e = experts_setup();
+  if (e == cudaSuccess) e = experts_setup(&ctx->group_blocks);
   if (e == cudaSuccess) e = matmul8_setup(ctx->matmul8_slots);
   if (e == cudaSuccess) e = sample_setup();
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&ctx->d_status), sizeof(DeviceStatus));
@@ -1492,7 +1493,7 @@ rk_status rk_moe_route(rk_ctx* ctx, const rk_route* rt, const void* logits, int3
   p.top_groups = rt->top_groups;
   p.group_top = rt->group_top;
   p.scale = rt->scale;
-  cudaError_t e = launch_moe_route(p, static_cast<cudaStream_t>(stream));
+  cudaError_t e = launch_moe_route(p, ctx->sm_count, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "routing launch");
 }
 
@@ -1508,7 +1509,7 @@ rk_status rk_moe_group(rk_ctx* ctx, const int32_t* ids, const uint8_t* keep, int
   rk_status s = device_check(ctx);
   if (s != RK_OK) return s;
   GroupParams p = {ids, keep, row_off, rows, n, k, n_experts};
-  cudaError_t e = launch_moe_group(p, static_cast<cudaStream_t>(stream));
+  cudaError_t e = launch_moe_group(p, ctx->group_blocks, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "expert list launch");
 }
 

@@ -280,9 +280,10 @@ struct RouteParams {
   int64_t n, stride;
   int32_t bf16, softmax, renorm, k, n_groups, group_size, top_groups, group_top;
   float scale;
-  int32_t lanes_log2;  // set by the launcher: lanes of a warp per group
+  // set by the launcher: lanes of a warp per group; tokens of a warp; experts of a lane; whether all lanes have as many, aligned
+  int32_t lanes_log2, turns, per, whole;
 };
-cudaError_t launch_moe_route(RouteParams p, cudaStream_t stream);
+cudaError_t launch_moe_route(RouteParams p, int sm_count, cudaStream_t stream);
 
 struct GroupParams {
   const int32_t* ids;   // [n][k]
@@ -292,8 +293,9 @@ struct GroupParams {
   int64_t n;
   int32_t k, n_experts;
 };
-cudaError_t experts_setup();
-cudaError_t launch_moe_group(const GroupParams& p, cudaStream_t stream);
+// group_blocks: thread blocks of the cluster that makes long lists
+cudaError_t experts_setup(int32_t* group_blocks);
+cudaError_t launch_moe_group(const GroupParams& p, int32_t group_blocks, cudaStream_t stream);
 
 struct Matmul8Params {
   CUtensorMap tm_w;      // [n_mat * n_out][k_pad] bytes, box 128 x 128
