@@ -274,12 +274,41 @@ class Q8:
         shape = codes.shape
         if len(shape) not in (2, 3) or shape[-1] != (k + 15) // 16 * 16:
             raise ValueError(f"codes of k = {k} must be [n_mat, n_rows, {(k + 15) // 16 * 16}], not {tuple(shape)}")
-        self.codes = _need(codes, "codes", torch.int8, None)
-        self.scales = _need(scales, "scales", torch.float32, shape[:-1])
-        self.n_mat, self.n_rows, self.k = (shape[0] if len(shape) == 3 else 1), shape[-2], int(k)
-        self.index = codes.get_device()
-        self.struct = rk_q8(self.n_mat, self.n_rows, self.k, _ptr(codes), _ptr(scales))
+        self._codes = _need(codes, "codes", torch.int8, None)
+        self._scales = _need(scales, "scales", torch.float32, shape[:-1])
+        self._set(shape[:-1], int(k), codes.get_device(), codes.device, _ptr(codes), _ptr(scales))
+
+    def _set(self, rows, k, index, device, codes, scales):
+        self.rows, self.k, self.index, self.device = rows, k, index, device
+        self.n_mat, self.n_rows = (rows[0] if len(rows) == 2 else 1), rows[-1]
+        self.struct = rk_q8(self.n_mat, self.n_rows, k, codes, scales)
         self.ref = C.byref(self.struct)
+
+    @classmethod
+    def _new(cls, rows, k: int, device: torch.device) -> "Q8":
+        """For a call's own result: one allocation, of which codes and scales become views when somebody asks for them."""
+        self = object.__new__(cls)
+        at = 1
+        for extent in rows:
+            at *= extent
+        self._split = at * ((k + 15) // 16 * 16)
+        self._buf = _empty(self._split + 4 * at, torch.int8, device)
+        self._codes = self._scales = None
+        base = self._buf.data_ptr()
+        self._set(rows, k, self._buf.get_device(), device, base, base + self._split)
+        return self
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            self._codes = self._buf[:self._split].view(self.rows + ((self.k + 15) // 16 * 16,))
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            self._scales = self._buf[self._split:].view(torch.float32).view(self.rows)
+        return self._scales
 
 
 def _rows(t: torch.Tensor, name: str, dtypes, width: int = -1) -> int:
@@ -298,6 +327,7 @@ def _rows(t: torch.Tensor, name: str, dtypes, width: int = -1) -> int:
 
 _FLOATS = (torch.bfloat16, torch.float32)
 _SCORES = {"softmax": 0, "sigmoid": 1}
+_ROUTES = {}  # parameters of rk_moe_route as the C ABI takes them
 
 
 def make_layout_struct(seg_off, seg_delta, seg_has_artifact):
@@ -656,7 +686,12 @@ class Context:
             weights = _empty((n, k), torch.float32, logits.device)
         else:
             _need(weights, "weights", torch.float32, (n, k))
-        route = rk_route(n_experts, k, n_groups, top_groups, group_top, _SCORES[score], 1 if renorm else 0, scale)
+        key = (n_experts, k, n_groups, top_groups, group_top, score, renorm, scale)
+        route = _ROUTES.get(key)
+        if route is None:  # (a program has a few of them: one per kind of layer)
+            if len(_ROUTES) > 64:
+                _ROUTES.clear()
+            route = _ROUTES[key] = rk_route(n_experts, k, n_groups, top_groups, group_top, _SCORES[score], 1 if renorm else 0, scale)
         s = lib.rk_moe_route(self.handle, C.byref(route), logits.data_ptr(), 0 if logits.dtype is torch.bfloat16 else 1, stride,
                              None if bias is None else bias.data_ptr(), n, ids.data_ptr(), weights.data_ptr(), _quick_stream())
         if s:
@@ -693,8 +728,7 @@ class Context:
             stride = _rows(x, "x", (torch.bfloat16,))
         k = x.shape[-1]
         if q8 is None:
-            shape = tuple(x.shape[:-1])
-            q8 = Q8(_empty(shape + ((k + 15) // 16 * 16,), torch.int8, x.device), _empty(shape, torch.float32, x.device), k)
+            q8 = Q8._new(tuple(x.shape[:-1]), k, x.device)
         else:
             _here(q8, "q8")
             if (q8.n_mat, q8.n_rows, q8.k) != (x.shape[0] if x.dim() == 3 else 1, x.shape[-2], k):
@@ -714,7 +748,7 @@ class Context:
             raise TypeError(f"the products' outputs are bfloat16 or float32, not {out_dtype}")
         stride = w.n_rows
         if y is None:
-            y = _empty((n, stride), out_dtype, x.codes.device)
+            y = _empty((n, stride), out_dtype, x.device)
         else:
             stride = _rows(y, "y", _FLOATS, w.n_rows)
             if y.shape[0] != n:
