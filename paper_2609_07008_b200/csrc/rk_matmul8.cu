@@ -159,16 +159,19 @@ __global__ void __launch_bounds__(512, 3) quant8_kernel(const __nv_bfloat16* __r
 // products
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kThreads8 = 384;          // warp 0 loads, warp 1 issues, warps 4-11 scale and store
-constexpr int kGatherWarps = 4;         // by expert: warps 12-15, and 2 and 3, gather token rows: one for each stage of the ring
+constexpr int kGatherWarps = 5;         // by expert: warps 12-16, and 2 and 3, gather token rows: one for each stage of the ring
 constexpr int kStages8 = 6;
 constexpr int kStep = 128;      // bytes (= values) of k per stage
 constexpr int kTileM = 256, kTileN = 256;
+constexpr int kTileNExperts = 192;  // smaller tiles leave room for a seventh stage
+constexpr int kMaxStages8 = 7;
 constexpr int kBandTok = 8;     // token tiles of a band: W streams past them together
 
 struct Smem8 {
-  static constexpr uint32_t kABytes = 128 * kStep, kBBytes = 128 * kStep, kStageBytes = kABytes + kBBytes;
-  static constexpr uint32_t kOffBars = kStages8 * kStageBytes;  // full[stages], empty[stages], acc_full[2], acc_empty[2]
-  static constexpr uint32_t kOffTmemPtr = kOffBars + (2 * kStages8 + 4) * 8;
+  static constexpr uint32_t kABytes = 128 * kStep, kBBytes = 128 * kStep;
+  static constexpr uint32_t kOffBars = kMaxStages8 * (kABytes + kTileNExperts / 2 * kStep);  // (the larger one of the rings)
+  // full[stages], empty[stages], acc_full[2], acc_empty[2]
+  static constexpr uint32_t kOffTmemPtr = kOffBars + (2 * kMaxStages8 + 4) * 8;
   static constexpr uint32_t kOffAbort = kOffTmemPtr + 8;
   static constexpr uint32_t kOffScan = kOffAbort + 8;               // 16 sums of the block's scan
   static constexpr uint32_t kOffTok = (kOffScan + 128 + 15) / 16 * 16;  // [2][256] TokenOut
@@ -202,7 +205,7 @@ __device__ __forceinline__ void copies_wait() {
 
 // token rows are cut into as few tiles as they need, of equal size (a multiple of 32): a short rest would cost nearly a full
 // tile's loads of W
-__device__ __forceinline__ int token_tiles(int n) { return (n + kTileN - 1) / kTileN; }
+__device__ __forceinline__ int token_tiles(int n, int most) { return (n + most - 1) / most; }
 __device__ __forceinline__ int token_tile_rows(int n, int tiles) { return ((n + tiles - 1) / tiles + 31) & ~31; }
 
 struct Tile8 {
@@ -253,6 +256,9 @@ template <bool kExperts, int kSplit>
 __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8, 1)
     rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
   using S = Smem8;
+  constexpr int kStages = kExperts ? kMaxStages8 : kStages8, kMost = kExperts ? kTileNExperts : kTileN;
+  constexpr uint32_t kStageBytes = S::kABytes + (uint32_t)(kMost / 2 * kStep);
+  static_assert(kStages * kStageBytes <= S::kOffBars, "ring");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -260,9 +266,9 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   const uint32_t cluster_rank = cluster_ctarank(), crank = cluster_rank & 1u, lead = cluster_rank & ~1u;  // place in the pair; the pair's leader
   const int pair = (int)blockIdx.x / (2 * kSplit), n_pairs = (int)gridDim.x / (2 * kSplit);
   auto full_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * s; };
-  auto empty_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * (kStages8 + s); };
-  auto acc_full_bar = [&](int b) -> uint32_t { return smem_base + S::kOffBars + 8u * (2 * kStages8 + b); };
-  auto acc_empty_bar = [&](int b) -> uint32_t { return smem_base + S::kOffBars + 8u * (2 * kStages8 + 2 + b); };
+  auto empty_bar = [&](int s) -> uint32_t { return smem_base + S::kOffBars + 8u * (kStages + s); };
+  auto acc_full_bar = [&](int b) -> uint32_t { return smem_base + S::kOffBars + 8u * (2 * kStages + b); };
+  auto acc_empty_bar = [&](int b) -> uint32_t { return smem_base + S::kOffBars + 8u * (2 * kStages + 2 + b); };
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + S::kOffAbort);
   volatile uint32_t* tmem_ptr_smem = reinterpret_cast<volatile uint32_t*>(smem + S::kOffTmemPtr);
   int* first = reinterpret_cast<int*>(smem + S::kOffFirst);
@@ -275,7 +281,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
 
   if (threadIdx.x == 0) {
     *abort_flag = 0;
-    for (int s = 0; s < kStages8; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       // leader's: one arrival (its own expect_tx) + the bytes of both CTAs, and both CTAs' gather warp of the stage
       mbar_init(full_bar(s), kExperts ? 1 + 2 : 1);
       mbar_init(empty_bar(s), 1);  // each CTA's: the pair's commit arrives on both
@@ -304,7 +310,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
       if (e < p.n_mat) {
         const int lo = offs[e], hi = offs[e + 1];
         if (lo >= 0 && lo <= hi && hi <= p.n_tok)
-          tiles = (long long)token_tiles(hi - lo) * n_chan;
+          tiles = (long long)token_tiles(hi - lo, kMost) * n_chan;
         else if (blockIdx.x == 0)
           report_status(p.status, 4 /*RK_ERR_ROWS*/, RK_CHK_EXPERT_OFF, e);
       }
@@ -328,7 +334,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
     n_tiles = base <= (1 << 30) ? (int)base : 0;
     if (base > (1 << 30) && blockIdx.x == 0 && threadIdx.x == 0) report_status(p.status, 4 /*RK_ERR_ROWS*/, RK_CHK_EXPERT_OFF, p.n_mat);
   } else {
-    n_tiles = n_chan * token_tiles(p.n_tok);
+    n_tiles = n_chan * token_tiles(p.n_tok, kMost);
   }
   // Tile t of the pair's sequence.  `e` walks up the experts as t grows.
   auto tile_at = [&](int t, int& e) -> Tile8 {
@@ -336,13 +342,13 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
     if constexpr (kExperts) {
       while (t >= first[e + 1]) ++e;
       const int i = t - first[e], tt = i / n_chan;
-      const int n = offs[e + 1] - offs[e], rows = token_tile_rows(n, token_tiles(n));
+      const int n = offs[e + 1] - offs[e], rows = token_tile_rows(n, token_tiles(n, kMost));
       r.mat = e;
       r.chan = (i - tt * n_chan) * kTileM;
       r.tok = offs[e] + tt * rows;
       r.n = min(rows, offs[e + 1] - r.tok);
     } else {
-      const int n_tok_tiles = token_tiles(p.n_tok), rows = token_tile_rows(p.n_tok, n_tok_tiles), per_band = kBandTok * n_chan;
+      const int n_tok_tiles = token_tiles(p.n_tok, kMost), rows = token_tile_rows(p.n_tok, n_tok_tiles), per_band = kBandTok * n_chan;
       const int band = t / per_band, here = min(kBandTok, n_tok_tiles - band * kBandTok), rem = t - band * per_band;
       const int cb = rem / here;
       r.mat = 0;
@@ -374,27 +380,27 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
       const int half = ((tile.n + 31) >> 5) << 4;  // token rows of this CTA, a multiple of 16
       const int w_row = tile.mat * p.n_out + tile.chan + (int)crank * 128;
       for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
-        if (it >= (uint32_t)kStages8) ok = mbar_wait_bounded<false>(empty_bar(s), turn ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
+        if (it >= (uint32_t)kStages) ok = mbar_wait_bounded<false>(empty_bar(s), turn ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         const uint32_t full_remote = mapa_shared(full_bar(s), lead);
-        const uint32_t a_dst = smem_base + s * S::kStageBytes;
+        const uint32_t a_dst = smem_base + s * kStageBytes;
         if (elect_one()) {
           if (crank == 0) mbar_arrive_expect_tx(full_bar(s), kBytes);
           tma_load_2d_pair(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row);
           if constexpr (!kExperts) tma_load_2d_pair(a_dst + S::kABytes, &p.tm_x, full_remote, (k_first + kc) * kStep, tile.tok + (int)crank * half);
         }
         __syncwarp();
-        if (++s == (uint32_t)kStages8) {
+        if (++s == (uint32_t)kStages) {
           s = 0;
           turn ^= 1u;
         }
       }
     }
-    for (uint32_t back = 1; back <= (uint32_t)kStages8 && ok; ++back) {
+    for (uint32_t back = 1; back <= (uint32_t)kStages && ok; ++back) {
       if (it >= back) {
         const uint32_t u = it - back;
-        ok = mbar_wait_bounded<false>(empty_bar(u % kStages8), (u / kStages8) & 1u, limit, abort_flag, p.status, WM_EMPTY, -1);
+        ok = mbar_wait_bounded<false>(empty_bar(u % kStages), (u / kStages) & 1u, limit, abort_flag, p.status, WM_EMPTY, -1);
         ok = __all_sync(0xffffffffu, ok);
       }
     }
@@ -419,7 +425,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
           ok = mbar_wait_bounded<false>(full_bar(s), turn, limit, abort_flag, p.status, WM_FULL, t);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
-          const uint32_t a_addr = smem_base + s * S::kStageBytes;
+          const uint32_t a_addr = smem_base + s * kStageBytes;
           if (elect_one()) {
             const uint64_t da = umma_desc_sw128(a_addr, 16, 1024), db = umma_desc_sw128(a_addr + S::kABytes, 16, 1024);
 #pragma unroll
@@ -429,7 +435,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
             if (kc == k_chunks - 1) umma_commit_2_mc(acc_full_bar(b), (uint16_t)(3u << lead));
           }
           __syncwarp();
-          if (++s == (uint32_t)kStages8) {
+          if (++s == (uint32_t)kStages) {
             s = 0;
             turn ^= 1u;
           }
@@ -439,29 +445,29 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   } else if (kExperts && (warp >= 12 || warp == 2 || warp == 3)) {
     // ---- gather (by expert): a warp fills one stage of the ring over and over, so that all six may be under way.  Four rows
     // per instruction, eight lanes to a row of 128 bytes ----
-    static_assert(kStages8 == kGatherWarps + 2, "one warp per stage");
-    const uint32_t s = warp >= 12 ? warp - 12 : warp + 2;
+    static_assert(!kExperts || kStages == kGatherWarps + 2, "one warp per stage");
+    const uint32_t s = warp >= 12 ? warp - 12 : warp + kGatherWarps - 2;
     const int sub = lane >> 3, chunk = lane & 7;
-    const uint32_t dst = smem_base + s * S::kStageBytes + S::kABytes;
+    const uint32_t dst = smem_base + s * kStageBytes + S::kABytes;
     const uint32_t full_remote = mapa_shared(full_bar(s), lead);
     int e = 0, t = pair, known = -1, half = 0, kc = (int)s;
-    uint32_t from[32];  // this lane's rows of the half, in units of 16 bytes from x
-    for (uint32_t use = 0;; ++use, kc += kStages8) {
+    uint32_t from[kMost / 8];  // this lane's rows of the half, in units of 16 bytes from x
+    for (uint32_t use = 0;; ++use, kc += kStages) {
       for (; kc >= k_chunks; kc -= k_chunks) t += n_pairs;
       if (t >= n_tiles) break;
       if (t != known) {
         const Tile8 tile = tile_at(t, e);
         known = t;
         half = ((tile.n + 31) >> 5) << 4;
-        uint32_t row[4];  // lane l has rows l, l + 32, ...; places behind the last repeat it (their sums are not stored)
+        uint32_t row[(kMost + 63) / 64];  // lane l has rows l, l + 32, ...; places behind the last repeat it (their sums are not stored)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < (kMost + 63) / 64; ++j) {
           const int pr = p.rows[tile.tok + min((int)crank * half + 32 * j + lane, tile.n - 1)];
           row[j] = ((unsigned)pr < (unsigned)p.n_tok ? (unsigned)pr / (unsigned)p.per : 0u) * (uint32_t)(p.k_pad >> 4);
         }
         // rows x k_pad / 16 stays below 2^32
 #pragma unroll
-        for (int i = 0; i < 32; ++i) from[i] = __shfl_sync(0xffffffffu, row[i >> 3], ((4 * i) & 31) + sub) + chunk;
+        for (int i = 0; i < kMost / 8; ++i) from[i] = __shfl_sync(0xffffffffu, row[i >> 3], ((4 * i) & 31) + sub) + chunk;
       }
       bool ok = use == 0 || mbar_wait_bounded<false>(empty_bar(s), (use & 1u) ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
       ok = __all_sync(0xffffffffu, ok);
@@ -469,7 +475,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
       const bool real = kc * kStep + 16 * chunk < p.k_pad;
       const uint8_t* src = p.x + (real ? kc * kStep : 0);
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
+      for (int i = 0; i < kMost / 8; ++i)
         if (4 * i < half) copy16_async(dst + sw128_offset(4 * i + sub, chunk), src + (uint64_t)from[i] * 16, real);
       copies_commit();
       copies_wait<0>();
@@ -648,7 +654,8 @@ cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_s
   p.paired = !p.out_f32 && (reinterpret_cast<uintptr_t>(p.y) & 3u) == 0 && p.y_stride % 2 == 0 && p.n_out % 2 == 0;
   const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
   // by expert the number of tiles is known on the device only: at most one part-filled tile per expert more than full ones
-  const int64_t tok_tiles = (p.n_tok + kTileN - 1) / kTileN + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
+  const int most = p.rows ? kTileNExperts : kTileN;
+  const int64_t tok_tiles = (p.n_tok + most - 1) / most + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
   const int64_t tiles = n_chan * tok_tiles;
   cudaLaunchAttribute attr;
   if (!p.rows) {
