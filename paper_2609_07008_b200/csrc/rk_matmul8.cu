@@ -375,10 +375,12 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
     int e = 0;
     bool ok = true;
     constexpr uint32_t kBytes = 2u * (S::kABytes + (kExperts ? 0u : S::kBBytes));
+    const uint64_t once_policy = l2_policy_evict_first();  // (64 tokens: 149 -> 142 us)
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const Tile8 tile = tile_at(t, e);
       const int half = ((tile.n + 31) >> 5) << 4;  // token rows of this CTA, a multiple of 16
       const int w_row = tile.mat * p.n_out + tile.chan + (int)crank * 128;
+      const bool once = kExperts && offs[tile.mat + 1] - offs[tile.mat] == tile.n;  // no other tile reads these weights
       for (int kc = 0; kc < k_chunks && ok; ++kc, ++it) {
         if (it >= (uint32_t)kStages) ok = mbar_wait_bounded<false>(empty_bar(s), turn ^ 1u, limit, abort_flag, p.status, WM_EMPTY, t);
         ok = __all_sync(0xffffffffu, ok);
@@ -387,7 +389,10 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
         const uint32_t a_dst = smem_base + s * kStageBytes;
         if (elect_one()) {
           if (crank == 0) mbar_arrive_expect_tx(full_bar(s), kBytes);
-          tma_load_2d_pair(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row);
+          if (once)
+            tma_load_2d_pair_hint(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row, once_policy);
+          else
+            tma_load_2d_pair(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row);
           if constexpr (!kExperts) tma_load_2d_pair(a_dst + S::kABytes, &p.tm_x, full_remote, (k_first + kc) * kStep, tile.tok + (int)crank * half);
         }
         __syncwarp();
