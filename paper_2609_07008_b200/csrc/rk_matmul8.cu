@@ -257,6 +257,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
     rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
   using S = Smem8;
   constexpr int kStages = kExperts ? kMaxStages8 : kStages8, kMost = kExperts ? kTileNExperts : kTileN;
+  const int most = kExperts ? kMost : p.tile_rows;  // token rows of a tile
   constexpr uint32_t kStageBytes = S::kABytes + (uint32_t)(kMost / 2 * kStep);
   static_assert(kStages * kStageBytes <= S::kOffBars, "ring");
   extern __shared__ uint8_t smem_raw[];
@@ -334,7 +335,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
     n_tiles = base <= (1 << 30) ? (int)base : 0;
     if (base > (1 << 30) && blockIdx.x == 0 && threadIdx.x == 0) report_status(p.status, 4 /*RK_ERR_ROWS*/, RK_CHK_EXPERT_OFF, p.n_mat);
   } else {
-    n_tiles = n_chan * token_tiles(p.n_tok, kMost);
+    n_tiles = n_chan * token_tiles(p.n_tok, most);
   }
   // Tile t of the pair's sequence.  `e` walks up the experts as t grows.
   auto tile_at = [&](int t, int& e) -> Tile8 {
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
       r.tok = offs[e] + tt * rows;
       r.n = min(rows, offs[e + 1] - r.tok);
     } else {
-      const int n_tok_tiles = token_tiles(p.n_tok, kMost), rows = token_tile_rows(p.n_tok, n_tok_tiles), per_band = kBandTok * n_chan;
+      const int n_tok_tiles = token_tiles(p.n_tok, most), rows = token_tile_rows(p.n_tok, n_tok_tiles), per_band = kBandTok * n_chan;
       const int band = t / per_band, here = min(kBandTok, n_tok_tiles - band * kBandTok), rem = t - band * per_band;
       const int cb = rem / here;
       r.mat = 0;
@@ -661,12 +662,30 @@ cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_s
   // by expert the number of tiles is known on the device only: at most one part-filled tile per expert more than full ones
   const int most = p.rows ? kTileNExperts : kTileN;
   const int64_t tok_tiles = (p.n_tok + most - 1) / most + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
-  const int64_t tiles = n_chan * tok_tiles;
+  int64_t tiles = n_chan * tok_tiles;
   cudaLaunchAttribute attr;
   if (!p.rows) {
-    // few tiles: k is shared by the pairs of a cluster, as long as all tiles run at once and a pair keeps eight steps of k
+    // Few tiles: smaller ones, or k shared by the pairs of a cluster, put more SMs to work.  Clocks of a pair, measured: a step
+    // of k takes 2 N where the tensor cores set the pace and no less than 350, a token row's stores 14, the join 2000 + 10 N.
     const int k_chunks = (p.k_pad + kStep - 1) / kStep;
-    const int split = tiles <= split_slots[1] && k_chunks >= 32 ? 4 : tiles <= split_slots[0] && k_chunks >= 16 ? 2 : 1;
+    double best = 1e30;
+    int split = 1;
+    for (int most = kTileN; most >= 32; most /= 2) {
+      const int64_t n = n_chan * ((p.n_tok + most - 1) / most);
+      for (int s = 1; s <= 4; s *= 2) {
+        const int64_t slots = s == 1 ? sm_count / 2 : split_slots[s / 4];
+        const int64_t rounds = (n + slots - 1) / slots;
+        if (s > 1 && (rounds > 1 || k_chunks < 4 * s)) continue;
+        const double step = 2.1 * most > 350.0 ? 2.1 * most : 350.0;
+        const double clocks = (double)rounds * ((k_chunks + s - 1) / s) * step + 14.0 * most + (s > 1 ? 2000.0 + 10.0 * most : 0.0);
+        if (clocks < 0.97 * best) {  // (the larger tile where it makes no difference)
+          best = clocks;
+          p.tile_rows = most;
+          split = s;
+        }
+      }
+    }
+    tiles = n_chan * ((p.n_tok + p.tile_rows - 1) / p.tile_rows);
     if (split > 1) {
       const cudaLaunchConfig_t cfg = pair_config<false>((int)tiles * 2 * split, 2 * split, &attr, stream);
       return split == 4 ? cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, 4>, p) : cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, 2>, p);
