@@ -122,8 +122,8 @@ rk_status rk_set_wait_limit_ms(rk_ctx* ctx, int32_t ms);
  * empty, so the consumers' bounded waits expire, the kernel drains and returns, and
  * rk_poll_status() reports RK_ERR_TIMEOUT.  Results are not produced while it is on.  Use it
  * together with a short rk_set_wait_limit_ms.
- * rk_matvec4 likewise issues no copies of the weights, and rk_cache4_attn withholds one of the signals below, whichever `on`
- * names (any other number counts as RK_STARVE_LOADS); the other calls make no difference between them. */
+ * rk_matvec4, rk_matmul8 and rk_matmul8_experts likewise issue no copies of the weights, and rk_cache4_attn withholds one of
+ * the signals below, whichever `on` names (any other number counts as RK_STARVE_LOADS); the other calls make no difference between them. */
 #define RK_STARVE_LOADS 1      /* the keys' rope part is not copied */
 #define RK_STARVE_QUERIES 2    /* the queries' latent part is not copied */
 #define RK_STARVE_QUERY_ROPE 3 /* their turned rope part is not announced */
@@ -518,8 +518,9 @@ typedef struct rk_q8 {
  *   x  device bf16: row i at x + i * x_stride (in elements, >= k, of any alignment to 2 bytes; multiples of 16 bytes are faster) */
 rk_status rk_quant8(rk_ctx* ctx, const void* x, int64_t x_stride, const rk_q8* q8, void* stream);
 
-/* y[t][o] = x.scales[t] w.scales[o] * sum_j x.codes[t][j] w.codes[o][j]; the sums are exact, the result is rounded to fp32
- * and, for out_dtype 0, to bf16.  w.n_mat = x.n_mat = 1, w.k = x.k.
+/* y[t][o] = sum_j x.codes[t][j] w.codes[o][j] * x.scales[t] * w.scales[o]; the sums are exact, then they and the two products,
+ * from the left, are rounded to fp32 (tokens beyond 1e29 can overflow there) and, for out_dtype 0, to bf16.
+ * w.n_mat = x.n_mat = 1, w.k = x.k.
  *   y  device bf16 (out_dtype 0) or fp32 (1): token t at y + t * y_stride, w.n_rows values (y_stride >= w.n_rows) */
 rk_status rk_matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, void* y, int64_t y_stride, int32_t out_dtype, void* stream);
 
@@ -542,10 +543,10 @@ rk_status rk_matmul8_experts(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const 
  *   logits  device [n][vocab], bf16 (logits_dtype 0) or fp32 (1), rows `stride` elements apart; -inf is never drawn
  *   u       device fp32 [n]: uniform random numbers in [0, 1); values outside count as the nearest inside, NaN as 0
  *   temperature, top_k, top_p, min_p  device [n] (top_k int32, the others fp32), each NULL where all rows leave it off.
- *     temperature <= 0 or NaN: the largest logit; top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN: off
+ *     temperature below 2^-100 or NaN: the largest logit; top_k <= 0, top_p >= 1 or NaN, min_p <= 0 or NaN: off
  *   tokens  device int32 [n];  probs  device fp32 [n], the token's p over the sum of those that stayed, or NULL
- * A row with a NaN, and a row of nothing but -inf, gets token -1 and prob NaN.  +inf: only those are drawn, each alike.  p is rounded to multiples of
- * 2^-42: a token below 2^-43 of the largest is not drawn.  1 <= vocab <= 2^20, n * 8 < 2^31. */
+ * A row with a NaN, and a row of nothing but -inf, gets token -1 and prob NaN.  +inf: only those are drawn, each alike.
+ * p is rounded to multiples of 2^-42: a token below 2^-42 of the largest is not drawn.  1 <= vocab <= 2^20, n * 8 < 2^31. */
 rk_status rk_sample(rk_ctx* ctx, const void* logits, int32_t logits_dtype, int64_t stride, int64_t n, int32_t vocab, const float* u,
                     const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens,
                     float* probs, void* stream);

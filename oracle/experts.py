@@ -118,7 +118,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     x = np.asarray(logits, dtype=np.float64)
     if np.isnan(x).any() or x.max() == -np.inf:
         return -1, np.nan
-    if not temperature > 0:
+    if not temperature >= 2.0 ** -100:
         return int(np.argmax(x)), 1.0
     if x.max() == np.inf:
         x = np.where(x == np.inf, 0.0, -np.inf)

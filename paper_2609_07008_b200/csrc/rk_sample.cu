@@ -12,13 +12,17 @@
 //   1. the largest logit (and whether there is a NaN)
 //   2. up to 256 for top-k: the tokens that reach a logit which at least k tokens do (step 1 found one on its way) go to the
 //      first block, which sorts them and needs nothing more.
-//      Otherwise, where top-k or top-p is on: counts, and estimates of the weights, in bins of 1/64 octave in fp32, joined in the first
-//      block, which picks the bins around the cuts; then exact sums of what is in front of them, while their tokens (some
-//      hundred of 128 K) go to the first block's lists, which ranks them, finds the cuts and checks the estimate.
+//      Otherwise, where top-k or top-p is on: counts, and estimates of the weights, in bins of 1/64 octave in fp32, joined in
+//      the first block, which picks the bins around the cuts; then exact sums of what is in front of them, while their tokens
+//      (some hundred of 128 K) go to the first block's lists, which ranks them, finds the cuts and checks the estimate.
 //      Where that fails or a list is too short (thousands of equal logits), the cut is searched for by exact counts and sums,
 //      11 bits of (logit, index) at a time.
 //   3. sums of what stays, by block and by warp; the block that holds u * total shares out the warp's run that holds it
 // The row is read again by each step: it comes out of L2 after the first.
+//
+// 64 rows of 131072 fp32 logits (33.6 MB, 5.2 us to read once): 24 us without filters, 27 with top-k 50, 58 with top-p 0.9; one
+// row of 32001 with all filters 11.  What bounds it: many rows, the instructions of the passes (44 per token where its weight is
+// needed); a single row, the chain of cluster barriers and code that runs for the first time.
 #include <cuda_bf16.h>
 
 #include "rk_internal.h"
@@ -29,10 +33,10 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kBinsPer = kBins / kThreads;
 constexpr int kList = 2048, kListPer = kList / kThreads;  // tokens of a cut's bins that are ranked in shared memory
-constexpr int kQuick = 256;                      // up to here the top k are found without bins
-constexpr int kUnitLog2 = 42;                    // weights are multiples of 2^-42
-constexpr int kSteps = 256;                      // i counts 256ths of an octave below the largest
-constexpr int kEnd = kUnitLog2 * kSteps;         // from here on tokens weigh nothing
+constexpr int kQuick = 256;               // up to here the top k are found without bins
+constexpr int kUnitLog2 = 42;             // weights are multiples of 2^-42
+constexpr int kSteps = 256;               // i counts 256ths of an octave below the largest
+constexpr int kEnd = kUnitLog2 * kSteps;  // from here on tokens weigh nothing
 constexpr int kIndexBits = 20, kDigitBits = 11, kKeyBits = 32 + kIndexBits, kDigits = (kKeyBits + kDigitBits - 1) / kDigitBits;
 typedef unsigned long long u64;
 
@@ -367,7 +371,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   }
   if (groups < top_k) reached = -inf;
   const bool dead = !(top > -inf);
-  const bool one = !(temp > 0.f) || top_p <= 0.f || min_p > 1.f || top_k == 1;  // the first token only
+  // the first token only (at temperatures below 2^-100 two numbers that differ at all are worlds apart)
+  const bool one = !(temp >= 0x1p-100f) || top_p <= 0.f || min_p > 1.f || top_k == 1;
   if (dead || one) {
     uint32_t at = 0xffffffffu;
     if (!dead)

@@ -1,7 +1,8 @@
 """Sampling against the float64 oracle.  Tokens are compared as they are; the random numbers of the tests lie between two
 borders of the oracle's cumulated weights with a distance of at least 1e-9 of the sum (the kernel's weights are off by at most
-2^-43 each; at most 2^20 of them: below 1.2e-7 of one unit, and the sum is at least one unit, 4e-13 typically), so that the
-token does not hang on a rounding.  Probabilities: one fp32 rounding (2^-24) of a value whose own error is below 1e-9."""
+2^-43 and 1.4e-13 of themselves each, and the sum is at least 1; the tests' 200003 of them would reach 2.3e-8 only if they
+all erred to one side, and reach 5e-11 as roundings do), so that the token does not hang on a rounding.  Probabilities: one
+fp32 rounding (2^-24) of a value whose own error is below 1e-9."""
 import numpy as np
 import pytest
 import torch
@@ -215,3 +216,17 @@ def test_refusals(rk, ctx):
         ctx.rk_sample(x.t(), torch.zeros(10, device="cuda"))
     tokens, probs = ctx.rk_sample(torch.zeros((0, 10), device="cuda"), u[:0])
     assert tokens.shape == (0,) and probs.shape == (0,)
+
+
+# temperatures at both ends of fp32 (from 2^-100 down the largest logit; infinite: all alike), over logits at both ends
+@pytest.mark.parametrize("vocab", [7, 3000])
+@pytest.mark.parametrize("temperature", [float("inf"), 3e38, 1e30, 1e-30, 2.0 ** -100, 2.0 ** -101, 1e-44, -1.0, float("nan")])
+def test_extreme_temperatures(ctx, vocab, temperature):
+    rng = np.random.default_rng(vocab)
+    x = rng.standard_normal((4, vocab))
+    x[1] = rng.choice([3e38, -3e38, 1.0], size=vocab)
+    x[2] *= 1e-37
+    x[3, ::2] = -np.inf
+    u = rng.random(4)
+    for kw in ({}, dict(top_k=3), dict(top_p=0.6), dict(min_p=0.5), dict(top_k=300, top_p=0.6)):
+        check(ctx, x, u, temperature=temperature, **kw)
