@@ -1587,6 +1587,7 @@ static rk_status matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int3
   p.n_mat = w->n_mat;
   p.per = per;
   p.out_f32 = out_dtype;
+  p.starve = ctx->starve_loads;
   cudaError_t e = launch_matmul8(p, ctx->sm_count, ctx->matmul8_slots, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "8-bit product launch");
 }

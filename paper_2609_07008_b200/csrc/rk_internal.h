@@ -311,6 +311,7 @@ struct Matmul8Params {
   unsigned long long wait_ns;
   int32_t n_tok;  // token rows; by expert: pairs (places of the list, rows of y)
   int32_t n_out, k_pad, n_mat, per, out_f32;
+  int32_t starve;  // rk_test_starve_loads
   int32_t paired, tile_rows;  // set by the launcher: rows and channels allow 4-byte stores of bf16 pairs; token rows of a dense tile at most
 };
 // split_slots[i]: clusters of 4 << i thread blocks that run at the same time on the current device

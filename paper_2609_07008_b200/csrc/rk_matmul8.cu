@@ -8,14 +8,21 @@
 // are the rows of the accumulator (M = 256) and the tokens its columns, because the number of tokens is what varies:
 // N follows the rows that a tile really has, in steps of 32, down to the one or two rows an expert gets in a decode step.
 // Each CTA streams its 128 channels of W and its half of the token rows in 128-byte steps of k (16 + up to 16 KB per
-// stage); W is read once per 256 tokens, and with N = 256 an SM draws 64 bytes per clock from L2 at the full rate of the
-// tensor cores, below the 76 that it can.  Persistent: the accumulator is double buffered in tensor memory, so that the
-// scales and stores of one tile run under the products of the next.
+// stage); with N = 256 an SM draws 64 bytes per clock from L2 at the full rate of the tensor cores, below the 76 that it
+// can.  Persistent: the accumulator is double buffered in tensor memory, so that the scales and stores of one tile run under
+// the products of the next.  Where there are few tiles they are made smaller, or 2 or 4 pairs in a cluster share k and add
+// their sums through each other's shared memory (launch_matmul8; 256 x 4096 x 8192: 20.6 -> 15.4 us).
+//   8192 tokens x 7168 channels x 16384: 590 us, 3.26 POP/s, 0.96 of twice the bf16 library product's measured burst rate:
+//   bounded by the tensor cores.  5 x 4096 x 8192: 11.6 us, of which W's 33.6 MB cost 5.2 at the memory's measured rate and
+//   the rest is launch, setup, the join and the stores.
 //
-// By expert, the token rows of a tile are a gather (the tokens that chose the expert): four warps copy them with 16-byte
-// asynchronous loads into the swizzled operand layout, so that no sorted copy of the activations is made; the outputs go
-// straight to the pairs' rows of y.  (TMA's gather of four rows took 72 clocks of each SM's copy engine per instruction,
-// 2300 per 128 rows; a stage has 512.)
+// By expert, the token rows of a tile are a gather (the tokens that chose the expert): seven warps, one per stage, copy them
+// with 16-byte asynchronous loads into the swizzled operand layout, so that no sorted copy of the activations is made; the
+// outputs go straight to the pairs' rows of y.  Tiles have up to 192 rows, which leaves room for the seventh stage (64 tokens:
+// 154 -> 149 us).  (TMA's gather of four rows took 72 clocks of each SM's copy engine per instruction, 2300 per 128 rows; a
+// stage has 512.)
+//   64 tokens, all weights used once: 143 us, 0.98 of the measured copy rate.  8192 tokens: 313 us; by removal, the gather
+//   costs 30 us of it, the first bytes of each expert's weights out of memory 62, the stores 28.
 #include <cuda_bf16.h>
 
 #include "rk_internal.h"
@@ -109,7 +116,7 @@ __device__ __noinline__ void quant8_exact(unsigned who, const __nv_bfloat16* row
 }
 
 // A row per thread block, or per warp (kWarp: up to 1024 values).  A row of up to 32 values per thread is read once; longer
-// ones a second time out of L2.  HBM bound: two bytes in, one out per value.
+// ones a second time out of L2.  HBM bound: two bytes in, one out per value; 8192 x 16384: 75 us, 0.83 of the copy rate.
 template <bool kVec, bool kWarp>
 __global__ void __launch_bounds__(512, 3) quant8_kernel(const __nv_bfloat16* __restrict__ x, int64_t x_stride, int64_t n_rows, int k,
                                                         int k_pad, uint8_t* __restrict__ codes, float* __restrict__ scales) {
@@ -390,10 +397,12 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
         const uint32_t a_dst = smem_base + s * kStageBytes;
         if (elect_one()) {
           if (crank == 0) mbar_arrive_expect_tx(full_bar(s), kBytes);
-          if (once)
-            tma_load_2d_pair_hint(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row, once_policy);
-          else
-            tma_load_2d_pair(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row);
+          if (!p.starve) {  // (the timeout tests: announced and never sent)
+            if (once)
+              tma_load_2d_pair_hint(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row, once_policy);
+            else
+              tma_load_2d_pair(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row);
+          }
           if constexpr (!kExperts) tma_load_2d_pair(a_dst + S::kABytes, &p.tm_x, full_remote, (k_first + kc) * kStep, tile.tok + (int)crank * half);
         }
         __syncwarp();
@@ -449,7 +458,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
       }
     }
   } else if (kExperts && (warp >= 12 || warp == 2 || warp == 3)) {
-    // ---- gather (by expert): a warp fills one stage of the ring over and over, so that all six may be under way.  Four rows
+    // ---- gather (by expert): a warp fills one stage of the ring over and over, so that all of them may be under way.  Four rows
     // per instruction, eight lanes to a row of 128 bytes ----
     static_assert(!kExperts || kStages == kGatherWarps + 2, "one warp per stage");
     const uint32_t s = warp >= 12 ? warp - 12 : warp + kGatherWarps - 2;
