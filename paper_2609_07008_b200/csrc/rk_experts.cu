@@ -14,13 +14,15 @@ namespace {
 //
 // Scores are compared in 64 bits: with a few hundred experts the k-th and the next score of a token are closer than fp32
 // rounding about once in 10^4 tokens, and the choice would depend on the instruction that computed them.  Hence the order
-// is first taken in fp32, and kept where every decision in it (k + 1 neighbouring scores, all pairs of group ranks) is
-// clearer than the error of the fp32 scores, bounded below; one token in a hundred or two is done again in 64 bits.
+// is first taken in fp32, and kept where every decision in it (k + 1 neighbouring scores, the last group that takes part and the
+// first that does not) is clearer than the error of the fp32 scores, bounded below.  Where only the order of scores is open,
+// those few are compared in 64 bits, one per lane; other open tokens are done again as a whole (6 us more for the call that
+// meets one: 777 tokens of 160 experts 11.8 -> 5.7 us, 32768 of 256 39 -> 35).
 // The weights of the chosen experts are computed in 64 bits, for the tokens of a warp together.
 //
 // A warp's cost is instructions, not the logits' bytes: every lane sorts its keys once, and the k rounds of "largest key of
-// the warp, its lane moves up" are about 20 each.  32768 tokens, 256 experts, 8 of them, softmax: 39 us (33.6 MB of fp32
-// logits: 5.2 us); 64 tokens, 8 groups: 5.4 us, most of it launch and code that runs for the first time.
+// the warp, its lane moves up" are about 20 each.  32768 tokens, 256 experts, 8 of them, sigmoid and bias: 35 us (33.6 MB of fp32
+// logits: 5.2 us); 64 tokens, 8 groups: 5.1 us, most of it launch and code that runs for the first time.
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kRouteWarps = 8;
 constexpr double kNone = -__builtin_huge_val();
@@ -286,10 +288,20 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 3 : 1) moe_route
         for (int h = 0; h < p.n_groups; ++h) {
           const float r = __shfl_sync(kAll, rank, h << p.lanes_log2);
           better += r > rank || (r == rank && h < g);
-          clear &= h == g || g >= p.n_groups || (r == -inf && rank == -inf) || (plain ? r == rank || fabsf(r - rank) > 0x1p-45f : fabsf(r - rank) > near);
         }
-        if (plain && g < p.n_groups && rank != -inf) clear &= p.softmax ? rank - top > -600.f : rank < 15.f;
         closed = better >= p.top_groups;
+        // the worst group that takes part against the best one that does not: their order among themselves is nobody's concern
+        float worst_in = g < p.n_groups && !closed ? rank : inf, best_out = g < p.n_groups && closed ? rank : -inf;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+          worst_in = fminf(worst_in, __shfl_xor_sync(kAll, worst_in, d));
+          best_out = fmaxf(best_out, __shfl_xor_sync(kAll, best_out, d));
+        }
+        const float gap = closed ? worst_in - rank : rank - best_out;
+        if (g < p.n_groups && best_out != -inf && rank != -inf) {
+          clear = plain ? gap == 0.f || gap > 0x1p-45f : gap > near;
+          if (plain) clear &= p.softmax ? rank - top > -600.f : rank < 15.f;
+        }
       }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) key[i] = __float_as_int(p.bias ? s[i] : x[i]);
@@ -308,49 +320,77 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 3 : 1) moe_route
     }
     sort_down(key);
     // k rounds and one more: the largest key of the warp, equal ones by their lane (the experts of a lane, and the lanes, are in
-    // order); its lane moves up
-    int won = (int)0x80000000, from = 0, last = won;  // choice q of the token: its key, and the lane that had it
-    const int q_mine = lane - turn * span;
-    for (int q = 0; q <= p.k; ++q) {
+    // order); its lane moves up.  Lane q keeps choice q: its key, and the lane that had it.
+    int won = (int)0x80000000, from = 0, n_won = 0;
+    auto draw = [&]() -> bool {
       const int v = __reduce_max_sync(kAll, key[0] & ~kPlace);
-      last = v;
-      if (v < kNoKey) break;
+      if (v < kNoKey) return false;
       const int owner = __ffs(__ballot_sync(kAll, (key[0] & ~kPlace) == v)) - 1;
       const int whole = __shfl_sync(kAll, key[0], owner);
-      won = q_mine == q ? whole : won;
-      from = q_mine == q ? owner : from;
+      won = lane == n_won ? whole : won;
+      from = lane == n_won ? owner : from;
       const bool up = lane == owner;
 #pragma unroll
       for (int i = 0; i + 1 < kPer; ++i) key[i] = up ? key[i + 1] : key[i];
       key[kPer - 1] = up ? (int)0x80000000 : key[kPer - 1];
+      ++n_won;
+      return true;
+    };
+    while (n_won <= p.k && draw()) {
     }
-    const bool has = q_mine >= 0 && q_mine < p.k && won >= kNoKey;
-    const int chosen = has ? (from >> p.lanes_log2) * p.group_size + (from & (width - 1)) * p.per + kPlace - (won & kPlace) : -1;
-    won &= ~kPlace;
-    // neighbours of the order have to be further apart than both may be off
+    auto expert = [&] { return (from >> p.lanes_log2) * p.group_size + (from & (width - 1)) * p.per + kPlace - (won & kPlace); };
+    // is v certainly in front of v2 (keys without their places), or an equal logit in the right order?
+    auto apart = [&](int v, int v2) -> bool {
+      const float c = __int_as_float(ordered(v)), c2 = __int_as_float(ordered(v2));
+      if (p.bias) return c - c2 > (p.softmax ? 0x1p-16f * scale : 0x1p-20f) + kKeyStep * (fabsf(c) + fabsf(c2)) + 0x1p-100f;
+      if (kBf16 && v == v2) return true;  // (the places have bits of their own)
+      return v != v2 && (fmaxf(fabsf(c), fabsf(c2)) >= 0x1p-20f || c - c2 > 0x1p-36f) && (p.softmax ? c2 - top > -600.f : c < 15.f);
+    };
+    bool sure = true;
     {
-      int next = __shfl_down_sync(kAll, won, 1);
-      const int other = __shfl_down_sync(kAll, chosen, 1);
-      if (q_mine == p.k - 1) next = last;
-      if (has && next >= kNoKey) {
-        const float c = __int_as_float(ordered(won)), c2 = __int_as_float(ordered(next));
-        bool apart;
-        if (p.bias) {
-          apart = c - c2 > (p.softmax ? 0x1p-16f * scale : 0x1p-20f) + kKeyStep * (fabsf(c) + fabsf(c2)) + 0x1p-100f;
-        } else {
-          apart = c - c2 > kKeyStep * (fabsf(c) + fabsf(c2)) + 0x1p-45f;
-          // equal logits are in order already (but those at the end of the list: which of them is out is not known here)
-          if (!apart && q_mine < p.k - 1) apart = route_logit<kBf16>(p, token, chosen) == route_logit<kBf16>(p, token, other);
-          apart &= p.softmax ? c2 - top > -600.f : c < 15.f;
+      const int next = __shfl_down_sync(kAll, won, 1);
+      if (lane < p.k && lane + 1 < n_won) sure = apart(won & ~kPlace, next & ~kPlace);
+    }
+    int mine = lane < p.k && lane < n_won ? expert() : -1;
+    bool exact = !__all_sync(kAll, clear && worst < inf);
+    if (!exact && !__all_sync(kAll, sure)) {
+      // The order of a few is open: those, as far down as they may belong to the k, are compared in 64 bits, one per lane.
+      const int last = __shfl_sync(kAll, won, p.k - 1) & ~kPlace;
+      exact = p.softmax ? p.bias != nullptr : !p.bias && __int_as_float(ordered(__shfl_sync(kAll, won, 0) & ~kPlace)) >= 15.f;
+      while (!exact && n_won > p.k && !apart(last, __shfl_sync(kAll, won, n_won - 1) & ~kPlace)) {
+        exact = n_won == 32;
+        if (exact || !draw()) break;
+      }
+      if (!exact) {
+        double d = kNone;
+        const int at = lane < n_won ? expert() : 0x7fffffff;
+        if (lane < n_won) {
+          d = (double)route_logit<kBf16>(p, token, at);
+          if (!p.softmax) {
+            d = 1.0 / (1.0 + exp(-d));
+            if (p.bias) d += (double)p.bias[at];
+          } else if (d - (double)top <= -600.0) {
+            exact = true;
+          }
         }
-        clear &= apart;
+        int front = 0;
+        for (int j = 0; j < n_won; ++j) {
+          const double other = __shfl_sync(kAll, d, j);
+          const int other_at = __shfl_sync(kAll, at, j);
+          front += other > d || (other == d && other_at < at);
+          exact |= p.softmax && lane < n_won && other != d && fabs(other - d) <= 0x1p-45;
+        }
+        mine = -1;
+        for (int j = 0; j < n_won; ++j) {
+          const int place = __shfl_sync(kAll, front, j), other_at = __shfl_sync(kAll, at, j);
+          if (lane < p.k && place == lane) mine = other_at;
+        }
+        exact = __any_sync(kAll, exact);
       }
     }
-    int mine = chosen;
-    if (!__all_sync(kAll, clear && worst < inf)) {
-      const int e = route_exact<kPer, kBf16>(p, token);
-      mine = __shfl_sync(kAll, e, q_mine & 31);
-    }
+    if (exact) mine = route_exact<kPer, kBf16>(p, token);
+    const int q_mine = lane - turn * span;
+    mine = __shfl_sync(kAll, mine, q_mine & 31);
     const bool here = q_mine >= 0 && q_mine < p.k;
     if (here) {
       id = mine;
@@ -390,7 +430,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 3 : 1) moe_route
 // Every warp owns a run of consecutive pairs and a count per expert in shared memory.  Scans over warps, over the cluster's
 // blocks (through distributed shared memory) and over experts turn the counts into places; a second walk over the same run
 // writes the list: lanes with the same expert find one another by votes on the bits of its number (match.any takes an SM
-// 70 clocks).  What bounds it: short lists, the chain of launch, loads, scans and stores (384 pairs: 6.2 us); long ones, the
+// 70 clocks).  What bounds it: short lists, the chain of launch, loads, scans and stores (384 pairs: 5.2 us); long ones, the
 // votes of the cluster's SMs (262144 pairs: 18 us).
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kGroupThreads = 1024, kGroupWarps = kGroupThreads / 32;
@@ -416,7 +456,9 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
   const int64_t run = ((n + (int64_t)n_blocks * kGroupThreads - 1) / ((int64_t)n_blocks * kGroupThreads)) * 32;
   const int64_t lo = ((int64_t)rank * kGroupWarps + warp) * run, hi = lo + run < n ? lo + run : n;
   int* mine = count + warp * n_e;
-  for (int e = threadIdx.x; e < kGroupWarps * n_e; e += kGroupThreads) count[e] = 0;
+  const int64_t rest = n - (int64_t)rank * kGroupWarps * run;
+  const int busy = rest <= 0 ? 0 : rest >= kGroupWarps * run ? kGroupWarps : (int)((rest + run - 1) / run);  // warps with pairs
+  for (int i = threadIdx.x; i < busy * n_e; i += kGroupThreads) count[i] = 0;
   __syncthreads();
   auto expert_of = [&](int64_t i) -> int {
     if (i >= hi) return -1;
@@ -428,8 +470,8 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
     }
     return e;
   };
+  int e[kGroupAhead];
   for (int64_t i = lo; i < hi; i += 32 * kGroupAhead) {
-    int e[kGroupAhead];
 #pragma unroll
     for (int j = 0; j < kGroupAhead; ++j) e[j] = expert_of(i + 32 * j + lane);
 #pragma unroll
@@ -437,16 +479,16 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
       if (e[j] >= 0) atomicAdd(mine + e[j], 1);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < n_e; e += kGroupThreads) {
+  for (int x = threadIdx.x; x < n_e; x += kGroupThreads) {
     int v[kGroupWarps], sum = 0;
 #pragma unroll
-    for (int w = 0; w < kGroupWarps; ++w) v[w] = count[w * n_e + e];
+    for (int w = 0; w < kGroupWarps; ++w) v[w] = w < busy ? count[w * n_e + x] : 0;
 #pragma unroll
     for (int w = 0; w < kGroupWarps; ++w) {
-      count[w * n_e + e] = sum;
+      if (w < busy) count[w * n_e + x] = sum;
       sum += v[w];
     }
-    total[e] = sum;
+    total[x] = sum;
   }
   cluster_arrive();
   cluster_wait();
@@ -490,11 +532,13 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
     return same;
   };
   for (int64_t i = lo; i < hi; i += 32 * kGroupAhead) {
-    int e[kGroupAhead];
+    if (run > 32 * kGroupAhead) {  // (a shorter run's are still there)
 #pragma unroll
-    for (int j = 0; j < kGroupAhead; ++j) e[j] = expert_of(i + 32 * j + lane);
+      for (int j = 0; j < kGroupAhead; ++j) e[j] = expert_of(i + 32 * j + lane);
+    }
 #pragma unroll
     for (int j = 0; j < kGroupAhead; ++j) {
+      if (i + 32 * j >= hi) break;
       const unsigned same = same_expert(e[j]), below = same & ((1u << lane) - 1u);
       int at = 0;
       if (e[j] >= 0) at = mine[e[j]];
@@ -585,9 +629,15 @@ cudaError_t launch_moe_route(RouteParams p, int sm_count, cudaStream_t stream) {
 }
 
 cudaError_t launch_moe_group(const GroupParams& p, int32_t group_blocks, cudaStream_t stream) {
-  // several blocks where their walks (32 pairs per warp and step) are longer than the cluster's two barriers
+  // Up to eight blocks, one step (32 pairs) of a warp costs more than the barriers of a cluster twice the size; sixteen pay from four
+  // steps on (256 experts, in 1 / 2 / 4 / 8 / 16 blocks: 768 pairs 5.5 / 5.5 / 5.7 / 6.1 / 6.7 us, 6144 pairs
+  // 8.8 / 7.2 / 6.8 / 6.3 / 7.0, 49152 pairs 40.6 / 22.9 / 14.5 / 9.4 / 8.2)
+  const int64_t pairs = p.n * p.k;
+  int blocks = 1;
+  while (blocks < 8 && pairs > (int64_t)blocks * kGroupThreads) blocks *= 2;
+  if (pairs > 4 * 8 * kGroupThreads) blocks = group_blocks;
   cudaLaunchAttribute attr;
-  const cudaLaunchConfig_t cfg = group_config(p.n * p.k > 4 * kGroupThreads ? group_blocks : 1, p.n_experts, &attr, stream);
+  const cudaLaunchConfig_t cfg = group_config(blocks, p.n_experts, &attr, stream);
   return cudaLaunchKernelEx(&cfg, group_kernel(p.n_experts), p);
 }
 

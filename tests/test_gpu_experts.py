@@ -199,3 +199,28 @@ def test_wrong_tensors_are_refused(rk, ctx):
         ctx.rk_moe_group(ids, 1025)
     with pytest.raises(TypeError):
         ctx.rk_moe_group(ids.long(), 4)
+
+
+# Scores a few fp32 steps apart, where the order is settled in 64 bits: among a token's own choices, at the last place, over more
+# experts than a warp compares at once, and between groups.  Logits are multiples of 2^-23 around a few levels (scores of different
+# logits are at least 2^-36 apart, equal ones equal; groups go by one score, as sums of two could differ by less than their
+# rounding), biases from two values.
+@pytest.mark.parametrize("n_e, k, groups, top_groups, group_top", [(64, 6, 1, 1, 1), (256, 8, 1, 1, 1), (160, 6, 8, 3, 1), (256, 6, 8, 4, 1), (1024, 16, 1, 1, 1), (24, 3, 3, 2, 1)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("steps", [1, 5, 40, 400])
+def test_scores_that_are_nearly_equal(ctx, n_e, k, groups, top_groups, group_top, score, biased, steps):
+    rng = np.random.default_rng(n_e + k + steps)
+    n = 60
+    levels = np.array([0.5, 1.0 - 2.0 ** -12, -1.5, 0.0])
+    x = levels[rng.integers(0, 4, size=(n, n_e))] + rng.integers(0, steps + 1, size=(n, n_e)) * 2.0 ** -23
+    x[n // 2:] = levels[rng.integers(0, 4, size=(n - n // 2, 1))] + rng.integers(0, steps + 1, size=(n - n // 2, n_e)) * 2.0 ** -23
+    x[-3, ::2] = 0.0
+    x[-3, 1::2] = -0.0
+    x = x.astype(np.float32)
+    bias = rng.choice([0.0, 0.25], size=n_e) if biased else None
+    ids, w = ctx.rk_moe_route(torch.from_numpy(x).cuda(), k, bias=None if bias is None else torch.from_numpy(bias.astype(np.float32)).cuda(),
+                              score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
+    want, ww = X.route(x.astype(np.float64), k, bias=bias, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
+    assert np.array_equal(ids.cpu().numpy(), want)
+    assert np.abs(w.double().cpu().numpy() - ww).max() <= 2.0 ** -24 + 1e-12
