@@ -21,10 +21,10 @@ namespace {
 // The weights of the chosen experts are computed in 64 bits, for the tokens of a warp together.
 //
 // A warp's cost is instructions, not the logits' bytes: every lane sorts its keys once, and the k rounds of "largest key of
-// the warp, its lane moves up" are about 20 each.  32768 tokens, 256 experts, 8 of them, sigmoid and bias: 35 us (33.6 MB of fp32
-// logits: 5.2 us); 64 tokens, 8 groups: 5.1 us, most of it launch and code that runs for the first time.
+// the warp, its lane moves up" are about 20 each.  32768 tokens, 256 experts, 8 of them, sigmoid and bias: 34 us (33.6 MB of fp32
+// logits: 5.2 us); 64 tokens, 8 groups: 4.5 us, most of it launch and code that runs for the first time.
 // ------------------------------------------------------------------------------------------------------------
-constexpr int kRouteWarps = 8;
+constexpr int kRouteWarps = 2;  // small thread blocks: few tokens spread over more SMs (64 tokens: 4.5 us, with eight 5.2)
 constexpr double kNone = -__builtin_huge_val();
 constexpr unsigned kAll = 0xffffffffu;
 
@@ -180,7 +180,7 @@ __device__ __forceinline__ void sort_down(int (&v)[kN]) {
 }
 
 template <int kPer, bool kBf16>
-__global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 3 : 1) moe_route_kernel(const RouteParams p) {
+__global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 14 : 1) moe_route_kernel(const RouteParams p) {
   constexpr int kPlace = kPer <= 2 ? 1 : kPer <= 8 ? 7 : kPer <= 16 ? 15 : kPer <= 32 ? 31 : 63;  // bits of a key for its place
   constexpr float kKeyStep = (float)(kPlace + 2) * 0x1p-23f;                                     // ... and what that and the sum cost
   constexpr int kNoKey = (int)0x80800000;  // no finite number comes below it

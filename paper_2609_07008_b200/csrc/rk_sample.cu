@@ -21,7 +21,7 @@
 // The row is read again by each step: it comes out of L2 after the first.
 //
 // 64 rows of 131072 fp32 logits (33.6 MB, 5.2 us to read once): 24 us without filters, 27 with top-k 50, 58 with top-p 0.9; one
-// row of 32001 with all filters 11.  What bounds it: many rows, the instructions of the passes (44 per token where its weight is
+// row of 32001 with all filters 10.  What bounds it: many rows, the instructions of the passes (44 per token where its weight is
 // needed); a single row, the chain of cluster barriers and code that runs for the first time.
 #include <cuda_bf16.h>
 
@@ -322,15 +322,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   // ---- 1. the largest logit, and a logit that at least top_k tokens reach: the smallest of the largest logits of that many
   // groups of threads that have tokens ----
   float top = run.top(), reached = top;
-  int group = kThreads;  // threads; the last warp's lanes may be without tokens
-  while (group > 1 && (group >= 32 ? run.warps * 32 / group : (run.warps - 1) * (32 / group)) < top_k) group >>= 1;
+  int group_log2 = 9;  // of threads; the last warp's lanes may be without tokens
+  static_assert(kThreads == 1 << 9, "threads");
+  while (group_log2 > 0 && (group_log2 >= 5 ? run.warps >> (group_log2 - 5) : (run.warps - 1) << (5 - group_log2)) < top_k) --group_log2;
+  const int group = 1 << group_log2;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     top = max_nan(top, __shfl_xor_sync(all, top, d));
     const float o = __shfl_xor_sync(all, reached, d);
     if (d < group) reached = fmaxf(reached, o);
   }
-  int groups = __popc(__ballot_sync(all, reached > -inf)) / min(group, 32);
+  int groups = __popc(__ballot_sync(all, reached > -inf)) >> min(group_log2, 5);
   if (group < 32) {
     reached = reached > -inf ? reached : inf;
 #pragma unroll
@@ -349,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       const float o = __uint_as_float((uint32_t)sh.warp64[w]);
       top = max_nan(top, __uint_as_float(sh.warp32[w]));
       best = group <= 32 ? o : fmaxf(best, o);
-      if (((w + 1) * 32) % group != 0) continue;
+      if ((((w + 1) * 32) & (group - 1)) != 0) continue;
       if (best > -inf) {
         reached = fminf(reached, best);
         groups += group <= 32 ? (int)(sh.warp64[w] >> 32) : 1;
@@ -361,13 +363,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     sh.first[rank] = (uint32_t)groups;
   }
   cluster_sync();
-  top = -inf;
-  reached = inf;
-  groups = 0;
-  for (int r = 0; r < n_blocks; ++r) {
-    top = max_nan(top, __uint_as_float(ld_cluster_u32(peer(&sh.top[r], r))));
-    reached = fminf(reached, __uint_as_float(ld_cluster_u32(peer(&sh.low[r], r))));
-    groups += (int)ld_cluster_u32(peer(&sh.first[r], r));
+  {  // a lane per block
+    const bool there = lane < n_blocks;
+    const int r = there ? lane : 0;
+    top = there ? __uint_as_float(ld_cluster_u32(peer(&sh.top[r], r))) : -inf;
+    reached = there ? __uint_as_float(ld_cluster_u32(peer(&sh.low[r], r))) : inf;
+    groups = there ? (int)ld_cluster_u32(peer(&sh.first[r], r)) : 0;
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) {
+      top = max_nan(top, __shfl_xor_sync(all, top, d));
+      reached = fminf(reached, __shfl_xor_sync(all, reached, d));
+      groups += __shfl_xor_sync(all, groups, d);
+    }
+    top = __shfl_sync(all, top, 0);
+    reached = __shfl_sync(all, reached, 0);
+    groups = __shfl_sync(all, groups, 0);
   }
   if (groups < top_k) reached = -inf;
   const bool dead = !(top > -inf);
@@ -885,12 +895,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   for (int v = 0; v < kWarps; ++v) mine += sh.warp64[v];
   if (tid == 0) sh.slot64b[rank] = mine;
   cluster_sync();
-  u64 before = 0, total = 0;
-  for (int r = 0; r < n_blocks; ++r) {
-    const u64 t = ld_cluster_u64(peer(&sh.slot64b[r], r));
-    if (r < rank) before += t;
-    total += t;
+  const u64 part_sum = lane < n_blocks ? ld_cluster_u64(peer(&sh.slot64b[lane], lane)) : 0ull;  // a lane per block
+  u64 before = lane < rank ? part_sum : 0ull, total = part_sum;
+#pragma unroll
+  for (int d = 4; d > 0; d >>= 1) {
+    before += __shfl_xor_sync(all, before, d);
+    total += __shfl_xor_sync(all, total, d);
   }
+  before = __shfl_sync(all, before, 0);
+  total = __shfl_sync(all, total, 0);
   cluster_arrive();
   const u64 want = place_of(total);
   if (before <= want && want < before + mine) {  // this block has it
