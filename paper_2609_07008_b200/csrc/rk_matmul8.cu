@@ -16,13 +16,12 @@
 //   bounded by the tensor cores.  5 x 4096 x 8192: 11.6 us, of which W's 33.6 MB cost 5.2 at the memory's measured rate and
 //   the rest is launch, setup, the join and the stores.
 //
-// By expert, the token rows of a tile are a gather (the tokens that chose the expert): seven warps, one per stage, copy them
+// By expert, the token rows of a tile are a gather (the tokens that chose the expert): six or seven warps, one per stage, copy them
 // with 16-byte asynchronous loads into the swizzled operand layout, so that no sorted copy of the activations is made; the
-// outputs go straight to the pairs' rows of y.  Tiles have up to 192 rows, which leaves room for the seventh stage (64 tokens:
-// 154 -> 149 us).  (TMA's gather of four rows took 72 clocks of each SM's copy engine per instruction, 2300 per 128 rows; a
+// outputs go straight to the pairs' rows of y.  (TMA's gather of four rows took 72 clocks of each SM's copy engine per instruction, 2300 per 128 rows; a
 // stage has 512.)
-//   64 tokens, all weights used once: 143 us, 0.98 of the measured copy rate.  8192 tokens: 313 us; by removal, the gather
-//   costs 30 us of it, the first bytes of each expert's weights out of memory 62, the stores 28.
+//   64 tokens, all weights used once: 143 us, 0.98 of the measured copy rate.  8192 tokens: 300 us, of which (by removal, at
+//   313) the gather costs 30, the first bytes of each expert's weights out of memory 62, the stores 28.
 #include <cuda_bf16.h>
 
 #include "rk_internal.h"
@@ -166,17 +165,19 @@ __global__ void __launch_bounds__(512, 3) quant8_kernel(const __nv_bfloat16* __r
 // products
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kThreads8 = 384;          // warp 0 loads, warp 1 issues, warps 4-11 scale and store
-constexpr int kGatherWarps = 5;         // by expert: warps 12-16, and 2 and 3, gather token rows: one for each stage of the ring
 constexpr int kStages8 = 6;
 constexpr int kStep = 128;      // bytes (= values) of k per stage
 constexpr int kTileM = 256, kTileN = 256;
-constexpr int kTileNExperts = 192;  // smaller tiles leave room for a seventh stage
+constexpr int kTileNFew = 192;  // by expert, few rows: smaller tiles leave room for a seventh stage
 constexpr int kMaxStages8 = 7;
+__host__ __device__ constexpr int stages8(bool few) { return few ? kMaxStages8 : kStages8; }
+// by expert, warps 12 and up, and 2 and 3, gather token rows: one for each stage of the ring
+__host__ __device__ constexpr int threads8(bool experts, bool few) { return kThreads8 + (experts ? 32 * (stages8(few) - 2) : 0); }
 constexpr int kBandTok = 8;     // token tiles of a band: W streams past them together
 
 struct Smem8 {
   static constexpr uint32_t kABytes = 128 * kStep, kBBytes = 128 * kStep;
-  static constexpr uint32_t kOffBars = kMaxStages8 * (kABytes + kTileNExperts / 2 * kStep);  // (the larger one of the rings)
+  static constexpr uint32_t kOffBars = kMaxStages8 * (kABytes + kTileNFew / 2 * kStep);  // (the larger one of the rings)
   // full[stages], empty[stages], acc_full[2], acc_empty[2]
   static constexpr uint32_t kOffTmemPtr = kOffBars + (2 * kMaxStages8 + 4) * 8;
   static constexpr uint32_t kOffAbort = kOffTmemPtr + 8;
@@ -259,11 +260,11 @@ __device__ __forceinline__ void store_columns_paired(const uint32_t (&o)[32], co
 
 // kSplit > 1: that many pairs of a cluster share the k of one tile (a cluster has one tile then), and a CTA joins the sums of its
 // share of the token columns out of the others' shared memory.
-template <bool kExperts, int kSplit>
-__global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8, 1)
-    rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
+// kFew (by expert): tiles of up to 192 token rows in a ring of seven stages, in place of 256 and six.
+template <bool kExperts, bool kFew, int kSplit>
+__global__ void __launch_bounds__(threads8(kExperts, kFew), 1) rk_matmul8_pair_kernel(const __grid_constant__ Matmul8Params p) {
   using S = Smem8;
-  constexpr int kStages = kExperts ? kMaxStages8 : kStages8, kMost = kExperts ? kTileNExperts : kTileN;
+  constexpr int kStages = stages8(kFew), kMost = kFew ? kTileNFew : kTileN;
   const int most = kExperts ? kMost : p.tile_rows;  // token rows of a tile
   constexpr uint32_t kStageBytes = S::kABytes + (uint32_t)(kMost / 2 * kStep);
   static_assert(kStages * kStageBytes <= S::kOffBars, "ring");
@@ -460,8 +461,7 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   } else if (kExperts && (warp >= 12 || warp == 2 || warp == 3)) {
     // ---- gather (by expert): a warp fills one stage of the ring over and over, so that all of them may be under way.  Four rows
     // per instruction, eight lanes to a row of 128 bytes ----
-    static_assert(!kExperts || kStages == kGatherWarps + 2, "one warp per stage");
-    const uint32_t s = warp >= 12 ? warp - 12 : warp + kGatherWarps - 2;
+    const uint32_t s = warp >= 12 ? warp - 12 : warp + kStages - 4;
     const int sub = lane >> 3, chunk = lane & 7;
     const uint32_t dst = smem_base + s * kStageBytes + S::kABytes;
     const uint32_t full_remote = mapa_shared(full_bar(s), lead);
@@ -616,11 +616,10 @@ __global__ void __launch_bounds__(kExperts ? kThreads8 + 32 * kGatherWarps : kTh
   }
 }
 
-template <bool kExperts>
-cudaLaunchConfig_t pair_config(int n_blocks, int cluster, cudaLaunchAttribute* attr, cudaStream_t stream) {
+cudaLaunchConfig_t pair_config(int n_blocks, int n_threads, int cluster, cudaLaunchAttribute* attr, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n_blocks);
-  cfg.blockDim = dim3(kExperts ? kThreads8 + 32 * kGatherWarps : kThreads8);
+  cfg.blockDim = dim3(n_threads);
   cfg.dynamicSmemBytes = Smem8::kBytes;
   cfg.stream = stream;
   attr->id = cudaLaunchAttributeClusterDimension;
@@ -635,14 +634,15 @@ cudaLaunchConfig_t pair_config(int n_blocks, int cluster, cudaLaunchAttribute* a
 
 cudaError_t matmul8_setup(int32_t* split_slots) {
   cudaError_t e = cudaSuccess;
-  for (auto kernel : {rk_matmul8_pair_kernel<false, 1>, rk_matmul8_pair_kernel<true, 1>, rk_matmul8_pair_kernel<false, 2>, rk_matmul8_pair_kernel<false, 4>})
+  for (auto kernel : {rk_matmul8_pair_kernel<false, false, 1>, rk_matmul8_pair_kernel<true, false, 1>, rk_matmul8_pair_kernel<true, true, 1>,
+                      rk_matmul8_pair_kernel<false, false, 2>, rk_matmul8_pair_kernel<false, false, 4>})
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Smem8::kBytes);
   for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = pair_config<false>(4 << i, 4 << i, &attr, nullptr);
+    const cudaLaunchConfig_t cfg = pair_config(4 << i, kThreads8, 4 << i, &attr, nullptr);
     int n = 0;
-    e = i == 0 ? cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, 2>, &cfg)
-               : cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, 4>, &cfg);
+    e = i == 0 ? cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, false, 2>, &cfg)
+               : cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, false, 4>, &cfg);
     split_slots[i] = n;
   }
   return e;
@@ -669,7 +669,10 @@ cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_s
   p.paired = !p.out_f32 && (reinterpret_cast<uintptr_t>(p.y) & 3u) == 0 && p.y_stride % 2 == 0 && p.n_out % 2 == 0;
   const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
   // by expert the number of tiles is known on the device only: at most one part-filled tile per expert more than full ones
-  const int most = p.rows ? kTileNExperts : kTileN;
+  // Tiles of 256 rows where experts have more than 128 on average (at 192 an expert of 200 or 400 rows costs a tile more:
+  // 8192 tokens, 384 rows on average: 325 -> 300 us), the deeper ring where their weights' bytes count (64 tokens: 154 -> 149)
+  const bool few = p.rows != nullptr && p.n_tok <= 128 * (int64_t)p.n_mat;
+  const int most = few ? kTileNFew : kTileN;
   const int64_t tok_tiles = (p.n_tok + most - 1) / most + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
   int64_t tiles = n_chan * tok_tiles;
   cudaLaunchAttribute attr;
@@ -696,17 +699,14 @@ cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_s
     }
     tiles = n_chan * ((p.n_tok + p.tile_rows - 1) / p.tile_rows);
     if (split > 1) {
-      const cudaLaunchConfig_t cfg = pair_config<false>((int)tiles * 2 * split, 2 * split, &attr, stream);
-      return split == 4 ? cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, 4>, p) : cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, 2>, p);
+      const cudaLaunchConfig_t cfg = pair_config((int)tiles * 2 * split, kThreads8, 2 * split, &attr, stream);
+      return split == 4 ? cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false, 4>, p) : cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false, 2>, p);
     }
   }
   const int n_pairs = (int)(tiles < sm_count / 2 ? tiles : sm_count / 2);
-  if (p.rows) {
-    const cudaLaunchConfig_t cfg = pair_config<true>(2 * n_pairs, 2, &attr, stream);
-    return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<true, 1>, p);
-  }
-  const cudaLaunchConfig_t cfg = pair_config<false>(2 * n_pairs, 2, &attr, stream);
-  return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, 1>, p);
+  const cudaLaunchConfig_t cfg = pair_config(2 * n_pairs, threads8(p.rows != nullptr, few), 2, &attr, stream);
+  if (!p.rows) return cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false, 1>, p);
+  return few ? cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<true, true, 1>, p) : cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<true, false, 1>, p);
 }
 
 }  // namespace rk
