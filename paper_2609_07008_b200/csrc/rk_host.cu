@@ -1537,11 +1537,11 @@ rk_status rk_quant8(rk_ctx* ctx, const void* x, int64_t x_stride, const rk_q8* q
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "quantisation launch");
 }
 
-// 2-D tensor map of bytes with 128-byte swizzle, boxes of 128 columns x 128 rows
-static rk_status make_tmap8(const rk_ctx* ctx, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols) {
+// 2-D tensor map of bytes with 128-byte swizzle, boxes of 128 columns
+static rk_status make_tmap8(const rk_ctx* ctx, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
   cuuint64_t dims[2] = {cols, rows};
   cuuint64_t strides[1] = {cols};
-  cuuint32_t box[2] = {128, 128};
+  cuuint32_t box[2] = {128, box_rows};
   cuuint32_t estr[2] = {1, 1};
   CUresult r = ctx->encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -1570,9 +1570,6 @@ static rk_status matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int3
   Matmul8Params p;
   memset(&p, 0, sizeof(p));
   p.k_pad = (w->k + 15) / 16 * 16;
-  s = make_tmap8(ctx, &p.tm_w, w->codes, (uint64_t)w->n_mat * w->n_rows, p.k_pad);
-  if (s == RK_OK && !rows) s = make_tmap8(ctx, &p.tm_x, x->codes, (uint64_t)x->n_rows, p.k_pad);
-  if (s != RK_OK) return s;
   p.x = static_cast<const uint8_t*>(x->codes);
   p.sw = w->scales;
   p.sx = x->scales;
@@ -1588,7 +1585,13 @@ static rk_status matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int3
   p.per = per;
   p.out_f32 = out_dtype;
   p.starve = ctx->starve_loads;
-  cudaError_t e = launch_matmul8(p, ctx->sm_count, ctx->matmul8_slots, static_cast<cudaStream_t>(stream));
+  s = make_tmap8(ctx, &p.tm_w, w->codes, (uint64_t)w->n_mat * w->n_rows, p.k_pad, 128);
+  if (s == RK_OK && !rows) {
+    matmul8_plan(p, ctx->sm_count, ctx->matmul8_slots);
+    s = make_tmap8(ctx, &p.tm_x, x->codes, (uint64_t)x->n_rows, p.k_pad, (uint32_t)p.tile_rows / 2);
+  }
+  if (s != RK_OK) return s;
+  cudaError_t e = launch_matmul8(p, ctx->sm_count, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? RK_OK : cuda_fail(ctx, e, "8-bit product launch");
 }
 

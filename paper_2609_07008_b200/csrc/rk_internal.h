@@ -299,7 +299,7 @@ cudaError_t launch_moe_group(const GroupParams& p, int32_t group_blocks, cudaStr
 
 struct Matmul8Params {
   CUtensorMap tm_w;      // [n_mat * n_out][k_pad] bytes, box 128 x 128
-  CUtensorMap tm_x;      // dense: [token rows][k_pad] bytes, box 128 x 128
+  CUtensorMap tm_x;      // dense: [token rows][k_pad] bytes, box 128 x tile_rows / 2
   const uint8_t* x;      // by expert: the same rows
   const float* sw;       // [n_mat * n_out]
   const float* sx;       // [token rows]
@@ -312,12 +312,15 @@ struct Matmul8Params {
   int32_t n_tok;  // token rows; by expert: pairs (places of the list, rows of y)
   int32_t n_out, k_pad, n_mat, per, out_f32;
   int32_t starve;  // rk_test_starve_loads
-  int32_t paired, tile_rows;  // set by the launcher: rows and channels allow 4-byte stores of bf16 pairs; token rows of a dense tile at most
+  int32_t paired;  // set by the launcher: rows and channels allow 4-byte stores of bf16 pairs
+  int32_t tile_rows, split;  // set by matmul8_plan for the dense product: token rows of a tile at most, pairs that share its k
 };
 // split_slots[i]: clusters of 4 << i thread blocks that run at the same time on the current device
 cudaError_t matmul8_setup(int32_t* split_slots);
 cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32_t k, void* codes, float* scales, cudaStream_t stream);
-cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_slots, cudaStream_t stream);
+// chooses the dense product's tiles; split_slots[i]: clusters of 4 << i thread blocks that run at the same time
+void matmul8_plan(Matmul8Params& p, int sm_count, const int32_t* split_slots);
+cudaError_t launch_matmul8(Matmul8Params p, int sm_count, cudaStream_t stream);
 
 struct SampleParams {
   const void* logits;  // [n][vocab], rows `stride` elements apart

@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(threads8(kExperts, kFew), 1) rk_matmul8_pair_k
     uint32_t it = 0, s = 0, turn = 0;  // uses of stages; the stage of this one, and its place among the stage's uses (mod 2)
     int e = 0;
     bool ok = true;
-    constexpr uint32_t kBytes = 2u * (S::kABytes + (kExperts ? 0u : S::kBBytes));
+    const uint32_t bytes = 2u * (S::kABytes + (kExperts ? 0u : (uint32_t)(most / 2 * kStep)));
     const uint64_t once_policy = l2_policy_evict_first();  // (64 tokens: 149 -> 142 us)
     for (int t = pair; t < n_tiles && ok; t += n_pairs) {
       const Tile8 tile = tile_at(t, e);
@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(threads8(kExperts, kFew), 1) rk_matmul8_pair_k
         const uint32_t full_remote = mapa_shared(full_bar(s), lead);
         const uint32_t a_dst = smem_base + s * kStageBytes;
         if (elect_one()) {
-          if (crank == 0) mbar_arrive_expect_tx(full_bar(s), kBytes);
+          if (crank == 0) mbar_arrive_expect_tx(full_bar(s), bytes);
           if (!p.starve) {  // (the timeout tests: announced and never sent)
             if (once)
               tma_load_2d_pair_hint(a_dst, &p.tm_w, full_remote, (k_first + kc) * kStep, w_row, once_policy);
@@ -665,7 +665,30 @@ cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32
   return cudaGetLastError();
 }
 
-cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_slots, cudaStream_t stream) {
+// Few tiles: smaller ones, or k shared by the pairs of a cluster, put more SMs to work.  Clocks of a pair, measured: a step
+// of k takes 2 N where the tensor cores set the pace and no less than 350, a token row's stores 14, the join 2000 + 10 N.
+void matmul8_plan(Matmul8Params& p, int sm_count, const int32_t* split_slots) {
+  const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
+  const int k_chunks = (p.k_pad + kStep - 1) / kStep;
+  double best = 1e30;
+  for (int most = kTileN; most >= 32; most /= 2) {
+    const int64_t n = n_chan * ((p.n_tok + most - 1) / most);
+    for (int s = 1; s <= 4; s *= 2) {
+      const int64_t slots = s == 1 ? sm_count / 2 : split_slots[s / 4];
+      const int64_t rounds = (n + slots - 1) / slots;
+      if (s > 1 && (rounds > 1 || k_chunks < 4 * s)) continue;
+      const double step = 2.1 * most > 350.0 ? 2.1 * most : 350.0;
+      const double clocks = (double)rounds * ((k_chunks + s - 1) / s) * step + 14.0 * most + (s > 1 ? 2000.0 + 10.0 * most : 0.0);
+      if (clocks < 0.97 * best) {  // (the larger tile where it makes no difference)
+        best = clocks;
+        p.tile_rows = most;
+        p.split = s;
+      }
+    }
+  }
+}
+
+cudaError_t launch_matmul8(Matmul8Params p, int sm_count, cudaStream_t stream) {
   p.paired = !p.out_f32 && (reinterpret_cast<uintptr_t>(p.y) & 3u) == 0 && p.y_stride % 2 == 0 && p.n_out % 2 == 0;
   const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
   // by expert the number of tiles is known on the device only: at most one part-filled tile per expert more than full ones
@@ -677,30 +700,10 @@ cudaError_t launch_matmul8(Matmul8Params p, int sm_count, const int32_t* split_s
   int64_t tiles = n_chan * tok_tiles;
   cudaLaunchAttribute attr;
   if (!p.rows) {
-    // Few tiles: smaller ones, or k shared by the pairs of a cluster, put more SMs to work.  Clocks of a pair, measured: a step
-    // of k takes 2 N where the tensor cores set the pace and no less than 350, a token row's stores 14, the join 2000 + 10 N.
-    const int k_chunks = (p.k_pad + kStep - 1) / kStep;
-    double best = 1e30;
-    int split = 1;
-    for (int most = kTileN; most >= 32; most /= 2) {
-      const int64_t n = n_chan * ((p.n_tok + most - 1) / most);
-      for (int s = 1; s <= 4; s *= 2) {
-        const int64_t slots = s == 1 ? sm_count / 2 : split_slots[s / 4];
-        const int64_t rounds = (n + slots - 1) / slots;
-        if (s > 1 && (rounds > 1 || k_chunks < 4 * s)) continue;
-        const double step = 2.1 * most > 350.0 ? 2.1 * most : 350.0;
-        const double clocks = (double)rounds * ((k_chunks + s - 1) / s) * step + 14.0 * most + (s > 1 ? 2000.0 + 10.0 * most : 0.0);
-        if (clocks < 0.97 * best) {  // (the larger tile where it makes no difference)
-          best = clocks;
-          p.tile_rows = most;
-          split = s;
-        }
-      }
-    }
     tiles = n_chan * ((p.n_tok + p.tile_rows - 1) / p.tile_rows);
-    if (split > 1) {
-      const cudaLaunchConfig_t cfg = pair_config((int)tiles * 2 * split, kThreads8, 2 * split, &attr, stream);
-      return split == 4 ? cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false, 4>, p) : cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false, 2>, p);
+    if (p.split > 1) {
+      const cudaLaunchConfig_t cfg = pair_config((int)tiles * 2 * p.split, kThreads8, 2 * p.split, &attr, stream);
+      return p.split == 4 ? cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false, 4>, p) : cudaLaunchKernelEx(&cfg, rk_matmul8_pair_kernel<false, false, 2>, p);
     }
   }
   const int n_pairs = (int)(tiles < sm_count / 2 ? tiles : sm_count / 2);
