@@ -35,7 +35,7 @@ namespace {
 constexpr int kQuantHeld = 4;  // 8-value chunks that a thread keeps in registers between the maximum and the codes
 constexpr int kQuantRows = 8;  // rows of a thread block where a warp has a row to itself
 
-constexpr float kQuantNear = 0.49998f;
+constexpr float kQuantNear = 0.49997f;  // quotients (off by less than 1e-5) this far from a whole number are looked at again
 
 // round(x / scale), half to even, exactly, and limited to -127 .. 127.  The quick quotient t tells the two codes; the sign of
 // |x| - scale (m + 1/2), one fused product in double that is rounded once, the side of the middle between them.  Where 1 / scale
@@ -68,16 +68,16 @@ __device__ __forceinline__ uint32_t chunk_top(const uint4& c) {
   return max(t & 0xffffu, t >> 16);
 }
 // Codes of eight values.  x * inv + 1.5 * 2^23 is rounded to a whole number, half to even, whose two's complement is in the
-// low byte.  `off` collects the largest distance from a whole number: inv is off by 2^-24 of itself, the quotient by less than
-// 1e-5, so that up to 0.49998 the code is right.
-__device__ __forceinline__ uint2 chunk_codes(const uint4& c, float inv, float& off) {
+// low byte.  `off` collects the largest |x - scale code|: the fused product is exact (a multiple of the last bit of scale, or x
+// itself), so that the code is right below scale / 2.  inv is off by 2^-24 of itself, and a few values in 10^6 are found wrong.
+__device__ __forceinline__ uint2 chunk_codes(const uint4& c, float scale, float inv, float& off) {
   constexpr float kMagic = 12582912.f;
   const uint32_t w[4] = {c.x, c.y, c.z, c.w};
   uint32_t y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float x = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16), r = fmaf(x, inv, kMagic);
-    off = fmaxf(off, fabsf(fmaf(x, inv, kMagic - r)));
+    off = fmaxf(off, fabsf(fmaf(-scale, r - kMagic, x)));
     y[i] = __float_as_uint(r);
   }
   return make_uint2(__byte_perm(__byte_perm(y[0], y[1], 0x0040), __byte_perm(y[2], y[3], 0x0040), 0x5410),
@@ -93,7 +93,7 @@ __device__ __noinline__ void quant8_exact(unsigned who, const __nv_bfloat16* row
   const int lane = threadIdx.x & 31;
   auto fix = [&](int i, float x) {
     const float t = x * inv;
-    if (inv == 0.f || fabsf(t - rintf(t)) >= kQuantNear - 1e-5f) codes[i] = (uint8_t)quant8_code(x, scale, inv);
+    if (inv == 0.f || fabsf(t - rintf(t)) >= kQuantNear) codes[i] = (uint8_t)quant8_code(x, scale, inv);
   };
   __syncwarp();
   if (__popc(who) <= 4) {
@@ -145,18 +145,18 @@ __global__ void __launch_bounds__(512, 3) quant8_kernel(const __nv_bfloat16* __r
   const bool blank = !finite || scale == 0.f;
   // 0 in place of the reciprocal makes codes of 0, and, for rows of tiny values, has all of them done exactly
   const float inv = blank || scale < 1e-30f ? 0.f : __fdiv_rn(1.f, scale);
-  float off = !blank && inv == 0.f ? 1.f : 0.f;
+  float off = !blank && inv == 0.f ? __int_as_float(0x7f800000) : 0.f;
   uint8_t* to = codes + row * k_pad;
   uint2* dst = reinterpret_cast<uint2*>(to);
 #pragma unroll
   for (int i = 0; i < kQuantHeld; ++i) {
     const int c = tid + i * nt;
-    if (c < n_chunks) dst[c] = finite ? chunk_codes(held[i], inv, off) : make_uint2(0u, 0u);
+    if (c < n_chunks) dst[c] = finite ? chunk_codes(held[i], scale, inv, off) : make_uint2(0u, 0u);
   }
   for (int c = tid + kQuantHeld * nt; c < n_chunks; c += nt)
-    dst[c] = finite ? chunk_codes(load_chunk<kVec>(src, 8 * c, k), inv, off) : make_uint2(0u, 0u);
+    dst[c] = finite ? chunk_codes(load_chunk<kVec>(src, 8 * c, k), scale, inv, off) : make_uint2(0u, 0u);
   // (with a power of two for a scale, one row in 128, the quick quotient is the quotient, and ties are many)
-  const unsigned near = __ballot_sync(0xffffffffu, off >= kQuantNear && (inv == 0.f || (__float_as_uint(scale) & 0x7fffffu) != 0u));
+  const unsigned near = __ballot_sync(0xffffffffu, !blank && off >= 0.5f * scale && (inv == 0.f || (__float_as_uint(scale) & 0x7fffffu) != 0u));
   if (near != 0u) quant8_exact<kVec>(near, src, k, tid & ~31, nt, n_chunks, scale, inv, to);
   if (tid == 0) scales[row] = scale;
 }
