@@ -11,15 +11,15 @@
 // stage); with N = 256 an SM draws 64 bytes per clock from L2 at the full rate of the tensor cores, below the 76 that it
 // can.  Persistent: the accumulator is double buffered in tensor memory, so that the scales and stores of one tile run under
 // the products of the next.  Where there are few tiles they are made smaller, or 2 or 4 pairs in a cluster share k and add
-// their sums through each other's shared memory (launch_matmul8; 256 x 4096 x 8192: 20.6 -> 15.4 us).
+// their sums through each other's shared memory (matmul8_plan; 256 x 4096 x 8192: 20.6 -> 15.4 us).
 //   8192 tokens x 7168 channels x 16384: 590 us, 3.26 POP/s, 0.96 of twice the bf16 library product's measured burst rate:
 //   bounded by the tensor cores.  5 x 4096 x 8192: 11.6 us, of which W's 33.6 MB cost 5.2 at the memory's measured rate and
 //   the rest is launch, setup, the join and the stores.
 //
-// By expert, the token rows of a tile are a gather (the tokens that chose the expert): six or seven warps, one per stage, copy them
-// with 16-byte asynchronous loads into the swizzled operand layout, so that no sorted copy of the activations is made; the
-// outputs go straight to the pairs' rows of y.  (TMA's gather of four rows took 72 clocks of each SM's copy engine per instruction, 2300 per 128 rows; a
-// stage has 512.)
+// By expert, the token rows of a tile are a gather (the tokens that chose the expert): six or seven warps, one per stage,
+// copy them with 16-byte asynchronous loads into the swizzled operand layout, so that no sorted copy of the activations is made; the
+// outputs go straight to the pairs' rows of y.  (TMA's gather of four rows took 72 clocks of each SM's copy engine per
+// instruction, 2300 per 128 rows; a stage has 512.)
 //   64 tokens, all weights used once: 143 us, 0.98 of the measured copy rate.  8192 tokens: 300 us, of which (by removal, at
 //   313) the gather costs 30, the first bytes of each expert's weights out of memory 62, the stores 28.
 #include <cuda_bf16.h>
@@ -115,7 +115,9 @@ __device__ __noinline__ void quant8_exact(unsigned who, const __nv_bfloat16* row
 }
 
 // A row per thread block, or per warp (kWarp: up to 1024 values).  A row of up to 32 values per thread is read once; longer
-// ones a second time out of L2.  HBM bound: two bytes in, one out per value; 8192 x 16384: 75 us, 0.83 of the copy rate.
+// ones a second time out of L2.  Two bytes in, one out per value, 17
+// instructions: 8192 x 16384 takes 73 to 83 us (by the data: rows with codes to correct), 0.75 to 0.85 of the copy rate; issue
+// slots are 76% busy.
 template <bool kVec, bool kWarp>
 __global__ void __launch_bounds__(512, 3) quant8_kernel(const __nv_bfloat16* __restrict__ x, int64_t x_stride, int64_t n_rows, int k,
                                                         int k_pad, uint8_t* __restrict__ codes, float* __restrict__ scales) {
