@@ -166,3 +166,63 @@ def test_large_rows_against_a_64_bit_evaluation(ctx, n, vocab, spread, k, p, m):
         want = torch.cat([reference_tokens(x[i:i + 16], u[i:i + 16], float(np.float32(T)), k, P, M) for i in range(0, n, 16)])
         assert torch.equal(tokens, want)
     ctx.rk_poll_status()
+
+
+def test_rows_that_lie_beyond_32_bits(ctx):
+    """Three rows 2^30 elements apart: offsets of 2^31 elements, 2^32 bytes and more, into and out of every call."""
+    far = 1 << 30
+    n, k, n_out = 3, 1000, 264
+    g = torch.Generator(device="cuda").manual_seed(9)
+
+    def spread(t):
+        room = torch.empty(2 * far + t.shape[1], dtype=t.dtype, device="cuda")
+        view = room.as_strided(t.shape, (far, 1))
+        view.copy_(t)
+        return view
+
+    x = torch.randn((n, k), generator=g, device="cuda").to(torch.bfloat16)
+    w = ctx.rk_quant8(torch.randn((1, n_out, k), generator=g, device="cuda").to(torch.bfloat16))
+    q = ctx.rk_quant8(x)
+    apart = spread(x)
+    q2 = ctx.rk_quant8(apart)
+    assert torch.equal(q.codes, q2.codes) and torch.equal(q.scales, q2.scales)
+    for a, b in zip(ctx.rk_moe_route(x, 6), ctx.rk_moe_route(apart, 6)):
+        assert torch.equal(a, b)
+    u = torch.rand(n, generator=g, device="cuda")
+    p = torch.full((n,), 0.8, device="cuda")
+    for a, b in zip(ctx.rk_sample(x, u, top_p=p), ctx.rk_sample(apart, u, top_p=p)):
+        assert torch.equal(a, b)
+    del apart
+    off, rows = torch.tensor([0, n], dtype=torch.int32, device="cuda"), torch.tensor([2, 0, 1], dtype=torch.int32, device="cuda")
+    for dtype in (torch.bfloat16, torch.float32):
+        want = ctx.rk_matmul8(w, q, out_dtype=dtype)
+        y = spread(torch.zeros((n, n_out), dtype=dtype, device="cuda"))
+        assert torch.equal(ctx.rk_matmul8(w, q, y=y), want)
+        y.zero_()
+        assert torch.equal(ctx.rk_matmul8_experts(w, q, off, rows, 1, y=y), want)
+        del y
+    ctx.rk_poll_status()
+
+
+def test_codes_that_lie_beyond_32_bits(ctx):
+    """140000 rows of 16384 codes (2.3 GB): the last rows give what they give alone, as tokens, as listed pairs and as weights."""
+    n, k, tail = 140000, 16384, 40
+    g = torch.Generator(device="cuda").manual_seed(10)
+    x = torch.zeros((n, k), dtype=torch.bfloat16, device="cuda")
+    x[-tail:] = torch.randn((tail, k), generator=g, device="cuda").to(torch.bfloat16)
+    few = x[-tail:].clone()
+    w = ctx.rk_quant8(torch.randn((1, 48, k), generator=g, device="cuda").to(torch.bfloat16))
+    q, q_few = ctx.rk_quant8(x), ctx.rk_quant8(few)
+    assert torch.equal(q.codes[-tail:], q_few.codes) and torch.equal(q.scales[-tail:], q_few.scales)
+    want = ctx.rk_matmul8(w, q_few, out_dtype=torch.float32)
+    y = ctx.rk_matmul8(w, q, out_dtype=torch.float32)
+    assert torch.equal(y[-tail:], want) and (y[:-tail] == 0).all()
+    off = torch.tensor([0, tail], dtype=torch.int32, device="cuda")
+    rows = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    rows[:tail] = torch.arange(n - tail, n, device="cuda")
+    y = torch.full((n, 48), 7.0, device="cuda")
+    ctx.rk_matmul8_experts(w, q, off, rows, 1, y=y)
+    assert torch.equal(y[-tail:], want) and (y[:-tail] == 7.0).all()
+    y = ctx.rk_matmul8(q, w, out_dtype=torch.float32)[:, -tail:]  # the same rows as weights: the scales' two roundings (2^-24 each, on both sides) swap
+    assert ((y - want.T).abs() <= 2.0 ** -22 * want.T.abs()).all()
+    ctx.rk_poll_status()
