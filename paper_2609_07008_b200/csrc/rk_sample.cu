@@ -517,10 +517,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       cluster_wait();
       return;
     }
-    cluster_sync();  // everyone has seen the number: too many (equal logits, or falling ones); the bins sort it out
-    if (rank == 0 && tid == 0) sh.listed[0] = 0u;
-    clear_bins();
-    __syncthreads();
+    // Too many (equal logits, or falling ones): the bins sort it out.  They are as they were cleared in the beginning: others may
+    // add to the first block's from here on, so that it must not clear them now.
+    cluster_sync();  // everyone has seen the number
+    if (rank == 0 && tid == 0) sh.listed[0] = 0u;  // (two barriers of the cluster before the next token comes)
   }
   bool summed = false;  // the sums of what stays are there already: sh.slot_part, and the first block's extra_*
   if (by_count || by_mass) {

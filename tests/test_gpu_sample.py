@@ -230,3 +230,28 @@ def test_extreme_temperatures(ctx, vocab, temperature):
     u = rng.random(4)
     for kw in ({}, dict(top_k=3), dict(top_p=0.6), dict(min_p=0.5), dict(top_k=300, top_p=0.6)):
         check(ctx, x, u, temperature=temperature, **kw)
+
+
+def test_top_k_among_too_many_candidates_is_the_same_every_time(ctx):
+    """Rows of which half is one low logit: more tokens reach what the quick search starts from than its list holds, and the
+    cluster goes on with bins.  The calls follow one another with other kernels in between, so that the thread blocks of a
+    row run apart; all of them have to give the oracle's tokens."""
+    rng = np.random.default_rng(28)
+    n, vocab = 28, 28479
+    x = rng.standard_normal((n, vocab)) * 2.5
+    x[:, vocab // 2:] = 0.0
+    u = rng.random(n)
+    first, probs = check(ctx, x, u, top_k=200, top_p=0.999)
+    t, f = dev(x), lambda v, dt=torch.float32: torch.full((n,), v, dtype=dt, device="cuda")  # noqa: E731
+    uu = dev(np.array([clear_of_borders(t[i].double().cpu().numpy(), float(u[i]), 1.0, 200, float(np.float32(0.999)), 0.0) for i in range(n)]).astype(np.float32))
+    k, p, room = f(200, torch.int32), f(0.999), torch.empty(64 << 20, device="cuda")
+    w, tokens = ctx.rk_quant8(torch.randn((1, 2048, 2048), device="cuda").to(torch.bfloat16)), ctx.rk_quant8(torch.randn((300, 2048), device="cuda").to(torch.bfloat16))
+    for i in range(200):
+        if i % 2:
+            room.zero_()
+        else:
+            ctx.rk_matmul8(w, tokens)
+            ctx.rk_moe_route(room[:64 * 1024].view(64, 1024), 8)
+        got, got_p = ctx.rk_sample(t, uu, top_k=k, top_p=p)
+        assert torch.equal(got, first) and torch.equal(got_p, probs)
+    ctx.rk_poll_status()
