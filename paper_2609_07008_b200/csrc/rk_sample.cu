@@ -5,7 +5,7 @@
 // (2^-42 per token) is far below the distance at which two neighbouring tokens' borders could be confused.  The
 // exponential is taken in double: 256 x = i + r with i whole, 2^-i/256 from a table and a shift, 2^-r/256 by its Taylor
 // series to degree 3 (|r| <= 1/2: 1.4e-13).  A token costs eleven double-precision instructions that way, which bounds the
-// passes that need every token's weight; 64-bit conversions, four times as slow, are done in integers.
+// passes that need every token's weight; conversions from fp32 are done in integers, which takes infinities along.
 //
 // The three filters each keep a prefix of one order, falling logit and then rising index, so together they keep the tokens
 // not below one (logit, index) pair, the cut.  A row belongs to a cluster of thread blocks, each with a run of consecutive tokens.
@@ -20,7 +20,7 @@
 //   3. sums of what stays, by block and by warp; the block that holds u * total shares out the warp's run that holds it
 // The row is read again by each step: it comes out of L2 after the first.
 //
-// 64 rows of 131072 fp32 logits (33.6 MB, 5.2 us to read once): 24 us without filters, 27 with top-k 50, 58 with top-p 0.9; one
+// 64 rows of 131072 fp32 logits (33.6 MB, 5.2 us to read once): 24 us without filters, 27 with top-k 50, 56 with top-p 0.9; one
 // row of 32001 with all filters 10.  What bounds it: many rows, the instructions of the passes (44 per token where its weight is
 // needed); a single row, the chain of cluster barriers and code that runs for the first time.
 #include <cuda_bf16.h>
@@ -535,10 +535,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       for (int e = 0; e < 4; ++e) {
         uint32_t weight;
         const int b = bins.bin(l[e], weight);
-        if (l[e] >= floor_all) {
-          if (by_count) atomicAdd(&sh.count[b], 1u);
-          if (by_mass) atomicAdd(&sh.lo[b], weight);
-        }
+        if (by_count && l[e] >= floor_all) atomicAdd(&sh.count[b], 1u);
+        if (by_mass && l[e] >= floor_all) atomicAdd(&sh.lo[b], weight);
       }
     });
     __syncthreads();
@@ -654,10 +652,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             if (l[e] >= all_low) everything += u;
             if (l[e] >= p_high) above += u;
           }
+          const float high = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])), low = fminf(fminf(l[0], l[1]), fminf(l[2], l[3]));
+          if (high >= p_low && !(low >= p_high)) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (l[e] >= p_low && !(l[e] >= p_high)) keep(1, l[e], at + e);
-            if (bin_k >= 0 && l[e] >= k_low && !(l[e] >= k_high)) keep(0, l[e], at + e);
+            for (int e = 0; e < 4; ++e)
+              if (l[e] >= p_low && !(l[e] >= p_high)) keep(1, l[e], at + e);
+          }
+          if (bin_k >= 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (l[e] >= k_low && !(l[e] >= k_high)) keep(0, l[e], at + e);
           }
         });
         u64 s0 = (u64)everything, s1 = (u64)above;
