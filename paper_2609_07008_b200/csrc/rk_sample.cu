@@ -584,6 +584,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         constexpr uint32_t kAround = 96;
         const int last = sh.found.bin_k >= 0 ? sh.found.bin_k : kBins - 1;
         const double want = (double)top_p * (double)sh.pick_mass;
+        __syncthreads();  // (pick_mass is written anew)
         cb = cb0;
         mb = mb0;
 #pragma unroll
