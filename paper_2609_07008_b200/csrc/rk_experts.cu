@@ -129,7 +129,7 @@ __device__ __noinline__ int route_exact(const RouteParams& p, int64_t token) {
 //   softmax  s (2^-21 + |x - top| 2^-23.5 + 2^-21)        <  2^-17 s   up to |x - top| = 80; what is left below that is 0
 // A score plus bias is rounded once (2^-24 of it), and its last bits are the place that it has in its lane.  Without a bias
 // the logits themselves are the order, and equal logits are equal scores; only where scores of different logits could round
-// to the same 64-bit number (logits closer than 2^-45, sigmoid above 15, softmax 600 below the largest) is it left open.
+// to the same 64-bit number (logits closer than 2^-45, sigmoid above 15, softmax both 600 below the largest) is it left open.
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -343,8 +343,9 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 14 : 1) moe_rout
     auto apart = [&](int v, int v2) -> bool {
       const float c = __int_as_float(ordered(v)), c2 = __int_as_float(ordered(v2));
       if (p.bias) return c - c2 > (p.softmax ? 0x1p-16f * scale : 0x1p-20f) + kKeyStep * (fabsf(c) + fabsf(c2)) + 0x1p-100f;
-      if (kBf16 && v == v2) return true;  // (the places have bits of their own)
-      return v != v2 && (fmaxf(fabsf(c), fabsf(c2)) >= 0x1p-20f || c - c2 > 0x1p-36f) && (p.softmax ? c2 - top > -600.f : c < 15.f);
+      // equal keys are equal logits in bf16 (the places have bits of their own), in their right order, and the next smaller bf16 number
+      // scores less here
+      return (kBf16 || v != v2) && (fmaxf(fabsf(c), fabsf(c2)) >= 0x1p-20f || c - c2 > 0x1p-36f) && (p.softmax ? c - top > -600.f : c < 15.f);
     };
     bool sure = true;
     {
@@ -353,6 +354,19 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 14 : 1) moe_rout
     }
     int mine = lane < p.k && lane < n_won ? expert() : -1;
     bool exact = !__all_sync(kAll, clear && worst < inf);
+    if (kBf16 && !exact && !p.bias && !__all_sync(kAll, sure)) {
+      // equal logits elsewhere (zeros of a padded token, masks): the order of those up to the k-th is right, and if the next one equals
+      // the k-th, the largest logit below has to score less
+      const int v = won & ~kPlace, next = __shfl_down_sync(kAll, v, 1), last = __shfl_sync(kAll, v, p.k - 1);
+      int below = (int)0x80000000;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int o = ordered(__float_as_int(x[i])) & ~kPlace;
+        below = o < last ? max(below, o) : below;
+      }
+      below = __reduce_max_sync(kAll, below);
+      if (lane < p.k && lane + 1 < n_won && v == next) sure = lane + 1 < p.k || below < kNoKey || apart(last, below);
+    }
     if (!exact && !__all_sync(kAll, sure)) {
       // The order of a few is open: those, as far down as they may belong to the k, are compared in 64 bits, one per lane.
       const int last = __shfl_sync(kAll, won, p.k - 1) & ~kPlace;
