@@ -129,7 +129,8 @@ __device__ __noinline__ int route_exact(const RouteParams& p, int64_t token) {
 //   softmax  s (2^-21 + |x - top| 2^-23.5 + 2^-21)        <  2^-17 s   up to |x - top| = 80; what is left below that is 0
 // A score plus bias is rounded once (2^-24 of it), and its last bits are the place that it has in its lane.  Without a bias
 // the logits themselves are the order, and equal logits are equal scores; only where scores of different logits could round
-// to the same 64-bit number (logits closer than 2^-45, sigmoid above 15, softmax both 600 below the largest) is it left open.
+// to the same 64-bit number (logits closer than 2^-45, sigmoid above 15 or both below -700, next to where exp(-x) overflows and
+// scores are 0, softmax both 600 below the largest) is it left open.
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -299,8 +300,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 14 : 1) moe_rout
         }
         const float gap = closed ? worst_in - rank : rank - best_out;
         if (g < p.n_groups && best_out != -inf && rank != -inf) {
-          clear = plain ? gap == 0.f || gap > 0x1p-45f : gap > near;
-          if (plain) clear &= p.softmax ? rank - top > -600.f : rank < 15.f;
+          const float larger = closed ? worst_in : rank;
+          clear = plain ? gap == 0.f || (gap > 0x1p-45f && (p.softmax ? larger - top > -600.f : larger < 15.f && larger > -700.f)) : gap > near;
         }
       }
 #pragma unroll
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 14 : 1) moe_rout
       if (p.bias) return c - c2 > (p.softmax ? 0x1p-16f * scale : 0x1p-20f) + kKeyStep * (fabsf(c) + fabsf(c2)) + 0x1p-100f;
       // equal keys are equal logits in bf16 (the places have bits of their own), in their right order, and the next smaller bf16 number
       // scores less here
-      return (kBf16 || v != v2) && (fmaxf(fabsf(c), fabsf(c2)) >= 0x1p-20f || c - c2 > 0x1p-36f) && (p.softmax ? c - top > -600.f : c < 15.f);
+      return (kBf16 || v != v2) && (fmaxf(fabsf(c), fabsf(c2)) >= 0x1p-20f || c - c2 > 0x1p-36f) && (p.softmax ? c - top > -600.f : c < 15.f && c > -700.f);
     };
     bool sure = true;
     {
@@ -370,7 +371,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 14 : 1) moe_rout
     if (!exact && !__all_sync(kAll, sure)) {
       // The order of a few is open: those, as far down as they may belong to the k, are compared in 64 bits, one per lane.
       const int last = __shfl_sync(kAll, won, p.k - 1) & ~kPlace;
-      exact = p.softmax ? p.bias != nullptr : !p.bias && __int_as_float(ordered(__shfl_sync(kAll, won, 0) & ~kPlace)) >= 15.f;
+      exact = p.softmax ? p.bias != nullptr || __int_as_float(ordered(last)) - top <= -600.f
+                        : !p.bias && __int_as_float(ordered(__shfl_sync(kAll, won, 0) & ~kPlace)) >= 15.f;
       while (!exact && n_won > p.k && !apart(last, __shfl_sync(kAll, won, n_won - 1) & ~kPlace)) {
         exact = n_won == 32;
         if (exact || !draw()) break;
