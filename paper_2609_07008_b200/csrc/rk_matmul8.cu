@@ -183,11 +183,13 @@ struct Smem8 {
   // full[stages], empty[stages], acc_full[2], acc_empty[2]
   static constexpr uint32_t kOffTmemPtr = kOffBars + (2 * kMaxStages8 + 4) * 8;
   static constexpr uint32_t kOffAbort = kOffTmemPtr + 8;
-  static constexpr uint32_t kOffScan = kOffAbort + 8;               // 16 sums of the block's scan
-  static constexpr uint32_t kOffTok = (kOffScan + 128 + 15) / 16 * 16;  // [2][256] TokenOut
+  static constexpr uint32_t kOffScan = kOffAbort + 8;               // by expert: a sum per warp, of the block's scan
+  static constexpr int kMaxWarps = threads8(true, true) / 32;
+  static constexpr uint32_t kOffTok = (kOffScan + 8 * kMaxWarps + 15) / 16 * 16;  // [2][256] TokenOut
   static constexpr uint32_t kOffFirst = kOffTok + 2 * 256 * 16;     // by expert: first tile of each, [n_mat + 1]; then row_off
   static constexpr uint32_t kBytes = kOffFirst + 2 * (kMaxExperts + 1) * 4 + 1024 + 16;
 };
+static_assert(Smem8::kBytes <= 227 * 1024, "shared memory");
 enum { WM_EMPTY = 61, WM_FULL, WM_ACC_EMPTY, WM_ACC_FULL };
 
 // D[tmem] (+)= A B^T in int8 -> int32, both operands in shared memory, by a CTA pair
@@ -270,6 +272,7 @@ __global__ void __launch_bounds__(threads8(kExperts, kFew), 1) rk_matmul8_pair_k
   const int most = kExperts ? kMost : p.tile_rows;  // token rows of a tile
   constexpr uint32_t kStageBytes = S::kABytes + (uint32_t)(kMost / 2 * kStep);
   static_assert(kStages * kStageBytes <= S::kOffBars, "ring");
+  static_assert(!kExperts || S::kOffScan + 8 * (threads8(kExperts, kFew) / 32) <= S::kOffTok, "scan");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
