@@ -1587,7 +1587,7 @@ static rk_status matmul8(rk_ctx* ctx, const rk_q8* w, const rk_q8* x, const int3
   p.starve = ctx->starve_loads;
   s = make_tmap8(ctx, &p.tm_w, w->codes, (uint64_t)w->n_mat * w->n_rows, p.k_pad, 128);
   if (s == RK_OK && !rows) {
-    matmul8_plan(p, ctx->sm_count, ctx->matmul8_slots);
+    rk_matmul8_plan(p.n_out, p.n_tok, p.k_pad, ctx->sm_count, ctx->matmul8_slots, &p.tile_rows, &p.split);
     s = make_tmap8(ctx, &p.tm_x, x->codes, (uint64_t)x->n_rows, p.k_pad, (uint32_t)p.tile_rows / 2);
   }
   if (s != RK_OK) return s;

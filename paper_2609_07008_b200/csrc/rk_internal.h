@@ -313,13 +313,14 @@ struct Matmul8Params {
   int32_t n_out, k_pad, n_mat, per, out_f32;
   int32_t starve;  // rk_test_starve_loads
   int32_t paired;  // set by the launcher: rows and channels allow 4-byte stores of bf16 pairs
-  int32_t tile_rows, split;  // set by matmul8_plan for the dense product: token rows of a tile at most, pairs that share its k
+  int32_t tile_rows, split;  // set by rk_matmul8_plan for the dense product: token rows of a tile at most, pairs that share its k
 };
-// split_slots[i]: clusters of 4 << i thread blocks that run at the same time on the current device
+// split_slots[i]: clusters of 4 << i thread blocks that run at the same time on the current device, 0 where there is no room for one
 cudaError_t matmul8_setup(int32_t* split_slots);
 cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32_t k, void* codes, float* scales, cudaStream_t stream);
-// chooses the dense product's tiles; split_slots[i]: clusters of 4 << i thread blocks that run at the same time
-void matmul8_plan(Matmul8Params& p, int sm_count, const int32_t* split_slots);
+// chooses the dense product's tiles (host arithmetic alone; by a C name, which the tests call)
+extern "C" void rk_matmul8_plan(int64_t n_out, int64_t n_tok, int32_t k_pad, int32_t sm_count, const int32_t* split_slots, int32_t* tile_rows,
+                                int32_t* split);
 cudaError_t launch_matmul8(Matmul8Params p, int sm_count, cudaStream_t stream);
 
 struct SampleParams {

@@ -11,7 +11,7 @@
 // stage); with N = 256 an SM draws 64 bytes per clock from L2 at the full rate of the tensor cores, below the 76 that it
 // can.  Persistent: the accumulator is double buffered in tensor memory, so that the scales and stores of one tile run under
 // the products of the next.  Where there are few tiles they are made smaller, or 2 or 4 pairs in a cluster share k and add
-// their sums through each other's shared memory (matmul8_plan; 256 x 4096 x 8192: 20.6 -> 15.4 us).
+// their sums through each other's shared memory (rk_matmul8_plan; 256 x 4096 x 8192: 20.6 -> 15.4 us).
 //   8192 tokens x 7168 channels x 16384: 590 us, 3.26 POP/s, 0.96 of twice the bf16 library product's measured burst rate:
 //   bounded by the tensor cores.  5 x 4096 x 8192: 11.6 us, of which W's 33.6 MB cost 5.2 at the memory's measured rate and
 //   the rest is launch, setup, the join and the stores.
@@ -646,9 +646,10 @@ cudaError_t matmul8_setup(int32_t* split_slots) {
     cudaLaunchAttribute attr;
     const cudaLaunchConfig_t cfg = pair_config(4 << i, kThreads8, 4 << i, &attr, nullptr);
     int n = 0;
-    e = i == 0 ? cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, false, 2>, &cfg)
-               : cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, false, 4>, &cfg);
-    split_slots[i] = n;
+    const cudaError_t asked = i == 0 ? cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, false, 2>, &cfg)
+                                     : cudaOccupancyMaxActiveClusters(&n, rk_matmul8_pair_kernel<false, false, 4>, &cfg);
+    split_slots[i] = asked == cudaSuccess ? n : 0;  // 0: a device without room for such a cluster, whose products do not share k
+    if (asked != cudaSuccess) cudaGetLastError();
   }
   return e;
 }
@@ -672,22 +673,24 @@ cudaError_t launch_quant8(const void* x, int64_t x_stride, int64_t n_rows, int32
 
 // Few tiles: smaller ones, or k shared by the pairs of a cluster, put more SMs to work.  Clocks of a pair, measured: a step
 // of k takes 2 N where the tensor cores set the pace and no less than 350, a token row's stores 14, the join 2000 + 10 N.
-void matmul8_plan(Matmul8Params& p, int sm_count, const int32_t* split_slots) {
-  const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
-  const int k_chunks = (p.k_pad + kStep - 1) / kStep;
+extern "C" void rk_matmul8_plan(int64_t n_out, int64_t n_tok, int32_t k_pad, int32_t sm_count, const int32_t* split_slots, int32_t* tile_rows,
+                                int32_t* split) {
+  const int64_t n_chan = (n_out + kTileM - 1) / kTileM;
+  const int k_chunks = (k_pad + kStep - 1) / kStep;
   double best = 1e30;
   for (int most = kTileN; most >= 32; most /= 2) {
-    const int64_t n = n_chan * ((p.n_tok + most - 1) / most);
+    const int64_t n = n_chan * ((n_tok + most - 1) / most);
     for (int s = 1; s <= 4; s *= 2) {
-      const int64_t slots = s == 1 ? sm_count / 2 : split_slots[s / 4];
+      const int64_t slots = s == 1 ? (sm_count < 2 ? 1 : sm_count / 2) : split_slots[s / 4];
+      if (slots < 1) continue;
       const int64_t rounds = (n + slots - 1) / slots;
       if (s > 1 && (rounds > 1 || k_chunks < 4 * s)) continue;
       const double step = 2.1 * most > 350.0 ? 2.1 * most : 350.0;
       const double clocks = (double)rounds * ((k_chunks + s - 1) / s) * step + 14.0 * most + (s > 1 ? 2000.0 + 10.0 * most : 0.0);
       if (clocks < 0.97 * best) {  // (the larger tile where it makes no difference)
         best = clocks;
-        p.tile_rows = most;
-        p.split = s;
+        *tile_rows = most;
+        *split = s;
       }
     }
   }
