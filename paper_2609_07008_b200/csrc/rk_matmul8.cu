@@ -548,6 +548,7 @@ __global__ void __launch_bounds__(threads8(kExperts, kFew), 1) rk_matmul8_pair_k
       tc_fence_after_sync();
       for (int c0 = 32 * group; c0 < tile.n; c0 += 64) {
         uint32_t o[32];
+        __syncwarp();  // (lanes beyond the last channel store nothing)
         tmem_ld_x32(tmem_base + lane_base + b * kTileN + c0, o);
         tmem_wait_ld();
         if constexpr (kSplit > 1) {  // into the ring, whose products are done: [token][channel]
