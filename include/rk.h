@@ -484,7 +484,8 @@ typedef struct rk_route {
 /* Routes n tokens.  s = the scores of the token's logits, c = s + bias.  The top_groups groups of the highest rank take
  * part (equal: the lower group), and the k experts of the largest c in them are chosen (equal: the lower index), in
  * descending order.  Their weights are their s (without bias), divided by their sum with `renorm` (0 where that is 0),
- * times scale.  Scores are compared and weighted in 64 bits; the weights are rounded to fp32.
+ * times scale.  Scores are compared and weighted in 64 bits (the sum of a softmax whose weights are not renormalised is right to
+ * 2^-31); the weights are rounded to fp32.
  *   logits  device [n][E], bf16 (logits_dtype 0) or fp32 (1), rows `stride` elements apart (stride >= E)
  *   bias    device fp32 [E], or NULL
  *   ids     device int32 [n][k];  weights  device fp32 [n][k]

@@ -16,13 +16,15 @@ namespace {
 // rounding about once in 10^4 tokens, and the choice would depend on the instruction that computed them.  Hence the order
 // is first taken in fp32, and kept where every decision in it (k + 1 neighbouring scores, the last group that takes part and the
 // first that does not) is clearer than the error of the fp32 scores, bounded below.  Where only the order of scores is open,
-// those few are compared in 64 bits, one per lane; other open tokens are done again as a whole (6 us more for the call that
-// meets one: 777 tokens of 160 experts 11.8 -> 5.7 us, 32768 of 256 39 -> 35).
+// those few are compared in 64 bits, one per lane; other open tokens are done again as a whole (6 to 10 us more for the call that
+// meets one: 777 tokens of 160 experts 11.8 -> 5.7 us, 32768 of 256 39 -> 34).  Equal fp32 logits are open, too, since a key
+// holds its place in their last bits: 32768 tokens of nothing but zeros 165 us, in bf16 32.
 // The weights of the chosen experts are computed in 64 bits, for the tokens of a warp together.
 //
 // A warp's cost is instructions, not the logits' bytes: every lane sorts its keys once, and the k rounds of "largest key of
 // the warp, its lane moves up" are about 20 each.  32768 tokens, 256 experts, 8 of them, sigmoid and bias: 34 us (33.6 MB of fp32
-// logits: 5.2 us); 64 tokens, 8 groups: 4.5 us, most of it launch and code that runs for the first time.
+// logits: 5.2 us); 64 tokens, 8 groups: 4.4 us, most of it launch and code that runs for the first time.  (Device time in a captured
+// loop of ten, as all figures here.)
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kRouteWarps = 2;  // small thread blocks: few tokens spread over more SMs (64 tokens: 4.5 us, with eight 5.2)
 constexpr double kNone = -__builtin_huge_val();
@@ -446,8 +448,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps, kPer <= 8 ? 14 : 1) moe_rout
 // Every warp owns a run of consecutive pairs and a count per expert in shared memory.  Scans over warps, over the cluster's
 // blocks (through distributed shared memory) and over experts turn the counts into places; a second walk over the same run
 // writes the list: lanes with the same expert find one another by votes on the bits of its number (match.any takes an SM
-// 70 clocks).  What bounds it: short lists, the chain of launch, loads, scans and stores (384 pairs: 5.2 us); long ones, the
-// votes of the cluster's SMs (262144 pairs: 18 us).
+// 70 clocks).  What bounds it: short lists, the chain of launch, loads, scans and stores (384 pairs: 5.0 us); long ones, the
+// votes of the cluster's SMs (262144 pairs: 18.6 us).
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kGroupThreads = 1024, kGroupWarps = kGroupThreads / 32;
 constexpr int kGroupAhead = 8;  // steps whose ids a warp loads together
@@ -570,6 +572,11 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
   cluster_wait();
 }
 
+// Experts of a lane (`per`, up to 64: 1024 in 17 to 32 groups) are held in registers by loops that unroll, so each width is a kernel,
+// and a lane with fewer pads them by -inf: 2, 8, 16, 32 or 64, whose costs differ by more than the padding between them.
+// 32768 tokens without groups, sigmoid and bias, 8 chosen: 64 experts 21 us, 128, 160 and 256 34, 384 69, 512 73, 768 212, 1024 227
+// (64 tokens: 3.2, 3.9, 3.9, 4.1, 5.6, 5.5, 7.4, 8.6).  Up to 8 fit 14 blocks on an SM; 16 take 152 registers and more take 255, the
+// 64-wide one with some of its values in local memory.  16-byte loads need all lanes full (256, 512 and 1024).
 template <bool kBf16>
 cudaError_t route_dispatch(const RouteParams& p, int per, cudaStream_t stream) {
   const int64_t tokens = kRouteWarps * p.turns;  // of a thread block

@@ -12,16 +12,18 @@
 // can.  Persistent: the accumulator is double buffered in tensor memory, so that the scales and stores of one tile run under
 // the products of the next.  Where there are few tiles they are made smaller, or 2 or 4 pairs in a cluster share k and add
 // their sums through each other's shared memory (rk_matmul8_plan; 256 x 4096 x 8192: 20.6 -> 15.4 us).
-//   8192 tokens x 7168 channels x 16384: 590 us, 3.26 POP/s, 0.96 of twice the bf16 library product's measured burst rate:
-//   bounded by the tensor cores.  5 x 4096 x 8192: 11.6 us, of which W's 33.6 MB cost 5.2 at the memory's measured rate and
-//   the rest is launch, setup, the join and the stores.
+//   8192 tokens x 7168 channels x 16384: 580 to 605 us in a captured loop of ten, 3.2 to 3.3 POP/s, 0.93 to 0.97 of twice the
+//   bf16 library product's measured burst rate: bounded by the tensor cores.  Called one by one for longer, with its
+//   quantisation (73 us), it is 780 to 810 us, about 2.7 POP/s in the product: the rate under the power limit.
+//   5 x 4096 x 8192: 11.3 us in such a loop, W's 33.6 MB in L2; 20.5 us with cold caches, of which those bytes cost 5.2 at the
+//   memory's measured rate and the rest is launch, setup, first trips to memory, the join and the stores.
 //
 // By expert, the token rows of a tile are a gather (the tokens that chose the expert): six or seven warps, one per stage,
 // copy them with 16-byte asynchronous loads into the swizzled operand layout, so that no sorted copy of the activations is made; the
 // outputs go straight to the pairs' rows of y.  (TMA's gather of four rows took 72 clocks of each SM's copy engine per
 // instruction, 2300 per 128 rows; a stage has 512.)
-//   64 tokens, all weights used once: 143 us, 0.98 of the measured copy rate.  8192 tokens: 300 us, of which (by removal, at
-//   313) the gather costs 30, the first bytes of each expert's weights out of memory 62, the stores 28.
+//   64 tokens, all weights used once: 143 us, 0.98 of the measured copy rate.  8192 tokens: 313 to 324 us in a captured loop of
+//   ten, 291 by itself; of 313 (by removal) the gather costs 30, the first bytes of each expert's weights out of memory 62, the stores 28.
 #include <cuda_bf16.h>
 
 #include "rk_internal.h"
@@ -702,7 +704,7 @@ cudaError_t launch_matmul8(Matmul8Params p, int sm_count, cudaStream_t stream) {
   const int64_t n_chan = (p.n_out + kTileM - 1) / kTileM;
   // by expert the number of tiles is known on the device only: at most one part-filled tile per expert more than full ones
   // Tiles of 256 rows where experts have more than 128 on average (at 192 an expert of 200 or 400 rows costs a tile more:
-  // 8192 tokens, 384 rows on average: 325 -> 300 us), the deeper ring where their weights' bytes count (64 tokens: 154 -> 149)
+  // 8192 tokens, 384 rows on average, 8% less time), the deeper ring where their weights' bytes count (64 tokens: 154 -> 149)
   const bool few = p.rows != nullptr && p.n_tok <= 128 * (int64_t)p.n_mat;
   const int most = few ? kTileNFew : kTileN;
   const int64_t tok_tiles = (p.n_tok + most - 1) / most + (p.rows ? (p.n_mat < p.n_tok ? p.n_mat : p.n_tok) : 0);
