@@ -508,6 +508,7 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
     }
     total[x] = sum;
   }
+  __syncwarp();
   cluster_arrive();
   cluster_wait();
   {  // n_experts <= kGroupThreads: one expert per thread
@@ -539,6 +540,7 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
     }
   }
   __syncthreads();
+  __syncwarp();
   cluster_arrive();  // no block leaves before the others have read its counts
   auto same_expert = [&](int e) -> unsigned {  // lanes with the same expert; whatever for those without
     unsigned same = __ballot_sync(kAll, e >= 0);
@@ -569,6 +571,7 @@ __global__ void __launch_bounds__(kGroupThreads, 1) moe_group_kernel(const Group
     }
   }
   for (int64_t i = (int64_t)sum_all + (int64_t)rank * kGroupThreads + threadIdx.x; i < n; i += (int64_t)n_blocks * kGroupThreads) p.rows[i] = -1;
+  __syncwarp();
   cluster_wait();
 }
 

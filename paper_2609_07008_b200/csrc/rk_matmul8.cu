@@ -376,6 +376,7 @@ __global__ void __launch_bounds__(threads8(kExperts, kFew), 1) rk_matmul8_pair_k
   };
   tc_fence_before_sync();
   __syncthreads();
+  __syncwarp();
   cluster_arrive();
   cluster_wait();
   tc_fence_after_sync();
@@ -616,6 +617,7 @@ __global__ void __launch_bounds__(threads8(kExperts, kFew), 1) rk_matmul8_pair_k
   __syncwarp();
   tc_fence_before_sync();
   __syncthreads();
+  __syncwarp();
   cluster_arrive();
   cluster_wait();
   if (warp == 0) {

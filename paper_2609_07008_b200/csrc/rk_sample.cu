@@ -96,7 +96,9 @@ __device__ __forceinline__ uint32_t add_cluster_u32(uint32_t addr, uint32_t v) {
   asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(addr), "r"(v) : "memory");
   return old;
 }
+// (the barrier is .aligned: it asks for all lanes of the warp at once, and the code in front may have parted them)
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
   cluster_arrive();
   cluster_wait();
 }
@@ -472,6 +474,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     cluster_sync();
     const int n = (int)min(ld_cluster_u32(peer(&sh.listed[0], 0)), (uint32_t)kList + 1u);
     if (n <= kList) {
+      __syncwarp();
       cluster_arrive();
       if (rank == 0) {
         u64* sorted = sh.list[0];
@@ -514,6 +517,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           }
         }
       }
+      __syncwarp();
       cluster_wait();
       return;
     }
@@ -909,6 +913,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   }
   before = __shfl_sync(all, before, 0);
   total = __shfl_sync(all, total, 0);
+  __syncwarp();
   cluster_arrive();
   const u64 want = place_of(total);
   if (before <= want && want < before + mine) {  // this block has it
@@ -968,6 +973,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       }
     }
   }
+  __syncwarp();
   cluster_wait();
 }
 
